@@ -47,7 +47,7 @@ enum {
   SWAM_ERR_WORKSPACE = 3,    /* workspace missing or too small */
   SWAM_ERR_STATE = 4,        /* reuse requested before any refresh */
   SWAM_ERR_CUDA = 5,         /* a CUDA runtime call failed; see swam_last_error */
-  SWAM_ERR_DEVICE_CHECK = 6, /* a kernel met an out-of-range map entry or an impossible count */
+  SWAM_ERR_DEVICE_CHECK = 6, /* a kernel met an out-of-range map entry or length, or an impossible count */
   SWAM_ERR_TIMEOUT = 7       /* a bounded device-side wait ran out */
 };
 
@@ -150,6 +150,70 @@ int swam_sparse_attn(swam_ctx* ctx, const void* qp, const void* kp, const void* 
  * last full step's result).  inv_map is only read when cached != out. */
 int swam_scatter(swam_ctx* ctx, const void* out_p, const int32_t* pack_map, const int32_t* inv_map,
                  const void* cached, void* out, void* stream);
+
+/* (6) Attention to keys outside the joint sequence (no counterpart in the paper, whose backbones hold these operators in
+ * the same Transformer blocks).  A row with visible keys c gets out = sum_c softmax_c(scale * q . k_c) v_c and
+ * lse = ln sum_c exp(scale * q . k_c); a row that sees no key gets out = 0 and lse = -inf.  Element type, number of
+ * samples, query heads, head dim and scale are the context's.  bf16: fp32 scores, maxima, sums and accumulation, the
+ * probabilities are rounded to bf16 for the product with v; fp32: fp32 throughout.
+ *
+ * Strides are in elements and count from one token (or sample, or group) to the next; 0 = contiguous.  The heads of a
+ * token are contiguous (N_h*D or n_kv_heads*D elements), so a K/V projection that interleaves k and v is read in place.
+ * Strides must be multiples of 16 bytes, pointers 16-byte aligned, tokens must not overlap, and out must not overlap
+ * any input.  Lengths (device int32) may be NULL: all rows are real.  Rows behind a length are never used, whatever they
+ * hold (NaN included); a length outside [0, n] is clamped and reported by swam_check (SWAM_ERR_DEVICE_CHECK).  A tensor of
+ * length 0 may be NULL.  Rows of out and lse that the call does not own are left untouched.
+ *
+ * scratch: device memory of swam_*_attn_scratch_bytes (256-byte aligned, NULL if 0), where long key ranges that are cut
+ * into pieces leave partial results.  The size depends on the sizes in the arguments only, not on pointers or
+ * lengths.  It need not be cleared; calls that may overlap on the device (other streams, other captured graphs) need
+ * scratch of their own.  A workspace must be bound (it holds the status word).  Both calls only enqueue kernels and can be
+ * captured in a CUDA graph; repeated calls give the same bits.  SWAM_OPT_ATTN_VARIANT applies, visibility does not.
+ * Limits: n_q, n_kv, n_prefix, n_own at most 2^30; batch*n_q*N_h at most 2^31-1 (SWAM_ERR_UNSUPPORTED beyond).
+ *
+ * swam_cross_attn: the n_q queries of each sample attend an encoder's states of another length.
+ * q, out: [B, n_q, N_h, D]; k, v: [B, n_kv, n_kv_heads, D]; kv_len [B]: query rows of sample b see the keys
+ * [0, kv_len[b]).  lse: dev float [B, N_h, n_q] or NULL.  n_kv_heads: 0 = the context's; must divide n_heads. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v;
+  const int32_t* kv_len;
+  void* out;
+  float* lse;
+  void* scratch;
+  size_t scratch_bytes;
+  int32_t n_q, n_kv, n_kv_heads, reserved; /* reserved: 0 */
+  int64_t q_token, q_sample, k_token, k_sample, v_token, v_sample, out_token, out_sample; /* strides */
+} swam_cross_args;
+int swam_cross_attn_scratch_bytes(swam_ctx* ctx, const swam_cross_args* args, size_t* bytes);
+int swam_cross_attn(swam_ctx* ctx, const swam_cross_args* args, void* stream);
+
+/* swam_prefix_attn: samples that share a long prefix.  The B samples form n_groups groups of B / n_groups consecutive
+ * samples; the keys of a group's prefix exist once and are attended by all its samples, followed by each sample's own keys.
+ * The candidates of one observation, for example, share the observed tokens when those see only one another
+ * (SWAM_SEES_OBSERVED); single new tokens share a history.
+ * k_prefix, v_prefix: [n_groups, n_prefix, n_kv_heads, D], prefix_len [n_groups]; k, v: [B, n_own, n_kv_heads, D], own_len [B].
+ * Every query of sample b sees the prefix keys [0, prefix_len[group]) and the own keys [0, own_len[b]); with causal != 0
+ * query t sees the own keys [0, own_len[b] - n_q + t + 1), i.e. the queries are the sample's last n_q tokens. */
+typedef struct {
+  const void* q;
+  const void* k_prefix;
+  const void* v_prefix;
+  const void* k;
+  const void* v;
+  const int32_t* prefix_len;
+  const int32_t* own_len;
+  void* out;
+  float* lse;
+  void* scratch;
+  size_t scratch_bytes;
+  int32_t n_q, n_prefix, n_own, n_groups, causal, n_kv_heads;
+  int64_t q_token, q_sample, k_prefix_token, k_prefix_group, v_prefix_token, v_prefix_group, k_token, k_sample, v_token,
+      v_sample, out_token, out_sample; /* strides */
+} swam_prefix_args;
+int swam_prefix_attn_scratch_bytes(swam_ctx* ctx, const swam_prefix_args* args, size_t* bytes);
+int swam_prefix_attn(swam_ctx* ctx, const swam_prefix_args* args, void* stream);
 
 /* One denoising step (Sec. 4.2).  q, k, v, out: dev [B, L, N_h, D]; out persists across steps and holds the
  * last full step's result on omitted rows.  mode: SWAM_REFRESH_FULL runs dense attention into out, scores the

@@ -1,0 +1,163 @@
+// Segment attention: how the work is cut, the merge of partial results, and the dispatch to the kernels.
+//
+// Partial results of the pieces i of a row are merged exactly: with reference maxima m_i, sums l_i and unnormalised
+// outputs o_i, m = max m_i, out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i, lse = ln 2 (m + log2 sum).
+#include "seg_attn.cuh"
+
+namespace swam {
+namespace {
+
+constexpr int kMaxSplits = 64;
+
+// One warp per row; lanes hold the pieces' weights and then D / 32 output columns each.
+template <int D, typename T>
+__global__ void __launch_bounds__(256) seg_merge_kernel(const __grid_constant__ SegParams p, const int parts) {
+  constexpr int CPL = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);   // (sample, query, head)
+  if (row >= p.rows) return;
+  const SegArgs& a = p.a;
+  // up to 128 pieces: four per lane
+  float mi[4], wi[4], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int i = j * 32 + lane;
+    const float2 v = i < parts ? p.part_ml[(int64_t)i * p.rows + row] : make_float2(-INFINITY, 0.f);
+    mi[j] = v.x;
+    wi[j] = v.y;
+    m = fmaxf(m, v.x);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float f = mi[j] == -INFINITY ? 0.f : exp2f(mi[j] - m);   // a piece without keys has weight 0
+    l += f * wi[j];
+    wi[j] = f;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  float acc[CPL];
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) acc[c] = 0.f;
+  const float* src = p.part_o + row * D + lane * CPL;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int n = min(32, parts - j * 32);
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+      const float f = __shfl_sync(0xffffffffu, wi[j], i);
+      const float* x = src + (int64_t)(j * 32 + i) * p.rows * D;
+      float v[CPL];
+      if constexpr (CPL == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(x);
+      else if constexpr (CPL == 2) *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(x);
+      else v[0] = x[0];
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) acc[c] = fmaf(f, v[c], acc[c]);
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const int h = (int)(row % a.N_h);
+  const int64_t bt = row / a.N_h;
+  const int t = (int)(bt % a.n_q), b = (int)(bt / a.n_q);
+  T* out = (T*)a.out + b * a.o_smp + t * a.o_tok + (int64_t)h * D + lane * CPL;
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) out[c] = (T)(acc[c] * inv);
+  if (a.lse && lane == 0) a.lse[((int64_t)b * a.N_h + h) * a.n_q + t] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <typename T>
+cudaError_t launch_merge(const SegParams& p, int parts, cudaStream_t st, int* launches) {
+  const int64_t blocks = (p.rows + 7) / 8;
+  ++*launches;
+  switch (p.a.D) {
+    case 32: seg_merge_kernel<32, T><<<(unsigned)blocks, 256, 0, st>>>(p, parts); break;
+    case 64: seg_merge_kernel<64, T><<<(unsigned)blocks, 256, 0, st>>>(p, parts); break;
+    default: seg_merge_kernel<128, T><<<(unsigned)blocks, 256, 0, st>>>(p, parts); break;
+  }
+  return cudaGetLastError();
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// pieces over `keys` keys so that `items` row tiles become at least `want` work items, no piece below `min_keys` keys
+int pick_splits(int64_t items, int64_t keys, int want, int min_keys) {
+  int64_t s = ceil_div(want, items > 0 ? items : 1);
+  if (s > keys / min_keys) s = keys / min_keys;
+  if (s > kMaxSplits) s = kMaxSplits;
+  return s < 1 ? 1 : (int)s;
+}
+
+int tile_rows(const SegArgs& a, int64_t rows) { return a.dtype == 0 ? seg_f32_tile_rows(rows) : seg_mma_tile_rows(rows); }
+
+}  // namespace
+
+SegPlan seg_plan(const SegArgs& a, bool warp_mma) {
+  (void)warp_mma;
+  SegPlan pl;
+  const int g = a.N_h / a.N_kv;
+  const int64_t rows = (int64_t)a.n_q * g;       // of one sample
+  const int want = 4 * sm_count();
+  // samples share the row tiles of segment 0 when a tile has room for two samples at least: the shared keys are then
+  // read once for all of them
+  pl.shared = a.per_group > 1 && a.n[0] > 0 && rows <= 32;
+  if (pl.shared) {
+    const int64_t block_rows = rows * a.per_group;
+    const int64_t items0 = (int64_t)(a.B / a.per_group) * a.N_kv * ceil_div(block_rows, tile_rows(a, block_rows));
+    const int64_t items1 = (int64_t)a.B * a.N_kv * ceil_div(rows, tile_rows(a, rows));
+    pl.splits[0] = pick_splits(items0, a.n[0], want, 256);
+    pl.splits[1] = a.n[1] > 0 ? pick_splits(items1, a.n[1], want, 256) : 0;
+  } else {
+    const int64_t items = (int64_t)a.B * a.N_kv * ceil_div(rows, tile_rows(a, rows));
+    pl.splits[0] = pick_splits(items, (int64_t)a.n[0] + a.n[1], want, 256);
+    pl.splits[1] = 0;
+  }
+  return pl;
+}
+
+size_t seg_scratch_bytes(const SegArgs& a, const SegPlan& p) {
+  if (!p.partial()) return 0;
+  const size_t rows = (size_t)a.B * a.n_q * a.N_h;
+  return (size_t)p.parts() * rows * ((size_t)a.D * sizeof(float) + sizeof(float2));
+}
+
+cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& pl, bool warp_mma, void* scratch, int* status, cudaStream_t st,
+                            int* launches) {
+  (void)warp_mma;
+  SegParams p;
+  p.a = a;
+  p.g = a.N_h / a.N_kv;
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.rows = (int64_t)a.B * a.n_q * a.N_h;
+  p.direct = !pl.partial();
+  p.part_o = (float*)scratch;
+  p.part_ml = (float2*)((float*)scratch + (size_t)pl.parts() * p.rows * a.D);
+  p.status = status;
+  const int64_t rows = (int64_t)a.n_q * p.g;
+  const int n_pass = pl.shared && pl.splits[1] > 0 ? 2 : 1;
+  int64_t block_rows[2];
+  for (int i = 0; i < 2; ++i) {
+    SegPass& ps = p.pass[i];
+    const bool mixed = pl.shared && i == 0;
+    ps.seg_lo = pl.shared ? i : 0;
+    ps.seg_hi = mixed ? 0 : 1;
+    ps.block_samples = mixed ? a.per_group : 1;
+    ps.blocks = a.B / ps.block_samples;
+    block_rows[i] = rows * ps.block_samples;
+    ps.row_tiles = (int)ceil_div(block_rows[i], tile_rows(a, block_rows[i]));
+    ps.splits = i < n_pass ? pl.splits[i] : 0;
+    ps.part0 = i == 0 ? 0 : pl.splits[0];
+    const int64_t items = (int64_t)ps.blocks * a.N_kv * ps.row_tiles * ps.splits;
+    if (items > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    ps.items = (int)items;
+  }
+  for (int i = 0; i < n_pass; ++i) {
+    const cudaError_t e = a.dtype == 0 ? launch_seg_f32(p, i, (int)(block_rows[i] > 64 ? 64 : block_rows[i]), st, launches)
+                                       : launch_seg_mma(p, i, (int)(block_rows[i] > 64 ? 64 : block_rows[i]), st, launches);
+    if (e != cudaSuccess) return e;
+  }
+  if (p.direct) return cudaSuccess;
+  return a.dtype == 0 ? launch_merge<float>(p, pl.parts(), st, launches) : launch_merge<__nv_bfloat16>(p, pl.parts(), st, launches);
+}
+
+}  // namespace swam

@@ -1,0 +1,109 @@
+// Work decomposition shared by the segment-attention kernels (cross attention and shared-prefix attention).
+//
+// The rows of a block (one sample, or all samples of a group) that read one key/value head are flattened in the order
+// (sample, query, head of the group) and cut into row tiles; the keys of the block are the tiles of segment 0 followed
+// by the tiles of segment 1.  A work item is (block, key/value head, row tile, piece of the key tiles).  Lengths live
+// on the device, so the pieces are cut there: the real key tiles of an item's block are shared out evenly.
+#pragma once
+#include "swam_internal.cuh"
+
+namespace swam {
+
+struct SegPass {
+  int seg_lo, seg_hi;       // segments this pass walks over
+  int block_samples;        // samples per block
+  int blocks, row_tiles;    // blocks; row tiles per (block, key/value head)
+  int splits, part0;        // pieces over the keys; index of the first piece's partial results
+  int items;                // blocks * N_kv * row_tiles * splits
+};
+
+struct SegParams {
+  SegArgs a;
+  SegPass pass[2];
+  int direct;               // 1: an item's result is final, 0: unnormalised partial results go to scratch
+  int g;                    // query heads per key/value head
+  float scale_log2;
+  float* part_o;            // [parts][B * n_q * N_h][D]
+  float2* part_ml;          // [parts][B * n_q * N_h] reference maximum (log2 domain) and sum
+  int64_t rows;             // B * n_q * N_h
+  int* status;
+};
+
+struct SegItem {
+  int block, h_kv, row0, split;
+};
+
+__device__ __forceinline__ SegItem seg_item(const SegPass& ps, int N_kv, int tile_rows, int w) {
+  SegItem it;
+  it.row0 = (w % ps.row_tiles) * tile_rows;
+  w /= ps.row_tiles;
+  it.split = w % ps.splits;
+  w /= ps.splits;
+  it.h_kv = w % N_kv;
+  it.block = w / N_kv;
+  return it;
+}
+
+// real keys of segment s for group / sample idx; lengths out of range are clamped and flagged
+__device__ __forceinline__ int seg_len(const SegParams& p, int s, int idx) {
+  const int n = p.a.n[s];
+  if (n == 0 || !p.a.len[s]) return n;
+  const int l = p.a.len[s][idx];
+  if (l < 0 || l > n) {
+    if (threadIdx.x == 0) atomicOr(p.status, ST_BAD_LEN);
+    return l < 0 ? 0 : n;
+  }
+  return l;
+}
+
+// a flattened row of a block: its sample, query and head
+struct SegRow {
+  int b, t, h;
+  bool real;
+};
+__device__ __forceinline__ SegRow seg_row(const SegParams& p, const SegPass& ps, const SegItem& it, int row) {
+  SegRow r;
+  const int per_sample = p.a.n_q * p.g;
+  r.real = row < ps.block_samples * per_sample;
+  const int rr = r.real ? row : 0;
+  r.b = it.block * ps.block_samples + rr / per_sample;
+  const int i = rr % per_sample;
+  r.t = i / p.g;
+  r.h = it.h_kv * p.g + i % p.g;
+  return r;
+}
+// keys of segment 1 that query t sees when the sample has `len` of them
+__device__ __forceinline__ int seg_limit1(const SegArgs& a, int len, int t) {
+  return a.causal ? max(0, len - a.n_q + t + 1) : len;
+}
+
+// the key tiles (KT keys each) of an item: [begin, end) of the concatenated tiles of segment 0 (len0 keys, n0 tiles)
+// and segment 1 (len1 keys: no row of the tile sees more of them)
+struct SegKeys {
+  int len0, len1, n0, begin, end;
+};
+__device__ __forceinline__ SegKeys seg_keys(const SegParams& p, const SegPass& ps, const SegItem& it, int tile_rows, int KT) {
+  SegKeys k;
+  const int b0 = it.block * ps.block_samples;
+  k.len0 = ps.seg_lo == 0 ? seg_len(p, 0, b0 / p.a.per_group) : 0;
+  k.len1 = 0;
+  if (ps.seg_hi == 1) {      // such a block is one sample
+    const int last = min(it.row0 + tile_rows, p.a.n_q * p.g) - 1;
+    k.len1 = seg_limit1(p.a, seg_len(p, 1, b0), last / p.g);
+  }
+  k.n0 = (k.len0 + KT - 1) / KT;
+  const int total = k.n0 + (k.len1 + KT - 1) / KT;
+  const int per = (total + ps.splits - 1) / ps.splits;
+  k.begin = min(total, it.split * per);
+  k.end = min(total, k.begin + per);
+  return k;
+}
+
+// rows of a row tile of the warp-level and of the fp32 kernel for blocks of `rows` rows
+inline int seg_mma_tile_rows(int64_t rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
+inline int seg_f32_tile_rows(int64_t rows) { return rows <= 16 ? 16 : 64; }
+// rows: rows of a block, per key/value head (they choose the row tile)
+cudaError_t launch_seg_mma(const SegParams& p, int pass, int rows, cudaStream_t st, int* launches);
+cudaError_t launch_seg_f32(const SegParams& p, int pass, int rows, cudaStream_t st, int* launches);
+
+}  // namespace swam

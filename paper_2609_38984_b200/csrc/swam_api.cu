@@ -131,6 +131,113 @@ int run_attention(swam_ctx* c, const void* q, const void* k, const void* v, int 
   return SWAM_OK;
 }
 
+// Stride of `n_tok` tokens of `row` elements in `n_smp` samples: fills in the contiguous defaults and checks that strides are
+// multiples of 16 bytes and that no two tokens overlap (either dimension may be the outer one).
+bool set_strides(int64_t& tok, int64_t& smp, int64_t n_tok, int64_t n_smp, int64_t row, size_t elem) {
+  const int64_t unit = 16 / (int64_t)elem, most = (int64_t)1 << 40;
+  if (tok < 0 || smp < 0 || tok > most || smp > most) return false;
+  if (tok == 0) tok = row;
+  const __int128 span = n_tok > 1 ? (__int128)(n_tok - 1) * tok + row : row;      // of one sample
+  if (smp == 0) {
+    if ((__int128)n_tok * tok > most) return false;
+    smp = n_tok * tok;
+  }
+  if (tok % unit != 0 || smp % unit != 0) return false;
+  if (n_tok > 1 && tok < row) return false;
+  if (n_smp > 1 && n_tok > 0 && smp < row) return false;
+  // every offset fits 62 bits: at most 2^30 tokens and 2^16 samples, strides up to 2^40
+  if (span + (__int128)(n_smp - 1) * smp > ((__int128)1 << 60)) return false;
+  if (n_tok > 1 && n_smp > 1) return smp >= span || tok >= (__int128)(n_smp - 1) * smp + row;
+  return true;
+}
+
+constexpr int32_t kMaxSegTokens = 1 << 30;
+
+// What both segment-attention calls share once their arguments are in `a`: the remaining checks, and the plan.
+int check_seg(swam_ctx* c, SegArgs& a, int32_t n_kv_heads, const char* name, SegPlan* plan, bool pointers) {
+  const Dims& d = c->d;
+  auto bad = [&](int code, const char* why) {
+    snprintf(c->err, sizeof(c->err), "%s: %s", name, why);
+    return code;
+  };
+  if (n_kv_heads < 0) return bad(SWAM_ERR_INVALID_ARG, "negative n_kv_heads");
+  a.N_h = d.N_h;
+  a.N_kv = n_kv_heads > 0 ? n_kv_heads : d.N_kv;
+  a.B = d.B;
+  a.D = d.D;
+  a.dtype = d.dtype;
+  a.scale = d.scale;
+  if (a.N_h % a.N_kv != 0) return bad(SWAM_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
+  if (a.n_q < 0 || a.n[0] < 0 || a.n[1] < 0) return bad(SWAM_ERR_INVALID_ARG, "negative length");
+  if (a.n_q > kMaxSegTokens || a.n[0] > kMaxSegTokens || a.n[1] > kMaxSegTokens)
+    return bad(SWAM_ERR_UNSUPPORTED, "length beyond 2^30");
+  if ((int64_t)a.n_q * a.N_h > 0x7fffffffll / a.B) return bad(SWAM_ERR_UNSUPPORTED, "batch * n_q * n_heads beyond 2^31 - 1");
+  const size_t eb = elem_bytes(d);
+  const int64_t row = (int64_t)a.N_h * a.D, row_kv = (int64_t)a.N_kv * a.D;
+  const int blocks[2] = {a.B / a.per_group, a.B};
+  bool ok = set_strides(a.q_tok, a.q_smp, a.n_q, a.B, row, eb) && set_strides(a.o_tok, a.o_smp, a.n_q, a.B, row, eb);
+  for (int s = 0; s < 2; ++s)
+    ok = ok && set_strides(a.k_tok[s], a.k_smp[s], a.n[s], blocks[s], row_kv, eb) &&
+         set_strides(a.v_tok[s], a.v_smp[s], a.n[s], blocks[s], row_kv, eb);
+  if (!ok) return bad(SWAM_ERR_INVALID_ARG, "strides must be non-negative multiples of 16 bytes without overlapping tokens");
+  *plan = seg_plan(a, c->attn_variant == SWAM_ATTN_WARP_MMA);
+  if (!pointers || a.n_q == 0) return SWAM_OK;
+  if (!a.q || !a.out) return bad(SWAM_ERR_INVALID_ARG, "null q or out");
+  for (int s = 0; s < 2; ++s) {
+    if (a.n[s] > 0 && (!a.k[s] || !a.v[s])) return bad(SWAM_ERR_INVALID_ARG, "null k or v");
+    if (!aligned16(a.k[s]) || !aligned16(a.v[s])) return bad(SWAM_ERR_INVALID_ARG, "misaligned pointer");
+  }
+  if (!aligned16(a.q) || !aligned16(a.out)) return bad(SWAM_ERR_INVALID_ARG, "misaligned pointer");
+  return SWAM_OK;
+}
+
+int run_seg(swam_ctx* c, const SegArgs& a, const SegPlan& plan, void* scratch, size_t scratch_bytes, const char* name,
+            cudaStream_t st) {
+  if (!c->ws) return fail(c, SWAM_ERR_WORKSPACE, "no workspace bound");
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev != c->device)
+    return fail(c, SWAM_ERR_INVALID_ARG, "current device differs from the context's device");
+  if (a.n_q == 0) return SWAM_OK;
+  const size_t need = seg_scratch_bytes(a, plan);
+  if (need > 0 && (!scratch || scratch_bytes < need || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0)) {
+    snprintf(c->err, sizeof(c->err), "%s: needs %zu bytes of 256-byte aligned scratch", name, need);
+    return SWAM_ERR_WORKSPACE;
+  }
+  cudaError_t e = launch_seg_attn(a, plan, c->attn_variant == SWAM_ATTN_WARP_MMA, scratch, (int*)(c->ws + c->off_status), st,
+                                  &c->launches_i);
+  count(c);
+  if (e != cudaSuccess) return fail_cuda(c, e, name);
+  return SWAM_OK;
+}
+
+int cross_args(swam_ctx* c, const swam_cross_args* x, SegArgs& a, SegPlan* plan, bool pointers) {
+  if (x->reserved != 0) return fail(c, SWAM_ERR_INVALID_ARG, "swam_cross_attn: reserved must be 0");
+  memset(&a, 0, sizeof(a));
+  a.q = x->q; a.out = x->out; a.lse = x->lse;
+  a.k[0] = x->k; a.v[0] = x->v; a.len[0] = x->kv_len; a.n[0] = x->n_kv;
+  a.n_q = x->n_q;
+  a.q_tok = x->q_token; a.q_smp = x->q_sample; a.o_tok = x->out_token; a.o_smp = x->out_sample;
+  a.k_tok[0] = x->k_token; a.k_smp[0] = x->k_sample; a.v_tok[0] = x->v_token; a.v_smp[0] = x->v_sample;
+  a.per_group = 1;
+  return check_seg(c, a, x->n_kv_heads, "swam_cross_attn", plan, pointers);
+}
+
+int prefix_args(swam_ctx* c, const swam_prefix_args* x, SegArgs& a, SegPlan* plan, bool pointers) {
+  if (x->n_groups <= 0 || c->d.B % x->n_groups != 0)
+    return fail(c, SWAM_ERR_INVALID_ARG, "swam_prefix_attn: n_groups must divide the batch");
+  memset(&a, 0, sizeof(a));
+  a.q = x->q; a.out = x->out; a.lse = x->lse;
+  a.k[0] = x->k_prefix; a.v[0] = x->v_prefix; a.len[0] = x->prefix_len; a.n[0] = x->n_prefix;
+  a.k[1] = x->k; a.v[1] = x->v; a.len[1] = x->own_len; a.n[1] = x->n_own;
+  a.n_q = x->n_q;
+  a.causal = x->causal != 0;
+  a.q_tok = x->q_token; a.q_smp = x->q_sample; a.o_tok = x->out_token; a.o_smp = x->out_sample;
+  a.k_tok[0] = x->k_prefix_token; a.k_smp[0] = x->k_prefix_group; a.v_tok[0] = x->v_prefix_token; a.v_smp[0] = x->v_prefix_group;
+  a.k_tok[1] = x->k_token; a.k_smp[1] = x->k_sample; a.v_tok[1] = x->v_token; a.v_smp[1] = x->v_sample;
+  a.per_group = c->d.B / x->n_groups;
+  return check_seg(c, a, x->n_kv_heads, "swam_prefix_attn", plan, pointers);
+}
+
 int need_ws(swam_ctx* c) {
   if (!c->ws) return fail(c, SWAM_ERR_WORKSPACE, "no workspace bound");
   return SWAM_OK;
@@ -418,6 +525,42 @@ int swam_sparse_attn(swam_ctx* c, const void* qp, const void* kp, const void* vp
   return run_attention(c, qp, kp, vp, seq_len, out_p, lse, 0, seq_len, (cudaStream_t)stream);
 }
 
+int swam_cross_attn_scratch_bytes(swam_ctx* c, const swam_cross_args* args, size_t* bytes) {
+  if (!c || !args || !bytes) return fail(c, SWAM_ERR_INVALID_ARG, "swam_cross_attn_scratch_bytes: null argument");
+  SegArgs a;
+  SegPlan plan;
+  if (int r = cross_args(c, args, a, &plan, false)) return r;
+  *bytes = seg_scratch_bytes(a, plan);
+  return SWAM_OK;
+}
+
+int swam_cross_attn(swam_ctx* c, const swam_cross_args* args, void* stream) {
+  Range trace_range("swam_cross_attn");
+  if (!c || !args) return fail(c, SWAM_ERR_INVALID_ARG, "swam_cross_attn: null argument");
+  SegArgs a;
+  SegPlan plan;
+  if (int r = cross_args(c, args, a, &plan, true)) return r;
+  return run_seg(c, a, plan, args->scratch, args->scratch_bytes, "swam_cross_attn", (cudaStream_t)stream);
+}
+
+int swam_prefix_attn_scratch_bytes(swam_ctx* c, const swam_prefix_args* args, size_t* bytes) {
+  if (!c || !args || !bytes) return fail(c, SWAM_ERR_INVALID_ARG, "swam_prefix_attn_scratch_bytes: null argument");
+  SegArgs a;
+  SegPlan plan;
+  if (int r = prefix_args(c, args, a, &plan, false)) return r;
+  *bytes = seg_scratch_bytes(a, plan);
+  return SWAM_OK;
+}
+
+int swam_prefix_attn(swam_ctx* c, const swam_prefix_args* args, void* stream) {
+  Range trace_range("swam_prefix_attn");
+  if (!c || !args) return fail(c, SWAM_ERR_INVALID_ARG, "swam_prefix_attn: null argument");
+  SegArgs a;
+  SegPlan plan;
+  if (int r = prefix_args(c, args, a, &plan, true)) return r;
+  return run_seg(c, a, plan, args->scratch, args->scratch_bytes, "swam_prefix_attn", (cudaStream_t)stream);
+}
+
 int swam_scatter(swam_ctx* c, const void* out_p, const int32_t* pack_map, const int32_t* inv_map, const void* cached,
                  void* out, void* stream) {
   Range trace_range("swam_scatter");
@@ -689,8 +832,9 @@ int swam_check(swam_ctx* c, void* stream) {
     // the arrival tickets of the one-pass scorer too: a launch that gave up may have left some behind
     e = cudaMemset(c->ws + c->off_status, 0, c->off_counters - c->off_status + score_counter_bytes(c->d));
     if (e != cudaSuccess) return fail_cuda(c, e, "status clear");
-    snprintf(c->err, sizeof(c->err), "device status word 0x%x%s%s%s", word, (word & ST_BAD_MAP) ? " [map entry out of range]" : "",
-             (word & ST_BAD_COUNT) ? " [selection count mismatch]" : "", (word & ST_TIMEOUT) ? " [bounded wait ran out]" : "");
+    snprintf(c->err, sizeof(c->err), "device status word 0x%x%s%s%s%s", word, (word & ST_BAD_MAP) ? " [map entry out of range]" : "",
+             (word & ST_BAD_COUNT) ? " [selection count mismatch]" : "", (word & ST_TIMEOUT) ? " [bounded wait ran out]" : "",
+             (word & ST_BAD_LEN) ? " [length out of range]" : "");
     return (word & ST_TIMEOUT) ? SWAM_ERR_TIMEOUT : SWAM_ERR_DEVICE_CHECK;
   }
   return SWAM_OK;

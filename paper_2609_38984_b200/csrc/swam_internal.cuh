@@ -7,7 +7,7 @@
 namespace swam {
 
 // bits of the device status word
-enum : int { ST_BAD_MAP = 1, ST_BAD_COUNT = 2, ST_TIMEOUT = 4 };
+enum : int { ST_BAD_MAP = 1, ST_BAD_COUNT = 2, ST_TIMEOUT = 4, ST_BAD_LEN = 8 };
 
 constexpr int kMaxGroup = 32;  // largest frame-aligned query group the tensor-core scorer handles
 
@@ -225,5 +225,34 @@ cudaError_t launch_attn_bf16_tc(const AttnArgs& a, int* status, void* scratch, s
 // pack_map names itself (TMA row gathers), so that no packed tensor exists.
 cudaError_t launch_attn_bf16_tc_gather(const AttnArgs& a, const int32_t* pack_map, int n_full, bool gather_kv, int* status,
                                        void* scratch, size_t scratch_bytes, cudaStream_t st, int* launches);
+
+// ---- seg_attn*.cu ---------------------------------------------------------
+// Attention of B x n_q queries to keys outside the query sequence: segment 0 is shared by per_group consecutive samples
+// (an encoder's states, a common prefix), segment 1 belongs to one sample.  Strides are in elements.
+struct SegArgs {
+  const void* q;
+  void* out;
+  float* lse;               // [B, N_h, n_q] or nullptr
+  const void* k[2];
+  const void* v[2];
+  const int32_t* len[2];    // device: real keys of each group / sample, nullptr = all n[s]
+  int n[2];                 // rows of the segment's tensors
+  int64_t q_tok, q_smp, o_tok, o_smp;
+  int64_t k_tok[2], k_smp[2], v_tok[2], v_smp[2];
+  int B, per_group, n_q, N_h, N_kv, D, dtype;
+  int causal;               // query t sees the first len - n_q + t + 1 keys of segment 1
+  float scale;
+};
+// How the work is cut (chosen on the host from sizes alone, so that the scratch size can be asked for in advance).
+struct SegPlan {
+  int shared;               // 1: the rows of several samples share the row tiles of segment 0, segment 1 has a pass of its own
+  int splits[2];            // pieces of each pass over the keys (joined plans have one pass: splits[1] = 0)
+  int parts() const { return splits[0] + splits[1]; }
+  bool partial() const { return parts() > 1; }
+};
+SegPlan seg_plan(const SegArgs& a, bool warp_mma);
+size_t seg_scratch_bytes(const SegArgs& a, const SegPlan& p);
+cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& p, bool warp_mma, void* scratch, int* status, cudaStream_t st,
+                            int* launches);
 
 }  // namespace swam

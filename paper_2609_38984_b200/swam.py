@@ -29,7 +29,8 @@ SPARSE_FUSED, SPARSE_STAGED, SPARSE_FUSED_KV = 0, 1, 2
 EXPORTS = [
     "swam_create", "swam_destroy", "swam_workspace_bytes", "swam_bind_workspace", "swam_score", "swam_score_noalloc",
     "swam_select", "swam_aggregate", "swam_select_maps",
-    "swam_pack", "swam_sparse_attn", "swam_scatter", "swam_step", "swam_host_io_bytes", "swam_bind_host_io",
+    "swam_pack", "swam_sparse_attn", "swam_scatter", "swam_cross_attn", "swam_cross_attn_scratch_bytes",
+    "swam_prefix_attn", "swam_prefix_attn_scratch_bytes", "swam_step", "swam_host_io_bytes", "swam_bind_host_io",
     "swam_step_host", "swam_host_join", "swam_get_selection", "swam_get_scores", "swam_set_selection", "swam_state_bytes",
     "swam_state_export", "swam_state_import", "swam_check", "swam_selftest_timeout", "swam_launch_floor", "swam_set_option", "swam_launch_count",
     "swam_last_error", "swam_version",
@@ -44,6 +45,24 @@ class SwamShape(ctypes.Structure):
         ("dtype", ctypes.c_int32), ("softmax_scale", ctypes.c_float), ("cv_beta", ctypes.c_float),
         ("query_weights", ctypes.POINTER(ctypes.c_float)), ("n_kv_heads", ctypes.c_int32),
     ]
+
+
+class SwamCrossArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k", "v", "kv_len", "out", "lse", "scratch")]
+                + [("scratch_bytes", ctypes.c_size_t)]
+                + [(n, ctypes.c_int32) for n in ("n_q", "n_kv", "n_kv_heads", "reserved")]
+                + [(n, ctypes.c_int64) for n in ("q_token", "q_sample", "k_token", "k_sample", "v_token", "v_sample",
+                                                 "out_token", "out_sample")])
+
+
+class SwamPrefixArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k_prefix", "v_prefix", "k", "v", "prefix_len", "own_len", "out", "lse",
+                                                "scratch")]
+                + [("scratch_bytes", ctypes.c_size_t)]
+                + [(n, ctypes.c_int32) for n in ("n_q", "n_prefix", "n_own", "n_groups", "causal", "n_kv_heads")]
+                + [(n, ctypes.c_int64) for n in ("q_token", "q_sample", "k_prefix_token", "k_prefix_group", "v_prefix_token",
+                                                 "v_prefix_group", "k_token", "k_sample", "v_token", "v_sample",
+                                                 "out_token", "out_sample")])
 
 
 class SwamError(RuntimeError):
@@ -78,6 +97,9 @@ def load_library() -> ctypes.CDLL:
         lib.swam_pack.argtypes = [vp] * 9
         lib.swam_sparse_attn.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp]
         lib.swam_scatter.argtypes = [vp] * 7
+        for name, args in (("cross", SwamCrossArgs), ("prefix", SwamPrefixArgs)):
+            getattr(lib, f"swam_{name}_attn").argtypes = [vp, ctypes.POINTER(args), vp]
+            getattr(lib, f"swam_{name}_attn_scratch_bytes").argtypes = [vp, ctypes.POINTER(args), ctypes.POINTER(ctypes.c_size_t)]
         lib.swam_step.argtypes = [vp, vp, vp, vp, i32, vp, vp]
         lib.swam_step_host.argtypes = [vp, vp, vp, vp, i32, vp, vp]
         lib.swam_host_join.argtypes = [vp, vp]
@@ -248,6 +270,95 @@ class Swam:
         out = torch.empty_like(qp)
         lse = torch.empty((self.B, self.N_h, n), dtype=torch.float32, device=self.device) if want_lse else None
         self._chk(self.lib.swam_sparse_attn(self.ctx, _ptr(qp), _ptr(kp), _ptr(vp), n, _ptr(out), _ptr(lse), _stream()))
+        return (out, lse) if want_lse else out
+
+    def _here(self, t: torch.Tensor) -> bool:
+        return t.is_cuda and (self.device.index is None or t.device.index == self.device.index)
+
+    def _tokens(self, name: str, t: torch.Tensor, lead: Optional[int], heads: int):
+        """Token and sample strides of a [samples, tokens, heads, D] tensor whose heads are contiguous (0 where the
+        dimension has one entry, or none)."""
+        if t.dtype != torch_dtype(self.dtype) or not self._here(t) or t.dim() != 4:
+            raise ValueError(f"{name}: expected a 4-dimensional {torch_dtype(self.dtype)} tensor on {self.device}")
+        n, tokens, h, d = t.shape
+        if (lead is not None and n != lead) or h != heads or d != self.D:
+            raise ValueError(f"{name}: expected shape [{'groups' if lead is None else lead}, tokens, {heads}, {self.D}], got {list(t.shape)}")
+        if t.numel() == 0:
+            return 0, 0
+        if t.stride(3) != 1 or (h > 1 and t.stride(2) != d):
+            raise ValueError(f"{name}: the heads of a token must be contiguous")
+        if (tokens > 1 and t.stride(1) == 0) or (n > 1 and t.stride(0) == 0):
+            raise ValueError(f"{name}: expanded (stride 0) tokens or samples are not accepted")
+        row = heads * d
+        tok = t.stride(1) if tokens > 1 else row
+        return tok, (t.stride(0) if n > 1 else tokens * tok)
+
+    def _lengths(self, name: str, t: Optional[torch.Tensor], n: int):
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or not self._here(t) or tuple(t.shape) != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous int32 tensor of shape [{n}] on {self.device}")
+        return t.data_ptr()
+
+    def _outputs(self, a, q, out, want_lse: bool):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        elif out.shape != q.shape:
+            raise ValueError(f"out: expected shape {list(q.shape)}")
+        a.q, a.out, a.n_q = q.data_ptr(), out.data_ptr(), q.shape[1]
+        a.q_token, a.q_sample = self._tokens("q", q, self.B, self.N_h)
+        a.out_token, a.out_sample = self._tokens("out", out, self.B, self.N_h)
+        lse = torch.empty((self.B, self.N_h, q.shape[1]), dtype=torch.float32, device=self.device) if want_lse else None
+        a.lse = lse.data_ptr() if want_lse else None
+        return out, lse
+
+    def _run_with_scratch(self, name: str, a):
+        n = ctypes.c_size_t()
+        self._chk(getattr(self.lib, f"swam_{name}_attn_scratch_bytes")(self.ctx, ctypes.byref(a), ctypes.byref(n)))
+        scratch = None
+        if n.value:
+            scratch = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
+            off = (-scratch.data_ptr()) % 256
+            a.scratch, a.scratch_bytes = scratch.data_ptr() + off, n.value
+        self._chk(getattr(self.lib, f"swam_{name}_attn")(self.ctx, ctypes.byref(a), _stream()))
+
+    def cross_attn(self, q, k, v, kv_len=None, out=None, want_lse: bool = False):
+        """Queries [B, n_q, N_h, D] attend an encoder's states k, v [B, n_kv, heads, D] (any divisor of N_h heads), of which
+        the first kv_len[b] (int32 CUDA tensor [B], default all) are real.  Tensors may be strided views with
+        contiguous heads.  A row without keys gives zeros (lse -inf).  Returns out, or (out, lse [B, N_h, n_q])."""
+        a = SwamCrossArgs()
+        heads = k.shape[2] if k.dim() == 4 else 0
+        if v.shape != k.shape:
+            raise ValueError("k and v differ in shape")
+        a.k_token, a.k_sample = self._tokens("k", k, self.B, heads)
+        a.v_token, a.v_sample = self._tokens("v", v, self.B, heads)
+        a.k, a.v, a.n_kv, a.n_kv_heads = k.data_ptr(), v.data_ptr(), k.shape[1], heads
+        a.kv_len = self._lengths("kv_len", kv_len, self.B)
+        out, lse = self._outputs(a, q, out, want_lse)
+        self._run_with_scratch("cross", a)
+        return (out, lse) if want_lse else out
+
+    def prefix_attn(self, q, k_prefix, v_prefix, k, v, prefix_len=None, own_len=None, causal: bool = False, out=None,
+                    want_lse: bool = False):
+        """Queries [B, n_q, N_h, D] attend a prefix k_prefix, v_prefix [groups, n_prefix, heads, D] that the B / groups
+        consecutive samples of a group share, followed by their own k, v [B, n_own, heads, D].  prefix_len [groups] and
+        own_len [B] (int32 CUDA tensors, default all) give the real lengths; `causal`: query t sees the own keys up to
+        own_len[b] - n_q + t.  A row without keys gives zeros (lse -inf).  Returns out, or (out, lse [B, N_h, n_q])."""
+        a = SwamPrefixArgs()
+        heads = k.shape[2] if k.dim() == 4 else 0
+        if v.shape != k.shape or v_prefix.shape != k_prefix.shape:
+            raise ValueError("k and v differ in shape")
+        a.k_prefix_token, a.k_prefix_group = self._tokens("k_prefix", k_prefix, None, heads)
+        a.v_prefix_token, a.v_prefix_group = self._tokens("v_prefix", v_prefix, None, heads)
+        a.k_token, a.k_sample = self._tokens("k", k, self.B, heads)
+        a.v_token, a.v_sample = self._tokens("v", v, self.B, heads)
+        a.k_prefix, a.v_prefix, a.k, a.v = k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(), v.data_ptr()
+        a.n_groups, a.n_prefix, a.n_own, a.n_kv_heads = k_prefix.shape[0], k_prefix.shape[1], k.shape[1], heads
+        a.causal = 1 if causal else 0
+        a.prefix_len = self._lengths("prefix_len", prefix_len, k_prefix.shape[0])
+        a.own_len = self._lengths("own_len", own_len, self.B)
+        out, lse = self._outputs(a, q, out, want_lse)
+        self._run_with_scratch("prefix", a)
         return (out, lse) if want_lse else out
 
     def scatter(self, out_p, pack_map, inv_map, cached, out=None):
