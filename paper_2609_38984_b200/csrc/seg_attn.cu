@@ -80,6 +80,16 @@ cudaError_t launch_merge(const SegParams& p, int parts, cudaStream_t st, int* la
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// The kernel of a pass whose blocks have `rows` rows per key/value head.
+enum Kind { kF32, kMma, kTc };
+Kind pass_kind(const SegArgs& a, int64_t rows, bool warp_mma) {
+  if (a.dtype == 0) return kF32;
+  return a.D < 64 || warp_mma || rows <= 32 ? kMma : kTc;
+}
+int tile_rows(Kind k, int64_t rows) {
+  return k == kF32 ? seg_f32_tile_rows(rows) : (k == kMma ? seg_mma_tile_rows(rows) : seg_tc_tile_rows(rows));
+}
+
 // pieces over `keys` keys so that `items` row tiles become at least `want` work items, no piece below `min_keys` keys
 int pick_splits(int64_t items, int64_t keys, int want, int min_keys) {
   int64_t s = ceil_div(want, items > 0 ? items : 1);
@@ -88,28 +98,31 @@ int pick_splits(int64_t items, int64_t keys, int want, int min_keys) {
   return s < 1 ? 1 : (int)s;
 }
 
-int tile_rows(const SegArgs& a, int64_t rows) { return a.dtype == 0 ? seg_f32_tile_rows(rows) : seg_mma_tile_rows(rows); }
+int plan_pass(const SegArgs& a, int64_t blocks, int64_t rows, int64_t keys, bool warp_mma) {
+  const Kind k = pass_kind(a, rows, warp_mma);
+  const int64_t items = blocks * a.N_kv * ceil_div(rows, tile_rows(k, rows));
+  const int sms = sm_count();
+  if (k != kTc) return pick_splits(items, keys, 4 * sms, 256);
+  // one CTA per SM: as many pieces as fill the last wave
+  int64_t s = sms / (items > 0 ? items : 1);
+  if (s > keys / 512) s = keys / 512;
+  if (s > kMaxSplits) s = kMaxSplits;
+  return s < 1 ? 1 : (int)s;
+}
 
 }  // namespace
 
 SegPlan seg_plan(const SegArgs& a, bool warp_mma) {
-  (void)warp_mma;
   SegPlan pl;
-  const int g = a.N_h / a.N_kv;
-  const int64_t rows = (int64_t)a.n_q * g;       // of one sample
-  const int want = 4 * sm_count();
+  const int64_t rows = (int64_t)a.n_q * (a.N_h / a.N_kv);       // of one sample
   // samples share the row tiles of segment 0 when a tile has room for two samples at least: the shared keys are then
   // read once for all of them
   pl.shared = a.per_group > 1 && a.n[0] > 0 && rows <= 32;
   if (pl.shared) {
-    const int64_t block_rows = rows * a.per_group;
-    const int64_t items0 = (int64_t)(a.B / a.per_group) * a.N_kv * ceil_div(block_rows, tile_rows(a, block_rows));
-    const int64_t items1 = (int64_t)a.B * a.N_kv * ceil_div(rows, tile_rows(a, rows));
-    pl.splits[0] = pick_splits(items0, a.n[0], want, 256);
-    pl.splits[1] = a.n[1] > 0 ? pick_splits(items1, a.n[1], want, 256) : 0;
+    pl.splits[0] = plan_pass(a, a.B / a.per_group, rows * a.per_group, a.n[0], warp_mma);
+    pl.splits[1] = a.n[1] > 0 ? plan_pass(a, a.B, rows, a.n[1], warp_mma) : 0;
   } else {
-    const int64_t items = (int64_t)a.B * a.N_kv * ceil_div(rows, tile_rows(a, rows));
-    pl.splits[0] = pick_splits(items, (int64_t)a.n[0] + a.n[1], want, 256);
+    pl.splits[0] = plan_pass(a, a.B, rows, (int64_t)a.n[0] + a.n[1], warp_mma);
     pl.splits[1] = 0;
   }
   return pl;
@@ -123,7 +136,6 @@ size_t seg_scratch_bytes(const SegArgs& a, const SegPlan& p) {
 
 cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& pl, bool warp_mma, void* scratch, int* status, cudaStream_t st,
                             int* launches) {
-  (void)warp_mma;
   SegParams p;
   p.a = a;
   p.g = a.N_h / a.N_kv;
@@ -133,9 +145,9 @@ cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& pl, bool warp_mma, 
   p.part_o = (float*)scratch;
   p.part_ml = (float2*)((float*)scratch + (size_t)pl.parts() * p.rows * a.D);
   p.status = status;
-  const int64_t rows = (int64_t)a.n_q * p.g;
   const int n_pass = pl.shared && pl.splits[1] > 0 ? 2 : 1;
-  int64_t block_rows[2];
+  int64_t rows[2];
+  Kind kind[2];
   for (int i = 0; i < 2; ++i) {
     SegPass& ps = p.pass[i];
     const bool mixed = pl.shared && i == 0;
@@ -143,8 +155,9 @@ cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& pl, bool warp_mma, 
     ps.seg_hi = mixed ? 0 : 1;
     ps.block_samples = mixed ? a.per_group : 1;
     ps.blocks = a.B / ps.block_samples;
-    block_rows[i] = rows * ps.block_samples;
-    ps.row_tiles = (int)ceil_div(block_rows[i], tile_rows(a, block_rows[i]));
+    rows[i] = (int64_t)a.n_q * p.g * ps.block_samples;
+    kind[i] = pass_kind(a, rows[i], warp_mma);
+    ps.row_tiles = (int)ceil_div(rows[i], tile_rows(kind[i], rows[i]));
     ps.splits = i < n_pass ? pl.splits[i] : 0;
     ps.part0 = i == 0 ? 0 : pl.splits[0];
     const int64_t items = (int64_t)ps.blocks * a.N_kv * ps.row_tiles * ps.splits;
@@ -152,8 +165,9 @@ cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& pl, bool warp_mma, 
     ps.items = (int)items;
   }
   for (int i = 0; i < n_pass; ++i) {
-    const cudaError_t e = a.dtype == 0 ? launch_seg_f32(p, i, (int)(block_rows[i] > 64 ? 64 : block_rows[i]), st, launches)
-                                       : launch_seg_mma(p, i, (int)(block_rows[i] > 64 ? 64 : block_rows[i]), st, launches);
+    const cudaError_t e = kind[i] == kF32   ? launch_seg_f32(p, i, rows[i], st, launches)
+                          : kind[i] == kMma ? launch_seg_mma(p, i, rows[i], st, launches)
+                                            : launch_seg_tc(p, i, rows[i], st, launches);
     if (e != cudaSuccess) return e;
   }
   if (p.direct) return cudaSuccess;

@@ -101,9 +101,12 @@ __device__ __forceinline__ SegKeys seg_keys(const SegParams& p, const SegPass& p
 
 // rows of a row tile of the warp-level and of the fp32 kernel for blocks of `rows` rows
 inline int seg_mma_tile_rows(int64_t rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
+// of the tcgen05 kernel: two query tiles, or one whose keys two streams take in turn
+inline int seg_tc_tile_rows(int64_t rows) { return rows <= 128 ? 128 : 256; }
 inline int seg_f32_tile_rows(int64_t rows) { return rows <= 16 ? 16 : 64; }
 // rows: rows of a block, per key/value head (they choose the row tile)
-cudaError_t launch_seg_mma(const SegParams& p, int pass, int rows, cudaStream_t st, int* launches);
-cudaError_t launch_seg_f32(const SegParams& p, int pass, int rows, cudaStream_t st, int* launches);
+cudaError_t launch_seg_mma(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches);
+cudaError_t launch_seg_tc(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches);
+cudaError_t launch_seg_f32(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches);
 
 }  // namespace swam

@@ -197,13 +197,13 @@ cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launc
   return cudaGetLastError();
 }
 template <int D>
-cudaError_t launch_rows(const SegParams& p, int pass, int rows, cudaStream_t st, int* launches) {
+cudaError_t launch_rows(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches) {
   return seg_f32_tile_rows(rows) == 16 ? launch_one<D, 1>(p, pass, st, launches) : launch_one<D, 4>(p, pass, st, launches);
 }
 
 }  // namespace
 
-cudaError_t launch_seg_f32(const SegParams& p, int pass, int rows, cudaStream_t st, int* launches) {
+cudaError_t launch_seg_f32(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches) {
   switch (p.a.D) {
     case 32: return launch_rows<32>(p, pass, rows, st, launches);
     case 64: return launch_rows<64>(p, pass, rows, st, launches);

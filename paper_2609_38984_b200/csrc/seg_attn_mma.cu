@@ -255,7 +255,7 @@ cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launc
   return cudaGetLastError();
 }
 template <int D>
-cudaError_t launch_rows(const SegParams& p, int pass, int rows, cudaStream_t st, int* launches) {
+cudaError_t launch_rows(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches) {
   switch (seg_mma_tile_rows(rows)) {
     case 16: return launch_one<D, 1>(p, pass, st, launches);
     case 32: return launch_one<D, 2>(p, pass, st, launches);
@@ -265,7 +265,7 @@ cudaError_t launch_rows(const SegParams& p, int pass, int rows, cudaStream_t st,
 
 }  // namespace
 
-cudaError_t launch_seg_mma(const SegParams& p, int pass, int rows, cudaStream_t st, int* launches) {
+cudaError_t launch_seg_mma(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches) {
   switch (p.a.D) {
     case 32: return launch_rows<32>(p, pass, rows, st, launches);
     case 64: return launch_rows<64>(p, pass, rows, st, launches);

@@ -134,7 +134,7 @@ int run_attention(swam_ctx* c, const void* q, const void* k, const void* v, int 
 // Stride of `n_tok` tokens of `row` elements in `n_smp` samples: fills in the contiguous defaults and checks that strides are
 // multiples of 16 bytes and that no two tokens overlap (either dimension may be the outer one).
 bool set_strides(int64_t& tok, int64_t& smp, int64_t n_tok, int64_t n_smp, int64_t row, size_t elem) {
-  const int64_t unit = 16 / (int64_t)elem, most = (int64_t)1 << 40;
+  const int64_t unit = 16 / (int64_t)elem, most = (int64_t)1 << 38;
   if (tok < 0 || smp < 0 || tok > most || smp > most) return false;
   if (tok == 0) tok = row;
   const __int128 span = n_tok > 1 ? (__int128)(n_tok - 1) * tok + row : row;      // of one sample
@@ -145,7 +145,7 @@ bool set_strides(int64_t& tok, int64_t& smp, int64_t n_tok, int64_t n_smp, int64
   if (tok % unit != 0 || smp % unit != 0) return false;
   if (n_tok > 1 && tok < row) return false;
   if (n_smp > 1 && n_tok > 0 && smp < row) return false;
-  // every offset fits 62 bits: at most 2^30 tokens and 2^16 samples, strides up to 2^40
+  // every offset fits 62 bits: at most 2^30 tokens and 2^16 samples, strides up to 2^38
   if (span + (__int128)(n_smp - 1) * smp > ((__int128)1 << 60)) return false;
   if (n_tok > 1 && n_smp > 1) return smp >= span || tok >= (__int128)(n_smp - 1) * smp + row;
   return true;
@@ -171,7 +171,7 @@ int check_seg(swam_ctx* c, SegArgs& a, int32_t n_kv_heads, const char* name, Seg
   if (a.n_q < 0 || a.n[0] < 0 || a.n[1] < 0) return bad(SWAM_ERR_INVALID_ARG, "negative length");
   if (a.n_q > kMaxSegTokens || a.n[0] > kMaxSegTokens || a.n[1] > kMaxSegTokens)
     return bad(SWAM_ERR_UNSUPPORTED, "length beyond 2^30");
-  if ((int64_t)a.n_q * a.N_h > 0x7fffffffll / a.B) return bad(SWAM_ERR_UNSUPPORTED, "batch * n_q * n_heads beyond 2^31 - 1");
+  if ((int64_t)a.n_q * a.N_h > (1ll << 30) / a.B) return bad(SWAM_ERR_UNSUPPORTED, "batch * n_q * n_heads beyond 2^30");
   const size_t eb = elem_bytes(d);
   const int64_t row = (int64_t)a.N_h * a.D, row_kv = (int64_t)a.N_kv * a.D;
   const int blocks[2] = {a.B / a.per_group, a.B};
