@@ -169,7 +169,7 @@ int swam_scatter(swam_ctx* ctx, const void* out_p, const int32_t* pack_map, cons
  * lengths.  It need not be cleared; calls that may overlap on the device (other streams, other captured graphs) need
  * scratch of their own.  A workspace must be bound (it holds the status word).  Both calls only enqueue kernels and can be
  * captured in a CUDA graph; repeated calls give the same bits.  SWAM_OPT_ATTN_VARIANT applies, visibility does not.
- * Limits: n_q, n_kv, n_prefix, n_own at most 2^30; batch*n_q*N_h at most 2^30 (SWAM_ERR_UNSUPPORTED beyond);
+ * Limits: n_q, n_kv, n_prefix, n_own at most 2^29; batch*n_q*N_h at most 2^30 (SWAM_ERR_UNSUPPORTED beyond);
  * strides at most 2^38.
  *
  * swam_cross_attn: the n_q queries of each sample attend an encoder's states of another length.

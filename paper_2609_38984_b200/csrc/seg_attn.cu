@@ -164,10 +164,13 @@ cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& pl, bool warp_mma, 
     if (items > 0x7fffffff) return cudaErrorInvalidConfiguration;
     ps.items = (int)items;
   }
-  for (int i = 0; i < n_pass; ++i) {
+  bool alt[2];
+  for (int i = 0; i < 2; ++i) alt[i] = seg_tc_tile_rows(rows[i]) == 128;
+  const bool both = n_pass == 2 && kind[0] == kTc && kind[1] == kTc && alt[0] == alt[1];
+  for (int i = 0; i < (both ? 1 : n_pass); ++i) {
     const cudaError_t e = kind[i] == kF32   ? launch_seg_f32(p, i, rows[i], st, launches)
                           : kind[i] == kMma ? launch_seg_mma(p, i, rows[i], st, launches)
-                                            : launch_seg_tc(p, i, rows[i], st, launches);
+                                            : launch_seg_tc(p, i, both, alt[i], st, launches);
     if (e != cudaSuccess) return e;
   }
   if (p.direct) return cudaSuccess;

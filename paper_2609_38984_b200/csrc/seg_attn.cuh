@@ -48,9 +48,9 @@ __device__ __forceinline__ SegItem seg_item(const SegPass& ps, int N_kv, int til
 __device__ __forceinline__ int seg_len(const SegParams& p, int s, int idx) {
   const int n = p.a.n[s];
   if (n == 0 || !p.a.len[s]) return n;
-  const int l = p.a.len[s][idx];
+  const int l = __ldg(p.a.len[s] + idx);
   if (l < 0 || l > n) {
-    if (threadIdx.x == 0) atomicOr(p.status, ST_BAD_LEN);
+    if ((threadIdx.x & 31) == 0) atomicOr(p.status, ST_BAD_LEN);
     return l < 0 ? 0 : n;
   }
   return l;
@@ -61,16 +61,20 @@ struct SegRow {
   int b, t, h;
   bool real;
 };
-__device__ __forceinline__ SegRow seg_row(const SegParams& p, const SegPass& ps, const SegItem& it, int row) {
+__device__ __forceinline__ SegRow seg_row(const SegParams& p, int block_samples, int b0, int h_kv, int row) {
   SegRow r;
   const int per_sample = p.a.n_q * p.g;
-  r.real = row < ps.block_samples * per_sample;
+  r.real = row < block_samples * per_sample;
   const int rr = r.real ? row : 0;
-  r.b = it.block * ps.block_samples + rr / per_sample;
-  const int i = rr % per_sample;
+  const int smp = block_samples > 1 ? rr / per_sample : 0;
+  const int i = rr - smp * per_sample;
+  r.b = b0 + smp;
   r.t = i / p.g;
-  r.h = it.h_kv * p.g + i % p.g;
+  r.h = h_kv * p.g + (i - r.t * p.g);
   return r;
+}
+__device__ __forceinline__ SegRow seg_row(const SegParams& p, const SegPass& ps, const SegItem& it, int row) {
+  return seg_row(p, ps.block_samples, it.block * ps.block_samples, it.h_kv, row);
 }
 // keys of segment 1 that query t sees when the sample has `len` of them
 __device__ __forceinline__ int seg_limit1(const SegArgs& a, int len, int t) {
@@ -106,7 +110,8 @@ inline int seg_tc_tile_rows(int64_t rows) { return rows <= 128 ? 128 : 256; }
 inline int seg_f32_tile_rows(int64_t rows) { return rows <= 16 ? 16 : 64; }
 // rows: rows of a block, per key/value head (they choose the row tile)
 cudaError_t launch_seg_mma(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches);
-cudaError_t launch_seg_tc(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches);
+// both: the items of pass 1 follow those of pass 0 in the same launch; alt: 128-row tiles whose keys two streams take in turn
+cudaError_t launch_seg_tc(const SegParams& p, int pass, bool both, bool alt, cudaStream_t st, int* launches);
 cudaError_t launch_seg_f32(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches);
 
 }  // namespace swam

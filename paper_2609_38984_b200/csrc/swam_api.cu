@@ -151,7 +151,7 @@ bool set_strides(int64_t& tok, int64_t& smp, int64_t n_tok, int64_t n_smp, int64
   return true;
 }
 
-constexpr int32_t kMaxSegTokens = 1 << 30;
+constexpr int32_t kMaxSegTokens = 1 << 29;
 
 // What both segment-attention calls share once their arguments are in `a`: the remaining checks, and the plan.
 int check_seg(swam_ctx* c, SegArgs& a, int32_t n_kv_heads, const char* name, SegPlan* plan, bool pointers) {
@@ -170,7 +170,7 @@ int check_seg(swam_ctx* c, SegArgs& a, int32_t n_kv_heads, const char* name, Seg
   if (a.N_h % a.N_kv != 0) return bad(SWAM_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
   if (a.n_q < 0 || a.n[0] < 0 || a.n[1] < 0) return bad(SWAM_ERR_INVALID_ARG, "negative length");
   if (a.n_q > kMaxSegTokens || a.n[0] > kMaxSegTokens || a.n[1] > kMaxSegTokens)
-    return bad(SWAM_ERR_UNSUPPORTED, "length beyond 2^30");
+    return bad(SWAM_ERR_UNSUPPORTED, "length beyond 2^29");
   if ((int64_t)a.n_q * a.N_h > (1ll << 30) / a.B) return bad(SWAM_ERR_UNSUPPORTED, "batch * n_q * n_heads beyond 2^30");
   const size_t eb = elem_bytes(d);
   const int64_t row = (int64_t)a.N_h * a.D, row_kv = (int64_t)a.N_kv * a.D;
