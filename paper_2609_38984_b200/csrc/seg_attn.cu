@@ -47,6 +47,7 @@ __global__ void __launch_bounds__(256) seg_merge_kernel(const __grid_constant__ 
 #pragma unroll 8
     for (int i = 0; i < n; ++i) {
       const float f = __shfl_sync(0xffffffffu, wi[j], i);
+      if (f == 0.f) continue;                      // a piece that the row sees no key of: its output was not written
       const float* x = src + (int64_t)(j * 32 + i) * p.rows * D;
       float v[CPL];
       if constexpr (CPL == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(x);

@@ -11,11 +11,19 @@
 //   warp 8       one elected thread issues every tcgen05.mma: S = Q K^T into TMEM, then O += P V with both operands in
 //                shared memory; O stays in TMEM for the whole range of keys
 //   warps 0-3    softmax of stream 0, one thread per row: S row from TMEM, exponentials against a running reference
-//   warps 4-7    maximum (exp2 domain, raised only when a row outgrows it by 2^8: exact either way), P as bf16 into shared
-//                memory; same for stream 1.  The streams' exponentials overlap each other's products.
+//   warps 4-7    maximum (exp2 domain, raised only when a row outgrows it by 2^8: exact either way), P as bf16; same for
+//                stream 1.  The streams' exponentials overlap each other's products.
+// Head dim 64: P goes back over the scores in TMEM, which holds three score buffers, so that Q K^T runs ahead of the
+// exponentials (through shared memory P would cost as many bytes again as all operands together, and that port was then
+// the bound).  Head dim 128: TMEM holds two score buffers beside the outputs; P goes through shared memory and a score
+// buffer is free as soon as it has been read.
+// Q K^T runs ahead of P V across the borders of items, so that the next item's first scores are there when the softmax warps
+// come to them.  Head dim 64 writes an item's output after the first exponentials of the next one: the wait for its last
+// product and the read of the accumulator then lie under work that is there anyway (head dim 128 has no memory left to
+// stage the output in but the P tile, which those exponentials would overwrite).
 // kAlt = false: a row tile has 256 rows; the streams are its two halves and share every key tile.
-// kAlt = true: a row tile has at most 128 rows; both streams hold the same rows and take the key tiles in turn, each with
-//   its own maximum, sum and output accumulator, and are merged in the epilogue.  The memory of the second query tile
+// kAlt = true: a row tile has at most 128 rows; both streams hold the same rows and take the key tiles in turn (over the
+//   borders of items), each with its own maximum, sum and output accumulator, and are merged in the epilogue.  The memory of the second query tile
 //   goes to the ring.
 // Rows of V behind a real length are overwritten with zeros in shared memory before the product (0 * NaN would poison the
 // row); scores behind a row's limit become -inf.
@@ -30,10 +38,10 @@ namespace swam {
 namespace {
 
 constexpr int kThreadsS = 384;
-constexpr int kDesc = 4;            // descriptors in flight
+constexpr int kDesc = 8;            // descriptors in flight
 
 // One work item as every warp sees it: tiles [0, na) are 128-key tiles of segment 0 (the first one starts at key base0), the
-// rest of segment 1 (tile i starts at key base1 + 128 i; base1 may be negative).  n = 0: no key, n < 0: no more items.
+// rest of segment 1 (tile i starts at key base1 + 128 i; base1 may be negative).  n = 0: no more items.
 struct __align__(16) SegDesc {
   int n, na, b0, h_kv;
   int row0, base0, base1, part;
@@ -45,20 +53,24 @@ struct SegCfg {
   static constexpr int DB = D / 64;                  // 64-column (128-byte) blocks per row
   static constexpr int kSub = kTile * 128;           // bytes of a [128 rows x 64 columns] block
   static constexpr int kTileBytes = DB * kSub;       // a 128 x D tile
-  static constexpr int kPBytes = 2 * kSub;           // a 128 x 128 bf16 P tile
+  static constexpr bool kPSmem = D == 128;
+  static constexpr int kPBytes = kPSmem ? 2 * kSub : 0;   // a 128 x 128 bf16 P tile
+  static constexpr int NB = kPSmem ? 2 : 3;          // score buffers in TMEM
   static constexpr int NQ = kAlt ? 1 : 2;            // query tiles of an item
   static constexpr int kRows = NQ * kTile;
   // Query buffers: with two, an item's queries arrive while the previous item still multiplies (head dim 128 has no room
   // beside three key/value slots)
-  static constexpr int QB = D == 64 ? 2 : 1;
-  static constexpr int ST = (D == 128) ? (kAlt ? 4 : 3) : (kAlt ? 8 : 6);     // ring slots: what fits beside Q and P
-  // Q K^T runs this many key tiles ahead of P V: in both forms one product of each stream is then in flight ahead
+  static constexpr int QB = kPSmem ? 1 : 2;
+  // A finished tile is staged in shared memory for its way out: in the stream's P tile, or in a tile of its own
+  static constexpr bool kDefer = !kPSmem;
+  static constexpr int kStageBytes = kPSmem ? 0 : NQ * kTileBytes;
+  static constexpr int ST = kPSmem ? (kAlt ? 4 : 3) : (kAlt ? 11 : 8);      // ring slots: what fits beside all that
+  // K_(i+LA) precedes V_i in the ring, as Q K^T precedes P V on the tensor pipe
   static constexpr int LA = kAlt ? 2 : 1;
-  static constexpr int kData = QB * NQ * kTileBytes + 2 * kPBytes + ST * kTileBytes;
-  static constexpr int kBars = 8 * (2 * QB + 2 * ST + 2 * kDesc + 15);
+  static constexpr int kData = QB * NQ * kTileBytes + 2 * kPBytes + ST * kTileBytes + kStageBytes;
+  static constexpr int kBars = 8 * (2 * QB + 2 * ST + 2 * kDesc + 2 * NB + 11);
   static constexpr int kDescOff = (kBars + 15) / 16 * 16;
   static constexpr int kTail = kDescOff + kDesc * (int)sizeof(SegDesc) + 16;
-  static constexpr int kMlOff = kTail;
   static constexpr int kBytes = kData + 1024 /*alignment*/ + kTail + (kAlt ? kTile * 8 : 0) /*maxima and sums of stream 1*/;
   static_assert(kBytes <= 227 * 1024, "shared memory");
   static constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
@@ -66,9 +78,9 @@ struct SegCfg {
 };
 
 struct SegTcArgs {
-  int box_q;        // queries come as boxes of map_q: box_tokens tokens of box_samples samples are the 128 rows of a tile
+  int box_q;        // queries come as boxes of map_q
   int box_out;      // finished tiles leave as boxes of map_o
-  int items;        // of both passes
+  int items;        // of the passes of this launch
 };
 
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, int c4) {
@@ -80,6 +92,11 @@ __device__ __forceinline__ void tma_store_5d(const CUtensorMap* map, uint32_t sr
   asm volatile("cp.async.bulk.tensor.5d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5, %6}], [%1];"
                ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
 }
+// 32 bytes in one store (a whole sector)
+__device__ __forceinline__ void st_global_32(void* dst, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
 
 template <int D, bool kAlt>
 __global__ void __launch_bounds__(kThreadsS, 1)
@@ -88,11 +105,13 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               const __grid_constant__ CUtensorMap map_k1, const __grid_constant__ CUtensorMap map_v1,
               const __grid_constant__ SegParams p, const int pass0, const SegTcArgs x) {
   using C = SegCfg<D, kAlt>;
-  constexpr int ST = C::ST, LA = C::LA, QB = C::QB;
+  constexpr int ST = C::ST, LA = C::LA, QB = C::QB, NB = C::NB;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_raw + (base - smem_addr(smem_raw));
   const uint32_t sQ = base, sP = sQ + QB * C::NQ * C::kTileBytes, sR = sP + 2 * C::kPBytes;
+  const uint32_t sStage = C::kPSmem ? sP : sR + ST * C::kTileBytes;
+  constexpr uint32_t kStageStride = C::kPSmem ? C::kPBytes : C::kTileBytes;
   const uint32_t bars = base + C::kData;
   auto bar_q = [&](int b) { return bars + 8 * b; };                          // queries have arrived
   auto bar_q_free = [&](int b) { return bars + 8 * (QB + b); };              // the item's last Q K^T has run
@@ -101,18 +120,18 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   auto bar_d_full = [&](int s) { return bars + 8 * (2 * QB + 2 * ST + s); };
   auto bar_d_empty = [&](int s) { return bars + 8 * (2 * QB + 2 * ST + kDesc + s); };
   constexpr int kB = 2 * QB + 2 * ST + 2 * kDesc;
-  auto bar_s_full = [&](int s) { return bars + 8 * (kB + s); };
-  auto bar_s_free = [&](int s) { return bars + 8 * (kB + 2 + s); };
-  auto bar_p_full = [&](int s) { return bars + 8 * (kB + 4 + s); };
-  auto bar_pv = [&](int s) { return bars + 8 * (kB + 6 + s); };
-  auto bar_stage = [&](int s) { return bars + 8 * (kB + 8 + s); };           // the staged output has been read
-  const uint32_t bar_o_final = bars + 8 * (kB + 10), bar_o_free = bars + 8 * (kB + 11);
-  const uint32_t bar_x = bars + 8 * (kB + 12);                               // kAlt: stream 1 has left its maxima and sums
-  auto bar_staged = [&](int s) { return bars + 8 * (kB + 13 + s); };         // every row of the output has been staged
+  auto bar_s_full = [&](int b) { return bars + 8 * (kB + b); };              // per score buffer
+  auto bar_p_full = [&](int b) { return bars + 8 * (kB + NB + b); };
+  auto bar_s_free = [&](int s) { return bars + 8 * (kB + 2 * NB + s); };     // per stream; head dim 128 only
+  auto bar_pv = [&](int s) { return bars + 8 * (kB + 2 * NB + 2 + s); };
+  const uint32_t bar_o_final = bars + 8 * (kB + 2 * NB + 4), bar_o_free = bars + 8 * (kB + 2 * NB + 5);
+  const uint32_t bar_x = bars + 8 * (kB + 2 * NB + 6);                       // kAlt: stream 1 has left its maxima and sums
+  auto bar_staged = [&](int s) { return bars + 8 * (kB + 2 * NB + 7 + s); }; // every row of the output has been staged
+  auto bar_stage = [&](int s) { return bars + 8 * (kB + 2 * NB + 9 + s); };  // the staged output has been read
   SegDesc* desc = reinterpret_cast<SegDesc*>(base_ptr + C::kData + C::kDescOff);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + C::kData + C::kTail - 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kData + C::kTail - 8);
-  float2* ml_x = reinterpret_cast<float2*>(base_ptr + C::kData + C::kMlOff);
+  float2* ml_x = reinterpret_cast<float2*>(base_ptr + C::kData + C::kTail);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const SegArgs& a = p.a;
@@ -130,13 +149,15 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       mbar_init(bar_d_full(s), 1);
       mbar_init(bar_d_empty(s), 11);        // producer, query warp, issuer, eight softmax warps
     }
+    for (int b = 0; b < NB; ++b) {
+      mbar_init(bar_s_full(b), 1);
+      mbar_init(bar_p_full(b), kTile);
+    }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(bar_s_full(s), 1);
       mbar_init(bar_s_free(s), kTile);
-      mbar_init(bar_p_full(s), kTile);
       mbar_init(bar_pv(s), 1);
-      mbar_init(bar_stage(s), x.box_out ? 1 : kTile);
       mbar_init(bar_staged(s), kTile);
+      mbar_init(bar_stage(s), x.box_out ? 1 : kTile);
     }
     mbar_init(bar_o_final, 1);
     mbar_init(bar_o_free, 2 * kTile);
@@ -152,8 +173,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  auto tm_S = [&](int s) { return tmem + (uint32_t)(s * kTile); };
-  auto tm_O = [&](int s) { return tmem + (uint32_t)(2 * kTile + s * D); };
+  auto tm_S = [&](int b) { return tmem + (uint32_t)(b * kTile); };
+  auto tm_O = [&](int s) { return tmem + (uint32_t)(NB * kTile + s * D); };
   // (a warp leaves its loops together: the TMEM instructions and shuffles need it converged)
   auto wait = [&](uint32_t bar, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag) ? 1 : 0) != 0;
@@ -166,57 +187,101 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_d_empty(slot));
     ++di;
-    return d.n >= 0;
+    return d.n > 0;
   };
   SegDesc d;
   int di = 0;
 
   // Every role walks through the same items; one whose rows see no key is only known to the softmax warps (they write
   // its zeros) and counts for nobody else, so all other barrier phases count the remaining items and their tiles.
-  // (setmaxnreg: 384 threads start with 168 registers each; 56 for the third warpgroup frees exactly what 224 for the
+  // (setmaxnreg: 384 threads start with 168 registers each; 40 for the third warpgroup frees exactly what 232 for the
   // other two takes)
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (warp == 11) {
       // ------------------------------------------------------------------ scheduler
-      for (int w = blockIdx.x, i = 0;; w += gridDim.x, ++i) {
+      int i = 0;
+      bool ok = true;
+      for (int w = blockIdx.x; ok && w < x.items; w += gridDim.x) {
+        const int q = pass0 == 0 && w >= p.pass[0].items ? 1 : pass0;
+        const SegPass& ps = p.pass[q];
+        const SegItem it = seg_item(ps, a.N_kv, C::kRows, q != pass0 ? w - p.pass[0].items : w);
+        const SegKeys kk = seg_keys(p, ps, it, C::kRows, kTile);
         SegDesc o;
-        o.n = -1;
-        o.na = o.b0 = o.h_kv = o.row0 = o.base0 = o.base1 = o.part = o.len0 = o.len1 = o.own = o.kv0 = 0;
-        if (w < x.items) {
-          const int q = pass0 == 0 && w >= p.pass[0].items ? 1 : pass0;
-          const SegPass& ps = p.pass[q];
-          const SegItem it = seg_item(ps, a.N_kv, C::kRows, q != pass0 ? w - p.pass[0].items : w);
-          const SegKeys kk = seg_keys(p, ps, it, C::kRows, kTile);
-          o.n = kk.end - kk.begin;
-          o.na = max(0, min(o.n, kk.n0 - kk.begin));
-          o.b0 = it.block * ps.block_samples;
-          o.h_kv = it.h_kv;
-          o.row0 = it.row0 | (q << 30);                // rows of a block stay below 2^30
-          o.base0 = kk.begin * kTile;
-          o.base1 = (kk.begin - kk.n0) * kTile;
-          o.part = ps.part0 + it.split;
-          o.len0 = kk.len0;
-          o.len1 = kk.len1;
-          o.own = o.na < o.n ? seg_len(p, 1, o.b0) : 0;
-          o.kv0 = o.b0 / a.per_group;
+        o.n = kk.end - kk.begin;
+        o.na = max(0, min(o.n, kk.n0 - kk.begin));
+        o.b0 = it.block * ps.block_samples;
+        o.h_kv = it.h_kv;
+        o.row0 = it.row0 | (q << 30);                // rows of a block stay below 2^30
+        o.base0 = kk.begin * kTile;
+        o.base1 = (kk.begin - kk.n0) * kTile;
+        o.part = ps.part0 + it.split;
+        o.len0 = kk.len0;
+        o.len1 = kk.len1;
+        o.own = o.na < o.n ? seg_len(p, 1, o.b0) : 0;
+        o.kv0 = o.b0 / a.per_group;
+        if (o.n == 0) {
+          // no key: rows of zeros (or a piece of weight 0), written here so that all other warps only meet items with keys
+          for (int r0 = 0; r0 < C::kRows; r0 += 32) {
+            const SegRow r = seg_row(p, ps.block_samples, o.b0, o.h_kv, it.row0 + r0 + lane);
+            if (!p.direct) {
+              if (r.real) p.part_ml[(int64_t)o.part * p.rows + ((int64_t)r.b * a.n_q + r.t) * a.N_h + r.h] = make_float2(-INFINITY, 0.f);
+              continue;
+            }
+            const int64_t off = r.real ? r.b * a.o_smp + r.t * a.o_tok + (int64_t)r.h * D : -1;
+            if (r.real && a.lse) a.lse[((int64_t)r.b * a.N_h + r.h) * a.n_q + r.t] = -INFINITY;
+            constexpr int CPR = D / 8, RPI = 32 / CPR;
+            for (int j = 0; j < 32 / RPI; ++j) {
+              const int64_t to = __shfl_sync(0xffffffffu, off, j * RPI + lane / CPR);
+              if (to >= 0) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + to + (lane % CPR) * 8) = make_uint4(0u, 0u, 0u, 0u);
+            }
+          }
+          continue;
         }
         const int slot = i % kDesc;
-        if (i >= kDesc && !wait(bar_d_empty(slot), ((i / kDesc) & 1) ^ 1)) break;
-        if (lane == 0) {
+        if (i >= kDesc) ok = wait(bar_d_empty(slot), ((i / kDesc) & 1) ^ 1);
+        if (ok && lane == 0) {
           desc[slot] = o;
           mbar_arrive(bar_d_full(slot));
         }
-        if (o.n < 0) break;
+        ++i;
+      }
+      const int slot = i % kDesc;
+      if (ok && i >= kDesc) ok = wait(bar_d_empty(slot), ((i / kDesc) & 1) ^ 1);
+      if (ok && lane == 0) {
+        desc[slot].n = 0;                            // the end
+        mbar_arrive(bar_d_full(slot));
       }
     } else if (warp == 10) {
-      // ------------------------------------------------------------------ query rows one by one
+      // ------------------------------------------------------------------ finished tiles, as boxes
+      if (x.box_out) {
+        int iter = 0;
+        bool ok = true;
+        while (ok && next_desc(di, d)) {
+          for (int s = 0; s < C::NQ && ok; ++s) {
+            ok = wait(bar_staged(s), iter & 1);
+            if (!ok) break;
+            const int row0 = d.row0 + s * kTile;     // (one pass of single samples: no flag in row0)
+            if (lane == 0) {
+              if (row0 < a.n_q * p.g) {
+                for (int db = 0; db < C::DB; ++db)
+                  tma_store_5d(&map_o, sStage + s * kStageStride + db * C::kSub, db * 64, 0, row0 / p.g, d.h_kv, d.b0);
+                tma_store_commit_wait();
+              }
+              mbar_arrive(bar_stage(s));
+            }
+            __syncwarp();
+          }
+          ++iter;
+        }
+      }
+      // ------------------------------------------------------------------ or query rows one by one
       constexpr int CPR = D / 8, RPI = 32 / CPR;     // 16-byte chunks per row, rows per warp instruction
       const int cc = lane % CPR, sub = lane / CPR;
       const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + cc * 8;
       int iter = 0;
-      while (next_desc(di, d)) {
-        if (d.n == 0 || x.box_q) continue;
+      while (!x.box_out && next_desc(di, d)) {
+        if (x.box_q) continue;
         const int qb = iter % QB;
         if (iter >= QB && !wait(bar_q_free(qb), ((iter / QB) & 1) ^ 1)) break;
         const int row0 = d.row0 & 0x3fffffff, block_samples = p.pass[d.row0 >> 30].block_samples;
@@ -238,175 +303,417 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       cp_async_wait_all();
     } else if (warp == 9) {
       // ------------------------------------------------------------------ TMA producer
-      int pos = 0, iter = 0;           // ring loads and items so far
-      bool ok = true;
-      while (ok && next_desc(di, d)) {
-        if (d.n == 0) continue;
-        const int n = d.n, qb = iter % QB;
-        auto load = [&](bool is_v, int i) {
-          const int st = pos % ST;
-          if (!wait(bar_empty(st), ((pos / ST) & 1) ^ 1)) return false;
-          if (lane == 0) {
-            const bool s1 = i >= d.na;
-            const CUtensorMap* m = s1 ? (is_v ? &map_v1 : &map_k1) : (is_v ? &map_v0 : &map_k0);
-            mbar_expect_tx(bar_full(st), C::kTileBytes);
-            for (int db = 0; db < C::DB; ++db)
-              tma_load_4d(sR + st * C::kTileBytes + db * C::kSub, m, bar_full(st), db * 64, (s1 ? d.base1 : d.base0) + i * kTile, d.h_kv,
-                          s1 ? d.b0 : d.kv0);
-          }
-          ++pos;
-          return true;
-        };
-        auto load_q = [&]() {
-          if (!x.box_q) return true;
-          if (iter >= QB && !wait(bar_q_free(qb), ((iter / QB) & 1) ^ 1)) return false;
-          if (lane == 0) {
-            mbar_expect_tx(bar_q(qb), C::NQ * C::kTileBytes);
-            const bool mixed = p.pass[d.row0 >> 30].block_samples > 1;
-            for (int q = 0; q < C::NQ; ++q) {
-              const int r = (d.row0 & 0x3fffffff) + q * kTile;
-              const int smp = mixed ? r / (a.n_q * p.g) : 0, tok = mixed ? 0 : r / p.g;
-              for (int db = 0; db < C::DB; ++db)
-                tma_load_5d(sQ + (qb * C::NQ + q) * C::kTileBytes + db * C::kSub, &map_q, bar_q(qb), db * 64, 0, tok, d.h_kv, d.b0 + smp);
+      // The key tiles of all items form one sequence T = 0, 1, ...; the ring holds K_0 .. K_(LA-1), then K_(T+LA), V_T for
+      // every T, in the order in which the tensor pipe takes them.  Behind the last K an empty slot takes the place of each
+      // missing one, so that V_T is always load 2 T + LA + 1.  A descriptor is released when the cursor of V leaves it.
+      int pos = 0, iter = 0;                       // ring loads and items (of K) so far
+      int ik = 0, nk = 0, iv = 0, nv = 0, dvi = 0; // next tile and tiles of the items of K (descriptor di - 1) and V (dvi - 1)
+      bool ok = true, k_end = false;
+      auto load = [&](const SegDesc& o, bool is_v, int i) {
+        const int st = pos % ST;
+        if (!wait(bar_empty(st), ((pos / ST) & 1) ^ 1)) return false;
+        if (lane == 0) {
+          const bool s1 = i >= o.na;
+          const CUtensorMap* m = s1 ? (is_v ? &map_v1 : &map_k1) : (is_v ? &map_v0 : &map_k0);
+          mbar_expect_tx(bar_full(st), C::kTileBytes);
+          for (int db = 0; db < C::DB; ++db)
+            tma_load_4d(sR + st * C::kTileBytes + db * C::kSub, m, bar_full(st), db * 64, (s1 ? o.base1 : o.base0) + i * kTile, o.h_kv,
+                        s1 ? o.b0 : o.kv0);
+        }
+        ++pos;
+        return true;
+      };
+      auto load_k = [&]() {
+        if (ik == nk && !k_end) {
+          const int slot = di % kDesc;
+          if (!wait(bar_d_full(slot), (di / kDesc) & 1)) return false;
+          ++di;
+          ik = 0;
+          nk = desc[slot].n;
+          k_end = nk == 0;
+          if (!k_end && x.box_q) {
+            // the item's queries: with one buffer they wait for the previous item's last Q K^T, which frees the slot of its
+            // last K tile at the same moment
+            const int qb = iter % QB;
+            if (iter >= QB && !wait(bar_q_free(qb), ((iter / QB) & 1) ^ 1)) return false;
+            if (lane == 0) {
+              const SegDesc& o = desc[slot];
+              mbar_expect_tx(bar_q(qb), C::NQ * C::kTileBytes);
+              const bool mixed = p.pass[o.row0 >> 30].block_samples > 1;
+              for (int q = 0; q < C::NQ; ++q) {
+                const int r = (o.row0 & 0x3fffffff) + q * kTile;
+                const int smp = mixed ? r / (a.n_q * p.g) : 0, tok = mixed ? 0 : r / p.g;
+                for (int db = 0; db < C::DB; ++db)
+                  tma_load_5d(sQ + (qb * C::NQ + q) * C::kTileBytes + db * C::kSub, &map_q, bar_q(qb), db * 64, 0, tok, o.h_kv, o.b0 + smp);
+              }
             }
           }
-          return true;
-        };
-        // With one query buffer the queries must wait for the previous item's last Q K^T; the ring's free slots are filled
-        // before that wait.
-        const int q_after = iter < QB || QB > 1 ? -1 : min(ST, 2 * n) - 1;
-        int m = 0;
-        if (q_after < 0) ok = load_q();
-        for (int i = 0; i < n + LA && ok; ++i) {
-          if (i < n) {
-            ok = load(false, i);
-            if (ok && m++ == q_after) ok = load_q();
-          }
-          if (ok && i >= LA) {
-            ok = load(true, i - LA);
-            if (ok && m++ == q_after) ok = load_q();
-          }
+          ++iter;
         }
-        ++iter;
+        if (!k_end) return load(desc[(di - 1) % kDesc], false, ik++);
+        const int st = pos % ST;
+        if (!wait(bar_empty(st), ((pos / ST) & 1) ^ 1)) return false;
+        if (lane == 0) mbar_arrive(bar_full(st));
+        ++pos;
+        return true;
+      };
+      for (int j = 0; j < LA && ok; ++j) ok = load_k();
+      while (ok) {
+        if (iv == nv) {
+          if (dvi > 0) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_d_empty((dvi - 1) % kDesc));
+          }
+          // (K is a tile ahead at least, so an item that V could enter has been entered by K)
+          if (dvi == di - (k_end ? 1 : 0)) break;
+          nv = desc[dvi % kDesc].n;
+          ++dvi;
+          iv = 0;
+        }
+        ok = load_k();
+        if (ok) ok = load(desc[(dvi - 1) % kDesc], true, iv++);
       }
     } else {
       // ------------------------------------------------------------------ MMA issuer (warp converged, one lane issues)
       const uint32_t el = elect_one();
       const uint32_t q_lo = desc_lo(sQ, 16), p_lo = desc_lo(sP, 16), k_lo = desc_lo(sR, 16), v_lo = desc_lo(sR, C::kSub);
-      bool ok = true;
-      int pos = 0, iter = 0;
-      int qk_n0 = 0, qk_n1 = 0, pv_n0 = 0, pv_n1 = 0;   // products issued so far per stream
-      while (ok && next_desc(di, d)) {
-        const int n = d.n, qb = iter % QB;
-        if (n == 0) continue;
-        ok = wait(bar_q(qb), (iter / QB) & 1);
-        if (!ok) break;
-        if (!x.box_q) fence_proxy_async();
-        auto qk = [&](int i) {
-          const int st = pos % ST;
-          if (!wait(bar_full(st), (pos / ST) & 1)) return false;
+      auto issue_qk = [&](int qt, int buf, int st) {
+        const uint32_t a_lo = q_lo + ((uint32_t)(qt * C::kTileBytes) >> 4), b_lo = k_lo + ((uint32_t)(st * C::kTileBytes) >> 4);
+        mma_ss<false>(tm_S(buf), a_lo, b_lo, kDescHi, C::kIdescQK, el);
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            if (kAlt && (i & 1) != s) continue;
-            int& cnt = s ? qk_n1 : qk_n0;
-            if (cnt > 0 && !wait(bar_s_free(s), (cnt - 1) & 1)) return false;
-            ++cnt;
-            tc_fence_after();
-            const uint32_t a_lo = q_lo + ((uint32_t)((qb * C::NQ + (kAlt ? 0 : s)) * C::kTileBytes) >> 4);
-            const uint32_t b_lo = k_lo + ((uint32_t)(st * C::kTileBytes) >> 4);
-            mma_ss<false>(tm_S(s), a_lo, b_lo, kDescHi, C::kIdescQK, el);
-#pragma unroll
-            for (int ks = 1; ks < D / 16; ++ks) {
-              constexpr int kSub16 = C::kSub >> 4;
-              const uint32_t off = (uint32_t)((ks >> 2) * kSub16 + (ks & 3) * 2);
-              mma_ss<true>(tm_S(s), a_lo + off, b_lo + off, kDescHi, C::kIdescQK, el);
-            }
-            tc_commit(bar_s_full(s), el);
-          }
-          tc_commit(bar_empty(st), el);
-          if (i == n - 1) tc_commit(bar_q_free(qb), el);     // the queries have been read for the last time
-          ++pos;
-          return true;
-        };
-        auto pv = [&](int i) {
-          const int st = pos % ST;
-          if (!wait(bar_full(st), (pos / ST) & 1)) return false;
-          // the first product of an item overwrites the accumulators: the previous item's epilogue must have read them
-          if (i == 0 && iter > 0 && !wait(bar_o_free, (iter - 1) & 1)) return false;
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            if (kAlt && (i & 1) != s) continue;
-            int& cnt = s ? pv_n1 : pv_n0;
-            if (!wait(bar_p_full(s), cnt & 1)) return false;
-            ++cnt;
-            tc_fence_after();
-            const uint32_t a_lo = p_lo + ((uint32_t)(s * C::kPBytes) >> 4), b_lo = v_lo + ((uint32_t)(st * C::kTileBytes) >> 4);
-            mma_ss_rt(tm_O(s), a_lo, b_lo, kDescHi, C::kIdescPV, (kAlt ? i > 1 : i > 0) ? 1u : 0u, el);
-#pragma unroll
-            for (int k = 1; k < kTile / 16; ++k) {
-              constexpr int kSub16 = C::kSub >> 4;
-              mma_ss_rt(tm_O(s), a_lo + (uint32_t)((k >> 2) * kSub16 + (k & 3) * 2), b_lo + k * (2048 >> 4), kDescHi, C::kIdescPV, 1u, el);
-            }
-            tc_commit(bar_pv(s), el);
-          }
-          tc_commit(bar_empty(st), el);
-          ++pos;
-          return true;
-        };
-        for (int i = 0; i < n + LA && ok; ++i) {
-          if (i < n) ok = qk(i);
-          if (ok && i >= LA) ok = pv(i - LA);
+        for (int ks = 1; ks < D / 16; ++ks) {
+          constexpr int kSub16 = C::kSub >> 4;
+          const uint32_t off = (uint32_t)((ks >> 2) * kSub16 + (ks & 3) * 2);
+          mma_ss<true>(tm_S(buf), a_lo + off, b_lo + off, kDescHi, C::kIdescQK, el);
         }
-        if (ok) tc_commit(bar_o_final, el);
-        ++iter;
+        tc_commit(bar_s_full(buf), el);
+      };
+      auto issue_pv = [&](int s, int buf, int st, bool accum) {
+        const uint32_t b_lo = v_lo + ((uint32_t)(st * C::kTileBytes) >> 4);
+        if constexpr (C::kPSmem) {
+          const uint32_t a_lo = p_lo + ((uint32_t)(s * C::kPBytes) >> 4);
+          mma_ss_rt(tm_O(s), a_lo, b_lo, kDescHi, C::kIdescPV, accum ? 1u : 0u, el);
+#pragma unroll
+          for (int k = 1; k < kTile / 16; ++k) {
+            constexpr int kSub16 = C::kSub >> 4;
+            mma_ss_rt(tm_O(s), a_lo + (uint32_t)((k >> 2) * kSub16 + (k & 3) * 2), b_lo + k * (2048 >> 4), kDescHi, C::kIdescPV, 1u, el);
+          }
+        } else {
+          mma_ts(tm_O(s), tm_S(buf), b_lo, kDescHi, C::kIdescPV, accum ? 1u : 0u, el);
+#pragma unroll
+          for (int k = 1; k < kTile / 16; ++k) mma_ts(tm_O(s), tm_S(buf) + k * 8, b_lo + k * (2048 >> 4), kDescHi, C::kIdescPV, 1u, el);
+        }
+        tc_commit(bar_pv(s), el);
+      };
+      // The tiles of all items form one sequence for Q K^T, which runs ahead over the borders of items, and for P V behind it.
+      // Every wait below ends without anything that this warp would have to issue first: the next item's queries are
+      // loaded when this one's last Q K^T has run, and a score buffer is free when its scores have been read.
+      bool ok = true, k_end = false;
+      int pos = 0;                                  // ring slots taken so far
+      int kn = 0, ki = 0, kiter = -1;               // item of Q K^T: tiles, next tile, number
+      int vn = 0, vi = 0, viter = -1;               // item of P V
+      int nq0 = 0, nq1 = 0, nq2 = 0, n_nq = 0;      // tiles of the items that Q K^T has entered and P V has not
+      int qk_c0 = 0, qk_c1 = 0, pv_c0 = 0, pv_c1 = 0;   // products issued so far per stream
+      int qk_u = 0, pv_u = 0;                       // and in all (they choose the score buffer at head dim 64)
+      int k_st = 0;                                 // slot of the current K tile
+      // makes (kn, ki) the next tile of Q K^T and takes its ring slot; false at the end
+      auto next_k = [&]() {
+        if (ki == kn && !k_end) {
+          const int slot = di % kDesc;
+          ok = wait(bar_d_full(slot), (di / kDesc) & 1);
+          if (!ok) return false;
+          kn = desc[slot].n;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_d_empty(slot));
+          ++di;
+          ki = 0;
+          k_end = kn == 0;
+        }
+        if (k_end) {
+          // the empty slot in the place of a missing K
+          const int st = pos % ST;
+          ok = wait(bar_full(st), (pos / ST) & 1);
+          if (lane == 0) mbar_arrive(bar_empty(st));
+          ++pos;
+          return false;
+        }
+        if (ki == 0) {
+          ++kiter;
+          if (n_nq == 0) nq0 = kn;
+          else if (n_nq == 1) nq1 = kn;
+          else nq2 = kn;
+          ++n_nq;
+          ok = wait(bar_q(kiter % QB), (kiter / QB) & 1);
+          if (!ok) return false;
+          if (!x.box_q) fence_proxy_async();
+        }
+        k_st = pos % ST;
+        ok = wait(bar_full(k_st), (pos / ST) & 1);
+        ++pos;
+        return ok;
+      };
+      // Q K^T of the current K tile and stream s; `last` releases the tile (and with the item's last tile the queries)
+      auto qk = [&](int s, bool last) {
+        if constexpr (C::kPSmem) {
+          const int cnt = s ? qk_c1 : qk_c0;
+          if (cnt > 0) ok = wait(bar_s_free(s), (cnt - 1) & 1);
+          if (!ok) return;
+          if (s) ++qk_c1; else ++qk_c0;
+        }
+        tc_fence_after();
+        issue_qk((kiter % QB) * C::NQ + (kAlt ? 0 : s), C::kPSmem ? s : qk_u % NB, k_st);
+        ++qk_u;
+        if (last) {
+          tc_commit(bar_empty(k_st), el);
+          if (++ki == kn) tc_commit(bar_q_free(kiter % QB), el);
+        }
+      };
+      int v_st = 0;
+      // (Q K^T is a tile ahead at least: an item that P V could enter has been entered by it)
+      auto v_left = [&]() { return ok && (vi < vn || n_nq > 0); };
+      // makes (vn, vi) the next tile of P V and takes its ring slot
+      auto next_v = [&]() {
+        if (vi == vn) {
+          vn = nq0;
+          nq0 = nq1;
+          nq1 = nq2;
+          --n_nq;
+          vi = 0;
+          ++viter;
+        }
+        v_st = pos % ST;
+        ok = wait(bar_full(v_st), (pos / ST) & 1);
+        ++pos;
+        // the first product of an item overwrites the accumulators: the previous item's must have been read
+        if (ok && vi == 0 && viter > 0) ok = wait(bar_o_free, (viter - 1) & 1);
+        return ok;
+      };
+      auto pv = [&](int s, bool last) {
+        if constexpr (C::kPSmem) {
+          ok = wait(bar_p_full(s), (s ? pv_c1 : pv_c0) & 1);
+          if (s) ++pv_c1; else ++pv_c0;
+        } else {
+          ok = wait(bar_p_full(pv_u % NB), (pv_u / NB) & 1);
+        }
+        if (!ok) return;
+        tc_fence_after();
+        issue_pv(s, pv_u % NB, v_st, kAlt ? vi > 1 : vi > 0);
+        ++pv_u;
+        if (last) {
+          tc_commit(bar_empty(v_st), el);
+          if (++vi == vn) tc_commit(bar_o_final, el);
+        }
+      };
+      // the tensor pipe runs one thread's instructions in order
+      if constexpr (!kAlt && C::kPSmem) {
+        // S(T+1) of both streams, then O += P(T) V(T) of both
+        if (next_k()) qk(0, false), qk(1, true);
+        while (v_left()) {
+          if (next_k()) qk(0, false), qk(1, true);
+          if (!ok || !next_v()) break;
+          pv(0, false);
+          if (ok) pv(1, true);
+        }
+      } else if constexpr (!kAlt) {
+        // three units (a tile of one stream) ahead: P V of a unit frees the score buffer that the Q K^T behind it takes
+        if (next_k()) qk(0, false), qk(1, true);
+        bool half = v_left() && next_k();           // stream 0 of a tile is out, stream 1 is not
+        if (half) qk(0, false);
+        while (v_left() && next_v()) {
+          pv(0, false);
+          if (ok && half) qk(1, true);
+          if (ok) pv(1, true);
+          half = v_left() && next_k();
+          if (half) qk(0, false);
+        }
+      } else {
+        auto qk_alt = [&]() {
+          if (!next_k()) return;
+          if (qk_u & 1) qk(1, true);
+          else qk(0, true);
+        };
+        auto pv_alt = [&]() {
+          if (pv_u & 1) pv(1, true);
+          else pv(0, true);
+        };
+        qk_alt();
+        if (ok) qk_alt();
+        if constexpr (C::kPSmem) {
+          while (v_left()) {
+            qk_alt();
+            if (!ok || !next_v()) break;
+            pv_alt();
+          }
+        } else {
+          if (v_left()) qk_alt();
+          while (v_left() && next_v()) {
+            pv_alt();
+            if (v_left()) qk_alt();
+          }
+        }
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
     // ------------------------------------------------------------------ softmax: one thread per row and stream
     const int s = warp >> 2;                     // stream
     const int r = (warp & 3) * 32 + lane;        // row inside the tile == TMEM lane
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t tS = tm_S(s) + lane_off, tO = tm_O(s) + lane_off;
+    const uint32_t tO = tm_O(s) + lane_off;
     const uint32_t p_row = sP + (uint32_t)(s * C::kPBytes + r * 128);
     bool ok = true;
-    int iter = 0, cnt = 0, pos0 = 0;             // items; tiles of this stream; ring loads before the current item
-    int staged = 0;                              // outputs staged in this stream's P tile so far
+    int iter = 0, cnt = 0, pos0 = 0, u0 = 0;     // items; tiles of this stream; tiles and units of finished items
+    // the finished item whose output is still in the accumulators
+    bool pend = false, pend_real = false, pend_warp = false;
+    int pend_row = 0, pend_part = 0;             // row in the order (sample, query, head)
+    int pend_lse = 0;                            // and in the order (sample, head, query)
+    int staged = 0;                              // outputs staged so far
+    const uint32_t stage = sStage + (uint32_t)(s * kStageStride + r * 128);
+    float pend_m = 0.f, pend_l = 0.f;
+    // Writes one row: accumulators times their weights; an accumulator of weight 0 may hold anything.
+    auto flush = [&]() {
+      pend = false;
+      if (kAlt && s == 1) return true;           // stream 0 writes for both
+      if (!wait(bar_o_final, (iter - 1) & 1)) return false;
+      if (p.direct && staged > 0 && !wait(bar_stage(s), (staged - 1) & 1)) return false;     // (a stream may have had no tile)
+      float m = pend_m, l = pend_l, f0 = m == -INFINITY ? 0.f : 1.f, f1 = 0.f;
+      if constexpr (kAlt) {
+        if (!wait(bar_x, (iter - 1) & 1)) return false;
+        const float2 x1 = ml_x[r];
+        const float mm = fmaxf(m, x1.x);
+        f0 = m == -INFINITY ? 0.f : ex2(m - mm);
+        f1 = x1.x == -INFINITY ? 0.f : ex2(x1.x - mm);
+        l = f0 * l + f1 * x1.y;
+        m = mm;
+      }
+      tc_fence_after();
+      if (pend_warp) {
+        if (p.direct) {
+          const float inv = l > 0.f ? 1.f / l : 0.f;
+          f0 *= inv;
+          f1 *= inv;
+          if (pend_real && a.lse) a.lse[pend_lse] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        }
+        const int64_t pr = (int64_t)pend_part * p.rows + pend_row;
+        if (!p.direct && pend_real) p.part_ml[pr] = make_float2(m, l);
+        const bool any_empty = __any_sync(0xffffffffu, f0 == 0.f);
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          float ov[32];
+          __syncwarp();
+          tmem_ld32(tO + c * 32, ov);
+          tmem_ld_wait();
+          if (any_empty) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) ov[j] = f0 != 0.f ? ov[j] : 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) ov[j] *= f0;
+          if constexpr (kAlt) {
+            float o1[32];
+            tmem_ld32(tm_O(1) + lane_off + c * 32, o1);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) ov[j] = f1 != 0.f ? fmaf(o1[j], f1, ov[j]) : ov[j];
+          }
+          if (p.direct) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int c16 = c * 4 + q;
+              st_shared_16(stage + (uint32_t)((c16 >> 3) * C::kSub + (((c16 & 7) ^ (r & 7)) << 4)), pack_bf16x2(ov[q * 8 + 0], ov[q * 8 + 1]),
+                           pack_bf16x2(ov[q * 8 + 2], ov[q * 8 + 3]), pack_bf16x2(ov[q * 8 + 4], ov[q * 8 + 5]),
+                           pack_bf16x2(ov[q * 8 + 6], ov[q * 8 + 7]));
+            }
+          } else if (pend_real) {
+            uint32_t w[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) w[j] = __float_as_uint(ov[j]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) st_global_32((unsigned char*)(p.part_o + pr * D) + c * 128 + q * 32, w + q * 8);
+          }
+        }
+      }
+      tc_fence_before();
+      mbar_arrive(bar_o_free);                   // the accumulators have been read
+      if (p.direct) {
+        // the staged tile leaves as a box, or row by row with 16-byte stores, a row or two per instruction
+        if (x.box_out) {
+          fence_proxy_async();
+          mbar_arrive(bar_staged(s));            // warp 10 sends it
+        } else {
+          __syncwarp();
+          constexpr int CPR = D / 8, RPI = 32 / CPR;
+          const int cc = lane % CPR, sub = lane / CPR;
+          const int row = pend_real ? pend_row : -1;
+          const unsigned char* src = base_ptr + (sStage - base) + s * kStageStride + (cc >> 3) * C::kSub + (warp & 3) * 32 * 128;
+#pragma unroll 4
+          for (int i = 0; i < 32 / RPI; ++i) {
+            const int rl = i * RPI + sub;
+            const int o = __shfl_sync(0xffffffffu, row, rl);
+            const int bt = o / a.N_h, h = o - bt * a.N_h, b = bt / a.n_q, t = bt - b * a.n_q;
+            if (o >= 0)
+              *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + b * a.o_smp + t * a.o_tok + (int64_t)h * D + cc * 8) =
+                  *reinterpret_cast<const uint4*>(src + rl * 128 + (((cc & 7) ^ (rl & 7)) << 4));
+          }
+          __syncwarp();
+          mbar_arrive(bar_stage(s));
+        }
+        ++staged;
+      }
+      return true;
+    };
     while (ok && next_desc(di, d)) {
-      const int n = d.n;
+      const int n = d.n, na = d.na, part = d.part;
       const int row0 = (d.row0 & 0x3fffffff) + (kAlt ? 0 : s * kTile);       // of the stream's tile
       const SegRow row = seg_row(p, p.pass[d.row0 >> 30].block_samples, d.b0, d.h_kv, row0 + r);
-      const bool warp_real = __any_sync(0xffffffffu, row.real);
-      const int lim1 = seg_limit1(a, d.own, row.t);
+      const int grow = (row.b * a.n_q + row.t) * a.N_h + row.h;
+      const bool row_real = row.real, warp_real = __any_sync(0xffffffffu, row_real);
+      // real keys ahead of each segment's first tile in this item, and those of segment 1 that this row sees; does the
+      // segment's tensor go on behind them
+      const int real0 = d.len0 - d.base0, real1 = d.len1 - d.base1, sees1 = seg_limit1(a, d.own, row.t) - d.base1;
+      const bool more0 = d.len0 < a.n[0], more1 = d.len1 < a.n[1];
       float m_used = -INFINITY, l_run = 0.f;
       bool any_key = false;
-      for (int i = kAlt ? s : 0; i < n; i += kAlt ? 2 : 1, ++cnt) {
-        ok = wait(bar_s_full(s), cnt & 1);
+      const int i0 = kAlt ? (s ^ pos0) & 1 : 0;                  // the stream's first tile of the item
+      for (int i = i0; i < n; i += kAlt ? 2 : 1, ++cnt) {
+        const int g = u0 + (kAlt ? i : 2 * i + s), buf = C::kPSmem ? s : g % NB;
+        const uint32_t tS = tm_S(buf) + lane_off;
+        ok = wait(bar_s_full(buf), (C::kPSmem ? cnt : g / NB) & 1);
         if (!ok) break;
-        const bool s1 = i >= d.na;
-        const int key0 = (s1 ? d.base1 : d.base0) + i * kTile;
-        const int real = (s1 ? d.len1 : d.len0) - key0;      // real keys of this tile
+        const bool s1 = i >= na;
+        const int real = (s1 ? real1 : real0) - i * kTile;      // real keys of this tile
         tc_fence_after();
         if (!warp_real) {
           // rows behind the last one: nothing is computed, the barriers are kept in step (what their P rows hold only
           // reaches their own accumulator rows, which nobody reads)
-          mbar_arrive(bar_s_free(s));
-          if (cnt > 0) ok = wait(bar_pv(s), (cnt - 1) & 1);       // no warp runs a phase ahead of the others
-          if (!ok) break;
+          if constexpr (C::kPSmem) {
+            mbar_arrive(bar_s_free(s));
+            if (cnt > 0) ok = wait(bar_pv(s), (cnt - 1) & 1);       // no warp runs a phase ahead of the others
+            if (!ok) break;
+          }
         } else {
           float sv[kTile];
+          auto load_scores = [&]() {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<float(*)[32]>(&sv[c * 32]));
-          tmem_ld_wait();
-          tc_fence_before();
-          mbar_arrive(bar_s_free(s));             // the scores are in registers
-          const int valid = s1 ? lim1 - key0 : real;
-          if (valid < kTile) {
-#pragma unroll
-            for (int c = 0; c < kTile; ++c)
-              if (c >= valid) sv[c] = -INFINITY;
+            for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<float(*)[32]>(&sv[c * 32]));
+            tmem_ld_wait();
+          };
+          load_scores();
+          if constexpr (C::kPSmem) {
+            tc_fence_before();
+            mbar_arrive(bar_s_free(s));           // the scores are in registers
           }
-          if (i == (kAlt ? s : 0)) {
+          const int valid = s1 ? sees1 - i * kTile : real;
+          auto mask_tail = [&]() {
+            if (valid < kTile) {
+#pragma unroll
+              for (int c = 0; c < kTile; ++c)
+                if (c >= valid) sv[c] = -INFINITY;
+            }
+          };
+          mask_tail();
+          const bool first = i == i0;
+          if (first) {
             // the first tile fixes the row's reference maximum.  A row that sees none of its keys sees no later key
             // either (limits are a prefix of segment 1, and segment 0 has no limits below its length).
             any_key = valid > 0;
@@ -421,20 +728,24 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             m_used = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])), fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7]))) * p.scale_log2;
             if (!any_key) m_used = 0.f;
           }
-          if (cnt > 0) {
-            // the P tile is free once the stream's previous product has read it, and the previous item's staged output
-            // has left it
+          if (C::kPSmem && cnt > 0) {
+            // the P tile is free once the stream's previous product has read it, and the previous item's output has left it
             ok = wait(bar_pv(s), (cnt - 1) & 1);
-            if (ok && staged > 0 && i == (kAlt ? s : 0)) ok = wait(bar_stage(s), (staged - 1) & 1);
+            if (ok && first && staged > 0) ok = wait(bar_stage(s), (staged - 1) & 1);
             if (!ok) break;
           }
           const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), negm2 = pack2(-m_used, -m_used);
           uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
+          // 32 probabilities of the row, part c of four
           auto store_p16 = [&](int c, const uint32_t* v) {
+            if constexpr (C::kPSmem) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int c16 = c * 4 + q;
-              st_shared_16(p_row + (uint32_t)((c16 >> 3) * C::kSub + (((c16 & 7) ^ (r & 7)) << 4)), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+              for (int q = 0; q < 4; ++q) {
+                const int c16 = c * 4 + q;
+                st_shared_16(p_row + (uint32_t)((c16 >> 3) * C::kSub + (((c16 & 7) ^ (r & 7)) << 4)), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+              }
+            } else {
+              tmem_st16(tS + c * 16, v);
             }
           };
           uint32_t pk[64];
@@ -452,14 +763,26 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             }
             acc2[j & 3] = add2(acc2[j & 3], pack2(p0, p1));
             pk[j] = pack_bf16x2(p0, p1);
-            if ((j & 15) == 15) store_p16(j >> 4, &pk[j - 15]);
+            if (C::kPSmem && (j & 15) == 15) store_p16(j >> 4, &pk[j - 15]);
           }
           float sum, a0, a1;
           unpack2(add2(add2(acc2[0], acc2[1]), add2(acc2[2], acc2[3])), a0, a1);
           sum = a0 + a1;
           const bool grew = !(sum <= 256.f * 128.f);           // some exponent above 2^8; also inf and NaN
-          if (__any_sync(0xffffffffu, grew)) {
+          const bool redo = __any_sync(0xffffffffu, grew);
+          if constexpr (!C::kPSmem) {
+            // P overwrites the scores only now that the pass is known to stand
+            if (!redo) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) store_p16(c, &pk[c * 16]);
+            }
+          }
+          if (redo) {
             // rare: raise the reference to the row's maximum, rescale O, repeat the pass
+            if constexpr (!C::kPSmem) {
+              load_scores();
+              mask_tail();
+            }
             float mraw = sv[0];
 #pragma unroll
             for (int c = 1; c < kTile; ++c) mraw = fmaxf(mraw, sv[c]);
@@ -467,7 +790,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             const float f = ex2(-delta);
             m_used += delta;
             l_run *= f;
-            if (i >= (kAlt ? 2 : 1)) {            // the previous product is complete (waited for above)
+            if (!first) {
+              // the accumulator must hold every product issued against the old reference
+              if (!C::kPSmem) ok = wait(bar_pv(s), (cnt - 1) & 1);
+              if (!ok) break;
               tc_fence_after();
 #pragma unroll
               for (int c = 0; c < D / 32; ++c) {
@@ -479,7 +805,6 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 for (int j = 0; j < 32; ++j) ou[j] = __float_as_uint(ov[j] * f);
                 tmem_st32(tO + c * 32, ou);
               }
-              tmem_st_wait();
             }
             sum = 0.f;
 #pragma unroll
@@ -496,163 +821,54 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             }
           }
           l_run += sum;
+          tmem_st_wait();
         }
-        // a tile that ends inside: rows of V behind the last real key become zeros.  One stream does it for both (the
-        // issuer waits for stream 0's P before either product).
-        if (real < kTile && (kAlt || s == 0)) {
-          const int vpos = pos0 + min(n, i + LA + 1) + i, st = vpos % ST;      // loads before V_i: K_0 .. K_(i+LA), V_0 .. V_(i-1)
-          ok = wait(bar_full(st), (vpos / ST) & 1);
+        // a tile that ends inside its tensor: rows of V behind the last real key become zeros (what lies behind the tensor
+        // arrives as zeros).  One stream does it for both: the issuer waits for stream 0's P before either product.
+        if (real < kTile && (kAlt || s == 0) && (s1 ? more1 : more0)) {
+          const int T = pos0 + i, pos = 2 * T + LA + 1, st = pos % ST;
+          ok = wait(bar_full(st), (pos / ST) & 1);
           if (!ok) break;
           if (r >= real) {
+#pragma unroll
             for (int c = 0; c < D / 8; ++c)
-              st_shared_16(sR + (uint32_t)(st * C::kTileBytes + (c >> 3) * C::kSub + r * 128 + ((c & 7) << 4)), 0u, 0u, 0u, 0u);
+              st_shared_16(sR + (uint32_t)(st * C::kTileBytes + (c >> 3) * C::kSub + r * 128 + (((c & 7) ^ (r & 7)) << 4)), 0u, 0u, 0u, 0u);
           }
+          fence_proxy_async();
         }
         tc_fence_before();
-        fence_proxy_async();                      // P and zeroed V rows: generic stores that the tensor core will read
-        mbar_arrive(bar_p_full(s));
+        if constexpr (C::kPSmem) fence_proxy_async();     // P is a generic store that the tensor core will read
+        mbar_arrive(bar_p_full(buf));
+        if (C::kDefer && pend) {
+          ok = flush();
+          if (!ok) break;
+        }
       }
       if (!ok) break;
-      if (n > 0) {
-        ok = wait(bar_o_final, iter & 1);
+      if (C::kDefer && pend) ok = flush();       // kAlt, stream 1: an item of one tile
+      if (!ok) break;
+      pend = true;
+      pend_real = row_real;
+      pend_warp = warp_real;
+      pend_m = any_key ? m_used : -INFINITY;
+      pend_l = any_key ? l_run : 0.f;
+      pend_row = grow;
+      pend_part = part;
+      pend_lse = (row.b * a.N_h + row.h) * a.n_q + row.t;
+      if (kAlt && s == 1) {
+        // stream 0 has read the previous item's values
+        if (iter > 0) ok = wait(bar_o_free, (iter - 1) & 1);
         if (!ok) break;
-        tc_fence_after();
+        ml_x[r] = make_float2(pend_m, pend_l);
+        mbar_arrive(bar_x);
+        mbar_arrive(bar_o_free);
       }
-      if (!any_key) {
-        m_used = -INFINITY;
-        l_run = 0.f;
-      }
-      // epilogue.  kAlt = true: stream 0 finishes the rows from both accumulators (same TMEM lanes, other columns)
-      float f0 = any_key ? 1.f : 0.f, f1 = 0.f;   // weights of the accumulators; one of weight 0 may hold anything
-      float m_all = m_used, l_all = l_run;
-      if (kAlt && n > 0) {
-        if (s == 1) {
-          // stream 0 has read the previous item's values
-          if (iter > 0) ok = wait(bar_o_free, (iter - 1) & 1);
-          if (!ok) break;
-          ml_x[r] = make_float2(m_used, l_run);
-          mbar_arrive(bar_x);
-        } else {
-          ok = wait(bar_x, iter & 1);
-          if (!ok) break;
-          const float2 x1 = ml_x[r];
-          m_all = fmaxf(m_used, x1.x);
-          f0 = m_used == -INFINITY ? 0.f : ex2(m_used - m_all);
-          f1 = x1.x == -INFINITY ? 0.f : ex2(x1.x - m_all);
-          l_all = f0 * l_run + f1 * x1.y;
-        }
-      }
-      const bool writes = !kAlt || s == 0;        // this stream's warps write the item's rows
-      const int64_t gr = ((int64_t)row.b * a.n_q + row.t) * a.N_h + row.h;
-      if (writes && p.direct) {
-        // the finished rows are staged in the stream's P tile (its last product is complete) and leave as a box, or row by
-        // row with 16-byte stores, a row or two per instruction
-        if (staged > 0 && n == 0) {               // otherwise waited for before the item's first P
-          ok = wait(bar_stage(s), (staged - 1) & 1);
-          if (!ok) break;
-        }
-        const float inv = l_all > 0.f ? 1.f / l_all : 0.f;
-        f0 *= inv;
-        f1 *= inv;
-        const uint32_t stage = sP + (uint32_t)(s * C::kPBytes + r * 128);
-        if (warp_real) {
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            float ov[32];
-            tmem_ld32(tO + c * 32, ov);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) ov[j] = f0 != 0.f ? ov[j] * f0 : 0.f;
-            if constexpr (kAlt) {
-              float o1[32];
-              tmem_ld32(tm_O(1) + lane_off + c * 32, o1);
-              tmem_ld_wait();
-#pragma unroll
-              for (int j = 0; j < 32; ++j) ov[j] += f1 != 0.f ? o1[j] * f1 : 0.f;
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int c16 = c * 4 + q;
-              st_shared_16(stage + (uint32_t)((c16 >> 3) * C::kSub + (((c16 & 7) ^ (r & 7)) << 4)), pack_bf16x2(ov[q * 8 + 0], ov[q * 8 + 1]),
-                           pack_bf16x2(ov[q * 8 + 2], ov[q * 8 + 3]), pack_bf16x2(ov[q * 8 + 4], ov[q * 8 + 5]),
-                           pack_bf16x2(ov[q * 8 + 6], ov[q * 8 + 7]));
-            }
-          }
-          if (row.real && a.lse)
-            a.lse[((int64_t)row.b * a.N_h + row.h) * a.n_q + row.t] = l_all > 0.f ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
-        }
-        if (n > 0) {
-          tc_fence_before();
-          mbar_arrive(bar_o_free);                // the accumulators have been read
-        }
-        if (x.box_out) {
-          fence_proxy_async();
-          mbar_arrive(bar_staged(s));
-          if ((warp & 3) == 0) ok = wait(bar_staged(s), staged & 1);
-          if (!ok) break;
-          if ((warp & 3) == 0 && lane == 0) {
-            if (row0 < a.n_q * p.g) {
-              for (int db = 0; db < C::DB; ++db)
-                tma_store_5d(&map_o, sP + s * C::kPBytes + db * C::kSub, db * 64, 0, row0 / p.g, d.h_kv, d.b0);
-              tma_store_commit_wait();
-            }
-            mbar_arrive(bar_stage(s));
-          }
-        } else {
-          __syncwarp();
-          constexpr int CPR = D / 8, RPI = 32 / CPR;
-          const int cc = lane % CPR, sub = lane / CPR;
-          const int64_t off = row.real ? row.b * a.o_smp + row.t * a.o_tok + (int64_t)row.h * D : -1;
-          const unsigned char* src = base_ptr + (sP - base) + s * C::kPBytes + (cc >> 3) * C::kSub + (warp & 3) * 32 * 128;
-#pragma unroll 4
-          for (int i = 0; i < 32 / RPI; ++i) {
-            const int rl = i * RPI + sub;
-            const int64_t o = __shfl_sync(0xffffffffu, off, rl);
-            if (o >= 0)
-              *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + o + cc * 8) =
-                  *reinterpret_cast<const uint4*>(src + rl * 128 + (((cc & 7) ^ (rl & 7)) << 4));
-          }
-          __syncwarp();
-          mbar_arrive(bar_stage(s));
-        }
-        ++staged;
-      } else {
-        if (writes && warp_real) {
-          const int64_t pr = (int64_t)d.part * p.rows + gr;
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            float ov[32];
-            __syncwarp();
-            tmem_ld32(tO + c * 32, ov);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) ov[j] = f0 != 0.f ? ov[j] * f0 : 0.f;
-            if constexpr (kAlt) {
-              float o1[32];
-              tmem_ld32(tm_O(1) + lane_off + c * 32, o1);
-              tmem_ld_wait();
-#pragma unroll
-              for (int j = 0; j < 32; ++j) ov[j] += f1 != 0.f ? o1[j] * f1 : 0.f;
-            }
-            if (row.real) {
-              float* dst = p.part_o + pr * D + c * 32;
-#pragma unroll
-              for (int q = 0; q < 8; ++q)
-                *reinterpret_cast<float4*>(dst + q * 4) = make_float4(ov[q * 4], ov[q * 4 + 1], ov[q * 4 + 2], ov[q * 4 + 3]);
-            }
-          }
-          if (row.real) p.part_ml[pr] = make_float2(m_all, l_all);
-        }
-        if (n > 0) {
-          tc_fence_before();
-          mbar_arrive(bar_o_free);
-        }
-      }
-      if (n > 0) {
-        ++iter;
-        pos0 += 2 * n;
-      }
+      ++iter;
+      pos0 += n;
+      u0 += kAlt ? n : 2 * n;
+      if (!C::kDefer) ok = flush();
     }
+    if (C::kDefer && ok && pend) flush();
   }
   tc_fence_before();
   __syncthreads();

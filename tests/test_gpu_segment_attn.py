@@ -201,6 +201,31 @@ def test_prefix_without_prefix_or_without_own_keys(dtype, variant):
     prefix_case(dt, 3, 3, 200, 2, 2, 64, 0, 300, [0, 0, 0], [300, 200, 17], True, variant=variant)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q", [100, 128, 300])
+@pytest.mark.parametrize("longest", [100, 300, 700])
+def test_many_short_samples(D, n_q, longest):
+    """Several work items per SM with one, two, three, ... key tiles and none, in every order."""
+    B = 100
+    gen = torch.Generator().manual_seed(longest)
+    lens = [int(x) for x in torch.randint(0, longest + 1, (B,), generator=gen)]
+    cross_case(torch.bfloat16, B, n_q, 8, 8, D, longest, lens, seed=longest)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q", [100, 300])
+def test_many_samples_without_keys_between_others(D, n_q):
+    """Long rows of work items without keys before, between and behind items with them (more items than SMs, so that one
+    CTA meets them in every order)."""
+    B = 120
+    lens = [130 if b % 29 == 7 else 0 for b in range(B)]
+    lens[-1] = 300
+    cross_case(torch.bfloat16, B, n_q, 8, 8, D, 300, lens, seed=11)
+    lens = [300 if b < 40 else 0 for b in range(B)]
+    cross_case(torch.bfloat16, B, n_q, 4, 4, D, 300, lens, seed=12)
+    cross_case(torch.bfloat16, B, n_q, 4, 4, D, 300, [0] * B, seed=13)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n_q", [3, 300])
 def test_strided_views_and_untouched_rows(dtype, n_q):
