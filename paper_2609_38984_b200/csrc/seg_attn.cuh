@@ -69,7 +69,7 @@ __device__ __forceinline__ SegRow seg_row(const SegParams& p, int block_samples,
   const int smp = block_samples > 1 ? rr / per_sample : 0;
   const int i = rr - smp * per_sample;
   r.b = b0 + smp;
-  r.t = i / p.g;
+  r.t = p.g == 1 ? i : i / p.g;
   r.h = h_kv * p.g + (i - r.t * p.g);
   return r;
 }

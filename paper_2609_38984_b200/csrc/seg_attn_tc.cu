@@ -13,14 +13,13 @@
 //   warps 0-3    softmax of stream 0, one thread per row: S row from TMEM, exponentials against a running reference
 //   warps 4-7    maximum (exp2 domain, raised only when a row outgrows it by 2^8: exact either way), P as bf16; same for
 //                stream 1.  The streams' exponentials overlap each other's products.
-// Head dim 64: P goes back over the scores in TMEM, which holds three score buffers, so that Q K^T runs ahead of the
-// exponentials (through shared memory P would cost as many bytes again as all operands together, and that port was then
-// the bound).  Head dim 128: TMEM holds two score buffers beside the outputs; P goes through shared memory and a score
-// buffer is free as soon as it has been read.
-// Q K^T runs ahead of P V across the borders of items, so that the next item's first scores are there when the softmax warps
-// come to them.  Head dim 64 writes an item's output after the first exponentials of the next one: the wait for its last
-// product and the read of the accumulator then lie under work that is there anyway (head dim 128 has no memory left to
-// stage the output in but the P tile, which those exponentials would overwrite).
+// P goes back over its scores in TMEM: a product of two operands in shared memory reads as many bytes as that port delivers
+// (8 KB per 64 clk at 128 x 128 x 16), so a P in shared memory, stored and read again, would bound the kernel at 1.5 times
+// the tensor pipe's time at head dim 128.  TMEM holds three score buffers beside the outputs at head dim 64 and two at 128;
+// P V of a unit (one key tile of one stream) frees the buffer that the Q K^T three (two) units on takes.
+// Q K^T runs ahead of P V across the borders of items.  An item's output is written after the first exponentials of the
+// next one: the wait for its last product and the read of the accumulator then lie under work that is there anyway.  It
+// leaves through the item's own query tiles, which are free by then; the next item's queries are in a second buffer.
 // kAlt = false: a row tile has 256 rows; the streams are its two halves and share every key tile.
 // kAlt = true: a row tile has at most 128 rows; both streams hold the same rows and take the key tiles in turn (over the
 //   borders of items), each with its own maximum, sum and output accumulator, and are merged in the epilogue.  The memory of the second query tile
@@ -53,26 +52,22 @@ struct SegCfg {
   static constexpr int DB = D / 64;                  // 64-column (128-byte) blocks per row
   static constexpr int kSub = kTile * 128;           // bytes of a [128 rows x 64 columns] block
   static constexpr int kTileBytes = DB * kSub;       // a 128 x D tile
-  static constexpr bool kPSmem = D == 128;
-  static constexpr int kPBytes = kPSmem ? 2 * kSub : 0;   // a 128 x 128 bf16 P tile
-  static constexpr int NB = kPSmem ? 2 : 3;          // score buffers in TMEM
+  static constexpr int NB = D == 64 ? 3 : 2;         // score buffers in TMEM
   static constexpr int NQ = kAlt ? 1 : 2;            // query tiles of an item
   static constexpr int kRows = NQ * kTile;
-  // Query buffers: with two, an item's queries arrive while the previous item still multiplies (head dim 128 has no room
-  // beside three key/value slots)
-  static constexpr int QB = kPSmem ? 1 : 2;
-  // A finished tile is staged in shared memory for its way out: in the stream's P tile, or in a tile of its own
-  static constexpr bool kDefer = !kPSmem;
-  static constexpr int kStageBytes = kPSmem ? 0 : NQ * kTileBytes;
-  static constexpr int ST = kPSmem ? (kAlt ? 4 : 3) : (kAlt ? 11 : 8);      // ring slots: what fits beside all that
-  // K_(i+LA) precedes V_i in the ring, as Q K^T precedes P V on the tensor pipe
-  static constexpr int LA = kAlt ? 2 : 1;
-  static constexpr int kData = QB * NQ * kTileBytes + 2 * kPBytes + ST * kTileBytes + kStageBytes;
-  static constexpr int kBars = 8 * (2 * QB + 2 * ST + 2 * kDesc + 2 * NB + 11);
+  // Query buffers.  A buffer is free again when its item's output has left through it, so Q K^T must not run into an item
+  // whose buffer belongs to one with products that are still to be issued: with items of one tile it is LK items ahead.
+  static constexpr int QB = D == 64 ? 3 : 2;
+  static constexpr int ST = (14 - QB * NQ * DB) / DB;     // ring slots, 224 KB in all: 3 (kAlt 5) at D = 128, 10 (11) at 64
+  // Key tiles that Q K^T has taken when P V takes its first one.  The ring holds K_0 .. K_(LK-1), then V_T, K_(T+LK) for
+  // every T: the order on the tensor pipe.
+  static constexpr int LK = kAlt ? NB : NB - 1;
+  static constexpr int kData = QB * NQ * kTileBytes + ST * kTileBytes;
+  static constexpr int kBars = 8 * (4 * QB + 2 * ST + 2 * kDesc + 2 * NB + 5);
   static constexpr int kDescOff = (kBars + 15) / 16 * 16;
   static constexpr int kTail = kDescOff + kDesc * (int)sizeof(SegDesc) + 16;
   static constexpr int kBytes = kData + 1024 /*alignment*/ + kTail + (kAlt ? kTile * 8 : 0) /*maxima and sums of stream 1*/;
-  static_assert(kBytes <= 227 * 1024, "shared memory");
+  static_assert(ST >= 3 && kData <= 224 * 1024 && kBytes <= 227 * 1024, "shared memory");
   static constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
   static constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
 };
@@ -105,16 +100,14 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               const __grid_constant__ CUtensorMap map_k1, const __grid_constant__ CUtensorMap map_v1,
               const __grid_constant__ SegParams p, const int pass0, const SegTcArgs x) {
   using C = SegCfg<D, kAlt>;
-  constexpr int ST = C::ST, LA = C::LA, QB = C::QB, NB = C::NB;
+  constexpr int ST = C::ST, LK = C::LK, QB = C::QB, NB = C::NB;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_raw + (base - smem_addr(smem_raw));
-  const uint32_t sQ = base, sP = sQ + QB * C::NQ * C::kTileBytes, sR = sP + 2 * C::kPBytes;
-  const uint32_t sStage = C::kPSmem ? sP : sR + ST * C::kTileBytes;
-  constexpr uint32_t kStageStride = C::kPSmem ? C::kPBytes : C::kTileBytes;
+  const uint32_t sQ = base, sR = sQ + QB * C::NQ * C::kTileBytes;
   const uint32_t bars = base + C::kData;
   auto bar_q = [&](int b) { return bars + 8 * b; };                          // queries have arrived
-  auto bar_q_free = [&](int b) { return bars + 8 * (QB + b); };              // the item's last Q K^T has run
+  auto bar_q_free = [&](int b) { return bars + 8 * (QB + b); };              // last Q K^T has run, staged output has been read
   auto bar_full = [&](int s) { return bars + 8 * (2 * QB + s); };
   auto bar_empty = [&](int s) { return bars + 8 * (2 * QB + ST + s); };
   auto bar_d_full = [&](int s) { return bars + 8 * (2 * QB + 2 * ST + s); };
@@ -122,12 +115,12 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   constexpr int kB = 2 * QB + 2 * ST + 2 * kDesc;
   auto bar_s_full = [&](int b) { return bars + 8 * (kB + b); };              // per score buffer
   auto bar_p_full = [&](int b) { return bars + 8 * (kB + NB + b); };
-  auto bar_s_free = [&](int s) { return bars + 8 * (kB + 2 * NB + s); };     // per stream; head dim 128 only
-  auto bar_pv = [&](int s) { return bars + 8 * (kB + 2 * NB + 2 + s); };
-  const uint32_t bar_o_final = bars + 8 * (kB + 2 * NB + 4), bar_o_free = bars + 8 * (kB + 2 * NB + 5);
-  const uint32_t bar_x = bars + 8 * (kB + 2 * NB + 6);                       // kAlt: stream 1 has left its maxima and sums
-  auto bar_staged = [&](int s) { return bars + 8 * (kB + 2 * NB + 7 + s); }; // every row of the output has been staged
-  auto bar_stage = [&](int s) { return bars + 8 * (kB + 2 * NB + 9 + s); };  // the staged output has been read
+  auto bar_pv = [&](int s) { return bars + 8 * (kB + 2 * NB + s); };         // per stream
+  const uint32_t bar_o_final = bars + 8 * (kB + 2 * NB + 2), bar_o_free = bars + 8 * (kB + 2 * NB + 3);
+  const uint32_t bar_x = bars + 8 * (kB + 2 * NB + 4);                       // kAlt: stream 1 has left its maxima and sums
+  // Every row of the output has been staged, per query buffer and stream.  (One barrier for all buffers could complete twice
+  // before the warp that stores the tiles looks at it.)
+  auto bar_staged = [&](int b, int s) { return bars + 8 * (kB + 2 * NB + 5 + 2 * b + s); };
   SegDesc* desc = reinterpret_cast<SegDesc*>(base_ptr + C::kData + C::kDescOff);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + C::kData + C::kTail - 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kData + C::kTail - 8);
@@ -139,7 +132,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   if (threadIdx.x == 0) {
     for (int b = 0; b < QB; ++b) {
       mbar_init(bar_q(b), x.box_q ? 1 : 32);
-      mbar_init(bar_q_free(b), 1);
+      mbar_init(bar_q_free(b), 1 + (!p.direct ? 0 : C::NQ * (x.box_out ? 1 : kTile)));
     }
     for (int s = 0; s < ST; ++s) {
       mbar_init(bar_full(s), 1);
@@ -154,10 +147,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       mbar_init(bar_p_full(b), kTile);
     }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(bar_s_free(s), kTile);
       mbar_init(bar_pv(s), 1);
-      mbar_init(bar_staged(s), kTile);
-      mbar_init(bar_stage(s), x.box_out ? 1 : kTile);
+      for (int b = 0; b < QB; ++b) mbar_init(bar_staged(b, s), kTile);
     }
     mbar_init(bar_o_final, 1);
     mbar_init(bar_o_free, 2 * kTile);
@@ -194,10 +185,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 
   // Every role walks through the same items; one whose rows see no key is only known to the softmax warps (they write
   // its zeros) and counts for nobody else, so all other barrier phases count the remaining items and their tiles.
-  // (setmaxnreg: 384 threads start with 168 registers each; 40 for the third warpgroup frees exactly what 232 for the
+  // (setmaxnreg: 384 threads start with 168 registers each; 72 for the third warpgroup frees exactly what 216 for the
   // other two takes)
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 11) {
       // ------------------------------------------------------------------ scheduler
       int i = 0;
@@ -259,16 +250,16 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         bool ok = true;
         while (ok && next_desc(di, d)) {
           for (int s = 0; s < C::NQ && ok; ++s) {
-            ok = wait(bar_staged(s), iter & 1);
+            ok = wait(bar_staged(iter % QB, s), (iter / QB) & 1);
             if (!ok) break;
             const int row0 = d.row0 + s * kTile;     // (one pass of single samples: no flag in row0)
             if (lane == 0) {
               if (row0 < a.n_q * p.g) {
                 for (int db = 0; db < C::DB; ++db)
-                  tma_store_5d(&map_o, sStage + s * kStageStride + db * C::kSub, db * 64, 0, row0 / p.g, d.h_kv, d.b0);
+                  tma_store_5d(&map_o, sQ + ((iter % QB) * C::NQ + s) * C::kTileBytes + db * C::kSub, db * 64, 0, row0 / p.g, d.h_kv, d.b0);
                 tma_store_commit_wait();
               }
-              mbar_arrive(bar_stage(s));
+              mbar_arrive(bar_q_free(iter % QB));
             }
             __syncwarp();
           }
@@ -303,9 +294,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       cp_async_wait_all();
     } else if (warp == 9) {
       // ------------------------------------------------------------------ TMA producer
-      // The key tiles of all items form one sequence T = 0, 1, ...; the ring holds K_0 .. K_(LA-1), then K_(T+LA), V_T for
-      // every T, in the order in which the tensor pipe takes them.  Behind the last K an empty slot takes the place of each
-      // missing one, so that V_T is always load 2 T + LA + 1.  A descriptor is released when the cursor of V leaves it.
+      // The key tiles of all items form one sequence T = 0, 1, ...  Behind the last K an empty slot takes the place of each
+      // missing one, so that V_T is always load LK + 2 T.  A descriptor is released when the cursor of V leaves it.
       int pos = 0, iter = 0;                       // ring loads and items (of K) so far
       int ik = 0, nk = 0, iv = 0, nv = 0, dvi = 0; // next tile and tiles of the items of K (descriptor di - 1) and V (dvi - 1)
       bool ok = true, k_end = false;
@@ -332,8 +322,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           nk = desc[slot].n;
           k_end = nk == 0;
           if (!k_end && x.box_q) {
-            // the item's queries: with one buffer they wait for the previous item's last Q K^T, which frees the slot of its
-            // last K tile at the same moment
+            // the item's queries
             const int qb = iter % QB;
             if (iter >= QB && !wait(bar_q_free(qb), ((iter / QB) & 1) ^ 1)) return false;
             if (lane == 0) {
@@ -357,7 +346,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         ++pos;
         return true;
       };
-      for (int j = 0; j < LA && ok; ++j) ok = load_k();
+      for (int j = 0; j < LK && ok; ++j) ok = load_k();
       while (ok) {
         if (iv == nv) {
           if (dvi > 0) {
@@ -370,13 +359,13 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           ++dvi;
           iv = 0;
         }
-        ok = load_k();
-        if (ok) ok = load(desc[(dvi - 1) % kDesc], true, iv++);
+        ok = load(desc[(dvi - 1) % kDesc], true, iv++);
+        if (ok) ok = load_k();
       }
     } else {
       // ------------------------------------------------------------------ MMA issuer (warp converged, one lane issues)
       const uint32_t el = elect_one();
-      const uint32_t q_lo = desc_lo(sQ, 16), p_lo = desc_lo(sP, 16), k_lo = desc_lo(sR, 16), v_lo = desc_lo(sR, C::kSub);
+      const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sR, 16), v_lo = desc_lo(sR, C::kSub);
       auto issue_qk = [&](int qt, int buf, int st) {
         const uint32_t a_lo = q_lo + ((uint32_t)(qt * C::kTileBytes) >> 4), b_lo = k_lo + ((uint32_t)(st * C::kTileBytes) >> 4);
         mma_ss<false>(tm_S(buf), a_lo, b_lo, kDescHi, C::kIdescQK, el);
@@ -390,31 +379,21 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       };
       auto issue_pv = [&](int s, int buf, int st, bool accum) {
         const uint32_t b_lo = v_lo + ((uint32_t)(st * C::kTileBytes) >> 4);
-        if constexpr (C::kPSmem) {
-          const uint32_t a_lo = p_lo + ((uint32_t)(s * C::kPBytes) >> 4);
-          mma_ss_rt(tm_O(s), a_lo, b_lo, kDescHi, C::kIdescPV, accum ? 1u : 0u, el);
+        mma_ts(tm_O(s), tm_S(buf), b_lo, kDescHi, C::kIdescPV, accum ? 1u : 0u, el);
 #pragma unroll
-          for (int k = 1; k < kTile / 16; ++k) {
-            constexpr int kSub16 = C::kSub >> 4;
-            mma_ss_rt(tm_O(s), a_lo + (uint32_t)((k >> 2) * kSub16 + (k & 3) * 2), b_lo + k * (2048 >> 4), kDescHi, C::kIdescPV, 1u, el);
-          }
-        } else {
-          mma_ts(tm_O(s), tm_S(buf), b_lo, kDescHi, C::kIdescPV, accum ? 1u : 0u, el);
-#pragma unroll
-          for (int k = 1; k < kTile / 16; ++k) mma_ts(tm_O(s), tm_S(buf) + k * 8, b_lo + k * (2048 >> 4), kDescHi, C::kIdescPV, 1u, el);
-        }
+        for (int k = 1; k < kTile / 16; ++k) mma_ts(tm_O(s), tm_S(buf) + k * 8, b_lo + k * (2048 >> 4), kDescHi, C::kIdescPV, 1u, el);
         tc_commit(bar_pv(s), el);
       };
       // The tiles of all items form one sequence for Q K^T, which runs ahead over the borders of items, and for P V behind it.
-      // Every wait below ends without anything that this warp would have to issue first: the next item's queries are
-      // loaded when this one's last Q K^T has run, and a score buffer is free when its scores have been read.
+      // Every wait below ends without anything that this warp would have to issue first: the next item's queries are in the
+      // other buffer, and the tensor pipe runs one thread's instructions in order, so that a score buffer is free for the
+      // Q K^T issued behind the P V that reads it.
       bool ok = true, k_end = false;
       int pos = 0;                                  // ring slots taken so far
       int kn = 0, ki = 0, kiter = -1;               // item of Q K^T: tiles, next tile, number
       int vn = 0, vi = 0, viter = -1;               // item of P V
       int nq0 = 0, nq1 = 0, nq2 = 0, n_nq = 0;      // tiles of the items that Q K^T has entered and P V has not
-      int qk_c0 = 0, qk_c1 = 0, pv_c0 = 0, pv_c1 = 0;   // products issued so far per stream
-      int qk_u = 0, pv_u = 0;                       // and in all (they choose the score buffer at head dim 64)
+      int qk_u = 0, pv_u = 0;                       // units issued so far: unit u uses score buffer u % NB
       int k_st = 0;                                 // slot of the current K tile
       // makes (kn, ki) the next tile of Q K^T and takes its ring slot; false at the end
       auto next_k = [&]() {
@@ -454,14 +433,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       };
       // Q K^T of the current K tile and stream s; `last` releases the tile (and with the item's last tile the queries)
       auto qk = [&](int s, bool last) {
-        if constexpr (C::kPSmem) {
-          const int cnt = s ? qk_c1 : qk_c0;
-          if (cnt > 0) ok = wait(bar_s_free(s), (cnt - 1) & 1);
-          if (!ok) return;
-          if (s) ++qk_c1; else ++qk_c0;
-        }
         tc_fence_after();
-        issue_qk((kiter % QB) * C::NQ + (kAlt ? 0 : s), C::kPSmem ? s : qk_u % NB, k_st);
+        issue_qk((kiter % QB) * C::NQ + (kAlt ? 0 : s), qk_u % NB, k_st);
         ++qk_u;
         if (last) {
           tc_commit(bar_empty(k_st), el);
@@ -469,7 +442,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
       };
       int v_st = 0;
-      // (Q K^T is a tile ahead at least: an item that P V could enter has been entered by it)
+      // (between two steps Q K^T is a tile ahead at least: an item that P V could enter has been entered by it)
       auto v_left = [&]() { return ok && (vi < vn || n_nq > 0); };
       // makes (vn, vi) the next tile of P V and takes its ring slot
       auto next_v = [&]() {
@@ -489,12 +462,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         return ok;
       };
       auto pv = [&](int s, bool last) {
-        if constexpr (C::kPSmem) {
-          ok = wait(bar_p_full(s), (s ? pv_c1 : pv_c0) & 1);
-          if (s) ++pv_c1; else ++pv_c0;
-        } else {
-          ok = wait(bar_p_full(pv_u % NB), (pv_u / NB) & 1);
-        }
+        ok = wait(bar_p_full(pv_u % NB), (pv_u / NB) & 1);
         if (!ok) return;
         tc_fence_after();
         issue_pv(s, pv_u % NB, v_st, kAlt ? vi > 1 : vi > 0);
@@ -504,20 +472,18 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           if (++vi == vn) tc_commit(bar_o_final, el);
         }
       };
-      // the tensor pipe runs one thread's instructions in order
-      if constexpr (!kAlt && C::kPSmem) {
-        // S(T+1) of both streams, then O += P(T) V(T) of both
+      if constexpr (!kAlt && NB == 2) {
         if (next_k()) qk(0, false), qk(1, true);
-        while (v_left()) {
-          if (next_k()) qk(0, false), qk(1, true);
-          if (!ok || !next_v()) break;
+        while (v_left() && next_v()) {
           pv(0, false);
+          const bool k = ok && next_k();            // (behind the last V too: only the descriptors tell that it was the last)
+          if (k) qk(0, false);
           if (ok) pv(1, true);
+          if (ok && k) qk(1, true);
         }
       } else if constexpr (!kAlt) {
-        // three units (a tile of one stream) ahead: P V of a unit frees the score buffer that the Q K^T behind it takes
         if (next_k()) qk(0, false), qk(1, true);
-        bool half = v_left() && next_k();           // stream 0 of a tile is out, stream 1 is not
+        bool half = ok && next_k();                 // stream 0 of a tile is out, stream 1 is not
         if (half) qk(0, false);
         while (v_left() && next_v()) {
           pv(0, false);
@@ -532,50 +498,39 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           if (qk_u & 1) qk(1, true);
           else qk(0, true);
         };
-        auto pv_alt = [&]() {
+        for (int j = 0; j < LK && ok; ++j) qk_alt();
+        while (v_left() && next_v()) {
           if (pv_u & 1) pv(1, true);
           else pv(0, true);
-        };
-        qk_alt();
-        if (ok) qk_alt();
-        if constexpr (C::kPSmem) {
-          while (v_left()) {
-            qk_alt();
-            if (!ok || !next_v()) break;
-            pv_alt();
-          }
-        } else {
           if (v_left()) qk_alt();
-          while (v_left() && next_v()) {
-            pv_alt();
-            if (v_left()) qk_alt();
-          }
         }
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ------------------------------------------------------------------ softmax: one thread per row and stream
     const int s = warp >> 2;                     // stream
     const int r = (warp & 3) * 32 + lane;        // row inside the tile == TMEM lane
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tO = tm_O(s) + lane_off;
-    const uint32_t p_row = sP + (uint32_t)(s * C::kPBytes + r * 128);
     bool ok = true;
     int iter = 0, cnt = 0, pos0 = 0, u0 = 0;     // items; tiles of this stream; tiles and units of finished items
     // the finished item whose output is still in the accumulators
     bool pend = false, pend_real = false, pend_warp = false;
     int pend_row = 0, pend_part = 0;             // row in the order (sample, query, head)
     int pend_lse = 0;                            // and in the order (sample, head, query)
-    int staged = 0;                              // outputs staged so far
-    const uint32_t stage = sStage + (uint32_t)(s * kStageStride + r * 128);
     float pend_m = 0.f, pend_l = 0.f;
     // Writes one row: accumulators times their weights; an accumulator of weight 0 may hold anything.
     auto flush = [&]() {
       pend = false;
       if (kAlt && s == 1) return true;           // stream 0 writes for both
       if (!wait(bar_o_final, (iter - 1) & 1)) return false;
-      if (p.direct && staged > 0 && !wait(bar_stage(s), (staged - 1) & 1)) return false;     // (a stream may have had no tile)
+      const int qb = (iter - 1) % QB;
+      // (the addresses are computed here, once per item: hoisted out of the loop over the items they would live, or be
+      // spilled, across the softmax pass)
+      int rr = r;
+      asm volatile("" : "+r"(rr));
+      const uint32_t stage = sQ + (uint32_t)((qb * C::NQ + s) * C::kTileBytes + rr * 128);
       float m = pend_m, l = pend_l, f0 = m == -INFINITY ? 0.f : 1.f, f1 = 0.f;
       if constexpr (kAlt) {
         if (!wait(bar_x, (iter - 1) & 1)) return false;
@@ -620,7 +575,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               const int c16 = c * 4 + q;
-              st_shared_16(stage + (uint32_t)((c16 >> 3) * C::kSub + (((c16 & 7) ^ (r & 7)) << 4)), pack_bf16x2(ov[q * 8 + 0], ov[q * 8 + 1]),
+              st_shared_16(stage + (uint32_t)((c16 >> 3) * C::kSub + (((c16 & 7) ^ (rr & 7)) << 4)), pack_bf16x2(ov[q * 8 + 0], ov[q * 8 + 1]),
                            pack_bf16x2(ov[q * 8 + 2], ov[q * 8 + 3]), pack_bf16x2(ov[q * 8 + 4], ov[q * 8 + 5]),
                            pack_bf16x2(ov[q * 8 + 6], ov[q * 8 + 7]));
             }
@@ -639,13 +594,15 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         // the staged tile leaves as a box, or row by row with 16-byte stores, a row or two per instruction
         if (x.box_out) {
           fence_proxy_async();
-          mbar_arrive(bar_staged(s));            // warp 10 sends it
+          mbar_arrive(bar_staged(qb, s));        // warp 10 sends it
         } else {
           __syncwarp();
           constexpr int CPR = D / 8, RPI = 32 / CPR;
-          const int cc = lane % CPR, sub = lane / CPR;
+          int ln = lane;
+          asm volatile("" : "+r"(ln));
+          const int cc = ln % CPR, sub = ln / CPR;
           const int row = pend_real ? pend_row : -1;
-          const unsigned char* src = base_ptr + (sStage - base) + s * kStageStride + (cc >> 3) * C::kSub + (warp & 3) * 32 * 128;
+          const unsigned char* src = base_ptr + (qb * C::NQ + s) * C::kTileBytes + (cc >> 3) * C::kSub + (warp & 3) * 32 * 128;
 #pragma unroll 4
           for (int i = 0; i < 32 / RPI; ++i) {
             const int rl = i * RPI + sub;
@@ -656,9 +613,9 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                   *reinterpret_cast<const uint4*>(src + rl * 128 + (((cc & 7) ^ (rl & 7)) << 4));
           }
           __syncwarp();
-          mbar_arrive(bar_stage(s));
+          fence_proxy_async();                   // the next loads of this buffer come through the other proxy
+          mbar_arrive(bar_q_free(qb));
         }
-        ++staged;
       }
       return true;
     };
@@ -676,78 +633,45 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       bool any_key = false;
       const int i0 = kAlt ? (s ^ pos0) & 1 : 0;                  // the stream's first tile of the item
       for (int i = i0; i < n; i += kAlt ? 2 : 1, ++cnt) {
-        const int g = u0 + (kAlt ? i : 2 * i + s), buf = C::kPSmem ? s : g % NB;
+        const int g = u0 + (kAlt ? i : 2 * i + s), buf = g % NB;      // unit
         const uint32_t tS = tm_S(buf) + lane_off;
-        ok = wait(bar_s_full(buf), (C::kPSmem ? cnt : g / NB) & 1);
+        ok = wait(bar_s_full(buf), (g / NB) & 1);
         if (!ok) break;
         const bool s1 = i >= na;
         const int real = (s1 ? real1 : real0) - i * kTile;      // real keys of this tile
         tc_fence_after();
-        if (!warp_real) {
-          // rows behind the last one: nothing is computed, the barriers are kept in step (what their P rows hold only
-          // reaches their own accumulator rows, which nobody reads)
-          if constexpr (C::kPSmem) {
-            mbar_arrive(bar_s_free(s));
-            if (cnt > 0) ok = wait(bar_pv(s), (cnt - 1) & 1);       // no warp runs a phase ahead of the others
-            if (!ok) break;
-          }
-        } else {
+        // rows behind the last one: nothing is computed, the barriers are kept in step (what their P rows hold only reaches
+        // their own accumulator rows, which nobody reads)
+        if (warp_real) {
           float sv[kTile];
-          auto load_scores = [&]() {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<float(*)[32]>(&sv[c * 32]));
-            tmem_ld_wait();
-          };
-          load_scores();
-          if constexpr (C::kPSmem) {
-            tc_fence_before();
-            mbar_arrive(bar_s_free(s));           // the scores are in registers
-          }
+          for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<float(*)[32]>(&sv[c * 32]));
+          tmem_ld_wait();
           const int valid = s1 ? sees1 - i * kTile : real;
-          auto mask_tail = [&]() {
-            if (valid < kTile) {
+          if (valid < kTile) {
 #pragma unroll
-              for (int c = 0; c < kTile; ++c)
-                if (c >= valid) sv[c] = -INFINITY;
-            }
-          };
-          mask_tail();
+            for (int c = 0; c < kTile; ++c)
+              if (c >= valid) sv[c] = -INFINITY;
+          }
           const bool first = i == i0;
           if (first) {
-            // the first tile fixes the row's reference maximum.  A row that sees none of its keys sees no later key
-            // either (limits are a prefix of segment 1, and segment 0 has no limits below its length).
+            // The first tile fixes the row's reference: the maximum of its first 32 scores will do, since a row that outgrows
+            // it raises it.  A row that sees none of its keys sees no later key either (limits are a prefix of segment 1, and
+            // segment 0 has no limits below its length).
             any_key = valid > 0;
-            float m8[8];
+            float m4[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) m8[j] = sv[j];
+            for (int j = 0; j < 4; ++j) m4[j] = sv[j];
 #pragma unroll
-            for (int c = 8; c < kTile; c += 8) {
+            for (int c = 4; c < 32; c += 4) {
 #pragma unroll
-              for (int j = 0; j < 8; ++j) m8[j] = fmaxf(m8[j], sv[c + j]);
+              for (int j = 0; j < 4; ++j) m4[j] = fmaxf(m4[j], sv[c + j]);
             }
-            m_used = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])), fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7]))) * p.scale_log2;
+            m_used = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2;
             if (!any_key) m_used = 0.f;
-          }
-          if (C::kPSmem && cnt > 0) {
-            // the P tile is free once the stream's previous product has read it, and the previous item's output has left it
-            ok = wait(bar_pv(s), (cnt - 1) & 1);
-            if (ok && first && staged > 0) ok = wait(bar_stage(s), (staged - 1) & 1);
-            if (!ok) break;
           }
           const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), negm2 = pack2(-m_used, -m_used);
           uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
-          // 32 probabilities of the row, part c of four
-          auto store_p16 = [&](int c, const uint32_t* v) {
-            if constexpr (C::kPSmem) {
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const int c16 = c * 4 + q;
-                st_shared_16(p_row + (uint32_t)((c16 >> 3) * C::kSub + (((c16 & 7) ^ (r & 7)) << 4)), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-              }
-            } else {
-              tmem_st16(tS + c * 16, v);
-            }
-          };
           uint32_t pk[64];
 #pragma unroll
           for (int j = 0; j < 64; ++j) {
@@ -763,39 +687,45 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             }
             acc2[j & 3] = add2(acc2[j & 3], pack2(p0, p1));
             pk[j] = pack_bf16x2(p0, p1);
-            if (C::kPSmem && (j & 15) == 15) store_p16(j >> 4, &pk[j - 15]);
           }
           float sum, a0, a1;
           unpack2(add2(add2(acc2[0], acc2[1]), add2(acc2[2], acc2[3])), a0, a1);
           sum = a0 + a1;
           const bool grew = !(sum <= 256.f * 128.f);           // some exponent above 2^8; also inf and NaN
           const bool redo = __any_sync(0xffffffffu, grew);
-          if constexpr (!C::kPSmem) {
+          if (!redo) {
             // P overwrites the scores only now that the pass is known to stand
-            if (!redo) {
 #pragma unroll
-              for (int c = 0; c < 4; ++c) store_p16(c, &pk[c * 16]);
-            }
+            for (int c = 0; c < 4; ++c) tmem_st16(tS + c * 16, &pk[c * 16]);
           }
           if (redo) {
-            // rare: raise the reference to the row's maximum, rescale O, repeat the pass
-            if constexpr (!C::kPSmem) {
-              load_scores();
-              mask_tail();
-            }
-            float mraw = sv[0];
+            // rare: raise the reference to the row's maximum, rescale O, repeat the pass (32 scores at a time, so that this
+            // path needs no more registers than the usual one)
+            auto scores32 = [&](int c, float (&v)[32]) {
+              tmem_ld32(tS + c * 32, v);
+              tmem_ld_wait();
 #pragma unroll
-            for (int c = 1; c < kTile; ++c) mraw = fmaxf(mraw, sv[c]);
+              for (int j = 0; j < 32; ++j)
+                if (c * 32 + j >= valid) v[j] = -INFINITY;
+            };
+            float mraw = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              float v[32];
+              scores32(c, v);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) mraw = fmaxf(mraw, v[j]);
+            }
             const float delta = fmaxf(fmaf(mraw, p.scale_log2, -m_used), 0.f);
             const float f = ex2(-delta);
             m_used += delta;
             l_run *= f;
             if (!first) {
               // the accumulator must hold every product issued against the old reference
-              if (!C::kPSmem) ok = wait(bar_pv(s), (cnt - 1) & 1);
+              ok = wait(bar_pv(s), (cnt - 1) & 1);
               if (!ok) break;
               tc_fence_after();
-#pragma unroll
+#pragma unroll 1
               for (int c = 0; c < D / 32; ++c) {
                 float ov[32];
                 tmem_ld32(tO + c * 32, ov);
@@ -807,17 +737,18 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               }
             }
             sum = 0.f;
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < 4; ++c) {
+              float v[32];
+              scores32(c, v);
               uint32_t pr[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
-                const float p0 = ex2(fmaf(sv[c * 32 + 2 * j], p.scale_log2, -m_used));
-                const float p1 = ex2(fmaf(sv[c * 32 + 2 * j + 1], p.scale_log2, -m_used));
+                const float p0 = ex2(fmaf(v[2 * j], p.scale_log2, -m_used)), p1 = ex2(fmaf(v[2 * j + 1], p.scale_log2, -m_used));
                 sum += p0 + p1;
                 pr[j] = pack_bf16x2(p0, p1);
               }
-              store_p16(c, pr);
+              tmem_st16(tS + c * 16, pr);         // over scores that have been read
             }
           }
           l_run += sum;
@@ -826,26 +757,29 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         // a tile that ends inside its tensor: rows of V behind the last real key become zeros (what lies behind the tensor
         // arrives as zeros).  One stream does it for both: the issuer waits for stream 0's P before either product.
         if (real < kTile && (kAlt || s == 0) && (s1 ? more1 : more0)) {
-          const int T = pos0 + i, pos = 2 * T + LA + 1, st = pos % ST;
-          ok = wait(bar_full(st), (pos / ST) & 1);
+          // (V's load may stand behind that of an item whose query buffer the pending output has still to leave)
+          if (pend) ok = flush();
+          const int pos = LK + 2 * (pos0 + i), st = pos % ST;
+          if (ok) ok = wait(bar_full(st), (pos / ST) & 1);
           if (!ok) break;
-          if (r >= real) {
+          int rr = r;
+          asm volatile("" : "+r"(rr));
+          if (rr >= real) {
 #pragma unroll
             for (int c = 0; c < D / 8; ++c)
-              st_shared_16(sR + (uint32_t)(st * C::kTileBytes + (c >> 3) * C::kSub + r * 128 + (((c & 7) ^ (r & 7)) << 4)), 0u, 0u, 0u, 0u);
+              st_shared_16(sR + (uint32_t)(st * C::kTileBytes + (c >> 3) * C::kSub + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)), 0u, 0u, 0u, 0u);
           }
           fence_proxy_async();
         }
         tc_fence_before();
-        if constexpr (C::kPSmem) fence_proxy_async();     // P is a generic store that the tensor core will read
         mbar_arrive(bar_p_full(buf));
-        if (C::kDefer && pend) {
+        if (pend) {
           ok = flush();
           if (!ok) break;
         }
       }
       if (!ok) break;
-      if (C::kDefer && pend) ok = flush();       // kAlt, stream 1: an item of one tile
+      if (pend) ok = flush();       // kAlt, stream 1: an item of one tile
       if (!ok) break;
       pend = true;
       pend_real = row_real;
@@ -866,9 +800,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       ++iter;
       pos0 += n;
       u0 += kAlt ? n : 2 * n;
-      if (!C::kDefer) ok = flush();
     }
-    if (C::kDefer && ok && pend) flush();
+    if (ok && pend) flush();
   }
   tc_fence_before();
   __syncthreads();
