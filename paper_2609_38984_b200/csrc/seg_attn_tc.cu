@@ -132,7 +132,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   if (threadIdx.x == 0) {
     for (int b = 0; b < QB; ++b) {
       mbar_init(bar_q(b), x.box_q ? 1 : 32);
-      mbar_init(bar_q_free(b), 1 + (!p.direct ? 0 : C::NQ * (x.box_out ? 1 : kTile)));
+      mbar_init(bar_q_free(b), 1 + (!p.direct ? 0 : C::NQ * (x.box_out ? 1 : 4)));
     }
     for (int s = 0; s < ST; ++s) {
       mbar_init(bar_full(s), 1);
@@ -144,15 +144,15 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     }
     for (int b = 0; b < NB; ++b) {
       mbar_init(bar_s_full(b), 1);
-      mbar_init(bar_p_full(b), kTile);
+      mbar_init(bar_p_full(b), 4);           // warps (an arrival of every thread would queue up at the barrier)
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar_pv(s), 1);
-      for (int b = 0; b < QB; ++b) mbar_init(bar_staged(b, s), kTile);
+      for (int b = 0; b < QB; ++b) mbar_init(bar_staged(b, s), 4);
     }
     mbar_init(bar_o_final, 1);
-    mbar_init(bar_o_free, 2 * kTile);
-    mbar_init(bar_x, kTile);
+    mbar_init(bar_o_free, 8);
+    mbar_init(bar_x, 4);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -169,6 +169,11 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   // (a warp leaves its loops together: the TMEM instructions and shuffles need it converged)
   auto wait = [&](uint32_t bar, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag) ? 1 : 0) != 0;
+  };
+  // one arrival for what all lanes of the warp have done
+  auto arrive = [&](uint32_t bar) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
   };
   // next descriptor: false at the end (or when a wait ran out).  di counts the descriptors read so far.
   auto next_desc = [&](int& di, SegDesc& d) {
@@ -589,12 +594,12 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
       }
       tc_fence_before();
-      mbar_arrive(bar_o_free);                   // the accumulators have been read
+      arrive(bar_o_free);                   // the accumulators have been read
       if (p.direct) {
         // the staged tile leaves as a box, or row by row with 16-byte stores, a row or two per instruction
         if (x.box_out) {
           fence_proxy_async();
-          mbar_arrive(bar_staged(qb, s));        // warp 10 sends it
+          arrive(bar_staged(qb, s));        // warp 10 sends it
         } else {
           __syncwarp();
           constexpr int CPR = D / 8, RPI = 32 / CPR;
@@ -614,7 +619,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           }
           __syncwarp();
           fence_proxy_async();                   // the next loads of this buffer come through the other proxy
-          mbar_arrive(bar_q_free(qb));
+          arrive(bar_q_free(qb));
         }
       }
       return true;
@@ -772,7 +777,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           fence_proxy_async();
         }
         tc_fence_before();
-        mbar_arrive(bar_p_full(buf));
+        arrive(bar_p_full(buf));
         if (pend) {
           ok = flush();
           if (!ok) break;
@@ -794,8 +799,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         if (iter > 0) ok = wait(bar_o_free, (iter - 1) & 1);
         if (!ok) break;
         ml_x[r] = make_float2(pend_m, pend_l);
-        mbar_arrive(bar_x);
-        mbar_arrive(bar_o_free);
+        arrive(bar_x);
+        arrive(bar_o_free);
       }
       ++iter;
       pos0 += n;
