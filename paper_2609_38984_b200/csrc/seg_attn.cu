@@ -118,7 +118,7 @@ SegPlan seg_plan(const SegArgs& a, bool warp_mma) {
   const int64_t rows = (int64_t)a.n_q * (a.N_h / a.N_kv);       // of one sample
   // samples share the row tiles of segment 0 when a tile has room for two samples at least: the shared keys are then
   // read once for all of them
-  pl.shared = a.per_group > 1 && a.n[0] > 0 && rows <= 32;
+  pl.shared = a.per_group > 1 && a.n[0] > 0 && rows <= 64;
   if (pl.shared) {
     pl.splits[0] = plan_pass(a, a.B / a.per_group, rows * a.per_group, a.n[0], warp_mma);
     pl.splits[1] = a.n[1] > 0 ? plan_pass(a, a.B, rows, a.n[1], warp_mma) : 0;
