@@ -132,6 +132,11 @@ def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _raw_stream() -> int:
+    # the handle without the Stream object around it, which costs several microseconds a call
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
 def torch_dtype(dtype: int) -> torch.dtype:
     return torch.float32 if dtype == F32 else torch.bfloat16
 
@@ -168,6 +173,9 @@ class Swam:
         self.L = n_obs + n_frames * n_spatial + n_action
         self.Lp = n_obs + n_frames * self.K + n_action
         self.dtype = dtype
+        self._torch_dtype = torch_dtype(dtype)
+        self._device_index = device.index if device.index is not None else torch.cuda.current_device()
+        self._scratch_need = {}
         self.workspace = None
         self.staging = None
         if bind:
@@ -272,70 +280,73 @@ class Swam:
         self._chk(self.lib.swam_sparse_attn(self.ctx, _ptr(qp), _ptr(kp), _ptr(vp), n, _ptr(out), _ptr(lse), _stream()))
         return (out, lse) if want_lse else out
 
-    def _here(self, t: torch.Tensor) -> bool:
-        return t.is_cuda and (self.device.index is None or t.device.index == self.device.index)
-
     def _tokens(self, name: str, t: torch.Tensor, lead: Optional[int], heads: int):
         """Token and sample strides of a [samples, tokens, heads, D] tensor whose heads are contiguous (0 where the
         dimension has one entry, or none)."""
-        if t.dtype != torch_dtype(self.dtype) or not self._here(t) or t.dim() != 4:
-            raise ValueError(f"{name}: expected a 4-dimensional {torch_dtype(self.dtype)} tensor on {self.device}")
+        if t.dtype is not self._torch_dtype or t.get_device() != self._device_index or t.dim() != 4:
+            raise ValueError(f"{name}: expected a 4-dimensional {self._torch_dtype} tensor on {self.device}")
         n, tokens, h, d = t.shape
         if (lead is not None and n != lead) or h != heads or d != self.D:
             raise ValueError(f"{name}: expected shape [{'groups' if lead is None else lead}, tokens, {heads}, {self.D}], got {list(t.shape)}")
-        if t.numel() == 0:
+        if n == 0 or tokens == 0 or h == 0:
             return 0, 0
-        if t.stride(3) != 1 or (h > 1 and t.stride(2) != d):
+        s0, s1, s2, s3 = t.stride()
+        if s3 != 1 or (h > 1 and s2 != d):
             raise ValueError(f"{name}: the heads of a token must be contiguous")
-        if (tokens > 1 and t.stride(1) == 0) or (n > 1 and t.stride(0) == 0):
+        if (tokens > 1 and s1 == 0) or (n > 1 and s0 == 0):
             raise ValueError(f"{name}: expanded (stride 0) tokens or samples are not accepted")
-        row = heads * d
-        tok = t.stride(1) if tokens > 1 else row
-        return tok, (t.stride(0) if n > 1 else tokens * tok)
+        tok = s1 if tokens > 1 else h * d
+        return tok, (s0 if n > 1 else tokens * tok)
 
     def _lengths(self, name: str, t: Optional[torch.Tensor], n: int):
         if t is None:
             return None
-        if t.dtype != torch.int32 or not self._here(t) or tuple(t.shape) != (n,) or not t.is_contiguous():
+        if t.dtype is not torch.int32 or t.get_device() != self._device_index or t.shape != (n,) or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous int32 tensor of shape [{n}] on {self.device}")
         return t.data_ptr()
 
-    def _outputs(self, a, q, out, want_lse: bool):
+    def _out_lse(self, q, out, want_lse: bool):
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
         elif out.shape != q.shape:
             raise ValueError(f"out: expected shape {list(q.shape)}")
-        a.q, a.out, a.n_q = q.data_ptr(), out.data_ptr(), q.shape[1]
-        a.q_token, a.q_sample = self._tokens("q", q, self.B, self.N_h)
-        a.out_token, a.out_sample = self._tokens("out", out, self.B, self.N_h)
         lse = torch.empty((self.B, self.N_h, q.shape[1]), dtype=torch.float32, device=self.device) if want_lse else None
-        a.lse = lse.data_ptr() if want_lse else None
         return out, lse
 
-    def _run_with_scratch(self, name: str, a):
-        n = ctypes.c_size_t()
-        self._chk(getattr(self.lib, f"swam_{name}_attn_scratch_bytes")(self.ctx, ctypes.byref(a), ctypes.byref(n)))
-        scratch = None
-        if n.value:
-            scratch = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
-            off = (-scratch.data_ptr()) % 256
-            a.scratch, a.scratch_bytes = scratch.data_ptr() + off, n.value
-        self._chk(getattr(self.lib, f"swam_{name}_attn")(self.ctx, ctypes.byref(a), _stream()))
+    def _scratch(self, query, a, key):
+        """Scratch of a call: the tensor that holds it (it stays alive until the call has been enqueued) and its aligned
+        address.  The size depends on the sizes of the call alone (and the attention variant), so it is asked for once."""
+        need = self._scratch_need.get(key)
+        if need is None:
+            n = ctypes.c_size_t()
+            self._chk(query(self.ctx, ctypes.byref(a), ctypes.byref(n)))
+            need = self._scratch_need[key] = n.value
+        if need == 0:
+            return None
+        buf = torch.empty(need + 256, dtype=torch.uint8, device=self.device)
+        a.scratch, a.scratch_bytes = (buf.data_ptr() + 255) & ~255, need
+        return buf
 
     def cross_attn(self, q, k, v, kv_len=None, out=None, want_lse: bool = False):
         """Queries [B, n_q, N_h, D] attend an encoder's states k, v [B, n_kv, heads, D] (any divisor of N_h heads), of which
         the first kv_len[b] (int32 CUDA tensor [B], default all) are real.  Tensors may be strided views with
         contiguous heads.  A row without keys gives zeros (lse -inf).  Returns out, or (out, lse [B, N_h, n_q])."""
-        a = SwamCrossArgs()
         heads = k.shape[2] if k.dim() == 4 else 0
         if v.shape != k.shape:
             raise ValueError("k and v differ in shape")
-        a.k_token, a.k_sample = self._tokens("k", k, self.B, heads)
-        a.v_token, a.v_sample = self._tokens("v", v, self.B, heads)
-        a.k, a.v, a.n_kv, a.n_kv_heads = k.data_ptr(), v.data_ptr(), k.shape[1], heads
-        a.kv_len = self._lengths("kv_len", kv_len, self.B)
-        out, lse = self._outputs(a, q, out, want_lse)
-        self._run_with_scratch("cross", a)
+        k_tok, k_smp = self._tokens("k", k, self.B, heads)
+        v_tok, v_smp = self._tokens("v", v, self.B, heads)
+        q_tok, q_smp = self._tokens("q", q, self.B, self.N_h)
+        out, lse = self._out_lse(q, out, want_lse)
+        o_tok, o_smp = self._tokens("out", out, self.B, self.N_h)
+        n_q, n_kv = q.shape[1], k.shape[1]
+        a = SwamCrossArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), self._lengths("kv_len", kv_len, self.B), out.data_ptr(),
+                          lse.data_ptr() if want_lse else None, None, 0, n_q, n_kv, heads, 0, q_tok, q_smp, k_tok, k_smp,
+                          v_tok, v_smp, o_tok, o_smp)
+        scratch = self._scratch(self.lib.swam_cross_attn_scratch_bytes, a, (n_q, n_kv, heads))  # noqa: F841
+        rc = self.lib.swam_cross_attn(self.ctx, ctypes.byref(a), _raw_stream())
+        if rc != OK:
+            self._chk(rc)
         return (out, lse) if want_lse else out
 
     def prefix_attn(self, q, k_prefix, v_prefix, k, v, prefix_len=None, own_len=None, causal: bool = False, out=None,
@@ -344,21 +355,27 @@ class Swam:
         consecutive samples of a group share, followed by their own k, v [B, n_own, heads, D].  prefix_len [groups] and
         own_len [B] (int32 CUDA tensors, default all) give the real lengths; `causal`: query t sees the own keys up to
         own_len[b] - n_q + t.  A row without keys gives zeros (lse -inf).  Returns out, or (out, lse [B, N_h, n_q])."""
-        a = SwamPrefixArgs()
         heads = k.shape[2] if k.dim() == 4 else 0
         if v.shape != k.shape or v_prefix.shape != k_prefix.shape:
             raise ValueError("k and v differ in shape")
-        a.k_prefix_token, a.k_prefix_group = self._tokens("k_prefix", k_prefix, None, heads)
-        a.v_prefix_token, a.v_prefix_group = self._tokens("v_prefix", v_prefix, None, heads)
-        a.k_token, a.k_sample = self._tokens("k", k, self.B, heads)
-        a.v_token, a.v_sample = self._tokens("v", v, self.B, heads)
-        a.k_prefix, a.v_prefix, a.k, a.v = k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(), v.data_ptr()
-        a.n_groups, a.n_prefix, a.n_own, a.n_kv_heads = k_prefix.shape[0], k_prefix.shape[1], k.shape[1], heads
-        a.causal = 1 if causal else 0
-        a.prefix_len = self._lengths("prefix_len", prefix_len, k_prefix.shape[0])
-        a.own_len = self._lengths("own_len", own_len, self.B)
-        out, lse = self._outputs(a, q, out, want_lse)
-        self._run_with_scratch("prefix", a)
+        kp_tok, kp_grp = self._tokens("k_prefix", k_prefix, None, heads)
+        vp_tok, vp_grp = self._tokens("v_prefix", v_prefix, None, heads)
+        k_tok, k_smp = self._tokens("k", k, self.B, heads)
+        v_tok, v_smp = self._tokens("v", v, self.B, heads)
+        q_tok, q_smp = self._tokens("q", q, self.B, self.N_h)
+        out, lse = self._out_lse(q, out, want_lse)
+        o_tok, o_smp = self._tokens("out", out, self.B, self.N_h)
+        n_q, n_prefix, n_own, groups = q.shape[1], k_prefix.shape[1], k.shape[1], k_prefix.shape[0]
+        a = SwamPrefixArgs(q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(), v.data_ptr(),
+                           self._lengths("prefix_len", prefix_len, groups), self._lengths("own_len", own_len, self.B),
+                           out.data_ptr(), lse.data_ptr() if want_lse else None, None, 0, n_q, n_prefix, n_own, groups,
+                           1 if causal else 0, heads, q_tok, q_smp, kp_tok, kp_grp, vp_tok, vp_grp, k_tok, k_smp, v_tok, v_smp,
+                           o_tok, o_smp)
+        key = (n_q, n_prefix, n_own, groups, heads, a.causal)
+        scratch = self._scratch(self.lib.swam_prefix_attn_scratch_bytes, a, key)  # noqa: F841
+        rc = self.lib.swam_prefix_attn(self.ctx, ctypes.byref(a), _raw_stream())
+        if rc != OK:
+            self._chk(rc)
         return (out, lse) if want_lse else out
 
     def scatter(self, out_p, pack_map, inv_map, cached, out=None):
@@ -434,6 +451,7 @@ class Swam:
         self._chk(self.lib.swam_selftest_timeout(self.ctx, limit_cycles, _stream()))
 
     def set_option(self, option: int, value: int):
+        self._scratch_need.clear()
         self._chk(self.lib.swam_set_option(self.ctx, option, value))
 
     def set_visibility(self, observed_rows_see: int, future_rows_see: int, action_rows_see: int):
