@@ -9,23 +9,41 @@ namespace {
 
 constexpr int kMaxSplits = 64;
 
-// One warp per row; lanes hold the pieces' weights and then D / 32 output columns each.
+// One warp per row; lanes hold the pieces' weights and then D / 32 output columns each.  The first pieces' outputs are
+// requested before the weights are known (an output of weight 0 may never have been written and is not used).
+constexpr int kMergeBatch = 8;
 template <int D, typename T>
-__global__ void __launch_bounds__(256) seg_merge_kernel(const __grid_constant__ SegParams p, const int parts) {
+__global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ SegParams p, const int parts) {
   constexpr int CPL = D / 32;
   const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);   // (sample, query, head)
-  if (row >= p.rows) return;
+  const uint32_t row = blockIdx.x * 4 + (threadIdx.x >> 5);           // (sample, query, head)
   const SegArgs& a = p.a;
+  const uint32_t bt = row / (uint32_t)a.N_h, h = row - bt * a.N_h, b = bt / (uint32_t)a.n_q, t = bt - b * a.n_q;
+  T* out = (T*)a.out + b * a.o_smp + t * a.o_tok + (int64_t)h * D + lane * CPL;
+  const float* src = p.part_o + (int64_t)row * D + lane * CPL;
+  const float2* ml = p.part_ml + row;
+  wait_previous();                                                    // everything above ran beside the last pieces
+  if (row >= p.rows) return;
+  float v[kMergeBatch][CPL];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < kMergeBatch; ++i) {
+      const float* x = src + (int64_t)min(i0 + i, parts - 1) * p.rows * D;
+      if constexpr (CPL == 4) *reinterpret_cast<float4*>(v[i]) = *reinterpret_cast<const float4*>(x);
+      else if constexpr (CPL == 2) *reinterpret_cast<float2*>(v[i]) = *reinterpret_cast<const float2*>(x);
+      else v[i][0] = x[0];
+    }
+  };
+  load(0);
   // up to 128 pieces: four per lane
   float mi[4], wi[4], m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int i = j * 32 + lane;
-    const float2 v = i < parts ? p.part_ml[(int64_t)i * p.rows + row] : make_float2(-INFINITY, 0.f);
-    mi[j] = v.x;
-    wi[j] = v.y;
-    m = fmaxf(m, v.x);
+    const float2 x = i < parts ? ml[(int64_t)i * p.rows] : make_float2(-INFINITY, 0.f);
+    mi[j] = x.x;
+    wi[j] = x.y;
+    m = fmaxf(m, x.x);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -40,43 +58,38 @@ __global__ void __launch_bounds__(256) seg_merge_kernel(const __grid_constant__ 
   float acc[CPL];
 #pragma unroll
   for (int c = 0; c < CPL; ++c) acc[c] = 0.f;
-  const float* src = p.part_o + row * D + lane * CPL;
+  for (int i0 = 0; i0 < parts; i0 += kMergeBatch) {
+    if (i0 > 0) load(i0);
+    const float w4 = i0 < 32 ? wi[0] : (i0 < 64 ? wi[1] : (i0 < 96 ? wi[2] : wi[3]));
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int n = min(32, parts - j * 32);
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-      const float f = __shfl_sync(0xffffffffu, wi[j], i);
-      if (f == 0.f) continue;                      // a piece that the row sees no key of: its output was not written
-      const float* x = src + (int64_t)(j * 32 + i) * p.rows * D;
-      float v[CPL];
-      if constexpr (CPL == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(x);
-      else if constexpr (CPL == 2) *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(x);
-      else v[0] = x[0];
+    for (int i = 0; i < kMergeBatch; ++i) {
+      const float f = i0 + i < parts ? __shfl_sync(0xffffffffu, w4, (i0 + i) & 31) : 0.f;
 #pragma unroll
-      for (int c = 0; c < CPL; ++c) acc[c] = fmaf(f, v[c], acc[c]);
+      for (int c = 0; c < CPL; ++c) acc[c] = f != 0.f ? fmaf(f, v[i][c], acc[c]) : acc[c];
     }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  const int h = (int)(row % a.N_h);
-  const int64_t bt = row / a.N_h;
-  const int t = (int)(bt % a.n_q), b = (int)(bt / a.n_q);
-  T* out = (T*)a.out + b * a.o_smp + t * a.o_tok + (int64_t)h * D + lane * CPL;
+  if constexpr (sizeof(T) == 4 && CPL == 4) {
+    *reinterpret_cast<float4*>(out) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  } else if constexpr (sizeof(T) == 2 && CPL >= 2) {
 #pragma unroll
-  for (int c = 0; c < CPL; ++c) out[c] = (T)(acc[c] * inv);
+    for (int c = 0; c < CPL; c += 2) *reinterpret_cast<__nv_bfloat162*>(out + c) = __floats2bfloat162_rn(acc[c] * inv, acc[c + 1] * inv);
+  } else {
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) out[c] = (T)(acc[c] * inv);
+  }
   if (a.lse && lane == 0) a.lse[((int64_t)b * a.N_h + h) * a.n_q + t] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <typename T>
 cudaError_t launch_merge(const SegParams& p, int parts, cudaStream_t st, int* launches) {
-  const int64_t blocks = (p.rows + 7) / 8;
+  const dim3 grid((unsigned)((p.rows + 3) / 4)), block(128);
   ++*launches;
   switch (p.a.D) {
-    case 32: seg_merge_kernel<32, T><<<(unsigned)blocks, 256, 0, st>>>(p, parts); break;
-    case 64: seg_merge_kernel<64, T><<<(unsigned)blocks, 256, 0, st>>>(p, parts); break;
-    default: seg_merge_kernel<128, T><<<(unsigned)blocks, 256, 0, st>>>(p, parts); break;
+    case 32: return launch_after(seg_merge_kernel<32, T>, grid, block, 0, st, p, parts);
+    case 64: return launch_after(seg_merge_kernel<64, T>, grid, block, 0, st, p, parts);
+    default: return launch_after(seg_merge_kernel<128, T>, grid, block, 0, st, p, parts);
   }
-  return cudaGetLastError();
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

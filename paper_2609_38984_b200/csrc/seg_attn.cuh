@@ -103,6 +103,27 @@ __device__ __forceinline__ SegKeys seg_keys(const SegParams& p, const SegPass& p
   return k;
 }
 
+// Kernels of one call follow each other without a gap: each lets the next one start once all its CTAs are past their last
+// key tile (allow_next), and the next one's CTAs wait (griddepcontrol.wait) for the end of the one before: the merge before
+// it reads, a second pass, which needs nothing from the first, before it ends, so that waiting for the second pass is
+// waiting for both.
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename... Params, typename... Args>
+cudaError_t launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // rows of a row tile of the warp-level and of the fp32 kernel for blocks of `rows` rows
 inline int seg_mma_tile_rows(int64_t rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
 // of the tcgen05 kernel: two query tiles, or one whose keys two streams take in turn

@@ -164,6 +164,7 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
     }
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
+  allow_next();
 #pragma unroll
   for (int i = 0; i < RPT; ++i) {
     float sum = l[i];
@@ -185,6 +186,7 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
         a.lse[((int64_t)row.b * a.N_h + row.h) * a.n_q + row.t] = sum > 0.f ? (m[i] + log2f(sum)) * 0.6931471805599453f : -INFINITY;
     }
   }
+  if (pass == 1) wait_previous();
 }
 
 template <int D, int RPT>
@@ -193,6 +195,7 @@ cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launc
   cudaError_t e = cudaFuncSetAttribute(seg_f32_kernel<D, RPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   ++*launches;
+  if (pass == 1) return launch_after(seg_f32_kernel<D, RPT>, dim3(p.pass[pass].items), dim3(kThreadsF), smem, st, p, pass);
   seg_f32_kernel<D, RPT><<<p.pass[pass].items, kThreadsF, smem, st>>>(p, pass);
   return cudaGetLastError();
 }

@@ -61,21 +61,6 @@ __global__ void __launch_bounds__(kThreadsM) seg_mma_kernel(const __grid_constan
   const int wr = warp % WR, wk = warp / WR;
   const int b0 = it.block * ps.block_samples;
 
-  // this thread's two rows (accumulator rows lane / 4 and lane / 4 + 8 of the warp's 16), their queries as A fragments
-  uint32_t qf[D / 16][4];
-  int lim1[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const SegRow r = seg_row(p, ps, it, it.row0 + wr * 16 + (lane >> 2) + 8 * i);
-    lim1[i] = seg_limit1(a, kk.end > kk.n0 ? seg_len(p, 1, r.b) : 0, r.t);
-    const uint32_t* src = reinterpret_cast<const uint32_t*>((const __nv_bfloat16*)a.q + r.b * a.q_smp + r.t * a.q_tok + (int64_t)r.h * D);
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      qf[ks][i] = r.real ? src[ks * 8 + (lane & 3)] : 0u;
-      qf[ks][i + 2] = r.real ? src[ks * 8 + 4 + (lane & 3)] : 0u;
-    }
-  }
-
   auto load_tile = [&](int t) {
     const int s = t >= kk.n0 ? 1 : 0;
     const int key0 = (s ? t - kk.n0 : t) * kKT;
@@ -94,16 +79,31 @@ __global__ void __launch_bounds__(kThreadsM) seg_mma_kernel(const __grid_constan
     }
   };
 
-  float o[D / 8][4];
-#pragma unroll
-  for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-
 #pragma unroll
   for (int i = 0; i < kStagesM - 1; ++i) {
     if (kk.begin + i < kk.end) load_tile(kk.begin + i);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
+  // this thread's two rows (accumulator rows lane / 4 and lane / 4 + 8 of the warp's 16), their queries as A fragments
+  uint32_t qf[D / 16][4];
+  int lim1[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const SegRow r = seg_row(p, ps, it, it.row0 + wr * 16 + (lane >> 2) + 8 * i);
+    lim1[i] = seg_limit1(a, kk.end > kk.n0 ? seg_len(p, 1, r.b) : 0, r.t);
+    const uint32_t* src = reinterpret_cast<const uint32_t*>((const __nv_bfloat16*)a.q + r.b * a.q_smp + r.t * a.q_tok + (int64_t)r.h * D);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      qf[ks][i] = r.real ? src[ks * 8 + (lane & 3)] : 0u;
+      qf[ks][i + 2] = r.real ? src[ks * 8 + 4 + (lane & 3)] : 0u;
+    }
+  }
+
+  float o[D / 8][4];
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
   for (int t = kk.begin; t < kk.end; ++t) {
     asm volatile("cp.async.wait_group %0;" ::"n"(kStagesM - 2) : "memory");
     __syncthreads();
@@ -186,6 +186,7 @@ __global__ void __launch_bounds__(kThreadsM) seg_mma_kernel(const __grid_constan
     l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
   }
 
+  allow_next();
   // merge the WK warps of each row through shared memory (the ring is free by now), then write
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
@@ -242,6 +243,7 @@ __global__ void __launch_bounds__(kThreadsM) seg_mma_kernel(const __grid_constan
       if (c == 0) p.part_ml[pr] = make_float2(mx, sum);
     }
   }
+  if (pass == 1) wait_previous();
 }
 
 template <int D, int WR>
@@ -251,6 +253,7 @@ cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launc
   cudaError_t e = cudaFuncSetAttribute(seg_mma_kernel<D, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   ++*launches;
+  if (pass == 1) return launch_after(seg_mma_kernel<D, WR>, dim3(p.pass[pass].items), dim3(kThreadsM), smem, st, p, pass);
   seg_mma_kernel<D, WR><<<p.pass[pass].items, kThreadsM, smem, st>>>(p, pass);
   return cudaGetLastError();
 }

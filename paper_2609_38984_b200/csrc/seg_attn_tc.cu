@@ -808,8 +808,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     }
     if (ok && pend) flush();
   }
+  allow_next();
   tc_fence_before();
   __syncthreads();
+  if (pass0 == 1) wait_previous();
   if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, ST_TIMEOUT);
   if (warp == 8) {
     tc_fence_after();
@@ -871,6 +873,7 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, cudaStream_t st, 
   if (e != cudaSuccess) return e;
   const int sms = sm_count(), grid = x.items < sms ? x.items : sms;
   ++*launches;
+  if (pass == 1) return launch_after(seg_tc_kernel<D, kAlt>, dim3(grid), dim3(kThreadsS), smem, st, mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x);
   seg_tc_kernel<D, kAlt><<<grid, kThreadsS, smem, st>>>(mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x);
   return cudaGetLastError();
 }
