@@ -11,8 +11,7 @@ constexpr int kMaxSplits = 64;
 
 // One warp per row; lanes hold the pieces' weights and then D / 32 output columns each.  The first pieces' outputs are
 // requested before the weights are known (an output of weight 0 may never have been written and is not used).
-constexpr int kMergeBatch = 8;
-template <int D, typename T>
+template <int D, typename T, int kMergeBatch>
 __global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ SegParams p, const int parts) {
   constexpr int CPL = D / 32;
   const int lane = threadIdx.x & 31;
@@ -81,47 +80,61 @@ __global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ 
   if (a.lse && lane == 0) a.lse[((int64_t)b * a.N_h + h) * a.n_q + t] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-template <typename T>
-cudaError_t launch_merge(const SegParams& p, int parts, cudaStream_t st, int* launches) {
+template <int D, typename T>
+cudaError_t launch_merge_d(const SegParams& p, int parts, cudaStream_t st, int* launches) {
   const dim3 grid((unsigned)((p.rows + 3) / 4)), block(128);
   ++*launches;
+  // (loads beyond the last piece are repeats of it: two pieces, the usual number of a shared plan, want a batch of their own)
+  if (parts <= 2) return launch_after(seg_merge_kernel<D, T, 2>, grid, block, 0, st, p, parts);
+  return launch_after(seg_merge_kernel<D, T, 8>, grid, block, 0, st, p, parts);
+}
+template <typename T>
+cudaError_t launch_merge(const SegParams& p, int parts, cudaStream_t st, int* launches) {
   switch (p.a.D) {
-    case 32: return launch_after(seg_merge_kernel<32, T>, grid, block, 0, st, p, parts);
-    case 64: return launch_after(seg_merge_kernel<64, T>, grid, block, 0, st, p, parts);
-    default: return launch_after(seg_merge_kernel<128, T>, grid, block, 0, st, p, parts);
+    case 32: return launch_merge_d<32, T>(p, parts, st, launches);
+    case 64: return launch_merge_d<64, T>(p, parts, st, launches);
+    default: return launch_merge_d<128, T>(p, parts, st, launches);
   }
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The kernel of a pass whose blocks have `rows` rows per key/value head.
+// How a pass runs: `blocks` blocks with `rows` rows per key/value head each and up to `keys` keys.
 enum Kind { kF32, kMma, kTc };
-Kind pass_kind(const SegArgs& a, int64_t rows, bool warp_mma) {
-  if (a.dtype == 0) return kF32;
-  return a.D < 64 || warp_mma || rows <= 32 ? kMma : kTc;
-}
-int tile_rows(Kind k, int64_t rows) {
-  return k == kF32 ? seg_f32_tile_rows(rows) : (k == kMma ? seg_mma_tile_rows(rows) : seg_tc_tile_rows(rows));
-}
-
-// pieces over `keys` keys so that `items` row tiles become at least `want` work items, no piece below `min_keys` keys
-int pick_splits(int64_t items, int64_t keys, int want, int min_keys) {
-  int64_t s = ceil_div(want, items > 0 ? items : 1);
+struct PassPlan {
+  Kind kind;
+  int tile_rows;
+  bool wide;            // kMma: eight warps along the keys
+  int splits;
+};
+PassPlan plan_pass(const SegArgs& a, int64_t blocks, int64_t rows, int64_t keys, bool warp_mma) {
+  PassPlan p;
+  const int sms = sm_count();
+  // Few rows stream their keys through the warp-level kernel; from 33 rows on the tensor cores' tiles are filled well enough
+  // (from 65 on with few keys, where the larger kernel's start costs more than its rate gains).
+  p.kind = a.dtype == 0 ? kF32 : (a.D < 64 || warp_mma || rows <= 32 || (rows <= 64 && keys <= 512) ? kMma : kTc);
+  p.tile_rows = p.kind == kF32 ? seg_f32_tile_rows(rows) : (p.kind == kMma ? seg_mma_tile_rows(rows) : seg_tc_tile_rows(rows));
+  const int64_t items = blocks * a.N_kv * ceil_div(rows, p.tile_rows);
+  // fewer items than two CTAs per SM: one CTA of eight warps streams an item twice as fast, and needs half the pieces
+  p.wide = p.kind == kMma && p.tile_rows == 16 && items < 2 * sms;
+  int64_t s, min_keys;
+  if (p.kind == kTc || p.wide) {
+    s = sms / (items > 0 ? items : 1);             // one CTA per SM: as many pieces as one wave holds
+    min_keys = 512;
+  } else {
+    s = ceil_div(4 * sms, items > 0 ? items : 1);  // several CTAs per SM, and waves that even out
+    min_keys = 256;
+  }
   if (s > keys / min_keys) s = keys / min_keys;
   if (s > kMaxSplits) s = kMaxSplits;
-  return s < 1 ? 1 : (int)s;
+  p.splits = s < 1 ? 1 : (int)s;
+  return p;
 }
-
-int plan_pass(const SegArgs& a, int64_t blocks, int64_t rows, int64_t keys, bool warp_mma) {
-  const Kind k = pass_kind(a, rows, warp_mma);
-  const int64_t items = blocks * a.N_kv * ceil_div(rows, tile_rows(k, rows));
-  const int sms = sm_count();
-  if (k != kTc) return pick_splits(items, keys, 4 * sms, 256);
-  // one CTA per SM: as many pieces as fill the last wave
-  int64_t s = sms / (items > 0 ? items : 1);
-  if (s > keys / 512) s = keys / 512;
-  if (s > kMaxSplits) s = kMaxSplits;
-  return s < 1 ? 1 : (int)s;
+// the plan of pass i
+PassPlan plan_of(const SegArgs& a, bool shared, int i, bool warp_mma) {
+  const int64_t rows = (int64_t)a.n_q * (a.N_h / a.N_kv);
+  if (!shared) return plan_pass(a, a.B, rows, (int64_t)a.n[0] + a.n[1], warp_mma);
+  return i == 0 ? plan_pass(a, a.B / a.per_group, rows * a.per_group, a.n[0], warp_mma) : plan_pass(a, a.B, rows, a.n[1], warp_mma);
 }
 
 }  // namespace
@@ -132,13 +145,8 @@ SegPlan seg_plan(const SegArgs& a, bool warp_mma) {
   // samples share the row tiles of segment 0 when a tile has room for two samples at least: the shared keys are then
   // read once for all of them
   pl.shared = a.per_group > 1 && a.n[0] > 0 && rows <= 64;
-  if (pl.shared) {
-    pl.splits[0] = plan_pass(a, a.B / a.per_group, rows * a.per_group, a.n[0], warp_mma);
-    pl.splits[1] = a.n[1] > 0 ? plan_pass(a, a.B, rows, a.n[1], warp_mma) : 0;
-  } else {
-    pl.splits[0] = plan_pass(a, a.B, rows, (int64_t)a.n[0] + a.n[1], warp_mma);
-    pl.splits[1] = 0;
-  }
+  pl.splits[0] = plan_of(a, pl.shared, 0, warp_mma).splits;
+  pl.splits[1] = pl.shared && a.n[1] > 0 ? plan_of(a, pl.shared, 1, warp_mma).splits : 0;
   return pl;
 }
 
@@ -160,31 +168,29 @@ cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& pl, bool warp_mma, 
   p.part_ml = (float2*)((float*)scratch + (size_t)pl.parts() * p.rows * a.D);
   p.status = status;
   const int n_pass = pl.shared && pl.splits[1] > 0 ? 2 : 1;
-  int64_t rows[2];
-  Kind kind[2];
+  p.early = n_pass == 2;
+  PassPlan pp[2];
   for (int i = 0; i < 2; ++i) {
     SegPass& ps = p.pass[i];
     const bool mixed = pl.shared && i == 0;
+    pp[i] = plan_of(a, pl.shared, i, warp_mma);
     ps.seg_lo = pl.shared ? i : 0;
     ps.seg_hi = mixed ? 0 : 1;
     ps.block_samples = mixed ? a.per_group : 1;
     ps.blocks = a.B / ps.block_samples;
-    rows[i] = (int64_t)a.n_q * p.g * ps.block_samples;
-    kind[i] = pass_kind(a, rows[i], warp_mma);
-    ps.row_tiles = (int)ceil_div(rows[i], tile_rows(kind[i], rows[i]));
+    ps.row_tiles = (int)ceil_div((int64_t)a.n_q * p.g * ps.block_samples, pp[i].tile_rows);
     ps.splits = i < n_pass ? pl.splits[i] : 0;
     ps.part0 = i == 0 ? 0 : pl.splits[0];
     const int64_t items = (int64_t)ps.blocks * a.N_kv * ps.row_tiles * ps.splits;
     if (items > 0x7fffffff) return cudaErrorInvalidConfiguration;
     ps.items = (int)items;
   }
-  bool alt[2];
-  for (int i = 0; i < 2; ++i) alt[i] = seg_tc_tile_rows(rows[i]) == 128;
-  const bool both = n_pass == 2 && kind[0] == kTc && kind[1] == kTc && alt[0] == alt[1];
+  const bool both = n_pass == 2 && pp[0].kind == kTc && pp[1].kind == kTc && pp[0].tile_rows == pp[1].tile_rows;
+  if (both) p.early = 0;
   for (int i = 0; i < (both ? 1 : n_pass); ++i) {
-    const cudaError_t e = kind[i] == kF32   ? launch_seg_f32(p, i, rows[i], st, launches)
-                          : kind[i] == kMma ? launch_seg_mma(p, i, rows[i], st, launches)
-                                            : launch_seg_tc(p, i, both, alt[i], st, launches);
+    const cudaError_t e = pp[i].kind == kF32   ? launch_seg_f32(p, i, pp[i].tile_rows, st, launches)
+                          : pp[i].kind == kMma ? launch_seg_mma(p, i, pp[i].tile_rows, pp[i].wide, st, launches)
+                                               : launch_seg_tc(p, i, both, pp[i].tile_rows == 128, st, launches);
     if (e != cudaSuccess) return e;
   }
   if (p.direct) return cudaSuccess;

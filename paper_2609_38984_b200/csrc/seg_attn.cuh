@@ -20,6 +20,7 @@ struct SegPass {
 struct SegParams {
   SegArgs a;
   SegPass pass[2];
+  int early;                // the second pass may start at once (it needs nothing from the first)
   int direct;               // 1: an item's result is final, 0: unnormalised partial results go to scratch
   int g;                    // query heads per key/value head
   float scale_log2;
@@ -103,8 +104,8 @@ __device__ __forceinline__ SegKeys seg_keys(const SegParams& p, const SegPass& p
   return k;
 }
 
-// Kernels of one call follow each other without a gap: each lets the next one start once all its CTAs are past their last
-// key tile (allow_next), and the next one's CTAs wait (griddepcontrol.wait) for the end of the one before: the merge before
+// Kernels of one call follow each other without a gap: each lets the next one start (allow_next) once all its CTAs are past
+// their last key tile, or, where that is a second pass, have started; and the next one's CTAs wait (griddepcontrol.wait) for the end of the one before: the merge before
 // it reads, a second pass, which needs nothing from the first, before it ends, so that waiting for the second pass is
 // waiting for both.
 __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -130,7 +131,8 @@ inline int seg_mma_tile_rows(int64_t rows) { return rows <= 16 ? 16 : (rows <= 3
 inline int seg_tc_tile_rows(int64_t rows) { return rows <= 128 ? 128 : 256; }
 inline int seg_f32_tile_rows(int64_t rows) { return rows <= 16 ? 16 : 64; }
 // rows: rows of a block, per key/value head (they choose the row tile)
-cudaError_t launch_seg_mma(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches);
+// wide: eight warps instead of four share the keys of a 16-row tile
+cudaError_t launch_seg_mma(const SegParams& p, int pass, int tile_rows, bool wide, cudaStream_t st, int* launches);
 // both: the items of pass 1 follow those of pass 0 in the same launch; alt: 128-row tiles whose keys two streams take in turn
 cudaError_t launch_seg_tc(const SegParams& p, int pass, bool both, bool alt, cudaStream_t st, int* launches);
 cudaError_t launch_seg_f32(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches);

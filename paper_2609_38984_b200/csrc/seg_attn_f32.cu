@@ -29,6 +29,7 @@ struct F32Cfg {
 template <int D, int RPT>
 __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constant__ SegParams p, const int pass) {
   using C = F32Cfg<D, RPT>;
+  if (p.early && pass == 0) allow_next();
   constexpr int MR = C::MR, QS = C::QS, PS = MR + 4;
   extern __shared__ float sf[];
   float* sQ = sf;

@@ -2,10 +2,10 @@
 // shared memory: the kernel for few query rows per key/value head (single tokens, short chunks), for head dim 32, and the
 // independent second opinion on the tcgen05 kernel.
 //
-// One CTA of four warps owns a row tile of 16 * WR rows and a piece of the keys.  WR warps lie along the rows and
-// WK = 4 / WR along the keys: with 16 rows or fewer every warp holds all rows and a quarter of each key tile, so that no
-// key is multiplied twice; every warp keeps its own running maximum and sum, and the warps of a row are merged once at the
-// end.  Key and value tiles (64 keys) arrive by 16-byte asynchronous copies into a ring of three stages; keys beyond the
+// One CTA of WR * WK warps owns a row tile of 16 * WR rows and a piece of the keys.  WR warps lie along the rows and WK
+// along the keys: with 16 rows or fewer every warp holds all rows and 16 keys of each tile, so that no key is multiplied
+// twice; every warp keeps its own running maximum and sum, and the warps of a row are merged once at the end.  Key and value
+// tiles (64 keys, or 128 with eight warps) arrive by 16-byte asynchronous copies into a ring of three stages; keys beyond the
 // real length are filled with zeros, so whatever the padding holds (NaN included) never meets a product.
 // Scores, maxima, sums and outputs are fp32; the probabilities are rounded to bf16 for the second product.
 #include "seg_attn.cuh"
@@ -13,9 +13,7 @@
 namespace swam {
 namespace {
 
-constexpr int kKT = 64;        // keys per tile
 constexpr int kStagesM = 3;
-constexpr int kThreadsM = 128;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, uint32_t bytes) {
@@ -46,13 +44,23 @@ __device__ __forceinline__ uint32_t tile_off(int r, int c) {
   return (uint32_t)(r * D * 2 + ((D >= 64 ? (c ^ (r & 7)) : (c ^ ((r >> 1) & 3))) << 4));
 }
 
-template <int D, int WR>
-__global__ void __launch_bounds__(kThreadsM) seg_mma_kernel(const __grid_constant__ SegParams p, const int pass) {
-  constexpr int WK = 4 / WR, MR = 16 * WR, KW = kKT / WK;
+template <int D, int WR, int WK>
+struct MmaCfg {
+  static constexpr int kThreads = 32 * WR * WK, MR = 16 * WR;
+  static constexpr int KT = WR == 1 ? 16 * WK : 64;      // keys per tile
+  static constexpr int kRing = kStagesM * 2 * KT * D * 2, kMerge = WK * MR * (D + 4 + 2) * 4;
+  static constexpr int kBytes = kRing > kMerge ? kRing : kMerge;
+};
+
+template <int D, int WR, int WK>
+__global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_constant__ SegParams p, const int pass) {
+  using C = MmaCfg<D, WR, WK>;
+  constexpr int MR = C::MR, kKT = C::KT, KW = kKT / WK, kThreadsM = C::kThreads;
   constexpr int CPR = D / 8;                       // 16-byte chunks per row
   constexpr int kTileB = kKT * D * 2;              // bytes of a key or value tile
   extern __shared__ unsigned char smem_raw[];
   const uint32_t s0 = smem_u32(smem_raw);
+  if (p.early && pass == 0) allow_next();
   const SegPass& ps = p.pass[pass];
   const SegArgs& a = p.a;
   const SegItem it = seg_item(ps, a.N_kv, MR, blockIdx.x);
@@ -246,33 +254,32 @@ __global__ void __launch_bounds__(kThreadsM) seg_mma_kernel(const __grid_constan
   if (pass == 1) wait_previous();
 }
 
-template <int D, int WR>
+template <int D, int WR, int WK>
 cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launches) {
-  constexpr int ring = kStagesM * 2 * kKT * D * 2, merge = (4 / WR) * 16 * WR * (D + 4 + 2) * 4;
-  constexpr int smem = ring > merge ? ring : merge;
-  cudaError_t e = cudaFuncSetAttribute(seg_mma_kernel<D, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  using C = MmaCfg<D, WR, WK>;
+  cudaError_t e = cudaFuncSetAttribute(seg_mma_kernel<D, WR, WK>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes);
   if (e != cudaSuccess) return e;
   ++*launches;
-  if (pass == 1) return launch_after(seg_mma_kernel<D, WR>, dim3(p.pass[pass].items), dim3(kThreadsM), smem, st, p, pass);
-  seg_mma_kernel<D, WR><<<p.pass[pass].items, kThreadsM, smem, st>>>(p, pass);
+  if (pass == 1) return launch_after(seg_mma_kernel<D, WR, WK>, dim3(p.pass[pass].items), dim3(C::kThreads), C::kBytes, st, p, pass);
+  seg_mma_kernel<D, WR, WK><<<p.pass[pass].items, C::kThreads, C::kBytes, st>>>(p, pass);
   return cudaGetLastError();
 }
 template <int D>
-cudaError_t launch_rows(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches) {
-  switch (seg_mma_tile_rows(rows)) {
-    case 16: return launch_one<D, 1>(p, pass, st, launches);
-    case 32: return launch_one<D, 2>(p, pass, st, launches);
-    default: return launch_one<D, 4>(p, pass, st, launches);
+cudaError_t launch_rows(const SegParams& p, int pass, int rows, bool wide, cudaStream_t st, int* launches) {
+  switch (rows) {
+    case 16: return wide ? launch_one<D, 1, 8>(p, pass, st, launches) : launch_one<D, 1, 4>(p, pass, st, launches);
+    case 32: return launch_one<D, 2, 2>(p, pass, st, launches);
+    default: return launch_one<D, 4, 1>(p, pass, st, launches);
   }
 }
 
 }  // namespace
 
-cudaError_t launch_seg_mma(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches) {
+cudaError_t launch_seg_mma(const SegParams& p, int pass, int tile_rows, bool wide, cudaStream_t st, int* launches) {
   switch (p.a.D) {
-    case 32: return launch_rows<32>(p, pass, rows, st, launches);
-    case 64: return launch_rows<64>(p, pass, rows, st, launches);
-    case 128: return launch_rows<128>(p, pass, rows, st, launches);
+    case 32: return launch_rows<32>(p, pass, tile_rows, wide, st, launches);
+    case 64: return launch_rows<64>(p, pass, tile_rows, wide, st, launches);
+    case 128: return launch_rows<128>(p, pass, tile_rows, wide, st, launches);
     default: return cudaErrorInvalidConfiguration;
   }
 }

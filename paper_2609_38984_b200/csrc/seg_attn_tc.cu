@@ -129,6 +129,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const SegArgs& a = p.a;
 
+  if (p.early && pass0 == 0) allow_next();
+
   if (threadIdx.x == 0) {
     for (int b = 0; b < QB; ++b) {
       mbar_init(bar_q(b), x.box_q ? 1 : 32);
