@@ -69,22 +69,40 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
   const int wr = warp % WR, wk = warp / WR;
   const int b0 = it.block * ps.block_samples;
 
+  // A thread copies the same 16-byte chunk of every RS-th row of a tile, so that one pointer per tensor and a fixed step
+  // address all its copies.  lr0, lc: its first row and its chunk.
+  constexpr int RS = kThreadsM / CPR, NL = kKT / RS;
+  const int lr0 = threadIdx.x / CPR, lc = threadIdx.x % CPR;
+  int next_seg = -1;                               // segment that the pointers stand in
+  const __nv_bfloat16 *kp = nullptr, *vp = nullptr;
+  int64_t k_step = 0, v_step = 0;
+  int left = 0;                                    // real keys from the thread's first row of the tile on
+  uint32_t stage_off = 0;
   auto load_tile = [&](int t) {
-    const int s = t >= kk.n0 ? 1 : 0;
-    const int key0 = (s ? t - kk.n0 : t) * kKT;
-    const int len = s ? kk.len1 : kk.len0;
-    const int64_t idx = s ? b0 : b0 / a.per_group;
-    const __nv_bfloat16* kb = (const __nv_bfloat16*)a.k[s] + idx * a.k_smp[s] + (int64_t)it.h_kv * D;
-    const __nv_bfloat16* vb = (const __nv_bfloat16*)a.v[s] + idx * a.v_smp[s] + (int64_t)it.h_kv * D;
-    const uint32_t ks = s0 + (uint32_t)((t - kk.begin) % kStagesM) * 2 * kTileB, vs = ks + kTileB;
-#pragma unroll
-    for (int i = threadIdx.x; i < kKT * CPR; i += kThreadsM) {
-      const int r = i / CPR, c = i % CPR;
-      const bool in = key0 + r < len;
-      const int64_t key = in ? key0 + r : 0;
-      cp16(ks + tile_off<D>(r, c), kb + key * a.k_tok[s] + c * 8, in ? 16u : 0u);
-      cp16(vs + tile_off<D>(r, c), vb + key * a.v_tok[s] + c * 8, in ? 16u : 0u);
+    const int sg = t >= kk.n0 ? 1 : 0;
+    if (sg != next_seg) {
+      next_seg = sg;
+      const int key0 = (sg ? t - kk.n0 : t) * kKT + lr0;
+      const int64_t idx = sg ? b0 : b0 / a.per_group;
+      kp = (const __nv_bfloat16*)a.k[sg] + idx * a.k_smp[sg] + (int64_t)it.h_kv * D + key0 * a.k_tok[sg] + lc * 8;
+      vp = (const __nv_bfloat16*)a.v[sg] + idx * a.v_smp[sg] + (int64_t)it.h_kv * D + key0 * a.v_tok[sg] + lc * 8;
+      k_step = RS * a.k_tok[sg];
+      v_step = RS * a.v_tok[sg];
+      left = (sg ? kk.len1 : kk.len0) - key0;
     }
+    const uint32_t ks = s0 + stage_off, vs = ks + kTileB;
+    stage_off = stage_off + 2 * kTileB == kStagesM * 2 * kTileB ? 0 : stage_off + 2 * kTileB;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const bool in = i * RS < left;
+      const uint32_t off = tile_off<D>(lr0 + i * RS, lc);
+      // (rows behind the real ones read nothing; the address stays inside the tensor)
+      cp16(ks + off, in ? kp : (const __nv_bfloat16*)a.k[sg], in ? 16u : 0u);
+      cp16(vs + off, in ? vp : (const __nv_bfloat16*)a.v[sg], in ? 16u : 0u);
+      kp += k_step;
+      vp += v_step;
+    }
+    left -= kKT;
   };
 
 #pragma unroll
@@ -168,6 +186,7 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
         l[e >> 1] += sc[nb][e];
       }
     }
+    if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f))   // rare after the first tiles
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) {
       o[i][0] *= corr[0];
