@@ -99,7 +99,7 @@ cudaError_t launch_merge(const SegParams& p, int parts, cudaStream_t st, int* la
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How a pass runs: `blocks` blocks with `rows` rows per key/value head each and up to `keys` keys.
+// How a pass runs: `blocks` blocks with `rows` rows per key/value head each and up to `keys` keys.  pass: -1 = the only one.
 enum Kind { kF32, kMma, kTc };
 struct PassPlan {
   Kind kind;
@@ -107,23 +107,26 @@ struct PassPlan {
   bool wide;            // kMma: eight warps along the keys
   int splits;
 };
-PassPlan plan_pass(const SegArgs& a, int64_t blocks, int64_t rows, int64_t keys, bool warp_mma) {
+PassPlan plan_pass(const SegArgs& a, int64_t blocks, int64_t rows, int64_t keys, bool warp_mma, int pass) {
   PassPlan p;
   const int sms = sm_count();
   // Few rows stream their keys through the warp-level kernel; from 33 rows on the tensor cores' tiles are filled well enough
   // (from 65 on with few keys, where the larger kernel's start costs more than its rate gains).
   p.kind = a.dtype == 0 ? kF32 : (a.D < 64 || warp_mma || rows <= 32 || (rows <= 64 && keys <= 512) ? kMma : kTc);
-  p.tile_rows = p.kind == kF32 ? seg_f32_tile_rows(rows) : (p.kind == kMma ? seg_mma_tile_rows(rows) : seg_tc_tile_rows(rows));
+  p.tile_rows = p.kind == kF32 ? seg_f32_tile_rows(rows, blocks * a.N_kv, sms) : (p.kind == kMma ? seg_mma_tile_rows(rows) : seg_tc_tile_rows(rows));
   const int64_t items = blocks * a.N_kv * ceil_div(rows, p.tile_rows);
   // fewer items than two CTAs per SM: one CTA of eight warps streams an item twice as fast, and needs half the pieces
   p.wide = p.kind == kMma && p.tile_rows == 16 && items < 2 * sms;
   int64_t s, min_keys;
   if (p.kind == kTc || p.wide) {
-    s = sms / (items > 0 ? items : 1);             // one CTA per SM: as many pieces as one wave holds
+    // one CTA per SM: as many pieces as one wave holds, or half a wave where a second pass with more keys fills the rest
+    s = (pass == 0 && a.B * (int64_t)a.n[1] > blocks * keys ? sms / 2 : sms) / (items > 0 ? items : 1);
     min_keys = 512;
   } else {
-    s = ceil_div(4 * sms, items > 0 ? items : 1);  // several CTAs per SM, and waves that even out
-    min_keys = 256;
+    // Two CTAs per SM.  A merge costs some 10 us with its partial results, so that more pieces for the sake of even waves pay
+    // only where there is one anyway (64 samples of 520 keys: 32 us in one piece each, 39 us in two).
+    s = (pass >= 0 ? 4 : 2) * sms / (items > 0 ? items : 1);
+    min_keys = p.kind == kF32 ? 96 : 256;
   }
   if (s > keys / min_keys) s = keys / min_keys;
   if (s > kMaxSplits) s = kMaxSplits;
@@ -133,8 +136,9 @@ PassPlan plan_pass(const SegArgs& a, int64_t blocks, int64_t rows, int64_t keys,
 // the plan of pass i
 PassPlan plan_of(const SegArgs& a, bool shared, int i, bool warp_mma) {
   const int64_t rows = (int64_t)a.n_q * (a.N_h / a.N_kv);
-  if (!shared) return plan_pass(a, a.B, rows, (int64_t)a.n[0] + a.n[1], warp_mma);
-  return i == 0 ? plan_pass(a, a.B / a.per_group, rows * a.per_group, a.n[0], warp_mma) : plan_pass(a, a.B, rows, a.n[1], warp_mma);
+  if (!shared) return plan_pass(a, a.B, rows, (int64_t)a.n[0] + a.n[1], warp_mma, -1);
+  if (i == 0) return plan_pass(a, a.B / a.per_group, rows * a.per_group, a.n[0], warp_mma, a.n[1] > 0 ? 0 : -1);
+  return plan_pass(a, a.B, rows, a.n[1], warp_mma, 1);
 }
 
 }  // namespace

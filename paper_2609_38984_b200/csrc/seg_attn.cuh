@@ -129,12 +129,17 @@ cudaError_t launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_
 inline int seg_mma_tile_rows(int64_t rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
 // of the tcgen05 kernel: two query tiles, or one whose keys two streams take in turn
 inline int seg_tc_tile_rows(int64_t rows) { return rows <= 128 ? 128 : 256; }
-inline int seg_f32_tile_rows(int64_t rows) { return rows <= 16 ? 16 : 64; }
+// of the fp32 kernel for `blocks` pairs of block and key/value head: 64 rows run at the best rate, 32 where there are not
+// enough of them to fill the SMs evenly
+inline int seg_f32_tile_rows(int64_t rows, int64_t blocks, int sms) {
+  if (rows <= 16) return 16;
+  return rows <= 32 || blocks * ((rows + 63) / 64) < 2 * sms ? 32 : 64;
+}
 // rows: rows of a block, per key/value head (they choose the row tile)
 // wide: eight warps instead of four share the keys of a 16-row tile
 cudaError_t launch_seg_mma(const SegParams& p, int pass, int tile_rows, bool wide, cudaStream_t st, int* launches);
 // both: the items of pass 1 follow those of pass 0 in the same launch; alt: 128-row tiles whose keys two streams take in turn
 cudaError_t launch_seg_tc(const SegParams& p, int pass, bool both, bool alt, cudaStream_t st, int* launches);
-cudaError_t launch_seg_f32(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches);
+cudaError_t launch_seg_f32(const SegParams& p, int pass, int tile_rows, cudaStream_t st, int* launches);
 
 }  // namespace swam

@@ -18,6 +18,19 @@ __device__ __forceinline__ void cp16(void* dst, const void* src, uint32_t bytes)
                ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes) : "memory");
 }
 
+// two multiply-adds in one instruction
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 template <int D, int RPT>
 struct F32Cfg {
   static constexpr int MR = 16 * RPT;
@@ -70,13 +83,14 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
     const SegRow row = seg_row(p, ps, it, it.row0 + ty + 16 * i);
     lim1[i] = seg_limit1(a, kk.end > kk.n0 ? seg_len(p, 1, row.b) : 0, row.t);
   }
-  float o[RPT][D / 8], m[RPT], l[RPT];
+  uint64_t o2[RPT][D / 16];                        // output columns 4 tx + 32 c + (0, 1) and (2, 3)
+  float m[RPT], l[RPT];
 #pragma unroll
   for (int i = 0; i < RPT; ++i) {
     m[i] = -INFINITY;
     l[i] = 0.f;
 #pragma unroll
-    for (int c = 0; c < D / 8; ++c) o[i][c] = 0.f;
+    for (int c = 0; c < D / 16; ++c) o2[i][c] = 0ull;
   }
   if (kk.begin < kk.end) load_tile(kk.begin);
   asm volatile("cp.async.commit_group;" ::: "memory");
@@ -89,25 +103,31 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
     const int st = (t - kk.begin) & 1;
     const float* K = sK + st * C::kK;
     const float* V = sV + st * C::kV;
-    float sc[RPT][4];
+    // sums over even and odd elements side by side
+    uint64_t sc2[RPT][4];
 #pragma unroll
-    for (int i = 0; i < RPT; ++i) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
-#pragma unroll 8
+    for (int i = 0; i < RPT; ++i) sc2[i][0] = sc2[i][1] = sc2[i][2] = sc2[i][3] = 0ull;
+#pragma unroll 4
     for (int d = 0; d < D; d += 4) {
-      float4 q4[RPT], k4[4];
+      ulonglong2 q4[RPT], k4[4];
 #pragma unroll
-      for (int i = 0; i < RPT; ++i) q4[i] = *reinterpret_cast<const float4*>(sQ + (ty + 16 * i) * QS + d);
+      for (int i = 0; i < RPT; ++i) q4[i] = *reinterpret_cast<const ulonglong2*>(sQ + (ty + 16 * i) * QS + d);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4*>(K + (tx + 8 * j) * QS + d);
+      for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const ulonglong2*>(K + (tx + 8 * j) * QS + d);
 #pragma unroll
       for (int i = 0; i < RPT; ++i) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          sc[i][j] = fmaf(q4[i].x, k4[j].x, sc[i][j]);
-          sc[i][j] = fmaf(q4[i].y, k4[j].y, sc[i][j]);
-          sc[i][j] = fmaf(q4[i].z, k4[j].z, sc[i][j]);
-          sc[i][j] = fmaf(q4[i].w, k4[j].w, sc[i][j]);
-        }
+        for (int j = 0; j < 4; ++j) sc2[i][j] = fma2(q4[i].y, k4[j].y, fma2(q4[i].x, k4[j].x, sc2[i][j]));
+      }
+    }
+    float sc[RPT][4];
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float lo, hi;
+        unpack2(sc2[i][j], lo, hi);
+        sc[i][j] = lo + hi;
       }
     }
     const int seg = t >= kk.n0 ? 1 : 0;
@@ -134,8 +154,9 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
         l[i] += e;
         sP[(tx + 8 * j) * PS + ty * RPT + i] = e;
       }
+      const uint64_t corr2 = pack2(corr, corr);
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) o[i][c] *= corr;
+      for (int c = 0; c < D / 16; ++c) o2[i][c] = fma2(o2[i][c], corr2, 0ull);
     }
     __syncwarp();                // a warp reads only the P columns of its own rows
 #pragma unroll 4
@@ -147,19 +168,22 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
         pr[1] = p4.y;
         pr[2] = p4.z;
         pr[3] = p4.w;
+      } else if constexpr (RPT == 2) {
+        const float2 p2 = *reinterpret_cast<const float2*>(sP + key * PS + ty * 2);
+        pr[0] = p2.x;
+        pr[1] = p2.y;
       } else {
 #pragma unroll
         for (int i = 0; i < RPT; ++i) pr[i] = sP[key * PS + ty * RPT + i];
       }
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
-        const float4 v4 = *reinterpret_cast<const float4*>(V + key * D + c * 32 + tx * 4);
+        const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(V + key * D + c * 32 + tx * 4);
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
-          o[i][c * 4 + 0] = fmaf(pr[i], v4.x, o[i][c * 4 + 0]);
-          o[i][c * 4 + 1] = fmaf(pr[i], v4.y, o[i][c * 4 + 1]);
-          o[i][c * 4 + 2] = fmaf(pr[i], v4.z, o[i][c * 4 + 2]);
-          o[i][c * 4 + 3] = fmaf(pr[i], v4.w, o[i][c * 4 + 3]);
+          const uint64_t p2 = pack2(pr[i], pr[i]);
+          o2[i][c * 2] = fma2(p2, v4.x, o2[i][c * 2]);
+          o2[i][c * 2 + 1] = fma2(p2, v4.y, o2[i][c * 2 + 1]);
         }
       }
     }
@@ -178,9 +202,12 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
     float* dst = p.direct ? (float*)a.out + row.b * a.o_smp + row.t * a.o_tok + (int64_t)row.h * D : p.part_o + pr * D;
     const float inv = p.direct ? (sum > 0.f ? 1.f / sum : 0.f) : 1.f;
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c)
-      *reinterpret_cast<float4*>(dst + c * 32 + tx * 4) =
-          make_float4(o[i][c * 4] * inv, o[i][c * 4 + 1] * inv, o[i][c * 4 + 2] * inv, o[i][c * 4 + 3] * inv);
+    for (int c = 0; c < D / 32; ++c) {
+      float4 w;
+      unpack2(o2[i][c * 2], w.x, w.y);
+      unpack2(o2[i][c * 2 + 1], w.z, w.w);
+      *reinterpret_cast<float4*>(dst + c * 32 + tx * 4) = make_float4(w.x * inv, w.y * inv, w.z * inv, w.w * inv);
+    }
     if (tx == 0) {
       if (!p.direct) p.part_ml[pr] = make_float2(m[i], sum);
       else if (a.lse)
@@ -201,17 +228,18 @@ cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launc
   return cudaGetLastError();
 }
 template <int D>
-cudaError_t launch_rows(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches) {
-  return seg_f32_tile_rows(rows) == 16 ? launch_one<D, 1>(p, pass, st, launches) : launch_one<D, 4>(p, pass, st, launches);
+cudaError_t launch_rows(const SegParams& p, int pass, int tile_rows, cudaStream_t st, int* launches) {
+  return tile_rows == 16 ? launch_one<D, 1>(p, pass, st, launches)
+                         : (tile_rows == 32 ? launch_one<D, 2>(p, pass, st, launches) : launch_one<D, 4>(p, pass, st, launches));
 }
 
 }  // namespace
 
-cudaError_t launch_seg_f32(const SegParams& p, int pass, int64_t rows, cudaStream_t st, int* launches) {
+cudaError_t launch_seg_f32(const SegParams& p, int pass, int tile_rows, cudaStream_t st, int* launches) {
   switch (p.a.D) {
-    case 32: return launch_rows<32>(p, pass, rows, st, launches);
-    case 64: return launch_rows<64>(p, pass, rows, st, launches);
-    case 128: return launch_rows<128>(p, pass, rows, st, launches);
+    case 32: return launch_rows<32>(p, pass, tile_rows, st, launches);
+    case 64: return launch_rows<64>(p, pass, tile_rows, st, launches);
+    case 128: return launch_rows<128>(p, pass, tile_rows, st, launches);
     default: return cudaErrorInvalidConfiguration;
   }
 }
