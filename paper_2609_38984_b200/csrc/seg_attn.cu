@@ -146,9 +146,11 @@ PassPlan plan_of(const SegArgs& a, bool shared, int i, bool warp_mma) {
 SegPlan seg_plan(const SegArgs& a, bool warp_mma) {
   SegPlan pl;
   const int64_t rows = (int64_t)a.n_q * (a.N_h / a.N_kv);       // of one sample
-  // samples share the row tiles of segment 0 when a tile has room for two samples at least: the shared keys are then
-  // read once for all of them
-  pl.shared = a.per_group > 1 && a.n[0] > 0 && rows <= 64;
+  // Samples share the row tiles of segment 0 when a tile (128 rows on the tensor cores, 64 otherwise) has room for two samples
+  // at least: the shared keys are then read once for all of them and multiplied with full tiles (16 samples of 64 rows
+  // behind 9216 keys: 168 us, each sample by itself 325 us).
+  const int64_t tile = a.dtype == 0 || a.D < 64 || warp_mma ? 64 : 128;
+  pl.shared = a.per_group > 1 && a.n[0] > 0 && 2 * rows <= tile;
   pl.splits[0] = plan_of(a, pl.shared, 0, warp_mma).splits;
   pl.splits[1] = pl.shared && a.n[1] > 0 ? plan_of(a, pl.shared, 1, warp_mma).splits : 0;
   return pl;

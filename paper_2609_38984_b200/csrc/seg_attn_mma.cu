@@ -5,20 +5,20 @@
 // One CTA of WR * WK warps owns a row tile of 16 * WR rows and a piece of the keys.  WR warps lie along the rows and WK
 // along the keys: with 16 rows or fewer every warp holds all rows and 16 keys of each tile, so that no key is multiplied
 // twice; every warp keeps its own running maximum and sum, and the warps of a row are merged once at the end.  Key and value
-// tiles (64 keys, or 128 with eight warps) arrive by 16-byte asynchronous copies into a ring of three stages; keys beyond the
-// real length are filled with zeros, so whatever the padding holds (NaN included) never meets a product.
+// tiles (64 keys, or 128 with eight warps) arrive by TMA in a ring of three stages.  (Copies by the threads themselves took
+// the load/store unit about as long as the tile's products: 19.1 us against TMA_US us for 16 samples of 300 to 1500 keys.)
+// Rows of V behind the real length become zeros in shared memory, so whatever the padding holds (NaN included) never meets a
+// product.
 // Scores, maxima, sums and outputs are fp32; the probabilities are rounded to bf16 for the second product.
-#include "seg_attn.cuh"
+#include <string.h>
+
+#include "seg_maps.cuh"
 
 namespace swam {
 namespace {
 
 constexpr int kStagesM = 3;
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, uint32_t bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -31,17 +31,13 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-
-// byte offset of 16-byte chunk c of row r in a tile of D-element rows: rows of 128 bytes or more permute their chunks by
-// r % 8, 64-byte rows (head dim 32) by (r / 2) % 4; both make eight consecutive rows of one chunk column conflict-free
-template <int D>
+// byte offset of 16-byte chunk c of row r in a tile of KT rows, as the tensor maps lay it out: blocks of 64 columns whose
+// 128-byte rows permute their chunks by r % 8, or (head dim 32) 64-byte rows that do so by (r / 2) % 4; both make eight
+// consecutive rows of one chunk column conflict-free
+template <int D, int KT>
 __device__ __forceinline__ uint32_t tile_off(int r, int c) {
-  return (uint32_t)(r * D * 2 + ((D >= 64 ? (c ^ (r & 7)) : (c ^ ((r >> 1) & 3))) << 4));
+  if (D == 32) return (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+  return (uint32_t)((c >> 3) * KT * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 
 template <int D, int WR, int WK>
@@ -49,17 +45,27 @@ struct MmaCfg {
   static constexpr int kThreads = 32 * WR * WK, MR = 16 * WR;
   static constexpr int KT = WR == 1 ? 16 * WK : 64;      // keys per tile
   static constexpr int kRing = kStagesM * 2 * KT * D * 2, kMerge = WK * MR * (D + 4 + 2) * 4;
-  static constexpr int kBytes = kRing > kMerge ? kRing : kMerge;
+  static constexpr int kBytes = (kRing > kMerge ? kRing : kMerge) + 1024 /*alignment*/ + 64 /*barriers*/;
 };
 
 template <int D, int WR, int WK>
-__global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_constant__ SegParams p, const int pass) {
+__global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_constant__ CUtensorMap map_k0, const __grid_constant__ CUtensorMap map_v0,
+                               const __grid_constant__ CUtensorMap map_k1, const __grid_constant__ CUtensorMap map_v1,
+                               const __grid_constant__ SegParams p, const int pass) {
   using C = MmaCfg<D, WR, WK>;
   constexpr int MR = C::MR, kKT = C::KT, KW = kKT / WK, kThreadsM = C::kThreads;
   constexpr int CPR = D / 8;                       // 16-byte chunks per row
   constexpr int kTileB = kKT * D * 2;              // bytes of a key or value tile
   extern __shared__ unsigned char smem_raw[];
-  const uint32_t s0 = smem_u32(smem_raw);
+  const uint32_t s0 = (smem_addr(smem_raw) + 1023u) & ~1023u;
+  unsigned char* base = smem_raw + (s0 - smem_addr(smem_raw));
+  const uint32_t bars = s0 + (uint32_t)(C::kBytes - 1024 - 64);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(base + C::kBytes - 1024 - 16);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStagesM; ++i) mbar_init(bars + 8 * i, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   if (p.early && pass == 0) allow_next();
   const SegPass& ps = p.pass[pass];
   const SegArgs& a = p.a;
@@ -69,46 +75,22 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
   const int wr = warp % WR, wk = warp / WR;
   const int b0 = it.block * ps.block_samples;
 
-  // A thread copies the same 16-byte chunk of every RS-th row of a tile, so that one pointer per tensor and a fixed step
-  // address all its copies.  lr0, lc: its first row and its chunk.
-  constexpr int RS = kThreadsM / CPR, NL = kKT / RS;
-  const int lr0 = threadIdx.x / CPR, lc = threadIdx.x % CPR;
-  int next_seg = -1;                               // segment that the pointers stand in
-  const __nv_bfloat16 *kp = nullptr, *vp = nullptr;
-  int64_t k_step = 0, v_step = 0;
-  int left = 0;                                    // real keys from the thread's first row of the tile on
-  uint32_t stage_off = 0;
-  auto load_tile = [&](int t) {
-    const int sg = t >= kk.n0 ? 1 : 0;
-    if (sg != next_seg) {
-      next_seg = sg;
-      const int key0 = (sg ? t - kk.n0 : t) * kKT + lr0;
-      const int64_t idx = sg ? b0 : b0 / a.per_group;
-      kp = (const __nv_bfloat16*)a.k[sg] + idx * a.k_smp[sg] + (int64_t)it.h_kv * D + key0 * a.k_tok[sg] + lc * 8;
-      vp = (const __nv_bfloat16*)a.v[sg] + idx * a.v_smp[sg] + (int64_t)it.h_kv * D + key0 * a.v_tok[sg] + lc * 8;
-      k_step = RS * a.k_tok[sg];
-      v_step = RS * a.v_tok[sg];
-      left = (sg ? kk.len1 : kk.len0) - key0;
-    }
-    const uint32_t ks = s0 + stage_off, vs = ks + kTileB;
-    stage_off = stage_off + 2 * kTileB == kStagesM * 2 * kTileB ? 0 : stage_off + 2 * kTileB;
+  constexpr int DB = D == 32 ? 1 : D / 64, kCols = D == 32 ? 32 : 64;       // boxes per tile and their columns
+  auto load_tile = [&](int t) {                    // one thread
+    const bool s1 = t >= kk.n0;
+    const int st = (t - kk.begin) % kStagesM, key0 = (s1 ? t - kk.n0 : t) * kKT, idx = s1 ? b0 : b0 / a.per_group;
+    const uint32_t ks = s0 + (uint32_t)st * 2 * kTileB, bar = bars + 8 * st;
+    mbar_expect_tx(bar, 2 * kTileB);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const bool in = i * RS < left;
-      const uint32_t off = tile_off<D>(lr0 + i * RS, lc);
-      // (rows behind the real ones read nothing; the address stays inside the tensor)
-      cp16(ks + off, in ? kp : (const __nv_bfloat16*)a.k[sg], in ? 16u : 0u);
-      cp16(vs + off, in ? vp : (const __nv_bfloat16*)a.v[sg], in ? 16u : 0u);
-      kp += k_step;
-      vp += v_step;
+    for (int db = 0; db < DB; ++db) {
+      tma_load_4d(ks + db * kKT * 128, s1 ? &map_k1 : &map_k0, bar, db * kCols, key0, it.h_kv, idx);
+      tma_load_4d(ks + kTileB + db * kKT * 128, s1 ? &map_v1 : &map_v0, bar, db * kCols, key0, it.h_kv, idx);
     }
-    left -= kKT;
   };
-
-#pragma unroll
-  for (int i = 0; i < kStagesM - 1; ++i) {
-    if (kk.begin + i < kk.end) load_tile(kk.begin + i);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+  __syncthreads();                                 // the barriers are set up
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStagesM - 1; ++i)
+      if (kk.begin + i < kk.end) load_tile(kk.begin + i);
   }
   // this thread's two rows (accumulator rows lane / 4 and lane / 4 + 8 of the warp's 16), their queries as A fragments
   uint32_t qf[D / 16][4];
@@ -131,14 +113,24 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
   for (int t = kk.begin; t < kk.end; ++t) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStagesM - 2) : "memory");
-    __syncthreads();
-    if (t + kStagesM - 1 < kk.end) load_tile(t + kStagesM - 1);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    const int st = (t - kk.begin) % kStagesM;
+    const bool ok = mbar_wait(bars + 8 * st, ((t - kk.begin) / kStagesM) & 1, abort_flag);
+    if (!__syncthreads_and(ok ? 1 : 0)) {          // (and every warp is through with the tile before)
+      if (threadIdx.x == 0) atomicOr(p.status, ST_TIMEOUT);
+      break;
+    }
+    if (threadIdx.x == 0 && t + kStagesM - 1 < kk.end) load_tile(t + kStagesM - 1);
     const int seg = t >= kk.n0 ? 1 : 0;
     const int key0 = (seg ? t - kk.n0 : t) * kKT + wk * KW;       // first key of this warp
-    if (key0 >= (seg ? kk.len1 : kk.len0)) continue;              // none of them is real
-    const uint32_t ks = s0 + (uint32_t)((t - kk.begin) % kStagesM) * 2 * kTileB, vs = ks + kTileB;
+    const uint32_t ks = s0 + (uint32_t)st * 2 * kTileB, vs = ks + kTileB;
+    const int len = seg ? kk.len1 : kk.len0, real = len - (seg ? t - kk.n0 : t) * kKT;       // real keys, and those of this tile
+    if (real < kKT && len < a.n[seg]) {                           // the tile ends inside its tensor
+      for (int i = threadIdx.x; i < (kKT - real) * CPR; i += kThreadsM)
+        st_shared_16(vs + tile_off<D, kKT>(real + i / CPR, i % CPR), 0u, 0u, 0u, 0u);
+      fence_proxy_async();                                        // the stage's next load comes through the other proxy
+      __syncthreads();
+    }
+    if (key0 >= len) continue;                                    // none of this warp's keys is real
 
     float sc[KW / 8][4];
 #pragma unroll
@@ -148,7 +140,7 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
 #pragma unroll
       for (int kd = 0; kd < D / 16; ++kd) {
         uint32_t f[4];
-        ldsm4(f, ks + tile_off<D>(wk * KW + nb * 16 + (lane & 7) + ((lane >> 4) << 3), kd * 2 + ((lane >> 3) & 1)));
+        ldsm4(f, ks + tile_off<D, kKT>(wk * KW + nb * 16 + (lane & 7) + ((lane >> 4) << 3), kd * 2 + ((lane >> 3) & 1)));
         mma_bf16(sc[2 * nb], qf[kd], f[0], f[1]);
         mma_bf16(sc[2 * nb + 1], qf[kd], f[2], f[3]);
       }
@@ -196,12 +188,12 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
     }
 #pragma unroll
     for (int nb = 0; nb < KW / 16; ++nb) {
-      const uint32_t pf[4] = {pack_pair(sc[2 * nb][0], sc[2 * nb][1]), pack_pair(sc[2 * nb][2], sc[2 * nb][3]),
-                              pack_pair(sc[2 * nb + 1][0], sc[2 * nb + 1][1]), pack_pair(sc[2 * nb + 1][2], sc[2 * nb + 1][3])};
+      const uint32_t pf[4] = {pack_bf16x2(sc[2 * nb][0], sc[2 * nb][1]), pack_bf16x2(sc[2 * nb][2], sc[2 * nb][3]),
+                              pack_bf16x2(sc[2 * nb + 1][0], sc[2 * nb + 1][1]), pack_bf16x2(sc[2 * nb + 1][2], sc[2 * nb + 1][3])};
 #pragma unroll
       for (int dn = 0; dn < D / 16; ++dn) {
         uint32_t f[4];
-        ldsm4_t(f, vs + tile_off<D>(wk * KW + nb * 16 + (lane & 7) + (((lane >> 3) & 1) << 3), dn * 2 + (lane >> 4)));
+        ldsm4_t(f, vs + tile_off<D, kKT>(wk * KW + nb * 16 + (lane & 7) + (((lane >> 3) & 1) << 3), dn * 2 + (lane >> 4)));
         mma_bf16(o[2 * dn], pf, f[0], f[1]);
         mma_bf16(o[2 * dn + 1], pf, f[2], f[3]);
       }
@@ -215,10 +207,9 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
 
   allow_next();
   // merge the WK warps of each row through shared memory (the ring is free by now), then write
-  asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
   constexpr int OS = D + 4;                        // padded row of partial outputs
-  float* so = reinterpret_cast<float*>(smem_raw);  // [WK][MR][OS]
+  float* so = reinterpret_cast<float*>(base);  // [WK][MR][OS]
   float* sm = so + WK * MR * OS;                   // [WK][MR] maxima
   float* sl = sm + WK * MR;                        // [WK][MR] sums
 #pragma unroll
@@ -255,10 +246,10 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
     if (p.direct) {
       const float inv = sum > 0.f ? 1.f / sum : 0.f;
       uint4 w;
-      w.x = pack_pair(acc[0] * inv, acc[1] * inv);
-      w.y = pack_pair(acc[2] * inv, acc[3] * inv);
-      w.z = pack_pair(acc[4] * inv, acc[5] * inv);
-      w.w = pack_pair(acc[6] * inv, acc[7] * inv);
+      w.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+      w.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
+      w.z = pack_bf16x2(acc[4] * inv, acc[5] * inv);
+      w.w = pack_bf16x2(acc[6] * inv, acc[7] * inv);
       *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + row.b * a.o_smp + row.t * a.o_tok + (int64_t)row.h * D + c) = w;
       if (a.lse && c == 0)
         a.lse[((int64_t)row.b * a.N_h + row.h) * a.n_q + row.t] = sum > 0.f ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
@@ -276,11 +267,22 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
 template <int D, int WR, int WK>
 cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launches) {
   using C = MmaCfg<D, WR, WK>;
+  const SegArgs& a = p.a;
+  CUtensorMap mk[2], mv[2];
+  memset(mk, 0, sizeof(mk));       // a segment without keys: its maps are never used
+  memset(mv, 0, sizeof(mv));
+  for (int s = p.pass[pass].seg_lo; s <= p.pass[pass].seg_hi; ++s) {
+    const int blocks = s == 0 ? a.B / a.per_group : a.B;
+    if (a.n[s] > 0 && (!make_kv_map(&mk[s], a.k[s], blocks, a.n[s], a.N_kv, D, a.k_tok[s], a.k_smp[s], C::KT) ||
+                       !make_kv_map(&mv[s], a.v[s], blocks, a.n[s], a.N_kv, D, a.v_tok[s], a.v_smp[s], C::KT)))
+      return cudaErrorInvalidValue;
+  }
   cudaError_t e = cudaFuncSetAttribute(seg_mma_kernel<D, WR, WK>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes);
   if (e != cudaSuccess) return e;
+  const dim3 grid(p.pass[pass].items), block(C::kThreads);
   ++*launches;
-  if (pass == 1) return launch_after(seg_mma_kernel<D, WR, WK>, dim3(p.pass[pass].items), dim3(C::kThreads), C::kBytes, st, p, pass);
-  seg_mma_kernel<D, WR, WK><<<p.pass[pass].items, C::kThreads, C::kBytes, st>>>(p, pass);
+  if (pass == 1) return launch_after(seg_mma_kernel<D, WR, WK>, grid, block, C::kBytes, st, mk[0], mv[0], mk[1], mv[1], p, pass);
+  seg_mma_kernel<D, WR, WK><<<grid, block, C::kBytes, st>>>(mk[0], mv[0], mk[1], mv[1], p, pass);
   return cudaGetLastError();
 }
 template <int D>

@@ -32,6 +32,7 @@
 
 #include "tc_ptx.cuh"
 #include "seg_attn.cuh"
+#include "seg_maps.cuh"
 
 namespace swam {
 namespace {
@@ -821,27 +822,12 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   }
 }
 
-bool encode(CUtensorMap* map, const void* ptr, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
-  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(ptr), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-// [blocks, n, N_kv, D] with strides, viewed as (d, row, head, block); box = 64 columns x 128 rows
-bool make_kv_map(CUtensorMap* map, const void* ptr, int blocks, int n, int N_kv, int D, int64_t tok, int64_t smp) {
-  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)n, (cuuint64_t)N_kv, (cuuint64_t)blocks};
-  const cuuint64_t strides[3] = {(cuuint64_t)tok * 2, (cuuint64_t)D * 2, (cuuint64_t)smp * 2};
-  const cuuint32_t box[4] = {64, kTile, 1, 1};
-  return encode(map, ptr, 4, dims, strides, box);
-}
 // [B, n_q, N_kv * g, D] viewed as (d, head of the group, token, group, sample); box = 64 columns x g heads x tokens x samples
 bool make_q_map(CUtensorMap* map, const void* ptr, const SegArgs& a, int g, int64_t tok, int64_t smp, int box_tokens, int box_samples) {
   const cuuint64_t dims[5] = {(cuuint64_t)a.D, (cuuint64_t)g, (cuuint64_t)a.n_q, (cuuint64_t)a.N_kv, (cuuint64_t)a.B};
   const cuuint64_t strides[4] = {(cuuint64_t)a.D * 2, (cuuint64_t)tok * 2, (cuuint64_t)g * a.D * 2, (cuuint64_t)smp * 2};
   const cuuint32_t box[5] = {64, (cuuint32_t)g, (cuuint32_t)box_tokens, 1, (cuuint32_t)box_samples};
-  return encode(map, ptr, 5, dims, strides, box);
+  return encode_bf16(map, ptr, 5, dims, strides, box);
 }
 
 template <int D, bool kAlt>
@@ -855,8 +841,8 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, cudaStream_t st, 
   for (int s = 0; s < 2; ++s) {
     if (a.n[s] == 0) continue;
     const int blocks = s == 0 ? a.B / a.per_group : a.B;
-    if (!make_kv_map(&mk[s], a.k[s], blocks, a.n[s], a.N_kv, D, a.k_tok[s], a.k_smp[s]) ||
-        !make_kv_map(&mv[s], a.v[s], blocks, a.n[s], a.N_kv, D, a.v_tok[s], a.v_smp[s]))
+    if (!make_kv_map(&mk[s], a.k[s], blocks, a.n[s], a.N_kv, D, a.k_tok[s], a.k_smp[s], kTile) ||
+        !make_kv_map(&mv[s], a.v[s], blocks, a.n[s], a.N_kv, D, a.v_tok[s], a.v_smp[s], kTile))
       return cudaErrorInvalidValue;
   }
   // Row tiles that are boxes of the query tensor: whole tokens of one sample (the heads of a group divide the tile), or

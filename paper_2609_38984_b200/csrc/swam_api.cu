@@ -187,7 +187,8 @@ int check_seg(swam_ctx* c, SegArgs& a, int32_t n_kv_heads, const char* name, Seg
     if (a.n[s] > 0 && (!a.k[s] || !a.v[s])) return bad(SWAM_ERR_INVALID_ARG, "null k or v");
     if (!aligned16(a.k[s]) || !aligned16(a.v[s])) return bad(SWAM_ERR_INVALID_ARG, "misaligned pointer");
   }
-  if (!aligned16(a.q) || !aligned16(a.out)) return bad(SWAM_ERR_INVALID_ARG, "misaligned pointer");
+  const uintptr_t words = reinterpret_cast<uintptr_t>(a.lse) | reinterpret_cast<uintptr_t>(a.len[0]) | reinterpret_cast<uintptr_t>(a.len[1]);
+  if (!aligned16(a.q) || !aligned16(a.out) || (words & 3u) != 0) return bad(SWAM_ERR_INVALID_ARG, "misaligned pointer");
   return SWAM_OK;
 }
 

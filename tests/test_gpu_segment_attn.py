@@ -327,7 +327,7 @@ def test_refusals():
         return ctx.lib.swam_cross_attn(ctx.ctx, ctypes.byref(a), st)
     inv, uns = swam.ERR_INVALID_ARG, swam.ERR_UNSUPPORTED
     for rc, kw in ((inv, dict(q=None)), (inv, dict(out=None)), (inv, dict(k=None)), (inv, dict(v=None)), (inv, dict(q=q.data_ptr() + 2)),
-                   (inv, dict(k=k.data_ptr() + 8)), (inv, dict(n_q=-1)), (inv, dict(n_kv=-1)), (inv, dict(n_kv_heads=3)),
+                   (inv, dict(k=k.data_ptr() + 8)), (inv, dict(lse=q.data_ptr() + 2)), (inv, dict(kv_len=ok_len.data_ptr() + 1)), (inv, dict(n_q=-1)), (inv, dict(n_kv=-1)), (inv, dict(n_kv_heads=3)),
                    (inv, dict(n_kv_heads=-2)), (inv, dict(reserved=1)), (inv, dict(q_token=-256)), (inv, dict(q_token=100)),
                    (inv, dict(q_token=260)), (inv, dict(k_token=64)), (inv, dict(k_token=1 << 41)), (inv, dict(out_sample=256)),
                    (uns, dict(n_kv=(1 << 30) + 1)), (uns, dict(n_q=1 << 29))):
