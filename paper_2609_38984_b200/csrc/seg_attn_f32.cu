@@ -4,7 +4,11 @@
 // arrive by asynchronous copies into two stages.  Thread (ty, tx) of a 16 x 8 arrangement holds rows ty + 16 i and keys
 // tx + 8 j of the score tile, then the same rows and output columns 4 tx + 32 c: every shared-memory load of four floats
 // feeds RPT or 4 * RPT multiply-adds, so with RPT = 4 the FMA pipes and not the shared-memory port are the bound.
-// RPT = 1 (16 rows) serves single tokens.  Keys beyond the real length are filled with zeros and masked.
+// RPT = 1 (16 rows) serves single tokens, RPT = 2 (32) calls too small to fill the SMs with 64 rows.  Keys beyond the real
+// length are filled with zeros and masked.
+// What bounds it: latency.  4 x 1000 rows, 8 heads of 64, 100 to 333 keys take 84 us (21 TFLOP/s of some 70 on the FMA pipes): three
+// CTAs an SM leave 2.3 warps a scheduler, which issue every 2.2 clk.  Four CTAs with single K and V buffers took 86 us, 32-row
+// tiles 92.
 #include "seg_attn.cuh"
 
 namespace swam {

@@ -13,10 +13,12 @@
 //   warps 0-3    softmax of stream 0, one thread per row: S row from TMEM, exponentials against a running reference
 //   warps 4-7    maximum (exp2 domain, raised only when a row outgrows it by 2^8: exact either way), P as bf16; same for
 //                stream 1.  The streams' exponentials overlap each other's products.
-// P goes back over its scores in TMEM: a product of two operands in shared memory reads as many bytes as that port delivers
-// (8 KB per 64 clk at 128 x 128 x 16), so a P in shared memory, stored and read again, would bound the kernel at 1.5 times
-// the tensor pipe's time at head dim 128.  TMEM holds three score buffers beside the outputs at head dim 64 and two at 128;
-// P V of a unit (one key tile of one stream) frees the buffer that the Q K^T three (two) units on takes.
+// P goes back over its scores in TMEM (rounded to bf16, the operand type: half a step, 2^-8, of each weight).  TMEM holds three
+// score buffers beside the outputs at head dim 64 and two at 128; P V of a unit (one key tile of one stream) frees the buffer
+// that the Q K^T three (two) units on takes.  (At head dim 128 the chain softmax, P V, Q K^T then sets the period: 3110 clk a
+// key tile for 2048 clk of tensor work.  P through shared memory breaks that chain, but its 64 KB are the second query buffer,
+// without which short key ranges pay: 13.3 us instead of 11.1 an item of 256 rows and 512 keys, for 65.1 instead of 62.4 at
+// 4096 keys.  P in halves, so that its first product starts earlier, was 3 % slower.)
 // Q K^T runs ahead of P V across the borders of items.  An item's output is written after the first exponentials of the
 // next one: the wait for its last product and the read of the accumulator then lie under work that is there anyway.  It
 // leaves through the item's own query tiles, which are free by then; the next item's queries are in a second buffer.
@@ -28,6 +30,10 @@
 // row); scores behind a row's limit become -inf.
 // Every wait on an mbarrier is bounded; when one runs out the kernel raises the timeout bit of the status word and every
 // role falls through to the exit.
+// What bounds it (cycles counted in the kernel, 1.65 to 1.85 GHz under this load): head dim 128, 3110 clk a key tile of an item
+// (1.33 PFLOP/s at 4096 keys, 0.8 of the measured burst rate) and 4300 clk an item; head dim 64, 2600 clk a key tile, of which the exp2
+// unit (16 a clk) needs 1792, and 2600 clk an item for its first scores' maximum, the read of the accumulators and the
+// bookkeeping between two items.
 #include <string.h>
 
 #include "tc_ptx.cuh"
