@@ -109,7 +109,7 @@ struct PassPlan {
 };
 PassPlan plan_pass(const SegArgs& a, int64_t blocks, int64_t rows, int64_t keys, bool warp_mma, int pass) {
   PassPlan p;
-  const int sms = sm_count();
+  const int sms = a.sms;
   // Few rows stream their keys through the warp-level kernel; from 33 rows on the tensor cores' tiles are filled well enough
   // (from 65 on with few keys, where the larger kernel's start costs more than its rate gains).
   p.kind = a.dtype == 0 ? kF32 : (a.D < 64 || warp_mma || rows <= 32 || (rows <= 64 && keys <= 512) ? kMma : kTc);

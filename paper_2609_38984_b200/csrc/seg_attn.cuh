@@ -5,6 +5,8 @@
 // by the tiles of segment 1.  A work item is (block, key/value head, row tile, piece of the key tiles).  Lengths live
 // on the device, so the pieces are cut there: the real key tiles of an item's block are shared out evenly.
 #pragma once
+#include <atomic>
+
 #include "swam_internal.cuh"
 
 namespace swam {
@@ -110,6 +112,17 @@ __device__ __forceinline__ SegKeys seg_keys(const SegParams& p, const SegPass& p
 // waiting for both.
 __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Opts a kernel in to its dynamic shared memory, once per device (every launch function has one of these).
+struct SmemOptIn {
+  std::atomic<uint64_t> done{0};
+  cudaError_t operator()(const void* kernel, int bytes, int device) {
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && device < 64) done.fetch_or(bit, std::memory_order_release);
+    return e;
+  }
+};
 template <typename... Params, typename... Args>
 cudaError_t launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchAttribute attr;

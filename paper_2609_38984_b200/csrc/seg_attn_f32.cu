@@ -224,7 +224,8 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
 template <int D, int RPT>
 cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launches) {
   constexpr int smem = F32Cfg<D, RPT>::kBytes;
-  cudaError_t e = cudaFuncSetAttribute(seg_f32_kernel<D, RPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static SmemOptIn opt_in;
+  cudaError_t e = opt_in((const void*)seg_f32_kernel<D, RPT>, smem, p.a.device);
   if (e != cudaSuccess) return e;
   ++*launches;
   if (pass == 1) return launch_after(seg_f32_kernel<D, RPT>, dim3(p.pass[pass].items), dim3(kThreadsF), smem, st, p, pass);

@@ -281,7 +281,8 @@ cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launc
                        !make_kv_map(&mv[s], a.v[s], blocks, a.n[s], a.N_kv, D, a.v_tok[s], a.v_smp[s], C::KT)))
       return cudaErrorInvalidValue;
   }
-  cudaError_t e = cudaFuncSetAttribute(seg_mma_kernel<D, WR, WK>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes);
+  static SmemOptIn opt_in;
+  cudaError_t e = opt_in((const void*)seg_mma_kernel<D, WR, WK>, C::kBytes, a.device);
   if (e != cudaSuccess) return e;
   const dim3 grid(p.pass[pass].items), block(C::kThreads);
   ++*launches;

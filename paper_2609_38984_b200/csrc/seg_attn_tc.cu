@@ -16,9 +16,9 @@
 // P goes back over its scores in TMEM (rounded to bf16, the operand type: half a step, 2^-8, of each weight).  TMEM holds three
 // score buffers beside the outputs at head dim 64 and two at 128; P V of a unit (one key tile of one stream) frees the buffer
 // that the Q K^T three (two) units on takes.  (At head dim 128 the chain softmax, P V, Q K^T then sets the period: 3110 clk a
-// key tile for 2048 clk of tensor work.  P through shared memory breaks that chain, but its 64 KB are the second query buffer,
-// without which short key ranges pay: 13.3 us instead of 11.1 an item of 256 rows and 512 keys, for 65.1 instead of 62.4 at
-// 4096 keys.  P in halves, so that its first product starts earlier, was 3 % slower.)
+// key tile for 2048 clk of tensor work.  P through shared memory breaks that chain, but its 64 KB are the second query
+// buffer: a build of it, with some register spills, took 13.3 us instead of 11.1 for an item of 256 rows and 512 keys, and 65.1
+// instead of 60.8 at 4096 keys.  P in halves, so that its first product starts earlier, was 3 % slower.)
 // Q K^T runs ahead of P V across the borders of items.  An item's output is written after the first exponentials of the
 // next one: the wait for its last product and the read of the accumulator then lie under work that is there anyway.  It
 // leaves through the item's own query tiles, which are free by then; the next item's queries are in a second buffer.
@@ -863,9 +863,10 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, cudaStream_t st, 
   if (x.box_out && !make_q_map(&mo, a.out, a, p.g, a.o_tok, a.o_smp, bt, bs)) return cudaErrorInvalidValue;
   x.items = p.pass[pass].items + (both ? p.pass[1].items : 0);
   constexpr int smem = SegCfg<D, kAlt>::kBytes;
-  cudaError_t e = cudaFuncSetAttribute(seg_tc_kernel<D, kAlt>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static SmemOptIn opt_in;
+  cudaError_t e = opt_in((const void*)seg_tc_kernel<D, kAlt>, smem, a.device);
   if (e != cudaSuccess) return e;
-  const int sms = sm_count(), grid = x.items < sms ? x.items : sms;
+  const int grid = x.items < a.sms ? x.items : a.sms;
   ++*launches;
   if (pass == 1) return launch_after(seg_tc_kernel<D, kAlt>, dim3(grid), dim3(kThreadsS), smem, st, mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x);
   seg_tc_kernel<D, kAlt><<<grid, kThreadsS, smem, st>>>(mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x);

@@ -16,6 +16,7 @@ struct swam_ctx {
   Dims d;
   Alpha alpha;
   int device;
+  int sms;           // of the device
   // workspace (device)
   unsigned char* ws;
   size_t ws_bytes;
@@ -167,6 +168,8 @@ int check_seg(swam_ctx* c, SegArgs& a, int32_t n_kv_heads, const char* name, Seg
   a.D = d.D;
   a.dtype = d.dtype;
   a.scale = d.scale;
+  a.device = c->device;
+  a.sms = c->sms;
   if (a.N_h % a.N_kv != 0) return bad(SWAM_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
   if (a.n_q < 0 || a.n[0] < 0 || a.n[1] < 0) return bad(SWAM_ERR_INVALID_ARG, "negative length");
   if (a.n_q > kMaxSegTokens || a.n[0] > kMaxSegTokens || a.n[1] > kMaxSegTokens)
@@ -305,6 +308,7 @@ int swam_create(const swam_shape* s, swam_ctx** out_ctx) {
   }
   if (select_smem_bytes(d) > 227 * 1024) { delete c; return SWAM_ERR_UNSUPPORTED; }
   if (cudaGetDevice(&c->device) != cudaSuccess) { delete c; return SWAM_ERR_CUDA; }
+  c->sms = sm_count();
 
   // workspace layout, every block 256-byte aligned
   size_t off = 0;

@@ -242,6 +242,7 @@ struct SegArgs {
   int B, per_group, n_q, N_h, N_kv, D, dtype;
   int causal;               // query t sees the first len - n_q + t + 1 keys of segment 1
   float scale;
+  int device, sms;          // the context's device and its number of SMs
 };
 // How the work is cut (chosen on the host from sizes alone, so that the scratch size can be asked for in advance).
 struct SegPlan {

@@ -176,6 +176,7 @@ class Swam:
         self._torch_dtype = torch_dtype(dtype)
         self._device_index = device.index if device.index is not None else torch.cuda.current_device()
         self._scratch_need = {}
+        self._lse_like = {}
         self.workspace = None
         self.staging = None
         if bind:
@@ -281,14 +282,15 @@ class Swam:
         return (out, lse) if want_lse else out
 
     def _tokens(self, name: str, t: torch.Tensor, lead: Optional[int], heads: int):
-        """Token and sample strides of a [samples, tokens, heads, D] tensor whose heads are contiguous (0 where the
-        dimension has one entry, or none)."""
+        """Token and sample strides of a [samples, tokens, heads, D] tensor whose heads are contiguous (0, 0: contiguous)."""
         if t.dtype is not self._torch_dtype or t.get_device() != self._device_index or t.dim() != 4:
             raise ValueError(f"{name}: expected a 4-dimensional {self._torch_dtype} tensor on {self.device}")
         n, tokens, h, d = t.shape
         if (lead is not None and n != lead) or h != heads or d != self.D:
             raise ValueError(f"{name}: expected shape [{'groups' if lead is None else lead}, tokens, {heads}, {self.D}], got {list(t.shape)}")
         if n == 0 or tokens == 0 or h == 0:
+            return 0, 0
+        if t.is_contiguous():
             return 0, 0
         s0, s1, s2, s3 = t.stride()
         if s3 != 1 or (h > 1 and s2 != d):
@@ -306,12 +308,20 @@ class Swam:
         return t.data_ptr()
 
     def _out_lse(self, q, out, want_lse: bool):
+        # (empty_like costs half of what empty does on the host; the pattern is one element expanded to the shape)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape:
             raise ValueError(f"out: expected shape {list(q.shape)}")
-        lse = torch.empty((self.B, self.N_h, q.shape[1]), dtype=torch.float32, device=self.device) if want_lse else None
-        return out, lse
+        if not want_lse:
+            return out, None
+        n_q = q.shape[1]
+        like = self._lse_like.get(n_q)
+        if like is None:
+            like = torch.empty(1, dtype=torch.float32, device=self.device).expand(self.B, self.N_h, n_q)
+            if len(self._lse_like) < 64:
+                self._lse_like[n_q] = like
+        return out, torch.empty_like(like, memory_format=torch.contiguous_format)
 
     def _scratch(self, query, a, key):
         """Scratch of a call: the tensor that holds it (it stays alive until the call has been enqueued) and its aligned
