@@ -205,58 +205,66 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 11) {
       // ------------------------------------------------------------------ scheduler
+      // Items with keys first, for the other warps; then the rows of those without, which are written here: in the order of
+      // the samples, a guided batch whose first half has no text would start 30 us late.
       int i = 0;
-      bool ok = true;
-      for (int w = blockIdx.x; ok && w < x.items; w += gridDim.x) {
-        const int q = pass0 == 0 && w >= p.pass[0].items ? 1 : pass0;
-        const SegPass& ps = p.pass[q];
-        const SegItem it = seg_item(ps, a.N_kv, C::kRows, q != pass0 ? w - p.pass[0].items : w);
-        const SegKeys kk = seg_keys(p, ps, it, C::kRows, kTile);
-        SegDesc o;
-        o.n = kk.end - kk.begin;
-        o.na = max(0, min(o.n, kk.n0 - kk.begin));
-        o.b0 = it.block * ps.block_samples;
-        o.h_kv = it.h_kv;
-        o.row0 = it.row0 | (q << 30);                // rows of a block stay below 2^30
-        o.base0 = kk.begin * kTile;
-        o.base1 = (kk.begin - kk.n0) * kTile;
-        o.part = ps.part0 + it.split;
-        o.len0 = kk.len0;
-        o.len1 = kk.len1;
-        o.own = o.na < o.n ? seg_len(p, 1, o.b0) : 0;
-        o.kv0 = o.b0 / a.per_group;
-        if (o.n == 0) {
-          // no key: rows of zeros (or a piece of weight 0), written here so that all other warps only meet items with keys
-          for (int r0 = 0; r0 < C::kRows; r0 += 32) {
-            const SegRow r = seg_row(p, ps.block_samples, o.b0, o.h_kv, it.row0 + r0 + lane);
-            if (!p.direct) {
-              if (r.real) p.part_ml[(int64_t)o.part * p.rows + ((int64_t)r.b * a.n_q + r.t) * a.N_h + r.h] = make_float2(-INFINITY, 0.f);
-              continue;
+      bool ok = true, empty = false;               // has an item without keys been passed over
+      auto walk = [&](bool keys) {
+        for (int w = blockIdx.x; ok && w < x.items; w += gridDim.x) {
+          const int q = pass0 == 0 && w >= p.pass[0].items ? 1 : pass0;
+          const SegPass& ps = p.pass[q];
+          const SegItem it = seg_item(ps, a.N_kv, C::kRows, q != pass0 ? w - p.pass[0].items : w);
+          const SegKeys kk = seg_keys(p, ps, it, C::kRows, kTile);
+          SegDesc o;
+          o.n = kk.end - kk.begin;
+          o.na = max(0, min(o.n, kk.n0 - kk.begin));
+          o.b0 = it.block * ps.block_samples;
+          o.h_kv = it.h_kv;
+          o.row0 = it.row0 | (q << 30);                // rows of a block stay below 2^30
+          o.base0 = kk.begin * kTile;
+          o.base1 = (kk.begin - kk.n0) * kTile;
+          o.part = ps.part0 + it.split;
+          o.len0 = kk.len0;
+          o.len1 = kk.len1;
+          o.own = o.na < o.n ? seg_len(p, 1, o.b0) : 0;
+          o.kv0 = o.b0 / a.per_group;
+          if (o.n == 0) empty = true;
+          if ((o.n > 0) != keys) continue;
+          if (o.n == 0) {
+            // rows of zeros (or a piece of weight 0)
+            for (int r0 = 0; r0 < C::kRows; r0 += 32) {
+              const SegRow r = seg_row(p, ps.block_samples, o.b0, o.h_kv, it.row0 + r0 + lane);
+              if (!p.direct) {
+                if (r.real) p.part_ml[(int64_t)o.part * p.rows + ((int64_t)r.b * a.n_q + r.t) * a.N_h + r.h] = make_float2(-INFINITY, 0.f);
+                continue;
+              }
+              const int64_t off = r.real ? r.b * a.o_smp + r.t * a.o_tok + (int64_t)r.h * D : -1;
+              if (r.real && a.lse) a.lse[((int64_t)r.b * a.N_h + r.h) * a.n_q + r.t] = -INFINITY;
+              constexpr int CPR = D / 8, RPI = 32 / CPR;
+              for (int j = 0; j < 32 / RPI; ++j) {
+                const int64_t to = __shfl_sync(0xffffffffu, off, j * RPI + lane / CPR);
+                if (to >= 0) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + to + (lane % CPR) * 8) = make_uint4(0u, 0u, 0u, 0u);
+              }
             }
-            const int64_t off = r.real ? r.b * a.o_smp + r.t * a.o_tok + (int64_t)r.h * D : -1;
-            if (r.real && a.lse) a.lse[((int64_t)r.b * a.N_h + r.h) * a.n_q + r.t] = -INFINITY;
-            constexpr int CPR = D / 8, RPI = 32 / CPR;
-            for (int j = 0; j < 32 / RPI; ++j) {
-              const int64_t to = __shfl_sync(0xffffffffu, off, j * RPI + lane / CPR);
-              if (to >= 0) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + to + (lane % CPR) * 8) = make_uint4(0u, 0u, 0u, 0u);
-            }
+            continue;
           }
-          continue;
+          const int slot = i % kDesc;
+          if (i >= kDesc) ok = wait(bar_d_empty(slot), ((i / kDesc) & 1) ^ 1);
+          if (ok && lane == 0) {
+            desc[slot] = o;
+            mbar_arrive(bar_d_full(slot));
+          }
+          ++i;
         }
-        const int slot = i % kDesc;
-        if (i >= kDesc) ok = wait(bar_d_empty(slot), ((i / kDesc) & 1) ^ 1);
-        if (ok && lane == 0) {
-          desc[slot] = o;
-          mbar_arrive(bar_d_full(slot));
-        }
-        ++i;
-      }
+      };
+      walk(true);
       const int slot = i % kDesc;
       if (ok && i >= kDesc) ok = wait(bar_d_empty(slot), ((i / kDesc) & 1) ^ 1);
       if (ok && lane == 0) {
         desc[slot].n = 0;                            // the end
         mbar_arrive(bar_d_full(slot));
       }
+      if (empty) walk(false);
     } else if (warp == 10) {
       // ------------------------------------------------------------------ finished tiles, as boxes
       if (x.box_out) {
