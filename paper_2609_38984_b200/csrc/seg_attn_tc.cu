@@ -26,8 +26,9 @@
 // kAlt = true: a row tile has at most 128 rows; both streams hold the same rows and take the key tiles in turn (over the
 //   borders of items), each with its own maximum, sum and output accumulator, and are merged in the epilogue.  The memory of the second query tile
 //   goes to the ring.
-// Rows of V behind a real length are overwritten with zeros in shared memory before the product (0 * NaN would poison the
-// row); scores behind a row's limit become -inf.
+// A tile that ends early costs what its real keys cost: Q K^T and P V stop at the 16-key step of the last one, the exponentials
+// at its 32.  Rows of V between it and the end of the step are overwritten with zeros in shared memory (0 * NaN would poison
+// the row); scores behind a row's limit become -inf.
 // Every wait on an mbarrier is bounded; when one runs out the kernel raises the timeout bit of the status word and every
 // role falls through to the exit.
 // What bounds it (cycles counted in the kernel, 1.65 to 1.85 GHz under this load): head dim 128, 3110 clk a key tile of an item
@@ -35,6 +36,8 @@
 // unit (16 a clk) needs 1792, and 2600 clk an item for its first scores' maximum, the read of the accumulators and the
 // bookkeeping between two items.
 #include <string.h>
+
+#include <type_traits>
 
 #include "tc_ptx.cuh"
 #include "seg_attn.cuh"
@@ -60,6 +63,7 @@ struct SegCfg {
   static constexpr int kSub = kTile * 128;           // bytes of a [128 rows x 64 columns] block
   static constexpr int kTileBytes = DB * kSub;       // a 128 x D tile
   static constexpr int NB = D == 64 ? 3 : 2;         // score buffers in TMEM
+  static constexpr int kW = 32;
   static constexpr int NQ = kAlt ? 1 : 2;            // query tiles of an item
   static constexpr int kRows = NQ * kTile;
   // Query buffers.  A buffer is free again when its item's output has left through it, so Q K^T must not run into an item
@@ -75,7 +79,7 @@ struct SegCfg {
   static constexpr int kTail = kDescOff + kDesc * (int)sizeof(SegDesc) + 16;
   static constexpr int kBytes = kData + 1024 /*alignment*/ + kTail + (kAlt ? kTile * 8 : 0) /*maxima and sums of stream 1*/;
   static_assert(ST >= 3 && kData <= 224 * 1024 && kBytes <= 227 * 1024, "shared memory");
-  static constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+  static constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 4) << 24);   // + N / 8 at bit 17
   static constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
 };
 
@@ -94,6 +98,14 @@ __device__ __forceinline__ void tma_store_5d(const CUtensorMap* map, uint32_t sr
   asm volatile("cp.async.bulk.tensor.5d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5, %6}], [%1];"
                ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+}
 // 32 bytes in one store (a whole sector)
 __device__ __forceinline__ void st_global_32(void* dst, const uint32_t* v) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -107,7 +119,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               const __grid_constant__ CUtensorMap map_k1, const __grid_constant__ CUtensorMap map_v1,
               const __grid_constant__ SegParams p, const int pass0, const SegTcArgs x) {
   using C = SegCfg<D, kAlt>;
-  constexpr int ST = C::ST, LK = C::LK, QB = C::QB, NB = C::NB;
+  constexpr int ST = C::ST, LK = C::LK, QB = C::QB, NB = C::NB, kW = C::kW;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_raw + (base - smem_addr(smem_raw));
@@ -184,6 +196,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     __syncwarp();
     if (lane == 0) mbar_arrive(bar);
   };
+  // 16-key steps of a tile with that many real keys
+  auto steps16 = [&](int real) { return min(kTile / 16, (max(real, 1) + 15) / 16); };
   // next descriptor: false at the end (or when a wait ran out).  di counts the descriptors read so far.
   auto next_desc = [&](int& di, SegDesc& d) {
     const int slot = di % kDesc;
@@ -388,22 +402,29 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       // ------------------------------------------------------------------ MMA issuer (warp converged, one lane issues)
       const uint32_t el = elect_one();
       const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sR, 16), v_lo = desc_lo(sR, C::kSub);
-      auto issue_qk = [&](int qt, int buf, int st) {
+      // k16: 16-key steps with real keys.  A tile that ends early takes no more columns of Q K^T and steps of P V than these.
+      auto issue_qk = [&](int qt, int buf, int st, int k16) {
         const uint32_t a_lo = q_lo + ((uint32_t)(qt * C::kTileBytes) >> 4), b_lo = k_lo + ((uint32_t)(st * C::kTileBytes) >> 4);
-        mma_ss<false>(tm_S(buf), a_lo, b_lo, kDescHi, C::kIdescQK, el);
+        const uint32_t idesc = C::kIdescQK + ((uint32_t)k16 << 18);
+        mma_ss<false>(tm_S(buf), a_lo, b_lo, kDescHi, idesc, el);
 #pragma unroll
         for (int ks = 1; ks < D / 16; ++ks) {
           constexpr int kSub16 = C::kSub >> 4;
           const uint32_t off = (uint32_t)((ks >> 2) * kSub16 + (ks & 3) * 2);
-          mma_ss<true>(tm_S(buf), a_lo + off, b_lo + off, kDescHi, C::kIdescQK, el);
+          mma_ss<true>(tm_S(buf), a_lo + off, b_lo + off, kDescHi, idesc, el);
         }
         tc_commit(bar_s_full(buf), el);
       };
-      auto issue_pv = [&](int s, int buf, int st, bool accum) {
+      auto issue_pv = [&](int s, int buf, int st, bool accum, int k16) {
         const uint32_t b_lo = v_lo + ((uint32_t)(st * C::kTileBytes) >> 4);
         mma_ts(tm_O(s), tm_S(buf), b_lo, kDescHi, C::kIdescPV, accum ? 1u : 0u, el);
+        if (k16 == kTile / 16) {
 #pragma unroll
-        for (int k = 1; k < kTile / 16; ++k) mma_ts(tm_O(s), tm_S(buf) + k * 8, b_lo + k * (2048 >> 4), kDescHi, C::kIdescPV, 1u, el);
+          for (int k = 1; k < kTile / 16; ++k) mma_ts(tm_O(s), tm_S(buf) + k * 8, b_lo + k * (2048 >> 4), kDescHi, C::kIdescPV, 1u, el);
+        } else {
+#pragma unroll 1
+          for (int k = 1; k < k16; ++k) mma_ts(tm_O(s), tm_S(buf) + k * 8, b_lo + k * (2048 >> 4), kDescHi, C::kIdescPV, 1u, el);
+        }
         tc_commit(bar_pv(s), el);
       };
       // The tiles of all items form one sequence for Q K^T, which runs ahead over the borders of items, and for P V behind it.
@@ -412,11 +433,12 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       // Q K^T issued behind the P V that reads it.
       bool ok = true, k_end = false;
       int pos = 0;                                  // ring slots taken so far
-      int kn = 0, ki = 0, kiter = -1;               // item of Q K^T: tiles, next tile, number
-      int vn = 0, vi = 0, viter = -1;               // item of P V
-      int nq0 = 0, nq1 = 0, nq2 = 0, n_nq = 0;      // tiles of the items that Q K^T has entered and P V has not
+      int kn = 0, ki = 0, kiter = -1;               // item of Q K^T (descriptor di - 1): tiles, next tile, number
+      int vn = 0, vi = 0, viter = -1;               // item of P V (descriptor viter)
+      int kna = 0, kr0 = 0, kr1 = 0;                // their tiles of segment 0, and real keys ahead of each segment's first tile
+      int vna = 0, vr0 = 0, vr1 = 0;
       int qk_u = 0, pv_u = 0;                       // units issued so far: unit u uses score buffer u % NB
-      int k_st = 0;                                 // slot of the current K tile
+      int k_st = 0, k_k16 = 0;                      // slot and steps of the current K tile
       // makes (kn, ki) the next tile of Q K^T and takes its ring slot; false at the end
       auto next_k = [&]() {
         if (ki == kn && !k_end) {
@@ -424,8 +446,9 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           ok = wait(bar_d_full(slot), (di / kDesc) & 1);
           if (!ok) return false;
           kn = desc[slot].n;
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar_d_empty(slot));
+          kna = desc[slot].na;
+          kr0 = desc[slot].len0 - desc[slot].base0;
+          kr1 = desc[slot].len1 - desc[slot].base1;
           ++di;
           ki = 0;
           k_end = kn == 0;
@@ -440,15 +463,12 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
         if (ki == 0) {
           ++kiter;
-          if (n_nq == 0) nq0 = kn;
-          else if (n_nq == 1) nq1 = kn;
-          else nq2 = kn;
-          ++n_nq;
           ok = wait(bar_q(kiter % QB), (kiter / QB) & 1);
           if (!ok) return false;
           if (!x.box_q) fence_proxy_async();
         }
         k_st = pos % ST;
+        k_k16 = steps16((ki >= kna ? kr1 : kr0) - ki * kTile);
         ok = wait(bar_full(k_st), (pos / ST) & 1);
         ++pos;
         return ok;
@@ -456,29 +476,44 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       // Q K^T of the current K tile and stream s; `last` releases the tile (and with the item's last tile the queries)
       auto qk = [&](int s, bool last) {
         tc_fence_after();
-        issue_qk((kiter % QB) * C::NQ + (kAlt ? 0 : s), qk_u % NB, k_st);
+        issue_qk((kiter % QB) * C::NQ + (kAlt ? 0 : s), qk_u % NB, k_st, k_k16);
         ++qk_u;
         if (last) {
           tc_commit(bar_empty(k_st), el);
           if (++ki == kn) tc_commit(bar_q_free(kiter % QB), el);
         }
       };
-      int v_st = 0;
+      int v_st = 0, v_k16 = 0;
       // (between two steps Q K^T is a tile ahead at least: an item that P V could enter has been entered by it)
-      auto v_left = [&]() { return ok && (vi < vn || n_nq > 0); };
+      auto v_left = [&]() { return ok && (vi < vn || viter < kiter); };
       // makes (vn, vi) the next tile of P V and takes its ring slot
       auto next_v = [&]() {
         if (vi == vn) {
-          vn = nq0;
-          nq0 = nq1;
-          nq1 = nq2;
-          --n_nq;
-          vi = 0;
+          // a descriptor is released when P V leaves it
+          __syncwarp();
+          if (viter >= 0 && lane == 0) mbar_arrive(bar_d_empty(viter % kDesc));
           ++viter;
+          vi = 0;
+          const SegDesc& o = desc[viter % kDesc];
+          vn = o.n;
+          vna = o.na;
+          vr0 = o.len0 - o.base0;
+          vr1 = o.len1 - o.base1;
         }
         v_st = pos % ST;
         ok = wait(bar_full(v_st), (pos / ST) & 1);
         ++pos;
+        const int real = (vi >= vna ? vr1 : vr0) - vi * kTile;
+        v_k16 = steps16(real);
+        if (ok && real < v_k16 * 16) {
+          // rows of V behind the last real key become zeros up to the end of the product's last step
+          for (int c = lane; c < (v_k16 * 16 - real) * (D / 8); c += 32) {
+            const int rr = real + c / (D / 8), cc = c % (D / 8);
+            st_shared_16(sR + (uint32_t)(v_st * C::kTileBytes + (cc >> 3) * C::kSub + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)), 0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async();
+          __syncwarp();
+        }
         // the first product of an item overwrites the accumulators: the previous item's must have been read
         if (ok && vi == 0 && viter > 0) ok = wait(bar_o_free, (viter - 1) & 1);
         return ok;
@@ -487,7 +522,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         ok = wait(bar_p_full(pv_u % NB), (pv_u / NB) & 1);
         if (!ok) return;
         tc_fence_after();
-        issue_pv(s, pv_u % NB, v_st, kAlt ? vi > 1 : vi > 0);
+        issue_pv(s, pv_u % NB, v_st, kAlt ? vi > 1 : vi > 0, v_k16);
         ++pv_u;
         if (last) {
           tc_commit(bar_empty(v_st), el);
@@ -647,151 +682,165 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       const SegRow row = seg_row(p, p.pass[d.row0 >> 30].block_samples, d.b0, d.h_kv, row0 + r);
       const int grow = (row.b * a.n_q + row.t) * a.N_h + row.h;
       const bool row_real = row.real, warp_real = __any_sync(0xffffffffu, row_real);
-      // real keys ahead of each segment's first tile in this item, and those of segment 1 that this row sees; does the
-      // segment's tensor go on behind them
+      // real keys ahead of each segment's first tile in this item, and those of segment 1 that this row sees
       const int real0 = d.len0 - d.base0, real1 = d.len1 - d.base1, sees1 = seg_limit1(a, d.own, row.t) - d.base1;
-      const bool more0 = d.len0 < a.n[0], more1 = d.len1 < a.n[1];
       float m_used = -INFINITY, l_run = 0.f;
       bool any_key = false;
       const int i0 = kAlt ? (s ^ pos0) & 1 : 0;                  // the stream's first tile of the item
       for (int i = i0; i < n; i += kAlt ? 2 : 1, ++cnt) {
         const int g = u0 + (kAlt ? i : 2 * i + s), buf = g % NB;      // unit
         const uint32_t tS = tm_S(buf) + lane_off;
-        ok = wait(bar_s_full(buf), (g / NB) & 1);
-        if (!ok) break;
         const bool s1 = i >= na;
         const int real = (s1 ? real1 : real0) - i * kTile;      // real keys of this tile
+        const int valid = s1 ? sees1 - i * kTile : real;        // those that the row sees
+        // kW scores at a time: chunks that every row of the warp sees, those that one of them sees something of, and those
+        // that the product reads
+        const int chunks_all = __reduce_min_sync(0xffffffffu, max(valid, 0) / kW);
+        const int chunks = __reduce_max_sync(0xffffffffu, min(kTile / kW, (max(valid, 0) + kW - 1) / kW));
+        const int chunks_pv = (steps16(real) * 16 + kW - 1) / kW;
+        ok = wait(bar_s_full(buf), (g / NB) & 1);
+        if (!ok) break;
         tc_fence_after();
         // rows behind the last one: nothing is computed, the barriers are kept in step (what their P rows hold only reaches
         // their own accumulator rows, which nobody reads)
         if (warp_real) {
-          float sv[kTile];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<float(*)[32]>(&sv[c * 32]));
-          tmem_ld_wait();
-          const int valid = s1 ? sees1 - i * kTile : real;
-          if (valid < kTile) {
-#pragma unroll
-            for (int c = 0; c < kTile; ++c)
-              if (c >= valid) sv[c] = -INFINITY;
-          }
           const bool first = i == i0;
-          if (first) {
-            // The first tile fixes the row's reference: the maximum of its first 32 scores will do, since a row that outgrows
-            // it raises it.  A row that sees none of its keys sees no later key either (limits are a prefix of segment 1, and
-            // segment 0 has no limits below its length).
+          const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
+          // weights of scores v[0 .. 2 n) as bf16 pairs, and their sum
+          auto weights = [&](auto n, const float* v, uint32_t* pk) {
+            const uint64_t negm2 = pack2(-m_used, -m_used);
+            uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+            for (int j = 0; j < decltype(n)::value; ++j) {
+              const uint64_t x2 = fma2(pack2(v[2 * j], v[2 * j + 1]), scale2, negm2);
+              float p0, p1;
+              if ((j & 7) == 0) {
+                exp2_poly2(x2, p0, p1);             // one pair in eight on the FMA pipes, which the exp2 unit leaves idle
+              } else {
+                float t0, t1;
+                unpack2(x2, t0, t1);
+                p0 = ex2(t0);
+                p1 = ex2(t1);
+              }
+              acc2[j & 3] = add2(acc2[j & 3], pack2(p0, p1));
+              pk[j] = pack_bf16x2(p0, p1);
+            }
+            float a0, a1;
+            unpack2(add2(add2(acc2[0], acc2[1]), add2(acc2[2], acc2[3])), a0, a1);
+            return a0 + a1;
+          };
+          // The first scores fix the row's reference: any of them will do, since a row that outgrows it raises it.  A row that
+          // sees none of its keys sees no later key either (limits are a prefix of segment 1, and segment 0 has no limits below
+          // its length).
+          auto reference = [&](const float* v) {
             any_key = valid > 0;
             float m4[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m4[j] = sv[j];
+            for (int j = 0; j < 4; ++j) m4[j] = v[j];
 #pragma unroll
-            for (int c = 4; c < 32; c += 4) {
+            for (int b = 4; b < 32; b += 4) {
 #pragma unroll
-              for (int j = 0; j < 4; ++j) m4[j] = fmaxf(m4[j], sv[c + j]);
+              for (int j = 0; j < 4; ++j) m4[j] = fmaxf(m4[j], v[b + j]);
             }
-            m_used = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2;
-            if (!any_key) m_used = 0.f;
-          }
-          const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), negm2 = pack2(-m_used, -m_used);
-          uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
-          uint32_t pk[64];
+            m_used = any_key ? fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2 : 0.f;
+          };
+          bool whole = chunks_all >= kTile / kW;
+          if (whole) {
+            float sv[kTile];
+            uint32_t pk[kTile / 2];
 #pragma unroll
-          for (int j = 0; j < 64; ++j) {
-            const uint64_t x2 = fma2(pack2(sv[2 * j], sv[2 * j + 1]), scale2, negm2);
-            float p0, p1;
-            if ((j & 7) == 0) {
-              exp2_poly2(x2, p0, p1);             // one pair in eight on the FMA pipes, which the exp2 unit leaves idle
-            } else {
-              float t0, t1;
-              unpack2(x2, t0, t1);
-              p0 = ex2(t0);
-              p1 = ex2(t1);
+            for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<float(*)[32]>(&sv[c * 32]));
+            tmem_ld_wait();
+            if (first) reference(sv);
+            const float sum = weights(std::integral_constant<int, kTile / 2>(), sv, pk);
+            whole = !__any_sync(0xffffffffu, !(sum <= 256.f * kTile));       // no exponent above 2^8; else (inf and NaN too) below
+            if (whole) {
+              // P overwrites the scores only now that the pass is known to stand
+#pragma unroll
+              for (int c = 0; c < 4; ++c) tmem_st16(tS + c * 16, &pk[c * 16]);
+              l_run += sum;
             }
-            acc2[j & 3] = add2(acc2[j & 3], pack2(p0, p1));
-            pk[j] = pack_bf16x2(p0, p1);
           }
-          float sum, a0, a1;
-          unpack2(add2(add2(acc2[0], acc2[1]), add2(acc2[2], acc2[3])), a0, a1);
-          sum = a0 + a1;
-          const bool grew = !(sum <= 256.f * 128.f);           // some exponent above 2^8; also inf and NaN
-          const bool redo = __any_sync(0xffffffffu, grew);
-          if (!redo) {
-            // P overwrites the scores only now that the pass is known to stand
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_st16(tS + c * 16, &pk[c * 16]);
-          }
-          if (redo) {
-            // rare: raise the reference to the row's maximum, rescale O, repeat the pass (32 scores at a time, so that this
-            // path needs no more registers than the usual one)
-            auto scores32 = [&](int c, float (&v)[32]) {
-              tmem_ld32(tS + c * 32, v);
-              tmem_ld_wait();
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (c * 32 + j >= valid) v[j] = -INFINITY;
-            };
-            float mraw = -INFINITY;
+          // Tiles of which some row of the warp does not see every key, and (rare) scores that outgrow the reference: kW scores
+          // at a time, in a loop.  Unrolled too, this path costs more in instruction fetches than it saves (13 us of 265 where
+          // half of the samples end inside a tile).
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-              float v[32];
-              scores32(c, v);
-#pragma unroll
-              for (int j = 0; j < 32; ++j) mraw = fmaxf(mraw, v[j]);
-            }
-            const float delta = fmaxf(fmaf(mraw, p.scale_log2, -m_used), 0.f);
-            const float f = ex2(-delta);
-            m_used += delta;
-            l_run *= f;
-            if (!first) {
-              // the accumulator must hold every product issued against the old reference
-              ok = wait(bar_pv(s), (cnt - 1) & 1);
-              if (!ok) break;
-              tc_fence_after();
+          for (int c = 0; !whole && c < chunks_pv; ++c) {
+            uint32_t pk[kW / 2];
+            if (c < chunks) {
+              const int left = valid - c * kW;
+              float sum;
 #pragma unroll 1
-              for (int c = 0; c < D / 32; ++c) {
-                float ov[32];
-                tmem_ld32(tO + c * 32, ov);
+              for (bool raised = false;; raised = true) {
+                float v[kW];
+#pragma unroll
+                for (int j = 0; j < kW / 32; ++j) tmem_ld32(tS + c * kW + j * 32, *reinterpret_cast<float(*)[32]>(&v[j * 32]));
                 tmem_ld_wait();
-                uint32_t ou[32];
+                if (c >= chunks_all) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) ou[j] = __float_as_uint(ov[j] * f);
-                tmem_st32(tO + c * 32, ou);
-              }
-            }
-            sum = 0.f;
+                  for (int j = 0; j < kW; ++j)
+                    if (j >= left) v[j] = -INFINITY;
+                }
+                if (first && c == 0 && !raised && chunks_all < kTile / kW) reference(v);
+                sum = weights(std::integral_constant<int, kW / 2>(), v, pk);
+                const bool grew = !(sum <= 256.f * kW);          // some exponent above 2^8; also inf and NaN
+                if (raised || !__any_sync(0xffffffffu, grew)) break;
+                // Rare: raise the reference to the row's maximum, in whole powers of two, so that the weights of this tile that
+                // are written already rescale without another rounding; then repeat the chunk.
+                float mraw = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-              float v[32];
-              scores32(c, v);
-              uint32_t pr[16];
+                for (int b = 0; b < kW / 32; ++b) {
+                  float w[32];
+                  tmem_ld32(tS + c * kW + b * 32, w);
+                  tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const float p0 = ex2(fmaf(v[2 * j], p.scale_log2, -m_used)), p1 = ex2(fmaf(v[2 * j + 1], p.scale_log2, -m_used));
-                sum += p0 + p1;
-                pr[j] = pack_bf16x2(p0, p1);
+                  for (int j = 0; j < 32; ++j)
+                    if (b * 32 + j < left) mraw = fmaxf(mraw, w[j]);
+                }
+                const float delta = grew ? ceilf(fmaxf(fmaf(mraw, p.scale_log2, -m_used), 0.f)) : 0.f;
+                const float f = ex2(-delta);
+                m_used += delta;
+                l_run *= f;
+                tmem_st_wait();
+#pragma unroll 1
+                for (int b = 0; b < c * (kW / 32); ++b) {
+                  uint32_t w[16];
+                  tmem_ld16(tS + b * 16, w);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(__uint_as_float(w[j] << 16) * f, __uint_as_float(w[j] & 0xffff0000u) * f);
+                  tmem_st16(tS + b * 16, w);
+                }
+                if (!first) {
+                  // the accumulator must hold every product issued against the old reference
+                  ok = wait(bar_pv(s), (cnt - 1) & 1);
+                  if (!ok) break;
+                  tc_fence_after();
+#pragma unroll 1
+                  for (int b = 0; b < D / 32; ++b) {
+                    float ov[32];
+                    tmem_ld32(tO + b * 32, ov);
+                    tmem_ld_wait();
+                    uint32_t ou[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) ou[j] = __float_as_uint(ov[j] * f);
+                    tmem_st32(tO + b * 32, ou);
+                  }
+                }
               }
-              tmem_st16(tS + c * 16, pr);         // over scores that have been read
-            }
-          }
-          l_run += sum;
-          tmem_st_wait();
-        }
-        // a tile that ends inside its tensor: rows of V behind the last real key become zeros (what lies behind the tensor
-        // arrives as zeros).  One stream does it for both: the issuer waits for stream 0's P before either product.
-        if (real < kTile && (kAlt || s == 0) && (s1 ? more1 : more0)) {
-          // (V's load may stand behind that of an item whose query buffer the pending output has still to leave)
-          if (pend) ok = flush();
-          const int pos = LK + 2 * (pos0 + i), st = pos % ST;
-          if (ok) ok = wait(bar_full(st), (pos / ST) & 1);
-          if (!ok) break;
-          int rr = r;
-          asm volatile("" : "+r"(rr));
-          if (rr >= real) {
+              if (!ok) break;
+              l_run += sum;
+            } else {
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c)
-              st_shared_16(sR + (uint32_t)(st * C::kTileBytes + (c >> 3) * C::kSub + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)), 0u, 0u, 0u, 0u);
+              for (int j = 0; j < kW / 2; ++j) pk[j] = 0u;
+            }
+            // over scores that have been read
+#pragma unroll
+            for (int j = 0; j < kW / 32; ++j) tmem_st16(tS + c * (kW / 2) + j * 16, &pk[j * 16]);
           }
-          fence_proxy_async();
+          if (!ok) break;
+          if (first && chunks == 0) m_used = 0.f;            // a warp of rows that see no key
+          tmem_st_wait();
         }
         tc_fence_before();
         arrive(bar_p_full(buf));
