@@ -176,6 +176,28 @@ def test_cross_growing_and_extreme_logits(dtype, variant, D):
 
 @pytest.mark.parametrize("D", [32, 64, 128])
 @pytest.mark.parametrize("dtype,variant", VARIANTS)
+@pytest.mark.parametrize("n_kv", [20, 77, 100, 128, 215])
+def test_cross_logits_that_grow_inside_a_tile(dtype, variant, D, n_kv):
+    """Every key outweighs the one before it by about a factor of two, so that weights of a tile are rescaled by later ones of
+    the same tile, at every place where a tile may end."""
+    B, n_q, H = 1, 150, 2
+    gen = torch.Generator(device="cuda").manual_seed(10 + n_kv)
+    dt = DT[dtype]
+    ctx = make_ctx(B, H, D, H, swam.F32 if dt == torch.float32 else swam.BF16)
+    ctx.set_option(swam.OPT_ATTN_VARIANT, variant)
+    q = rand(gen, B, n_q, H, D, dtype=dt).abs() + 0.25
+    k = (rand(gen, B, n_kv, H, D, dtype=dt) / 8 + torch.arange(n_kv, device="cuda")[None, :, None, None] / D ** 0.5).to(dt)
+    v = rand(gen, B, n_kv, H, D, dtype=dt)
+    lens = torch.tensor([n_kv - 3], dtype=torch.int32, device="cuda")
+    for n, kv_len in ((n_kv, None), (n_kv - 3, lens)):
+        out, lse = ctx.cross_attn(q, k, v, kv_len=kv_len, want_lse=True)
+        ctx.check()
+        compare(out, lse, q, lambda b, h: (k[b, :n, h].double(), v[b, :n, h].double(),
+                                           torch.ones(n_q, n, dtype=torch.bool, device="cuda")), D, dt)
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("dtype,variant", VARIANTS)
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("n_q,H,kv", [(1, 8, 2), (1, 4, 4), (7, 6, 2), (40, 4, 2), (140, 2, 2), (9, 20, 1)])
 def test_prefix_lengths(dtype, variant, D, causal, n_q, H, kv):
