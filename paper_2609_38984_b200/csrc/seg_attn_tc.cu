@@ -31,10 +31,10 @@
 // the row); scores behind a row's limit become -inf.
 // Every wait on an mbarrier is bounded; when one runs out the kernel raises the timeout bit of the status word and every
 // role falls through to the exit.
-// What bounds it (cycles counted in the kernel, 1.65 to 1.85 GHz under this load): head dim 128, 3110 clk a key tile of an item
-// (1.33 PFLOP/s at 4096 keys, 0.8 of the measured burst rate) and 4300 clk an item; head dim 64, 2600 clk a key tile, of which the exp2
-// unit (16 a clk) needs 1792, and 2600 clk an item for its first scores' maximum, the read of the accumulators and the
-// bookkeeping between two items.
+// What bounds it (cycles at the 1.65 to 1.85 GHz of this load): head dim 128, 3110 clk a key tile of an item (1.33 PFLOP/s at
+// 4096 keys, 0.8 of the measured burst rate) and 4300 clk an item; head dim 64, 2300 clk a key tile, of which the exp2 unit
+// (16 a clk) needs 1792, and 4400 clk an item: its first scores' maximum, the read of the accumulators, the bookkeeping between
+// two items, and the instruction fetches of all that (81 % hits; 97 % at long key ranges).
 #include <string.h>
 
 #include <type_traits>
