@@ -211,8 +211,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   SegDesc d;
   int di = 0;
 
-  // Every role walks through the same items; one whose rows see no key is only known to the softmax warps (they write
-  // its zeros) and counts for nobody else, so all other barrier phases count the remaining items and their tiles.
+  // Every role walks through the same items, those with keys: all barrier phases count them and their tiles.  An item whose rows
+  // see no key is only known to the scheduler, which writes its zeros.
   // (setmaxnreg: 384 threads start with 168 registers each; 72 for the third warpgroup frees exactly what 216 for the
   // other two takes)
   if (warp >= 8) {
