@@ -33,7 +33,7 @@
 // role falls through to the exit.
 // What bounds it (cycles at the 1.65 to 1.85 GHz of this load): head dim 128, 3110 clk a key tile of an item (1.33 PFLOP/s at
 // 4096 keys, 0.8 of the measured burst rate) and 4300 clk an item; head dim 64, 2300 clk a key tile, of which the exp2 unit
-// (16 a clk) needs 1792, and 4400 clk an item: its first scores' maximum, the read of the accumulators, the bookkeeping between
+// (16 a clk) needs 1920, and 4400 clk an item: its first scores' maximum, the read of the accumulators, the bookkeeping between
 // two items, and the instruction fetches of all that (81 % hits; 97 % at long key ranges).
 #include <string.h>
 
@@ -714,8 +714,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             for (int j = 0; j < decltype(n)::value; ++j) {
               const uint64_t x2 = fma2(pack2(v[2 * j], v[2 * j + 1]), scale2, negm2);
               float p0, p1;
-              if ((j & 7) == 0) {
-                exp2_poly2(x2, p0, p1);             // one pair in eight on the FMA pipes, which the exp2 unit leaves idle
+              if ((j & (D == 64 ? 15 : 7)) == 0) {
+                // one pair in eight on the FMA pipes, which the exp2 unit leaves idle (in sixteen at head dim 64, where the
+                // instructions cost more: ragged multi-view batch 245 us, 252 with eight, 240 with none; 608-row samples 72, 72, 74)
+                exp2_poly2(x2, p0, p1);
               } else {
                 float t0, t1;
                 unpack2(x2, t0, t1);
