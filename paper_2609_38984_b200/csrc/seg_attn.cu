@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ 
       for (int c = 0; c < CPL; ++c) acc[c] = f != 0.f ? fmaf(f, v[i][c], acc[c]) : acc[c];
     }
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = seg_inverse(l);
   if constexpr (sizeof(T) == 4 && CPL == 4) {
     *reinterpret_cast<float4*>(out) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
   } else if constexpr (sizeof(T) == 2 && CPL >= 2) {
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ 
 #pragma unroll
     for (int c = 0; c < CPL; ++c) out[c] = (T)(acc[c] * inv);
   }
-  if (a.lse && lane == 0) a.lse[((int64_t)b * a.N_h + h) * a.n_q + t] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+  if (a.lse && lane == 0) a.lse[((int64_t)b * a.N_h + h) * a.n_q + t] = seg_lse(m, l);
 }
 
 template <int D, typename T>

@@ -84,6 +84,11 @@ __device__ __forceinline__ int seg_limit1(const SegArgs& a, int len, int t) {
   return a.causal ? max(0, len - a.n_q + t + 1) : len;
 }
 
+// What a row's sum of weights makes of its result: only a sum of exactly 0 is a row without keys.  A NaN sum (a NaN or +inf logit
+// of a visible key) has to stay one.
+__device__ __forceinline__ float seg_inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+__device__ __forceinline__ float seg_lse(float m, float sum) { return sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f; }
+
 // the key tiles (KT keys each) of an item: [begin, end) of the concatenated tiles of segment 0 (len0 keys, n0 tiles)
 // and segment 1 (len1 keys: no row of the tile sees more of them)
 struct SegKeys {

@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
     const int64_t gr = ((int64_t)row.b * a.n_q + row.t) * a.N_h + row.h;
     const int64_t pr = (int64_t)(ps.part0 + it.split) * p.rows + gr;
     float* dst = p.direct ? (float*)a.out + row.b * a.o_smp + row.t * a.o_tok + (int64_t)row.h * D : p.part_o + pr * D;
-    const float inv = p.direct ? (sum > 0.f ? 1.f / sum : 0.f) : 1.f;
+    const float inv = p.direct ? seg_inverse(sum) : 1.f;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       float4 w;
@@ -214,8 +214,7 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
     }
     if (tx == 0) {
       if (!p.direct) p.part_ml[pr] = make_float2(m[i], sum);
-      else if (a.lse)
-        a.lse[((int64_t)row.b * a.N_h + row.h) * a.n_q + row.t] = sum > 0.f ? (m[i] + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+      else if (a.lse) a.lse[((int64_t)row.b * a.N_h + row.h) * a.n_q + row.t] = seg_lse(m[i], sum);
     }
   }
   if (pass == 1) wait_previous();

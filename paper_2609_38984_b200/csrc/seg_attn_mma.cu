@@ -248,15 +248,14 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
     }
     const int64_t gr = ((int64_t)row.b * a.n_q + row.t) * a.N_h + row.h;
     if (p.direct) {
-      const float inv = sum > 0.f ? 1.f / sum : 0.f;
+      const float inv = seg_inverse(sum);
       uint4 w;
       w.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
       w.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
       w.z = pack_bf16x2(acc[4] * inv, acc[5] * inv);
       w.w = pack_bf16x2(acc[6] * inv, acc[7] * inv);
       *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + row.b * a.o_smp + row.t * a.o_tok + (int64_t)row.h * D + c) = w;
-      if (a.lse && c == 0)
-        a.lse[((int64_t)row.b * a.N_h + row.h) * a.n_q + row.t] = sum > 0.f ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+      if (a.lse && c == 0) a.lse[((int64_t)row.b * a.N_h + row.h) * a.n_q + row.t] = seg_lse(mx, sum);
     } else {
       const int64_t pr = (int64_t)(ps.part0 + it.split) * p.rows + gr;
       float* dst = p.part_o + pr * D + c;

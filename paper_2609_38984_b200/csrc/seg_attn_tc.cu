@@ -601,10 +601,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       tc_fence_after();
       if (pend_warp) {
         if (p.direct) {
-          const float inv = l > 0.f ? 1.f / l : 0.f;
+          const float inv = seg_inverse(l);
           f0 *= inv;
           f1 *= inv;
-          if (pend_real && a.lse) a.lse[pend_lse] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+          if (pend_real && a.lse) a.lse[pend_lse] = seg_lse(m, l);
         }
         const int64_t pr = (int64_t)pend_part * p.rows + pend_row;
         if (!p.direct && pend_real) p.part_ml[pr] = make_float2(m, l);
