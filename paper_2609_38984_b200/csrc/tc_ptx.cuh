@@ -167,6 +167,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
@@ -178,16 +183,26 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+__device__ __forceinline__ float clamp_nan(float x, float lo, float hi) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(lo));
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(hi));
+  return x;
+}
+
 // 2^x for a pair of arguments on the FMA pipes instead of the special-function unit, which is the busiest pipe of the
 // softmax pass at head dim 64: x is clamped to [-126, 126] (so -inf of a masked key gives 2^-126, and an exponent that
 // outgrew its reference gives a sum large enough to trigger the exact redo), split into j = round(x) (magic-number
 // addition) and f = x - j in [-0.5, 0.5]; 2^f is a degree-4 minimax polynomial (relative error 2.6e-6, far below the
 // bf16 rounding of P) and j goes straight into the exponent field.
+// NaN: the clamps pass it on, and everything computed from it is the canonical 0x7fffffff.  The addition in the exponent field
+// makes the largest finite number of that, which triggers the redo too; kNan = true, for a pass that is not redone,
+// multiplies by 2^j instead, so that NaN stays NaN.
+template <bool kNan>
 __device__ __forceinline__ void exp2_poly2(uint64_t x2, float& r0, float& r1) {
   float x0, x1;
   unpack2(x2, x0, x1);
-  x0 = fminf(fmaxf(x0, -126.f), 126.f);
-  x1 = fminf(fmaxf(x1, -126.f), 126.f);
+  x0 = clamp_nan(x0, -126.f, 126.f);
+  x1 = clamp_nan(x1, -126.f, 126.f);
   const uint64_t xc = pack2(x0, x1);
   const uint64_t t2 = add2(xc, pack2(12582912.f, 12582912.f));        // 1.5 * 2^23: the low mantissa bits now hold round(x)
   const uint64_t j2 = add2(t2, pack2(-12582912.f, -12582912.f));
@@ -196,11 +211,17 @@ __device__ __forceinline__ void exp2_poly2(uint64_t x2, float& r0, float& r1) {
   p2 = fma2(p2, f2, pack2(0.240247443318367f, 0.240247443318367f));
   p2 = fma2(p2, f2, pack2(0.6931217908859253f, 0.6931217908859253f));
   p2 = fma2(p2, f2, pack2(0.9999992847442627f, 0.9999992847442627f));
-  float p0, p1, t0, t1;
-  unpack2(p2, p0, p1);
+  float t0, t1;
   unpack2(t2, t0, t1);
-  r0 = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
-  r1 = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
+  if constexpr (kNan) {
+    const float e0 = __int_as_float((__float_as_int(t0) << 23) + 0x3f800000), e1 = __int_as_float((__float_as_int(t1) << 23) + 0x3f800000);
+    unpack2(mul2(p2, pack2(e0, e1)), r0, r1);
+  } else {
+    float p0, p1;
+    unpack2(p2, p0, p1);
+    r0 = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
+    r1 = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
+  }
 }
 
 // Shared-memory matrix descriptor, 128-byte swizzle, tile rows of 128 bytes, 8-row groups 1024 bytes apart:

@@ -44,6 +44,38 @@ def context(plan, B):
     return ctx
 
 
+def positions(n_kv):
+    return sorted({0, 1, 2, 3, 15, 16, 17, 31, 32, 33, 64, 65, 100, 127, 128, 129, 160, n_kv - 2, n_kv - 1})
+
+
+@plans
+@pytest.mark.parametrize("what", [NAN, INF])
+def test_a_row_with_a_nan_or_infinite_logit_is_no_row_without_keys(plan, what):
+    """Sample b has one bad key, at the b-th position, in its first head only: every row of that head is lost, and none of
+    the other head's."""
+    dtype, variant, n_q, H, kv, D, n_kv = plan
+    dt, at = DT[dtype], positions(n_kv)
+    B = len(at)
+    gen = torch.Generator(device="cuda").manual_seed(n_q + D)
+    ctx = context(plan, B)
+    q = base.rand(gen, B, n_q, H, D, dtype=dt)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    k, v = base.rand(gen, B, n_kv, kv, D, dtype=dt), base.rand(gen, B, n_kv, kv, D, dtype=dt)
+    for b, c in enumerate(at):
+        if what != what:
+            k[b, c, 0] = what
+        else:
+            k[b, c, 0, 0] = what
+    out, lse = ctx.cross_attn(q, k, v, want_lse=True)
+    ctx.check()
+    for b, c in enumerate(at):
+        lost, e = out[b, :, 0], lse[b, 0]
+        assert not torch.isfinite(lost).any(), (c, lost[torch.isfinite(lost)][:4])
+        assert (torch.isnan(e) | (e == INF)).all(), (c, e[:4])
+    mask = torch.ones(n_q, n_kv, dtype=torch.bool, device="cuda")
+    base.compare(out[:, :, 1:], lse[:, 1:], q[:, :, 1:], lambda b, h: (k[b, :, 1].double(), v[b, :, 1].double(), mask), D, dt)
+
+
 @plans
 def test_a_nan_query_is_its_own_rows_loss_only(plan):
     dtype, variant, n_q, H, kv, D, n_kv = plan
@@ -66,3 +98,17 @@ def test_a_nan_query_is_its_own_rows_loss_only(plan):
     out[1, lost, 1], lse[1, 1, lost] = want[1, lost, 1], want_lse[1, 1, lost]
     mask = torch.ones(n_q, n_kv, dtype=torch.bool, device="cuda")
     base.compare(out, lse, clean, lambda b, h: (k[b, :, h].double(), v[b, :, h].double(), mask), D, dt)
+
+
+def test_joint_attention_passes_a_nan_key_on():
+    """The joint attention of the same block, at every position of a key tile."""
+    for D in (64, 128):
+        B, L = 132, 8 + 2 * 64 + 8
+        gen = torch.Generator(device="cuda").manual_seed(D)
+        ctx = swam.Swam(B, 8, 2, 64, 8, 1, D, 14, 18, dtype=swam.BF16)
+        q, k, v = (base.rand(gen, B, L, 1, D, dtype=torch.bfloat16) for _ in range(3))
+        for b in range(B):
+            k[b, b] = NAN
+        out, lse = ctx.sparse_attn(q, k, v, want_lse=True)
+        ctx.check()
+        assert torch.isnan(out).all() and torch.isnan(lse).all()
