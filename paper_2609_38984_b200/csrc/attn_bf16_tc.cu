@@ -634,7 +634,7 @@ attn_bf16_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         const uint64_t x2 = fma2(pack2(sv[2 * i], sv[2 * i + 1]), scale2, negm2);
         float p0, p1;
         if ((i & 7) < C::kPolyOf8) {
-          exp2_poly2<false>(x2, p0, p1);
+          exp2_poly2<false, false>(x2, p0, p1);
         } else {
           float t0, t1;
           unpack2(x2, t0, t1);

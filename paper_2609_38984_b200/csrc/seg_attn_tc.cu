@@ -717,7 +717,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               if ((j & (D == 64 ? 15 : 7)) == 0) {
                 // one pair in eight on the FMA pipes, which the exp2 unit leaves idle (in sixteen at head dim 64, where the
                 // instructions cost more: ragged multi-view batch 245 us, 252 with eight, 240 with none; 608-row samples 72, 72, 74)
-                exp2_poly2<decltype(n)::value != kTile / 2>(x2, p0, p1);
+                exp2_poly2<true, decltype(n)::value != kTile / 2>(x2, p0, p1);
               } else {
                 float t0, t1;
                 unpack2(x2, t0, t1);

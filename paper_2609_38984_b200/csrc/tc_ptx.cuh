@@ -197,20 +197,25 @@ __device__ __forceinline__ float clamp_nan(float x, float lo, float hi) {
 // NaN: the clamps pass it on, and everything computed from it is the canonical 0x7fffffff.  The addition in the exponent field
 // makes the largest finite number of that, which triggers the redo too; kNan = true, for a pass that is not redone,
 // multiplies by 2^j instead, so that NaN stays NaN.
-template <bool kNan>
+// kZero = true: x is clamped to [-127, 126] and the polynomial is exactly 1 at f = 0 (minimax under that condition: relative error
+// 2.9e-6), so that a masked key, or one 2^-127 below the reference, weighs exactly 0, however large its value.
+template <bool kZero, bool kNan>
 __device__ __forceinline__ void exp2_poly2(uint64_t x2, float& r0, float& r1) {
   float x0, x1;
   unpack2(x2, x0, x1);
-  x0 = clamp_nan(x0, -126.f, 126.f);
-  x1 = clamp_nan(x1, -126.f, 126.f);
+  x0 = clamp_nan(x0, kZero ? -127.f : -126.f, 126.f);
+  x1 = clamp_nan(x1, kZero ? -127.f : -126.f, 126.f);
   const uint64_t xc = pack2(x0, x1);
   const uint64_t t2 = add2(xc, pack2(12582912.f, 12582912.f));        // 1.5 * 2^23: the low mantissa bits now hold round(x)
   const uint64_t j2 = add2(t2, pack2(-12582912.f, -12582912.f));
   const uint64_t f2 = fma2(j2, pack2(-1.f, -1.f), xc);
-  uint64_t p2 = fma2(pack2(0.009570102207362652f, 0.009570102207362652f), f2, pack2(0.05591785907745361f, 0.05591785907745361f));
-  p2 = fma2(p2, f2, pack2(0.240247443318367f, 0.240247443318367f));
-  p2 = fma2(p2, f2, pack2(0.6931217908859253f, 0.6931217908859253f));
-  p2 = fma2(p2, f2, pack2(0.9999992847442627f, 0.9999992847442627f));
+  constexpr float c4 = kZero ? 0.009585382416844368f : 0.009570102207362652f, c3 = kZero ? 0.05590662732720375f : 0.05591785907745361f,
+                  c2 = kZero ? 0.24024038016796112f : 0.240247443318367f, c1 = kZero ? 0.6931241750717163f : 0.6931217908859253f,
+                  c0 = kZero ? 1.f : 0.9999992847442627f;
+  uint64_t p2 = fma2(pack2(c4, c4), f2, pack2(c3, c3));
+  p2 = fma2(p2, f2, pack2(c2, c2));
+  p2 = fma2(p2, f2, pack2(c1, c1));
+  p2 = fma2(p2, f2, pack2(c0, c0));
   float t0, t1;
   unpack2(t2, t0, t1);
   if constexpr (kNan) {

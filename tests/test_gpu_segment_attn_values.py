@@ -48,6 +48,17 @@ def positions(n_kv):
     return sorted({0, 1, 2, 3, 15, 16, 17, 31, 32, 33, 64, 65, 100, 127, 128, 129, 160, n_kv - 2, n_kv - 1})
 
 
+def one_component(plan, raw):
+    """q and k with a single component each, whose product (exact in 24 bits) is raw[b][c] for every query of sample b."""
+    dtype, variant, n_q, H, kv, D, n_kv = plan
+    B = len(raw)
+    q = torch.zeros(B, n_q, H, D, dtype=DT[dtype], device="cuda")
+    k = torch.zeros(B, n_kv, kv, D, dtype=DT[dtype], device="cuda")
+    q[..., 3] = 2.0 ** 20
+    k[..., 3] = (torch.tensor(raw, dtype=torch.float64, device="cuda") * 2.0 ** -20).to(DT[dtype])[:, :, None]
+    return q, k
+
+
 @plans
 @pytest.mark.parametrize("what", [NAN, INF])
 def test_a_row_with_a_nan_or_infinite_logit_is_no_row_without_keys(plan, what):
@@ -112,3 +123,49 @@ def test_joint_attention_passes_a_nan_key_on():
         out, lse = ctx.sparse_attn(q, k, v, want_lse=True)
         ctx.check()
         assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+@pytest.mark.parametrize("dtype,variant", base.VARIANTS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q", [100, 200])
+@pytest.mark.parametrize("lowest", [-1, 1])
+def test_the_types_lowest_value_behind_a_causal_limit(dtype, variant, D, n_q, lowest):
+    """Values of the type's lowest (largest) number at keys that the first rows do not see: those rows know nothing of them."""
+    dt, H, n_prefix, n_own, first = DT[dtype], 2, 50, n_q + 20, 64
+    gen = torch.Generator(device="cuda").manual_seed(n_q + D)
+    ctx = base.make_ctx(1, H, D, H, swam.F32 if dtype == "f32" else swam.BF16)
+    ctx.set_option(swam.OPT_ATTN_VARIANT, variant)
+    q = base.rand(gen, 1, n_q, H, D, dtype=dt)
+    kp, vp = (base.rand(gen, 1, n_prefix, H, D, dtype=dt) for _ in range(2))
+    k, v = (base.rand(gen, 1, n_own, H, D, dtype=dt) for _ in range(2))
+    v[:, first:] = lowest * torch.finfo(dt).max
+    out, lse = ctx.prefix_attn(q, kp, vp, k, v, causal=True, want_lse=True)
+    ctx.check()
+    rows = first - (n_own - n_q)                       # row t sees the own keys up to n_own - n_q + t
+    t = torch.arange(rows, device="cuda")[:, None]
+    mask = torch.ones(rows, n_prefix + first, dtype=torch.bool, device="cuda")
+    mask[:, n_prefix:] = torch.arange(first, device="cuda")[None, :] <= n_own - n_q + t
+
+    def segments(b, h):
+        return (torch.cat([kp[0, :, h], k[0, :first, h]]).double(), torch.cat([vp[0, :, h], v[0, :first, h]]).double(), mask)
+    base.compare(out[:, :rows], lse[:, :, :rows], q[:, :rows], segments, D, dt)
+
+
+@pytest.mark.parametrize("dtype,variant", base.VARIANTS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q", [100, 200])
+def test_the_types_lowest_value_at_keys_of_vanishing_weight(dtype, variant, D, n_q):
+    """Keys whose weights are below 2^-140 in fact, with values of the type's lowest number: 2^-140 * 2^128 is nothing beside
+    the tolerance, so the result is the mean over the other keys."""
+    dt, H, n_kv = DT[dtype], 1, 256
+    plan = (dtype, variant, n_q, H, H, D, n_kv)
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    ctx = context(plan, 1)
+    far = -256.0 * math.sqrt(D)                       # logits of 0 and -256: 2^-369
+    q, k = one_component(plan, [[0.0 if c % 2 else far for c in range(n_kv)]])
+    v = base.rand(gen, 1, n_kv, H, D, dtype=dt)
+    v[:, ::2] = torch.finfo(dt).min
+    out, lse = ctx.cross_attn(q, k, v, want_lse=True)
+    ctx.check()
+    keys, mask = k[0, 1::2, 0].double(), torch.ones(n_q, n_kv // 2, dtype=torch.bool, device="cuda")
+    base.compare(out, lse, q, lambda b, h: (keys, v[0, 1::2, 0].double(), mask), D, dt)
