@@ -84,6 +84,11 @@ __device__ __forceinline__ int seg_limit1(const SegArgs& a, int len, int t) {
   return a.causal ? max(0, len - a.n_q + t + 1) : len;
 }
 
+// An exponent is the scaled score minus the row's reference.  One fused multiply-add does not round the product as the reference was
+// rounded: half a step of the reference, which outgrows the exponents of fp32 from 2^31 on (step 256), would stand in the
+// exponent of the largest score itself.  From this magnitude on (half a step is 1 there) the product is rounded first.
+constexpr float kSegBig = 16777216.f;      // 2^24
+
 // What a row's sum of weights makes of its result: only a sum of exactly 0 is a row without keys.  A NaN sum (a NaN or +inf logit
 // of a visible key) has to stay one.
 __device__ __forceinline__ float seg_inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }

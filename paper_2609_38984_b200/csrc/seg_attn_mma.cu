@@ -115,6 +115,7 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
 #pragma unroll
   for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  bool big = false;                                // some row's reference is large: see kSegBig
 
   for (int t = kk.begin; t < kk.end; ++t) {
     const int st = (t - kk.begin) % kStagesM;
@@ -174,15 +175,26 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
       m[i] = mn;
       l[i] *= corr[i];
     }
+    const bool moved = __any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f);       // rare after the first tiles
+    if (moved) big = __any_sync(0xffffffffu, !(fmaxf(fabsf(ref[0]), fabsf(ref[1])) < kSegBig));
+    float scale = p.scale_log2;
+    if (big) {
+      scale = 1.f;
+#pragma unroll
+      for (int nb = 0; nb < KW / 8; ++nb) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[nb][e] *= p.scale_log2;
+      }
+    }
 #pragma unroll
     for (int nb = 0; nb < KW / 8; ++nb) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        sc[nb][e] = ex2(fmaf(sc[nb][e], p.scale_log2, -ref[e >> 1]));
+        sc[nb][e] = ex2(fmaf(sc[nb][e], scale, -ref[e >> 1]));
         l[e >> 1] += sc[nb][e];
       }
     }
-    if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f))   // rare after the first tiles
+    if (moved)
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) {
       o[i][0] *= corr[0];

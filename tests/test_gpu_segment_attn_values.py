@@ -35,6 +35,7 @@ PLANS = [
 ]
 IDS = ["-".join(map(str, (p[0], "warp" if p[1] else "auto") + p[2:])) for p in PLANS]
 plans = pytest.mark.parametrize("plan", PLANS, ids=IDS)
+streaming_plans = pytest.mark.parametrize("plan", PLANS[6:], ids=IDS[6:])       # the warp-level and fp32 kernels
 
 
 def context(plan, B):
@@ -169,3 +170,64 @@ def test_the_types_lowest_value_at_keys_of_vanishing_weight(dtype, variant, D, n
     ctx.check()
     keys, mask = k[0, 1::2, 0].double(), torch.ones(n_q, n_kv // 2, dtype=torch.bool, device="cuda")
     base.compare(out, lse, q, lambda b, h: (keys, v[0, 1::2, 0].double(), mask), D, dt)
+
+
+@streaming_plans
+@pytest.mark.parametrize("low,high", [(-1.5 * 2.0 ** 35, 3.0), (-1.25 * 2.0 ** 36, -1.125 * 2.0 ** 33), (2.0 ** 20, 1.625 * 2.0 ** 35),
+                                      (-1.0 * 2.0 ** 35, -1.0 * 2.0 ** 20), (-INF, 2.0), (-INF, -1.75 * 2.0 ** 37),
+                                      (-1.0 * 2.0 ** 146, 1.375 * 2.0 ** 60)])
+def test_one_key_far_above_all_others(plan, low, high):
+    """The weights are 1 and 0 (the logits lie at least 2^16 apart), wherever the one key stands: the result is its value, off by
+    the rounding of a weight that need not be 1 (its reference may be any number near the logit), of the result and of the
+    exponentials."""
+    dtype, variant, n_q, H, kv, D, n_kv = plan
+    dt, at = DT[dtype], positions(n_kv)
+    B = len(at)
+    gen = torch.Generator(device="cuda").manual_seed(n_q + D)
+    ctx = context(plan, B)
+    if low == -INF:
+        low = -1.0 * 2.0 ** 146               # 2^20 * -2^126 overflows to -inf
+    q, k = one_component(plan, [[high if c == x else low for c in range(n_kv)] for x in at])
+    v = base.rand(gen, B, n_kv, kv, D, dtype=dt)
+    out, lse = ctx.cross_attn(q, k, v, want_lse=True)
+    ctx.check()
+    want = torch.stack([v[b, c] for b, c in enumerate(at)])[:, None].double()
+    tol = ((2.0 ** -17 + 8 * U32) + (U16 * (2 + U16) if dtype == "bf16" else 0.0)) * want.abs()
+    assert ((out.double() - want).abs() <= tol).all(), [(c, out[b, 0, 0, :2].tolist(), want[b, 0, 0, :2].tolist())
+                                                        for b, c in enumerate(at) if not torch.allclose(out[b].double(), want[b].expand_as(out[b]), atol=0.05)]
+    logit = high / math.sqrt(D)
+    assert ((lse.double() - logit).abs() <= 8 * U32 * abs(logit) + 2.0 ** -17).all()
+
+
+@streaming_plans
+@pytest.mark.parametrize("raw", [1.625 * 2.0 ** 35, -1.625 * 2.0 ** 35, 1.171875 * 2.0 ** 40, -1.0 * 2.0 ** 60, 1.328125 * 2.0 ** 100])
+def test_equal_logits_of_any_size_weigh_the_same(plan, raw):
+    """All logits alike, however large: the mean of the values.  Tolerance: N sums in fp32, the rounding of the weights and of
+    the result."""
+    dtype, variant, n_q, H, kv, D, n_kv = plan
+    dt, B = DT[dtype], 2
+    gen = torch.Generator(device="cuda").manual_seed(n_q + D)
+    ctx = context(plan, B)
+    q, k = one_component(plan, [[raw] * n_kv] * B)
+    v = base.rand(gen, B, n_kv, kv, D, dtype=dt)
+    lens = [n_kv, n_kv - 37]
+    out, lse = ctx.cross_attn(q, k, v, kv_len=torch.tensor(lens, dtype=torch.int32, device="cuda"), want_lse=True)
+    ctx.check()
+    for b, n in enumerate(lens):
+        want, A = v[b, :n].double().mean(0), v[b, :n].double().abs().mean(0)
+        tol = (2.0 ** -17 + 2 * (n + 8) * U32) * A + (U16 * (A * (1 + U16) + want.abs() * (1 + 2 * U16)) if dtype == "bf16" else 0.0)
+        assert ((out[b].double() - want).abs() <= tol).all(), (b, out[b, 0, 0, :3], want[0, :3])
+        ref = raw / math.sqrt(D) + math.log(n)
+        assert ((lse[b].double() - ref).abs() <= 8 * U32 * abs(ref) + 2.0 ** -17 + (n + 8) * U32).all()
+
+
+@streaming_plans
+def test_rows_of_nothing_but_minus_infinity(plan):
+    """Logits that overflow to -inf throughout: no weight is above 0, zeros and -inf as for a row without keys."""
+    dtype, variant, n_q, H, kv, D, n_kv = plan
+    ctx = context(plan, 1)
+    q, k = one_component(plan, [[-1.0 * 2.0 ** 146] * n_kv])
+    v = base.rand(torch.Generator(device="cuda").manual_seed(1), 1, n_kv, kv, D, dtype=DT[dtype])
+    out, lse = ctx.cross_attn(q, k, v, want_lse=True)
+    ctx.check()
+    assert (out == 0).all() and (lse == -INF).all()
