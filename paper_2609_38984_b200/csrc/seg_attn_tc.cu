@@ -35,6 +35,7 @@
 // 4096 keys, 0.8 of the measured burst rate) and 4300 clk an item; head dim 64, 2300 clk a key tile, of which the exp2 unit
 // (16 a clk) needs 1920, and 4400 clk an item: its first scores' maximum, the read of the accumulators, the bookkeeping between
 // two items, and the instruction fetches of all that (81 % hits; 97 % at long key ranges).
+#include <float.h>
 #include <string.h>
 
 #include <type_traits>
@@ -705,19 +706,21 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         // their own accumulator rows, which nobody reads)
         if (warp_real) {
           const bool first = i == i0;
-          const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
           // weights of scores v[0 .. 2 n) as bf16 pairs, and their sum.  (A whole tile with a NaN is done again, in chunks.)
           auto weights = [&](auto n, const float* v, uint32_t* pk) {
-            const uint64_t negm2 = pack2(-m_used, -m_used);
+            const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), negm2 = pack2(-m_used, -m_used);
+            constexpr bool kWhole = decltype(n)::value == kTile / 2;
             uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
             for (int j = 0; j < decltype(n)::value; ++j) {
-              const uint64_t x2 = fma2(pack2(v[2 * j], v[2 * j + 1]), scale2, negm2);
+              const uint64_t v2 = pack2(v[2 * j], v[2 * j + 1]);
+              // (a product as such and the sum would be made one fused operation again)
+              const uint64_t x2 = kWhole ? fma2(v2, scale2, negm2) : add2(fma2(v2, scale2, 0ull), negm2);
               float p0, p1;
               if ((j & (D == 64 ? 15 : 7)) == 0) {
                 // one pair in eight on the FMA pipes, which the exp2 unit leaves idle (in sixteen at head dim 64, where the
                 // instructions cost more: ragged multi-view batch 245 us, 252 with eight, 240 with none; 608-row samples 72, 72, 74)
-                exp2_poly2<true, decltype(n)::value != kTile / 2>(x2, p0, p1);
+                exp2_poly2<true, !kWhole>(x2, p0, p1);
               } else {
                 float t0, t1;
                 unpack2(x2, t0, t1);
@@ -744,7 +747,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 #pragma unroll
               for (int j = 0; j < 4; ++j) m4[j] = fmaxf(m4[j], v[b + j]);
             }
-            m_used = any_key ? fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2 : 0.f;
+            // (a finite one: scores of -inf then weigh 0, and the first finite score raises it)
+            m_used = any_key ? fmaxf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2, -FLT_MAX) : 0.f;
           };
           bool whole = chunks_all >= kTile / kW;
           if (whole) {
@@ -755,7 +759,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             tmem_ld_wait();
             if (first) reference(sv);
             const float sum = weights(std::integral_constant<int, kTile / 2>(), sv, pk);
-            whole = !__any_sync(0xffffffffu, !(sum <= 256.f * kTile));       // no exponent above 2^8; else (inf and NaN too) below
+            // no weight far above 1 and no large reference (kSegBig); else, inf and NaN too, below
+            whole = !__any_sync(0xffffffffu, !(sum <= 256.f * kTile && fabsf(m_used) < kSegBig));
             if (whole) {
               // P overwrites the scores only now that the pass is known to stand
 #pragma unroll
@@ -785,10 +790,12 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 }
                 if (first && c == 0 && !raised && chunks_all < kTile / kW) reference(v);
                 sum = weights(std::integral_constant<int, kW / 2>(), v, pk);
-                const bool grew = !(sum <= 256.f * kW);          // some exponent above 2^8; also inf and NaN
+                const bool grew = !(sum <= 256.f * kW);          // weights far above 1; also inf and NaN
                 if (raised || !__any_sync(0xffffffffu, grew)) break;
                 // Rare: raise the reference to the row's maximum, in whole powers of two, so that the weights of this tile that
-                // are written already rescale without another rounding; then repeat the chunk.
+                // are written already rescale without another rounding; then repeat the chunk.  (A step of 2^8 or more leaves
+                // nothing of them, and large numbers are whole: then the reference becomes the maximum itself, since a
+                // sum of the two would be off by half a step of the larger one.)
                 float mraw = -INFINITY;
 #pragma unroll 1
                 for (int b = 0; b < kW / 32; ++b) {
@@ -799,9 +806,11 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                   for (int j = 0; j < 32; ++j)
                     if (b * 32 + j < left) mraw = fmaxf(mraw, w[j]);
                 }
-                const float delta = grew ? ceilf(fmaxf(fmaf(mraw, p.scale_log2, -m_used), 0.f)) : 0.f;
-                const float f = ex2(-delta);
-                m_used += delta;
+                const float delta = ceilf(fmaxf(fmaf(mraw, p.scale_log2, -m_used), 0.f));
+                const bool near = delta < 256.f && fabsf(m_used) < kSegBig;
+                const float next = !grew ? m_used : (near ? m_used + delta : fmaxf(m_used, mraw * p.scale_log2));
+                const float f = !grew ? 1.f : ex2(near ? -delta : m_used - next);
+                m_used = next;
                 l_run *= f;
                 tmem_st_wait();
 #pragma unroll 1

@@ -35,7 +35,6 @@ PLANS = [
 ]
 IDS = ["-".join(map(str, (p[0], "warp" if p[1] else "auto") + p[2:])) for p in PLANS]
 plans = pytest.mark.parametrize("plan", PLANS, ids=IDS)
-streaming_plans = pytest.mark.parametrize("plan", PLANS[6:], ids=IDS[6:])       # the warp-level and fp32 kernels
 
 
 def context(plan, B):
@@ -172,7 +171,7 @@ def test_the_types_lowest_value_at_keys_of_vanishing_weight(dtype, variant, D, n
     base.compare(out, lse, q, lambda b, h: (keys, v[0, 1::2, 0].double(), mask), D, dt)
 
 
-@streaming_plans
+@plans
 @pytest.mark.parametrize("low,high", [(-1.5 * 2.0 ** 35, 3.0), (-1.25 * 2.0 ** 36, -1.125 * 2.0 ** 33), (2.0 ** 20, 1.625 * 2.0 ** 35),
                                       (-1.0 * 2.0 ** 35, -1.0 * 2.0 ** 20), (-INF, 2.0), (-INF, -1.75 * 2.0 ** 37),
                                       (-1.0 * 2.0 ** 146, 1.375 * 2.0 ** 60)])
@@ -199,7 +198,7 @@ def test_one_key_far_above_all_others(plan, low, high):
     assert ((lse.double() - logit).abs() <= 8 * U32 * abs(logit) + 2.0 ** -17).all()
 
 
-@streaming_plans
+@plans
 @pytest.mark.parametrize("raw", [1.625 * 2.0 ** 35, -1.625 * 2.0 ** 35, 1.171875 * 2.0 ** 40, -1.0 * 2.0 ** 60, 1.328125 * 2.0 ** 100])
 def test_equal_logits_of_any_size_weigh_the_same(plan, raw):
     """All logits alike, however large: the mean of the values.  Tolerance: N sums in fp32, the rounding of the weights and of
@@ -221,7 +220,7 @@ def test_equal_logits_of_any_size_weigh_the_same(plan, raw):
         assert ((lse[b].double() - ref).abs() <= 8 * U32 * abs(ref) + 2.0 ** -17 + (n + 8) * U32).all()
 
 
-@streaming_plans
+@plans
 def test_rows_of_nothing_but_minus_infinity(plan):
     """Logits that overflow to -inf throughout: no weight is above 0, zeros and -inf as for a row without keys."""
     dtype, variant, n_q, H, kv, D, n_kv = plan
