@@ -8,6 +8,7 @@ namespace swam {
 namespace {
 
 constexpr int kMaxSplits = 64;
+constexpr int64_t kMaxItemKeys = 1 << 26;
 
 // One warp per row; lanes hold the pieces' weights and then D / 32 output columns each.  The first pieces' outputs are
 // requested before the weights are known (an output of weight 0 may never have been written and is not used).
@@ -130,6 +131,9 @@ PassPlan plan_pass(const SegArgs& a, int64_t blocks, int64_t rows, int64_t keys,
   }
   if (s > keys / min_keys) s = keys / min_keys;
   if (s > kMaxSplits) s = kMaxSplits;
+  // Waits of the tensor-core kernel last as long as an item, at some 3110 clk a tile of 128 keys, and give up after kWaitCycles:
+  // an item takes 1.6e9 of these 4e9 clk at most.  (2^30 keys, the most that a call may have, are 16 pieces.)
+  if (p.kind == kTc && s < ceil_div(keys, kMaxItemKeys)) s = ceil_div(keys, kMaxItemKeys);
   p.splits = s < 1 ? 1 : (int)s;
   return p;
 }

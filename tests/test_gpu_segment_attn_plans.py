@@ -1,0 +1,35 @@
+"""The ways in which the segment-attention calls cut their work, each against the definition in 64 bits, with the number
+of launches that tells which way was taken; and what the calls say about lengths and sizes at their limits."""
+import ctypes
+
+import pytest
+import torch
+
+import test_gpu_segment_attn as base
+from paper_2609_38984_b200 import swam
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def launches(ctx, call):
+    n = ctx.launch_count()
+    call()
+    ctx.check()
+    return ctx.launch_count() - n
+
+
+def scratch_bytes(ctx, **kw):
+    n = ctypes.c_size_t()
+    rc = ctx.lib.swam_cross_attn_scratch_bytes(ctx.ctx, ctypes.byref(swam.SwamCrossArgs(**kw)), ctypes.byref(n))
+    return rc, n.value
+
+
+def test_the_longest_key_ranges_are_cut_into_pieces_that_a_bounded_wait_outlasts():
+    """A wait in the tensor-core kernel may last as long as a work item: some 3110 clocks a tile of 128 keys, against a limit of 4e9
+    clocks.  So an item has at most 2^26 keys, whatever the number of items (here more than there are SMs)."""
+    B, H, D, n_q = 40, 8, 128, 300
+    ctx = base.make_ctx(B, H, D, 1, swam.BF16)
+    piece = B * n_q * H * (D * 4 + 8)
+    for n_kv, pieces in ((1 << 20, 0), (1 << 26, 0), ((1 << 26) + 1, 2), (1 << 27, 2), (1 << 29, 8)):
+        assert scratch_bytes(ctx, n_q=n_q, n_kv=n_kv) == (swam.OK, pieces * piece), n_kv
