@@ -98,6 +98,12 @@ cudaError_t launch_merge(const SegParams& p, int parts, cudaStream_t st, int* la
   }
 }
 
+// Lengths that belong to a tensor without rows: the other kernels have no reason to read them.
+__global__ void seg_check_lengths_kernel(const int32_t* len, int n, int* status) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x)
+    if (len[i] != 0) atomicOr(status, ST_BAD_LEN);
+}
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // How a pass runs: `blocks` blocks with `rows` rows per key/value head each and up to `keys` keys.  pass: -1 = the only one.
@@ -194,6 +200,13 @@ cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& pl, bool warp_mma, 
     const int64_t items = (int64_t)ps.blocks * a.N_kv * ps.row_tiles * ps.splits;
     if (items > 0x7fffffff) return cudaErrorInvalidConfiguration;
     ps.items = (int)items;
+  }
+  for (int i = 0; i < 2; ++i) {
+    if (a.n[i] > 0 || !a.len[i]) continue;
+    ++*launches;
+    seg_check_lengths_kernel<<<1, 128, 0, st>>>(a.len[i], i == 0 ? a.B / a.per_group : a.B, status);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
   }
   const bool both = n_pass == 2 && pp[0].kind == kTc && pp[1].kind == kTc && pp[0].tile_rows == pp[1].tile_rows;
   if (both) p.early = 0;

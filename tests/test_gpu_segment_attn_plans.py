@@ -33,3 +33,32 @@ def test_the_longest_key_ranges_are_cut_into_pieces_that_a_bounded_wait_outlasts
     piece = B * n_q * H * (D * 4 + 8)
     for n_kv, pieces in ((1 << 20, 0), (1 << 26, 0), ((1 << 26) + 1, 2), (1 << 27, 2), (1 << 29, 8)):
         assert scratch_bytes(ctx, n_q=n_q, n_kv=n_kv) == (swam.OK, pieces * piece), n_kv
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lengths_of_tensors_without_rows_are_checked(dtype):
+    """A length other than 0 for a tensor without rows is out of range like any other."""
+    dt, B = base.DT[dtype], 4
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    ctx = base.make_ctx(B, 4, 64, 2, swam.F32 if dtype == "f32" else swam.BF16)
+    some = base.rand(gen, B, 30, 2, 64, dtype=dt)
+    none = some[:, :0]
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    for n_q in (1, 3, 200):
+        q = base.rand(gen, B, n_q, 4, 64, dtype=dt)
+        for bad in (lambda: ctx.cross_attn(q, none, none, kv_len=ints(0, 0, 0, 5)),
+                    lambda: ctx.cross_attn(q, none, none, kv_len=ints(-1, 0, 0, 0)),
+                    lambda: ctx.prefix_attn(q, some[:2], some[:2], none, none, own_len=ints(0, 0, 3, 0)),
+                    lambda: ctx.prefix_attn(q, some[:2], some[:2], none, none, own_len=ints(0, -1, 0, 0), causal=True),
+                    lambda: ctx.prefix_attn(q, none[:1], none[:1], some, some, prefix_len=ints(1))):
+            out = bad()
+            with pytest.raises(swam.SwamError) as e:
+                ctx.check()
+            assert e.value.code == swam.ERR_DEVICE_CHECK and "length" in str(e.value)
+            assert torch.isfinite(out).all()
+        want = ctx.prefix_attn(q, some[:2], some[:2], none, none)
+        got = ctx.prefix_attn(q, some[:2], some[:2], none, none, own_len=ints(0, 0, 0, 0))
+        ctx.check()
+        assert torch.equal(got, want)
+        assert (ctx.cross_attn(q, none, none, kv_len=ints(0, 0, 0, 0)) == 0).all()
+        ctx.check()
