@@ -122,6 +122,8 @@ __global__ void __launch_bounds__(32 * WR * WK) seg_mma_kernel(const __grid_cons
     const bool ok = mbar_wait(bars + 8 * st, ((t - kk.begin) / kStagesM) & 1, abort_flag);
     if (!__syncthreads_and(ok ? 1 : 0)) {          // (and every warp is through with the tile before)
       if (threadIdx.x == 0) atomicOr(p.status, ST_TIMEOUT);
+      // the copies in flight write to memory that is used again below, and must not outlive the CTA
+      drain_loads(bars, kStagesM, min(kk.end, t + kStagesM - 1) - kk.begin);
       break;
     }
     if (threadIdx.x == 0 && t + kStagesM - 1 < kk.end) load_tile(t + kStagesM - 1);

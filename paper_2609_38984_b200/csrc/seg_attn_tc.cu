@@ -30,7 +30,7 @@
 // at its 32.  Rows of V between it and the end of the step are overwritten with zeros in shared memory (0 * NaN would poison
 // the row); scores behind a row's limit become -inf.
 // Every wait on an mbarrier is bounded; when one runs out the kernel raises the timeout bit of the status word and every
-// role falls through to the exit.
+// role falls through to the exit, where the copies and products in flight are waited for (again with a limit).
 // What bounds it (cycles at the 1.65 to 1.85 GHz of this load): head dim 128, 3110 clk a key tile of an item (1.33 PFLOP/s at
 // 4096 keys, 0.8 of the measured burst rate) and 4300 clk an item; head dim 64, 2300 clk a key tile, of which the exp2 unit
 // (16 a clk) needs 1920, and 4400 clk an item: its first scores' maximum, the read of the accumulators, the bookkeeping between
@@ -75,7 +75,7 @@ struct SegCfg {
   // every T: the order on the tensor pipe.
   static constexpr int LK = kAlt ? NB : NB - 1;
   static constexpr int kData = QB * NQ * kTileBytes + ST * kTileBytes;
-  static constexpr int kBars = 8 * (4 * QB + 2 * ST + 2 * kDesc + 2 * NB + 5);
+  static constexpr int kBars = 8 * (4 * QB + 2 * ST + 2 * kDesc + 2 * NB + 6);
   static constexpr int kDescOff = (kBars + 15) / 16 * 16;
   static constexpr int kTail = kDescOff + kDesc * (int)sizeof(SegDesc) + 16;
   static constexpr int kBytes = kData + 1024 /*alignment*/ + kTail + (kAlt ? kTile * 8 : 0) /*maxima and sums of stream 1*/;
@@ -141,6 +141,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   // Every row of the output has been staged, per query buffer and stream.  (One barrier for all buffers could complete twice
   // before the warp that stores the tiles looks at it.)
   auto bar_staged = [&](int b, int s) { return bars + 8 * (kB + 2 * NB + 5 + 2 * b + s); };
+  const uint32_t bar_drain = bars + 8 * (kB + 2 * NB + 5 + 2 * QB);          // the products in flight when a wait has run out
   SegDesc* desc = reinterpret_cast<SegDesc*>(base_ptr + C::kData + C::kDescOff);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + C::kData + C::kTail - 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kData + C::kTail - 8);
@@ -175,6 +176,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     mbar_init(bar_o_final, 1);
     mbar_init(bar_o_free, 8);
     mbar_init(bar_x, 4);
+    mbar_init(bar_drain, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -399,6 +401,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         ok = load(desc[(dvi - 1) % kDesc], true, iv++);
         if (ok) ok = load_k();
       }
+      if (!ok) {
+        drain_loads(bar_full(0), ST, pos);
+        if (x.box_q) drain_loads(bar_q(0), QB, k_end ? iter - 1 : iter);
+      }
     } else {
       // ------------------------------------------------------------------ MMA issuer (warp converged, one lane issues)
       const uint32_t el = elect_one();
@@ -562,6 +568,11 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           else pv(0, true);
           if (v_left()) qk_alt();
         }
+      }
+      if (!ok) {
+        // a wait has run out: the products in flight must have ended before the tensor memory is given back
+        tc_commit(bar_drain, el);
+        drain_loads(bar_drain, 1, 1);
       }
     }
   } else {

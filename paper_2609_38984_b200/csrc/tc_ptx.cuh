@@ -10,6 +10,7 @@ namespace {
 constexpr int kTile = 128;          // rows of an MMA tile (query rows per tile; keys per tile of the attention kernel)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr unsigned long long kWaitCycles = 4000000000ull;  // about two seconds at 1.9 GHz
+constexpr unsigned long long kDrainCycles = 200000000ull;  // for what is in flight when a wait has run out
 
 // ---------------------------------------------------------------------------------------------------------
 // PTX wrappers
@@ -28,6 +29,12 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 // bounded wait: false when the limit ran out or another role already gave up
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   return mbar_wait_bounded(bar, parity, kWaitCycles, abort_flag);
+}
+
+// When a wait has run out: the copies in flight must not outlive the CTA.  Of `issued` loads into the n barriers from bar on in turn,
+// waits for the last n.  (Out of line: a kernel's ordinary code should not be moved about by this.)
+__device__ __noinline__ void drain_loads(uint32_t bar, int n, int issued) {
+  for (int i = issued > n ? issued - n : 0; i < issued; ++i) mbar_wait_bounded(bar + 8 * (i % n), (i / n) & 1, kDrainCycles, nullptr);
 }
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2,
