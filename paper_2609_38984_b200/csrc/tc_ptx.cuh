@@ -32,8 +32,9 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 }
 
 // When a wait has run out: the copies in flight must not outlive the CTA.  Of `issued` loads into the n barriers from bar on in turn,
-// waits for the last n.  (Out of line: a kernel's ordinary code should not be moved about by this.)
-__device__ __noinline__ void drain_loads(uint32_t bar, int n, int issued) {
+// waits for the last n.
+__device__ __forceinline__ void drain_loads(uint32_t bar, int n, int issued) {
+#pragma unroll 1
   for (int i = issued > n ? issued - n : 0; i < issued; ++i) mbar_wait_bounded(bar + 8 * (i % n), (i / n) & 1, kDrainCycles, nullptr);
 }
 
