@@ -160,7 +160,7 @@ int swam_scatter(swam_ctx* ctx, const void* out_p, const int32_t* pack_map, cons
  * Strides are in elements and count from one token (or sample, or group) to the next; 0 = contiguous.  The heads of a
  * token are contiguous (N_h*D or n_kv_heads*D elements), so a K/V projection that interleaves k and v is read in place.
  * Strides must be multiples of 16 bytes, pointers 16-byte aligned, tokens must not overlap, and out must not overlap
- * any input.  Lengths (device int32) may be NULL: all rows are real.  Rows behind a length are never used, whatever they
+ * any input (refused where it starts at the same place, or where both are contiguous).  Lengths (device int32) may be NULL: all rows are real.  Rows behind a length are never used, whatever they
  * hold (NaN included); a length outside [0, n] is clamped and reported by swam_check (SWAM_ERR_DEVICE_CHECK; without queries
  * nothing is read).  A tensor of length 0 may be NULL.  Rows of out and lse that the call does not own are left untouched.
  *

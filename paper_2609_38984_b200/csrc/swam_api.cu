@@ -154,6 +154,21 @@ bool set_strides(int64_t& tok, int64_t& smp, int64_t n_tok, int64_t n_smp, int64
 
 constexpr int32_t kMaxSegTokens = 1 << 29;
 
+// Whether two tensors of `row`-element tokens certainly share memory: they start at the same place, or both are contiguous and their
+// ranges meet.  (Strided views of one buffer may lie in one another's gaps; they are taken to.)
+struct TokenSpan {
+  const void* ptr;
+  int64_t n_tok, n_smp, tok, smp, row;
+  bool contiguous() const { return (n_tok == 1 || tok == row) && (n_smp == 1 || smp == n_tok * row); }
+};
+bool share_memory(const TokenSpan& a, const TokenSpan& b, size_t elem) {
+  if (a.n_tok == 0 || b.n_tok == 0) return false;
+  if (a.ptr == b.ptr) return true;
+  if (!a.contiguous() || !b.contiguous()) return false;
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.ptr), pb = reinterpret_cast<uintptr_t>(b.ptr);
+  return pa < pb ? pb - pa < (uintptr_t)(a.n_smp * a.n_tok * a.row) * elem : pa - pb < (uintptr_t)(b.n_smp * b.n_tok * b.row) * elem;
+}
+
 // What both segment-attention calls share once their arguments are in `a`: the remaining checks, and the plan.
 int check_seg(swam_ctx* c, SegArgs& a, int32_t n_kv_heads, const char* name, SegPlan* plan, bool pointers) {
   const Dims& d = c->d;
@@ -192,6 +207,12 @@ int check_seg(swam_ctx* c, SegArgs& a, int32_t n_kv_heads, const char* name, Seg
   }
   const uintptr_t words = reinterpret_cast<uintptr_t>(a.lse) | reinterpret_cast<uintptr_t>(a.len[0]) | reinterpret_cast<uintptr_t>(a.len[1]);
   if (!aligned16(a.q) || !aligned16(a.out) || (words & 3u) != 0) return bad(SWAM_ERR_INVALID_ARG, "misaligned pointer");
+  const TokenSpan out{a.out, a.n_q, a.B, a.o_tok, a.o_smp, row};
+  bool over = share_memory(out, {a.q, a.n_q, a.B, a.q_tok, a.q_smp, row}, eb);
+  for (int s = 0; s < 2; ++s)
+    over = over || share_memory(out, {a.k[s], a.n[s], blocks[s], a.k_tok[s], a.k_smp[s], row_kv}, eb) ||
+           share_memory(out, {a.v[s], a.n[s], blocks[s], a.v_tok[s], a.v_smp[s], row_kv}, eb);
+  if (over) return bad(SWAM_ERR_INVALID_ARG, "out must not overlap an input");
   return SWAM_OK;
 }
 

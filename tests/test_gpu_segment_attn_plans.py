@@ -62,3 +62,38 @@ def test_lengths_of_tensors_without_rows_are_checked(dtype):
         assert torch.equal(got, want)
         assert (ctx.cross_attn(q, none, none, kv_len=ints(0, 0, 0, 0)) == 0).all()
         ctx.check()
+
+
+def test_an_output_over_an_input_is_refused():
+    """Results over an input that other rows still read: the same tensor, or two contiguous ones that share a part.  Different
+    heads or samples of one wider tensor are fine."""
+    ctx = base.make_ctx(2, 4, 64, 4, swam.BF16)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q = base.rand(gen, 2, 30, 4, 64, dtype=BF)
+    kv = base.rand(gen, 2, 30, 2, 4, 64, dtype=BF)
+    k, v = kv[:, :, 0], kv[:, :, 1]
+    flat = base.rand(gen, 2 * 30 * 4 * 64 * 2, dtype=BF)
+    a, b = flat[:15360].view(2, 30, 4, 64), flat[7680:23040].view(2, 30, 4, 64)
+    before = ctx.launch_count()
+    for args, out in (((q, k, v), q), ((q, k, v), k), ((q, k, v), v), ((a, k, v), b), ((b, k, v), a), ((q, a, k), b), ((q, k, b), a)):
+        with pytest.raises(swam.SwamError) as e:
+            ctx.cross_attn(*args, out=out)
+        assert e.value.code == swam.ERR_INVALID_ARG and "overlap" in str(e.value)
+    for pre, own, out in (((k[:1], v[:1]), (a, a), a), ((a[:1], k[:1]), (k, v), a)):
+        with pytest.raises(swam.SwamError) as e:
+            ctx.prefix_attn(q, *pre, *own, out=out)
+        assert e.value.code == swam.ERR_INVALID_ARG and "overlap" in str(e.value)
+    assert ctx.launch_count() == before
+    want = ctx.cross_attn(q, k, v)
+    wide = base.rand(gen, 2, 30, 16, 64, dtype=BF)
+    wide[:, :, :4], wide[:, :, 4:8], wide[:, :, 12:] = q, k, v
+    got = ctx.cross_attn(wide[:, :, :4], wide[:, :, 4:8], wide[:, :, 12:], out=wide[:, :, 8:12])
+    ctx.check()
+    assert torch.equal(got, want) and torch.equal(wide[:, :, :4], q) and torch.equal(wide[:, :, 12:], v)
+    # samples of one buffer side by side
+    two = base.rand(gen, 4, 30, 4, 64, dtype=BF)
+    two[:2] = q
+    assert torch.equal(ctx.cross_attn(two[:2], k, v, out=two[2:]), want)
+    two[::2] = q
+    assert torch.equal(ctx.cross_attn(two[::2], k, v, out=two[1::2]), want)
+    ctx.check()
