@@ -330,6 +330,8 @@ class Swam:
         if need is None:
             n = ctypes.c_size_t()
             self._chk(query(self.ctx, ctypes.byref(a), ctypes.byref(n)))
+            if len(self._scratch_need) >= 64:       # a decoding loop brings another length with every call
+                self._scratch_need.clear()
             need = self._scratch_need[key] = n.value
         if need == 0:
             return None

@@ -97,3 +97,15 @@ def test_an_output_over_an_input_is_refused():
     two[::2] = q
     assert torch.equal(ctx.cross_attn(two[::2], k, v, out=two[1::2]), want)
     ctx.check()
+
+
+def test_what_the_binding_keeps_of_past_sizes_is_bounded():
+    """A decoding loop calls with another length every time; the sizes that the binding remembers stay few."""
+    ctx = base.make_ctx(1, 2, 64, 2, swam.BF16)
+    q = torch.zeros(1, 1, 2, 64, dtype=BF, device="cuda")
+    k = torch.zeros(1, 400, 2, 64, dtype=BF, device="cuda")
+    for n in range(1, 400):
+        ctx.cross_attn(q, k[:, :n], k[:, :n])
+    ctx.check()
+    kept = [x for x in vars(ctx).values() if isinstance(x, dict)]
+    assert kept and all(len(x) <= 64 for x in kept)
