@@ -286,11 +286,9 @@ class Swam:
         if t.dtype is not self._torch_dtype or t.get_device() != self._device_index or t.dim() != 4:
             raise ValueError(f"{name}: expected a 4-dimensional {self._torch_dtype} tensor on {self.device}")
         n, tokens, h, d = t.shape
-        if (lead is not None and n != lead) or h != heads or d != self.D:
+        if (lead is not None and n != lead) or h != heads or h == 0 or d != self.D:
             raise ValueError(f"{name}: expected shape [{'groups' if lead is None else lead}, tokens, {heads}, {self.D}], got {list(t.shape)}")
-        if n == 0 or tokens == 0 or h == 0:
-            return 0, 0
-        if t.is_contiguous():
+        if n == 0 or tokens == 0 or t.is_contiguous():
             return 0, 0
         s0, s1, s2, s3 = t.stride()
         if s3 != 1 or (h > 1 and s2 != d):

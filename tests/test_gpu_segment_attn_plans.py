@@ -109,3 +109,13 @@ def test_what_the_binding_keeps_of_past_sizes_is_bounded():
     ctx.check()
     kept = [x for x in vars(ctx).values() if isinstance(x, dict)]
     assert kept and all(len(x) <= 64 for x in kept)
+
+
+def test_keys_without_heads_are_refused():
+    ctx = base.make_ctx(2, 4, 64, 2, swam.BF16)
+    q = torch.zeros(2, 3, 4, 64, dtype=BF, device="cuda")
+    k = torch.zeros(2, 0, 0, 64, dtype=BF, device="cuda")
+    with pytest.raises(ValueError):
+        ctx.cross_attn(q, k, k)
+    with pytest.raises(ValueError):
+        ctx.prefix_attn(q, k, k, k, k)
