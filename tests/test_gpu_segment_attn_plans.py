@@ -19,6 +19,66 @@ def launches(ctx, call):
     return ctx.launch_count() - n
 
 
+def prefix_again(ctx, t, causal):
+    q, kp, vp, k, v, pl, ol = t
+    ol = ol if k.shape[1] else None            # (lengths of a tensor without rows take a launch to check)
+    return launches(ctx, lambda: ctx.prefix_attn(q, kp, vp, k, v, prefix_len=pl, own_len=ol, causal=causal, want_lse=True))
+
+
+def ragged(n, most):
+    """Lengths from none to all, tile borders among them."""
+    steps = [most, 0, 1, 128, 129, most - 1, 16, 640, 255, 513]
+    return [min(most, steps[i % len(steps)]) for i in range(n)]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n_q,H,kv", [(64, 3, 3), (32, 4, 2), (40, 3, 3), (20, 4, 2), (9, 10, 2)])
+def test_both_passes_in_one_tensor_core_launch(D, causal, n_q, H, kv):
+    """33 to 64 rows a sample, two samples to a tile, and more than 512 own keys: shared tiles and samples' own tiles in one
+    launch (queries as boxes of 64-row samples, or row by row), then the merge."""
+    B, groups, n_own = 6, 3, 700
+    ctx, t, _, _ = base.prefix_case(BF, B, groups, n_q, H, kv, D, 400, n_own, [400, 0, 131], ragged(B, n_own), causal, seed=D + n_q)
+    assert prefix_again(ctx, t, causal) == 2
+    ctx, t, _, _ = base.prefix_case(BF, B, groups, n_q, H, kv, D, 3000, n_own, [3000, 2049, 130], ragged(B, n_own)[::-1], causal,
+                                    seed=D + n_q + 1)
+    assert prefix_again(ctx, t, causal) == 2
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n_q,H,kv", [(64, 3, 3), (32, 4, 2), (40, 3, 3), (20, 4, 2)])
+def test_shared_256_row_tiles_and_a_second_tensor_core_pass(D, causal, n_q, H, kv):
+    """Groups of five such samples: 256-row tiles over several samples (the last one of a group ends inside the next group's
+    samples), the own keys as a second launch on the tensor cores, and the merge."""
+    B, groups, n_own = 10, 2, 700
+    ctx, t, _, _ = base.prefix_case(BF, B, groups, n_q, H, kv, D, 3000, n_own, [3000, 1111], ragged(B, n_own), causal, seed=D + n_q)
+    assert prefix_again(ctx, t, causal) == 3
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("per_group,n_q,H,kv", [(4, 40, 3, 3), (4, 64, 3, 3), (2, 40, 3, 3), (2, 32, 4, 2), (9, 7, 10, 2)])
+def test_shared_tiles_without_own_keys(D, per_group, n_q, H, kv):
+    """Several samples to a tensor-core tile with a final result: one launch, no merge."""
+    B = 2 * per_group
+    ctx, t, _, _ = base.prefix_case(BF, B, 2, n_q, H, kv, D, 300, 0, [300, 129], [0] * B, False, seed=D + n_q)
+    assert prefix_again(ctx, t, False) == 1
+    ctx, t, _, _ = base.prefix_case(BF, B, 2, n_q, H, kv, D, 300, 0, [0, 17], [0] * B, True, seed=D + n_q)
+    assert prefix_again(ctx, t, True) == 1
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q,H,kv", [(300, 2, 2), (256, 4, 2), (100, 6, 2)])
+def test_256_row_tiles_in_pieces(D, n_q, H, kv):
+    """More than 128 rows and many keys for few heads: pieces of 256-row tiles, some of them without real keys."""
+    lens = [5000, 4097, 700, 0]
+    ctx, q, k, v, kv_len, _, _ = base.cross_case(BF, len(lens), n_q, H, kv, D, 5000, lens, seed=D + n_q, interleaved=True)
+    assert launches(ctx, lambda: ctx.cross_attn(q, k, v, kv_len=kv_len, want_lse=True)) == 2
+    # the same through a prefix of each sample's own
+    ctx, t, _, _ = base.prefix_case(BF, 2, 2, n_q, H, kv, D, 3000, 1500, [3000, 1025], [1500, 70], True, seed=D + n_q)
+    assert prefix_again(ctx, t, True) == 2
+
+
 def scratch_bytes(ctx, **kw):
     n = ctypes.c_size_t()
     rc = ctx.lib.swam_cross_attn_scratch_bytes(ctx.ctx, ctypes.byref(swam.SwamCrossArgs(**kw)), ctypes.byref(n))
