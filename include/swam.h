@@ -153,7 +153,9 @@ int swam_scatter(swam_ctx* ctx, const void* out_p, const int32_t* pack_map, cons
 
 /* (6) Attention to keys outside the joint sequence (no counterpart in the paper, whose backbones hold these operators in
  * the same Transformer blocks).  A row with visible keys c gets out = sum_c softmax_c(scale * q . k_c) v_c and
- * lse = ln sum_c exp(scale * q . k_c); a row that sees no key gets out = 0 and lse = -inf.  Element type, number of
+ * lse = ln sum_c exp(scale * q . k_c); a row that sees no key gets out = 0 and lse = -inf.  A NaN or +inf logit of a visible
+ * key leaves its row without a finite result (out and lse); a logit of -inf weighs 0, and a row of nothing else is as one
+ * without keys.  A NaN or infinite value of a real key may make NaN of rows that a causal limit hides it from.  Element type, number of
  * samples, query heads, head dim and scale are the context's.  bf16: fp32 scores, maxima, sums and accumulation, the
  * probabilities are rounded to bf16 for the product with v; fp32: fp32 throughout.
  *

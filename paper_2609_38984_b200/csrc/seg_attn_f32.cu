@@ -8,7 +8,7 @@
 // length are filled with zeros and masked.
 // What bounds it: latency.  4 x 1000 rows, 8 heads of 64, 100 to 333 keys take 84 us (21 TFLOP/s of some 70 on the FMA pipes): three
 // CTAs an SM leave 2.3 warps a scheduler, which issue every 2.2 clk.  Four CTAs with single K and V buffers took 86 us, 32-row
-// tiles 92.
+// tiles 92.  (Compiled to 128 registers, that instance, <64, 4>, spills 12 bytes a thread and loads 24; <128, 1> spills 4.)
 #include "seg_attn.cuh"
 
 namespace swam {

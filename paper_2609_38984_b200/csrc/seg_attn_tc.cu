@@ -7,12 +7,13 @@
 //   warp 9       TMA producer: K and V tiles into one ring of shared-memory slots, in the order the tensor pipe uses them,
 //                and the queries where a row tile is a box of the query tensor
 //   warp 10      fetches the query rows one by one where it is not (a number of heads per key/value head that does not
-//                divide the tile, samples that do not tile it), with 16-byte asynchronous copies into the same layout
-//   warp 8       one elected thread issues every tcgen05.mma: S = Q K^T into TMEM, then O += P V with both operands in
+//                divide the tile, samples that do not tile it), with 16-byte asynchronous copies into the same layout;
+//                where final results leave as boxes of the output tensor, it sends these instead
+//   warp 8       one elected thread issues every tcgen05.mma: S = Q K^T into TMEM, then O += P V with P in TMEM and V in
 //                shared memory; O stays in TMEM for the whole range of keys
 //   warps 0-3    softmax of stream 0, one thread per row: S row from TMEM, exponentials against a running reference
-//   warps 4-7    maximum (exp2 domain, raised only when a row outgrows it by 2^8: exact either way), P as bf16; same for
-//                stream 1.  The streams' exponentials overlap each other's products.
+//   warps 4-7    maximum (exp2 domain, raised only when the weights of 32 or 128 keys sum to more than 2^8 each on average: exact
+//                either way), P as bf16; same for stream 1.  The streams' exponentials overlap each other's products.
 // P goes back over its scores in TMEM (rounded to bf16, the operand type: half a step, 2^-8, of each weight).  TMEM holds three
 // score buffers beside the outputs at head dim 64 and two at 128; P V of a unit (one key tile of one stream) frees the buffer
 // that the Q K^T three (two) units on takes.  (At head dim 128 the chain softmax, P V, Q K^T then sets the period: 3110 clk a
@@ -34,7 +35,8 @@
 // What bounds it (cycles at the 1.65 to 1.85 GHz of this load): head dim 128, 3110 clk a key tile of an item (1.33 PFLOP/s at
 // 4096 keys, 0.8 of the measured burst rate) and 4300 clk an item; head dim 64, 2300 clk a key tile, of which the exp2 unit
 // (16 a clk) needs 1920, and 4400 clk an item: its first scores' maximum, the read of the accumulators, the bookkeeping between
-// two items, and the instruction fetches of all that (81 % hits; 97 % at long key ranges).
+// two items, and the instruction fetches of all that (83 % hits where items have some three key tiles; 96 % at head dim 128
+// and 28).  So short items are bound by their change and not by the exp2 unit, which is 45 % active there.
 #include <float.h>
 #include <string.h>
 
@@ -70,7 +72,7 @@ struct SegCfg {
   // Query buffers.  A buffer is free again when its item's output has left through it, so Q K^T must not run into an item
   // whose buffer belongs to one with products that are still to be issued: with items of one tile it is LK items ahead.
   static constexpr int QB = D == 64 ? 3 : 2;
-  static constexpr int ST = (14 - QB * NQ * DB) / DB;     // ring slots, 224 KB in all: 3 (kAlt 5) at D = 128, 10 (11) at 64
+  static constexpr int ST = (14 - QB * NQ * DB) / DB;     // ring slots, 224 KB in all: 3 (kAlt 5) at D = 128, 8 (11) at 64
   // Key tiles that Q K^T has taken when P V takes its first one.  The ring holds K_0 .. K_(LK-1), then V_T, K_(T+LK) for
   // every T: the order on the tensor pipe.
   static constexpr int LK = kAlt ? NB : NB - 1;
