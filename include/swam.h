@@ -218,6 +218,115 @@ typedef struct {
 int swam_prefix_attn_scratch_bytes(swam_ctx* ctx, const swam_prefix_args* args, size_t* bytes);
 int swam_prefix_attn(swam_ctx* ctx, const swam_prefix_args* args, void* stream);
 
+/* (7) The history of a sample in pages, with what fills it and what reads it (no counterpart in the paper: its backbones keep the keys
+ * and values of earlier observations between action chunks).  Element type, query heads, head dim and softmax scale are the
+ * context's; the number of samples is the call's own.  All calls only enqueue kernels and can be captured in a CUDA graph; a
+ * workspace must be bound (it holds the status word).  Strides are in elements, 0 = contiguous, multiples of 16 bytes, at
+ * most 2^38; pointers are 16-byte aligned (int32 and float arrays 4-byte, weights 16-byte).
+ *
+ * Rotary positions: pair i of the first rot_dim elements of a head turns by freq[i] radians per position along component
+ * axis[i] of the token's position:  (a, b) -> magnitude * (a cos - b sin, b cos + a sin).  Pairs are (i, i + rot_dim / 2), or
+ * (2i, 2i + 1) when interleaved.  The angle of any int32 position is reduced exactly (64-bit fixed point), so that far
+ * positions lose nothing.  Frequencies stretched for longer contexts are just other values of freq (and magnitude). */
+typedef struct {
+  const double* freq;   /* host, [rot_dim / 2], finite, |freq| <= 2^20; read during the call */
+  const int32_t* axis;  /* host, [rot_dim / 2] in [0, n_axes), or NULL: component 0 */
+  int32_t rot_dim;      /* even, 2 .. head_dim */
+  int32_t n_axes;       /* components of a position, 1 .. 8 */
+  int32_t interleaved;
+  float magnitude;      /* 0 => 1 */
+} swam_rope;
+
+/* swam_norm_rope: q and k as a projection writes them -> q and k as calls (1) to (6) expect them, in one pass.
+ *   x' = x / sqrt(mean(x^2) + eps) * weight over the head dim (where the weight is given), then the rotation (where rope is given),
+ * in fp32, rounded once.  q, q_out: [B, n, N_h, D]; k, k_out: [B, n, n_kv_heads, D]; q or k may be NULL (with its output).
+ * The heads of a token are contiguous.  An output may be its own input (same pointer and strides), and must not overlap an
+ * input otherwise (refused where that is certain).  q_weight, k_weight: dev float [D] or NULL (no norm).
+ * positions: dev int32 [B, n, n_axes], pos_sample elements from one sample's to the next (0: all samples share one
+ * [n, n_axes]); NULL: token t is at position t on every axis.  n_kv_heads: 0 = the context's.
+ * Limits: n at most 2^29, B * n * N_h at most 2^30 (SWAM_ERR_UNSUPPORTED beyond). */
+typedef struct {
+  const swam_rope* rope; /* host, or NULL: no rotation */
+  const void* q;
+  const void* k;
+  void* q_out;
+  void* k_out;
+  const float* q_weight;
+  const float* k_weight;
+  const int32_t* positions;
+  int32_t n, n_kv_heads;
+  float eps;
+  int32_t reserved; /* 0 */
+  int64_t pos_sample, q_token, q_sample, k_token, k_sample, q_out_token, q_out_sample, k_out_token, k_out_sample;
+} swam_norm_rope_args;
+int swam_norm_rope(swam_ctx* ctx, const swam_norm_rope_args* args, void* stream);
+
+/* A paged cache as both calls below see it.  Token c of sample b is row c % page_size of page page_table[b][c / page_size].  The
+ * call's n_tokens new tokens (packed, [n_tokens, heads, D]) belong to the samples in order: sample b owns the tokens
+ * [q_start[b], q_start[b + 1]), which are the last ones of its kv_len[b] tokens, new ones included; both calls of a step take
+ * the same kv_len.  Without q_start every sample has n_tokens / n_samples.  Tokens in front of q_start[0] and behind
+ * q_start[n_samples] are nobody's: nothing is done with them and their rows of any output stay as they are.
+ * On the device: a q_start that is out of order, out of range or gives a sample more than max_q tokens leaves that sample out; a
+ * kv_len outside [0, max_kv] is clamped; a page number outside [0, n_pages) that is needed reads as zeros and is not
+ * written; swam_check reports all of them (SWAM_ERR_DEVICE_CHECK).  Table entries behind a sample's last page are not used,
+ * and neither is what a page holds behind its sample's last token.  Samples may share pages that no call writes. */
+typedef struct {
+  void* k;                   /* dev [n_pages, page_size, n_kv_heads, D]; the heads of a token are contiguous */
+  void* v;
+  const int32_t* page_table; /* dev [n_samples, max_pages], table_sample elements from one row to the next (0: max_pages) */
+  const int32_t* kv_len;     /* dev [n_samples] */
+  const int32_t* q_start;    /* dev [n_samples + 1], or NULL */
+  int32_t n_samples, n_pages;
+  int32_t page_size;         /* a power of two, 16 .. 2^20 */
+  int32_t max_pages;         /* max_pages * page_size at most 2^29 */
+  int32_t n_kv_heads;        /* 0 = the context's; must divide n_heads */
+  int32_t reserved;          /* 0 */
+  int64_t table_sample, k_page, k_token, v_page, v_token;
+} swam_paged_cache;
+
+/* swam_append_kv: writes the new tokens' keys and values to their places in the cache: k normalised and rotated as swam_norm_rope
+ * does, v as it is; and, where q is given, q_out = q normalised and rotated, for the swam_paged_attn that follows.
+ * q, q_out: [n_tokens, N_h, D]; k, v: [n_tokens, n_kv_heads, D].  positions: dev int32 [n_tokens, n_axes] or NULL: a token's
+ * number in its sample (kv_len[b] - new tokens + i) on every axis.  A token whose number is outside [0, max_pages * page_size) is
+ * not written and reported.  Two new tokens with one place in the cache: either may stay.
+ * Limits: n_tokens * N_h at most 2^30 (SWAM_ERR_UNSUPPORTED beyond). */
+typedef struct {
+  const swam_paged_cache* cache; /* host */
+  const swam_rope* rope;         /* host, or NULL: no rotation */
+  const void* q;
+  const void* k;
+  const void* v;
+  void* q_out;
+  const float* q_weight;
+  const float* k_weight;
+  const int32_t* positions;
+  int32_t n_tokens;
+  float eps;
+  int64_t q_token, k_token, v_token, q_out_token;
+} swam_append_args;
+int swam_append_kv(swam_ctx* ctx, const swam_append_args* args, void* stream);
+
+/* swam_paged_attn: the new tokens attend their sample's cache.  Token i of the n of sample b sees the keys [0, kv_len[b]), with
+ * causal != 0 the keys [0, kv_len[b] - n + i + 1); results, special values and precision as in (6).
+ * q, out: [n_tokens, N_h, D]; lse: dev float [N_h, n_tokens] or NULL; out must not overlap q or the cache.
+ * max_q: no sample has more new tokens (0: n_tokens; without q_start n_tokens / n_samples); max_kv: no kv_len is larger (0: max_pages *
+ * page_size).  They choose the kernel and how the keys are cut, so close bounds pay.
+ * scratch: device memory of swam_paged_attn_scratch_bytes (256-byte aligned, NULL if 0), as in (6): the size depends on the
+ * sizes in the arguments only, and calls that may overlap need scratch of their own.  SWAM_OPT_ATTN_VARIANT applies.
+ * Limits: n_tokens * N_h at most 2^30, n_samples at most 2^20 (SWAM_ERR_UNSUPPORTED beyond). */
+typedef struct {
+  const swam_paged_cache* cache; /* host */
+  const void* q;
+  void* out;
+  float* lse;
+  void* scratch;
+  size_t scratch_bytes;
+  int32_t n_tokens, max_q, max_kv, causal;
+  int64_t q_token, out_token;
+} swam_paged_args;
+int swam_paged_attn_scratch_bytes(swam_ctx* ctx, const swam_paged_args* args, size_t* bytes);
+int swam_paged_attn(swam_ctx* ctx, const swam_paged_args* args, void* stream);
+
 /* One denoising step (Sec. 4.2).  q, k, v, out: dev [B, L, N_h, D]; out persists across steps and holds the
  * last full step's result on omitted rows.  mode: SWAM_REFRESH_FULL runs dense attention into out, scores the
  * future tokens with the dense pass's action-row normalisers, selects and builds the maps; SWAM_REUSE packs by

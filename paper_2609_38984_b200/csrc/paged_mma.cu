@@ -1,0 +1,579 @@
+// Attention of few new tokens to paged keys, bf16, on warp-level matrix instructions: the kernel for single tokens and short chunks, for
+// head dim 32, and the independent second opinion on the tcgen05 kernel.
+//
+// The new tokens' rows of a sample and key/value head, in the order (token, head of the group), are cut into row tiles of 16 * WR
+// rows.  A unit of work is a tile of 64 keys of a row tile, in the order (sample, key/value head, row tile, key tile); `shares` CTAs
+// own equal stretches of that sequence, so that samples of any lengths load the SMs evenly.  Lengths are on the device: every
+// CTA adds up the samples' units and finds its own first one.  A CTA keeps one pipeline of TMA loads running over the borders of its
+// row tiles; keys arrive page by page through the table, into the layout that seg_mma.cuh describes.
+// A row tile that one CTA holds as a whole is finished there.  One that is cut leaves an unnormalised fp32 piece per CTA, which a second
+// kernel joins: the block with the number of the CTA that holds the first piece.  A CTA has two pieces at most (it may end one row tile
+// and begin another), so the scratch does not depend on the lengths.
+// Inside a CTA, WR warps lie along the rows and WK along the keys, each with its own running maximum and sum (WR * WK = 4); they are
+// merged once per row tile, through the ring stage that was read last.
+// Rows of V behind the last key become zeros in shared memory, so whatever a page holds there (NaN included) never meets a product.
+// Scores, maxima, sums and outputs are fp32; the probabilities are rounded to bf16 for the second product (the operand type of
+// the matrix instruction; half a step, 2^-8, of each weight).
+#include <string.h>
+
+#include "seg_maps.cuh"
+#include "seg_mma.cuh"
+
+namespace swam {
+namespace {
+
+constexpr int kKT = 64;                // keys per tile
+constexpr int kThreadsP = 128;
+constexpr int kCtasPerSm = 2;
+constexpr int kMinUnits = 2;           // key tiles that a share has at least, where row tiles may be cut
+
+template <int D, int WR>
+struct PagedCfg {
+  static constexpr int WK = 4 / WR, MR = 16 * WR, KW = kKT / WK;
+  static constexpr int kTileB = kKT * D * 2;
+  static constexpr int kStages = D == 128 ? 3 : (D == 64 ? 6 : 8);       // 96 KB (64 at head dim 32): two CTAs an SM
+  static constexpr int kRing = kStages * 2 * kTileB;
+  static constexpr int kBytes = kRing + 1024 /*alignment*/ + 8 * kStages + 64 * 8 /*maxima and sums of the warps*/;
+};
+
+// A stretch of the sequence of units.  [t, t_end) are the key tiles of the current row tile that belong to it.
+struct Walk {
+  int64_t left;            // units behind the current piece
+  int b, h, r;             // sample, key/value head, row tile
+  int rt;                  // row tiles of the sample and head
+  int t, t_end, tiles;     // tiles: of the whole row tile
+  PagedSample s;
+};
+
+struct Place {
+  int64_t offset;          // units of the sample in front of the share's first one
+  int b;
+};
+
+template <int MR>
+__device__ __forceinline__ int row_tiles(const PagedSample& s, int g) { return (s.n * g + MR - 1) / MR; }
+template <int MR>
+__device__ __forceinline__ int key_tiles(const SegParams& p, const PagedSample& s, int r) {
+  const int last = min((r + 1) * MR, s.n * p.g) - 1;
+  return (paged_limit(p.a.causal, s, last / p.g) + kKT - 1) / kKT;
+}
+// units of one key/value head (a row tile without keys still has its zeros to write)
+template <int MR>
+__device__ __forceinline__ int64_t head_units(const SegParams& p, const PagedSample& s) {
+  const int rt = row_tiles<MR>(s, p.g);
+  if (!p.a.causal) return (int64_t)rt * max(1, (s.len + kKT - 1) / kKT);
+  int64_t u = 0;
+  for (int r = 0; r < rt; ++r) u += max(1, key_tiles<MR>(p, s, r));
+  return u;
+}
+
+// first unit of share c of `shares` equal ones of `total`; the share that holds unit u
+__device__ __forceinline__ int64_t share_begin(int64_t total, int shares, int c) {
+  const int64_t per = total / shares, more = total % shares;
+  return c * per + min((int64_t)c, more);
+}
+__device__ __forceinline__ int share_of(int64_t total, int shares, int64_t u) {
+  const int64_t per = total / shares, more = total % shares, big = more * (per + 1);
+  return (int)(u < big ? u / (per + 1) : more + (u - big) / per);
+}
+
+template <int D, int WR>
+__global__ void __launch_bounds__(kThreadsP, kCtasPerSm)
+paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ SegParams p,
+                 const __grid_constant__ PagedCache pc, const bool cut, int4* join) {
+  using C = PagedCfg<D, WR>;
+  constexpr int MR = C::MR, WK = C::WK, KW = C::KW, kStages = C::kStages, kTileB = C::kTileB;
+  constexpr int CPR = D / 8;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ int64_t warp_sum[4];
+  __shared__ Place place;
+  __shared__ int abort_flag;
+  const uint32_t s0 = (smem_addr(smem_raw) + 1023u) & ~1023u;
+  unsigned char* base = smem_raw + (s0 - smem_addr(smem_raw));
+  const uint32_t bars = s0 + C::kRing;
+  float2* ml = reinterpret_cast<float2*>(base + C::kRing + 8 * kStages);       // [WK][MR]
+  const SegArgs& a = p.a;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(bars + 8 * i, 1);
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (cut) join[blockIdx.x] = make_int4(0, 0, 0, 0);
+  }
+
+  // ---- the share of this CTA: add up the units, then find the sample of its first one
+  int64_t mine0 = 0, sum = 0;
+  for (int b0 = 0; b0 < pc.samples; b0 += kThreadsP) {
+    const int b = b0 + threadIdx.x;
+    const int64_t u = b < pc.samples ? head_units<MR>(p, paged_sample(pc, a.n_q, b, p.status)) * a.N_kv : 0;
+    if (b0 == 0) mine0 = u;
+    sum += u;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) warp_sum[warp] = sum;
+  __syncthreads();
+  const int64_t total = warp_sum[0] + warp_sum[1] + warp_sum[2] + warp_sum[3];
+  const int64_t most = cut ? (total + kMinUnits - 1) / kMinUnits : total;
+  const int shares = (int)min((int64_t)gridDim.x, most);
+  if ((int)blockIdx.x >= shares) {
+    allow_next();
+    return;
+  }
+  const int64_t u0 = share_begin(total, shares, blockIdx.x), u1 = share_begin(total, shares, blockIdx.x + 1);
+  int64_t before = 0;
+  for (int b0 = 0; b0 < pc.samples && before <= u0; b0 += kThreadsP) {
+    const int b = b0 + threadIdx.x;
+    const int64_t u = b0 == 0 ? mine0 : (b < pc.samples ? head_units<MR>(p, paged_sample(pc, a.n_q, b, p.status)) * a.N_kv : 0);
+    int64_t end = u;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, end, o);
+      if (lane >= o) end += y;
+    }
+    __syncthreads();
+    if (lane == 31) warp_sum[warp] = end;
+    __syncthreads();
+    for (int w = 0; w < 4; ++w) {
+      if (w < warp) end += warp_sum[w];
+    }
+    end += before;
+    if (u0 >= end - u && u0 < end) place = Place{u0 - (end - u), b};
+    before += warp_sum[0] + warp_sum[1] + warp_sum[2] + warp_sum[3];
+  }
+  __syncthreads();
+
+  // makes the current row tile's part of the stretch: from tile t on, as far as `left` reaches
+  auto take = [&](Walk& w) {
+    w.tiles = key_tiles<MR>(p, w.s, w.r);
+    const int units = max(1, w.tiles);
+    const int64_t n = cut ? min((int64_t)(units - w.t), w.left) : units;
+    w.left -= n;
+    w.t_end = w.tiles == 0 ? 0 : w.t + (int)n;
+  };
+  // the next row tile; false at the end of the stretch
+  auto next = [&](Walk& w) {
+    if (w.left <= 0) return false;
+    w.t = 0;
+    if (++w.r == w.rt) {
+      w.r = 0;
+      if (++w.h == a.N_kv) {
+        w.h = 0;
+        do {
+          if (++w.b >= pc.samples) return false;
+          w.s = paged_sample(pc, a.n_q, w.b, p.status);
+        } while (w.s.n == 0);
+        w.rt = row_tiles<MR>(w.s, p.g);
+      }
+    }
+    take(w);
+    return true;
+  };
+  Walk w;
+  bool more = true;
+  {
+    w.left = u1 - u0;
+    w.b = place.b;
+    w.s = paged_sample(pc, a.n_q, w.b, p.status);
+    w.rt = row_tiles<MR>(w.s, p.g);
+    const int64_t units = head_units<MR>(p, w.s);
+    w.h = (int)(place.offset / units);
+    int64_t off = place.offset - w.h * units;
+    w.r = 0;
+    if (!a.causal) {
+      const int each = max(1, (w.s.len + kKT - 1) / kKT);
+      w.r = (int)(off / each);
+      off -= (int64_t)w.r * each;
+    } else {
+      for (int n; off >= (n = max(1, key_tiles<MR>(p, w.s, w.r))); ++w.r) off -= n;
+    }
+    w.t = (int)off;
+    if (!cut && w.t > 0) {
+      // a row tile belongs to the share that holds its first unit
+      w.left -= max(1, key_tiles<MR>(p, w.s, w.r)) - w.t;
+      more = next(w);
+    } else {
+      take(w);
+    }
+  }
+
+  // ---- loads (warp 0): ahead of the products by kStages - 1 tiles
+  constexpr int DB = D == 32 ? 1 : D / 64, kCols = D == 32 ? 32 : 64, kColB = kCols * 2;       // boxes per row of a tile, their columns and bytes
+  Walk lw = w;
+  bool lmore = more;
+  int issued = 0;
+  PageWindow pages;
+  auto load_next = [&]() {
+    while (lmore && lw.t >= lw.t_end) lmore = next(lw);
+    if (!lmore) return;
+    const int key0 = lw.t * kKT, sh = pc.page_shift, first = key0 >> sh;
+    const int last = min((lw.r + 1) * MR, lw.s.n * p.g) - 1;
+    const int keys = paged_limit(a.causal, lw.s, last / p.g) - key0;
+    const int count = sh >= 6 ? 1 : min(kKT >> sh, (keys + (1 << sh) - 1) >> sh), rows = min(kKT, 1 << sh);
+    const int page = pages.get(pc, lw.b, first, lane < count ? lane : 0);
+    const int st = issued % kStages;
+    const uint32_t ks = s0 + (uint32_t)st * 2 * kTileB, bar = bars + 8 * st;
+    if (lane == 0) mbar_expect_tx(bar, 2 * count * rows * D * 2);
+    __syncwarp();
+    if (lane < count) {
+      const int at = paged_page(pc, page, p.status);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const uint32_t dst = ks + db * kKT * kColB + lane * rows * kColB;
+        tma_load_4d(dst, &map_k, bar, db * kCols, key0 & ((1 << sh) - 1), lw.h, at);
+        tma_load_4d(dst + kTileB, &map_v, bar, db * kCols, key0 & ((1 << sh) - 1), lw.h, at);
+      }
+    }
+    __syncwarp();
+    ++issued;
+    ++lw.t;
+  };
+  if (warp == 0)
+    for (int i = 0; i < kStages - 1; ++i) load_next();
+
+  const int wr = warp % WR, wk = warp / WR;
+  int cnt = 0;                                     // key tiles so far
+  bool ok = true;
+  for (; more; more = next(w)) {
+    const int row0 = (w.s.q0 * p.g) + w.r * MR;    // first row, counted from the call's first token
+    const int row_end = (w.s.q0 + w.s.n) * p.g;
+    const int t0 = w.t;
+    const bool whole = t0 == 0 && w.t_end == w.tiles;
+    const int last = min((w.r + 1) * MR, w.s.n * p.g) - 1;
+    const int len = paged_limit(a.causal, w.s, last / p.g);
+    // this thread's two rows (accumulator rows lane / 4 and lane / 4 + 8 of the warp's 16), their queries as A fragments
+    uint32_t qf[D / 16][4];
+    int lim[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = row0 + wr * 16 + (lane >> 2) + 8 * i;
+      const bool real = row < row_end;
+      const int tok = real ? row / p.g : 0, h = w.h * p.g + (real ? row - tok * p.g : 0);
+      lim[i] = real ? paged_limit(a.causal, w.s, tok - w.s.q0) : 0;
+      const uint32_t* src = reinterpret_cast<const uint32_t*>((const __nv_bfloat16*)a.q + tok * a.q_tok + (int64_t)h * D);
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        qf[ks][i] = real ? src[ks * 8 + (lane & 3)] : 0u;
+        qf[ks][i + 2] = real ? src[ks * 8 + 4 + (lane & 3)] : 0u;
+      }
+    }
+    float o[D / 8][4];
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    bool big = false;                              // some row's reference is large: see kSegBig
+
+    for (int t = t0; t < w.t_end; ++t, ++cnt) {
+      const int st = cnt % kStages;
+      ok = mbar_wait(bars + 8 * st, (cnt / kStages) & 1, &abort_flag);
+      ok = __syncthreads_and(ok ? 1 : 0);          // (and every warp is through with the tile before)
+      if (!ok) break;
+      if (warp == 0) load_next();
+      const int key0 = t * kKT + wk * KW;          // first key of this warp
+      const uint32_t ks = s0 + (uint32_t)st * 2 * kTileB, vs = ks + kTileB;
+      const int real = len - t * kKT;              // real keys of this tile
+      if (real < kKT) {
+        for (int i = threadIdx.x; i < (kKT - real) * CPR; i += kThreadsP)
+          st_shared_16(vs + tile_off<D, kKT>(real + i / CPR, i % CPR), 0u, 0u, 0u, 0u);
+        fence_proxy_async();                       // the stage's next load comes through the other proxy
+        __syncthreads();
+      }
+      if (key0 >= len) continue;                   // none of this warp's keys is real
+
+      float sc[KW / 8][4];
+#pragma unroll
+      for (int nb = 0; nb < KW / 16; ++nb) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[2 * nb][e] = sc[2 * nb + 1][e] = 0.f;
+#pragma unroll
+        for (int kd = 0; kd < D / 16; ++kd) {
+          uint32_t f[4];
+          ldsm4(f, ks + tile_off<D, kKT>(wk * KW + nb * 16 + (lane & 7) + ((lane >> 4) << 3), kd * 2 + ((lane >> 3) & 1)));
+          mma_bf16(sc[2 * nb], qf[kd], f[0], f[1]);
+          mma_bf16(sc[2 * nb + 1], qf[kd], f[2], f[3]);
+        }
+      }
+      const int v0 = lim[0] - key0, v1 = lim[1] - key0;       // keys of the warp's range that the rows see
+      if (min(v0, v1) < KW) {
+#pragma unroll
+        for (int nb = 0; nb < KW / 8; ++nb) {
+          const int c = nb * 8 + (lane & 3) * 2;
+          if (c >= v0) sc[nb][0] = -INFINITY;
+          if (c + 1 >= v0) sc[nb][1] = -INFINITY;
+          if (c >= v1) sc[nb][2] = -INFINITY;
+          if (c + 1 >= v1) sc[nb][3] = -INFINITY;
+        }
+      }
+      float corr[2], ref[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int nb = 0; nb < KW / 8; ++nb) mx = fmaxf(mx, fmaxf(sc[nb][2 * i], sc[nb][2 * i + 1]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        const float mn = fmaxf(m[i], mx * p.scale_log2);
+        ref[i] = mn == -INFINITY ? 0.f : mn;       // a row that has seen no key yet: every exponent stays -inf
+        corr[i] = ex2(m[i] - ref[i]);
+        m[i] = mn;
+        l[i] *= corr[i];
+      }
+      const bool moved = __any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f);       // rare after the first tiles
+      if (moved) big = __any_sync(0xffffffffu, !(fmaxf(fabsf(ref[0]), fabsf(ref[1])) < kSegBig));
+      float scale = p.scale_log2;
+      if (big) {
+        scale = 1.f;
+#pragma unroll
+        for (int nb = 0; nb < KW / 8; ++nb) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[nb][e] *= p.scale_log2;
+        }
+      }
+#pragma unroll
+      for (int nb = 0; nb < KW / 8; ++nb) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sc[nb][e] = ex2(fmaf(sc[nb][e], scale, -ref[e >> 1]));
+          l[e >> 1] += sc[nb][e];
+        }
+      }
+      if (moved) {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          o[i][0] *= corr[0];
+          o[i][1] *= corr[0];
+          o[i][2] *= corr[1];
+          o[i][3] *= corr[1];
+        }
+      }
+#pragma unroll
+      for (int nb = 0; nb < KW / 16; ++nb) {
+        const uint32_t pf[4] = {pack_bf16x2(sc[2 * nb][0], sc[2 * nb][1]), pack_bf16x2(sc[2 * nb][2], sc[2 * nb][3]),
+                                pack_bf16x2(sc[2 * nb + 1][0], sc[2 * nb + 1][1]), pack_bf16x2(sc[2 * nb + 1][2], sc[2 * nb + 1][3])};
+#pragma unroll
+        for (int dn = 0; dn < D / 16; ++dn) {
+          uint32_t f[4];
+          ldsm4_t(f, vs + tile_off<D, kKT>(wk * KW + nb * 16 + (lane & 7) + (((lane >> 3) & 1) << 3), dn * 2 + (lane >> 4)));
+          mma_bf16(o[2 * dn], pf, f[0], f[1]);
+          mma_bf16(o[2 * dn + 1], pf, f[2], f[3]);
+        }
+      }
+    }
+    if (!ok) break;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+    }
+
+    // ---- the row tile's result.  The warps of a row are merged through the ring stage that was read last, which nobody loads into
+    // before the next tile's barrier; every warp takes 1 / WK of the columns.  (A row tile without keys has nothing to merge.)
+    constexpr int NB = D / 8 / WK;                 // 8-column blocks of a warp
+    float out[NB][4], mm[2], ll[2];
+    if (WK > 1 && w.tiles > 0) {
+      float4* frag = reinterpret_cast<float4*>(base + (size_t)((cnt - 1) % kStages) * 2 * kTileB);       // [warp][D / 8][lane]
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) frag[(warp * (D / 8) + i) * 32 + lane] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+      if ((lane & 3) == 0) {
+        ml[wk * MR + wr * 16 + (lane >> 2)] = make_float2(m[0], l[0]);
+        ml[wk * MR + wr * 16 + (lane >> 2) + 8] = make_float2(m[1], l[1]);
+      }
+      __syncthreads();
+      float f[WK][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = wr * 16 + (lane >> 2) + 8 * i;
+        mm[i] = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < WK; ++k) mm[i] = fmaxf(mm[i], ml[k * MR + r].x);
+        ll[i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < WK; ++k) {
+          const float2 x = ml[k * MR + r];
+          f[k][i] = mm[i] == -INFINITY ? 0.f : exp2f(x.x - mm[i]);
+          ll[i] += f[k][i] * x.y;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        out[i][0] = out[i][1] = out[i][2] = out[i][3] = 0.f;
+#pragma unroll
+        for (int k = 0; k < WK; ++k) {
+          const float4 x = frag[((k * WR + wr) * (D / 8) + wk * NB + i) * 32 + lane];
+          out[i][0] += f[k][0] * x.x;
+          out[i][1] += f[k][0] * x.y;
+          out[i][2] += f[k][1] * x.z;
+          out[i][3] += f[k][1] * x.w;
+        }
+      }
+      fence_proxy_async();                         // the stage's next load comes through the other proxy
+    } else {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[i][e] = WK > 1 ? 0.f : o[i][e];      // (WK > 1: no keys)
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        mm[i] = m[i];
+        ll[i] = l[i];
+      }
+    }
+    const int slot = (int)blockIdx.x * 2 + (t0 == 0 ? 1 : 0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = wr * 16 + (lane >> 2) + 8 * i, row = row0 + r;
+      if (row >= row_end) continue;
+      const int tok = row / p.g, h = w.h * p.g + row - tok * p.g;
+      const int c = wk * NB * 8 + (lane & 3) * 2;
+      if (whole) {
+        const float inv = seg_inverse(ll[i]);
+        uint32_t* dst = reinterpret_cast<uint32_t*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + c);
+#pragma unroll
+        for (int k = 0; k < NB; ++k) dst[k * 4] = pack_bf16x2(out[k][2 * i] * inv, out[k][2 * i + 1] * inv);
+        if (a.lse && wk == 0 && (lane & 3) == 0) a.lse[(int64_t)h * a.n_q + tok] = seg_lse(mm[i], ll[i]);
+      } else {
+        float* dst = p.part_o + ((int64_t)slot * MR + r) * D + c;
+#pragma unroll
+        for (int k = 0; k < NB; ++k) *reinterpret_cast<float2*>(dst + k * 8) = make_float2(out[k][2 * i], out[k][2 * i + 1]);
+        if (wk == 0 && (lane & 3) == 0) p.part_ml[slot * MR + r] = make_float2(mm[i], ll[i]);
+      }
+    }
+    if (!whole && t0 == 0 && threadIdx.x == 0) {
+      // this is the first piece of a row tile that goes on in the next shares (left = 0: u1 is the unit behind this piece)
+      const int pieces = share_of(total, shares, u1 + (w.tiles - w.t_end) - 1) - (int)blockIdx.x + 1;
+      join[blockIdx.x] = make_int4(row0, min(row0 + MR, row_end), w.h, pieces);
+    }
+  }
+  allow_next();
+  if (!ok) {
+    if (threadIdx.x == 0) atomicOr(p.status, ST_TIMEOUT);
+    if (warp == 0) drain_loads(bars, kStages, issued);       // copies in flight must not outlive the CTA
+    __syncthreads();
+  }
+}
+
+// Joins the pieces of one row tile: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i, pieces in order.
+template <int D, int MR>
+__global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ SegParams p, const int4* join) {
+  __shared__ float2 row_ml[MR];
+  __shared__ float4 part[256];
+  const SegArgs& a = p.a;
+  wait_previous();
+  const int4 j = join[blockIdx.x];
+  const int pieces = j.w, rows = j.y - j.x;
+  if (pieces <= 1) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int first = (int)blockIdx.x;                         // piece 0 in its second slot, piece i in the first slot of share first + i
+  auto slot = [&](int i) { return i == 0 ? first * 2 + 1 : (first + i) * 2; };
+  for (int r = warp; r < rows; r += 8) {
+    float m = -INFINITY, l = 0.f;
+    for (int i = lane; i < pieces; i += 32) {
+      const float2 x = p.part_ml[slot(i) * MR + r];
+      const float mn = fmaxf(m, x.x);
+      if (mn != -INFINITY) l = l * exp2f(m - mn) + x.y * exp2f(x.x - mn);
+      m = mn;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
+      const float mn = fmaxf(m, m2);
+      // (both lanes of a pair form the same sum)
+      if (mn != -INFINITY) l = l * exp2f(m - mn) + l2 * exp2f(m2 - mn);
+      m = mn;
+    }
+    if (lane == 0) row_ml[r] = make_float2(m, l);
+  }
+  __syncthreads();
+  constexpr int V = D / 4;
+  const int items = rows * V, groups = items >= 256 ? 1 : 256 / items;
+  for (int x0 = 0; x0 < items; x0 += 256) {
+    const int x = x0 + (int)threadIdx.x;
+    const int grp = groups > 1 ? x / items : 0, item = x - grp * items;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const bool on = groups > 1 ? grp < groups : x < items;
+    if (on) {
+      const int r = item / V, c = (item - r * V) * 4;
+      const float m = row_ml[r].x;
+#pragma unroll 4
+      for (int i = grp; i < pieces; i += groups) {
+        const float mi = p.part_ml[slot(i) * MR + r].x;
+        const float4 v = *reinterpret_cast<const float4*>(p.part_o + ((int64_t)slot(i) * MR + r) * D + c);
+        const float f = mi == -INFINITY ? 0.f : exp2f(mi - m);
+        if (f != 0.f) {
+          acc.x = fmaf(f, v.x, acc.x);
+          acc.y = fmaf(f, v.y, acc.y);
+          acc.z = fmaf(f, v.z, acc.z);
+          acc.w = fmaf(f, v.w, acc.w);
+        }
+      }
+    }
+    if (groups > 1) {
+      part[threadIdx.x] = acc;
+      __syncthreads();
+      if ((int)threadIdx.x >= items) break;
+      for (int k = 1; k < groups; ++k) {
+        const float4 y = part[threadIdx.x + k * items];
+        acc.x += y.x;
+        acc.y += y.y;
+        acc.z += y.z;
+        acc.w += y.w;
+      }
+    }
+    if (x < items) {
+      const int r = x / V, c = (x - r * V) * 4, row = j.x + r, tok = row / p.g, h = j.z * p.g + row - tok * p.g;
+      const float2 s = row_ml[r];
+      const float inv = seg_inverse(s.y);
+      *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + c) =
+          make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+      if (a.lse && c == 0) a.lse[(int64_t)h * a.n_q + tok] = seg_lse(s.x, s.y);
+    }
+  }
+}
+
+template <int D, int WR>
+cudaError_t launch_one(const SegParams& p0, const PagedCache& c, int shares, bool cut, cudaStream_t st, int* launches) {
+  using C = PagedCfg<D, WR>;
+  SegParams p = p0;
+  const SegArgs& a = p.a;
+  // scratch: outputs, maxima and sums of two pieces per share, and the join's description
+  p.part_ml = (float2*)(p.part_o + (size_t)shares * 2 * C::MR * D);
+  int4* join = (int4*)(p.part_ml + (size_t)shares * 2 * C::MR);
+  CUtensorMap mk, mv;
+  const int page = 1 << c.page_shift, rows = page < kKT ? page : kKT;
+  if (!make_kv_map(&mk, a.k[1], c.n_pages, page, a.N_kv, D, c.k_tok, c.k_page, rows) ||
+      !make_kv_map(&mv, a.v[1], c.n_pages, page, a.N_kv, D, c.v_tok, c.v_page, rows))
+    return cudaErrorInvalidValue;
+  static SmemOptIn opt_in;
+  cudaError_t e = opt_in((const void*)paged_mma_kernel<D, WR>, C::kBytes, a.device);
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  paged_mma_kernel<D, WR><<<shares, kThreadsP, C::kBytes, st>>>(mk, mv, p, c, cut, join);
+  e = cudaGetLastError();
+  if (e != cudaSuccess || !cut) return e;
+  ++*launches;
+  return launch_after(paged_join_kernel<D, C::MR>, dim3(shares), dim3(256), 0, st, p, (const int4*)join);
+}
+template <int D>
+cudaError_t launch_rows(const SegParams& p, const PagedCache& c, int rows, int shares, bool cut, cudaStream_t st, int* launches) {
+  return rows == 16 ? launch_one<D, 1>(p, c, shares, cut, st, launches)
+                    : (rows == 32 ? launch_one<D, 2>(p, c, shares, cut, st, launches) : launch_one<D, 4>(p, c, shares, cut, st, launches));
+}
+
+}  // namespace
+
+int paged_mma_shares(int sms) { return kCtasPerSm * sms; }
+size_t paged_mma_scratch(int shares, int tile_rows, int D) {
+  return (size_t)shares * (2 * tile_rows * ((size_t)D * sizeof(float) + sizeof(float2)) + sizeof(int4));
+}
+cudaError_t launch_paged_mma(const SegParams& p, const PagedCache& c, int tile_rows, int shares, bool cut, cudaStream_t st, int* launches) {
+  switch (p.a.D) {
+    case 32: return launch_rows<32>(p, c, tile_rows, shares, cut, st, launches);
+    case 64: return launch_rows<64>(p, c, tile_rows, shares, cut, st, launches);
+    case 128: return launch_rows<128>(p, c, tile_rows, shares, cut, st, launches);
+    default: return cudaErrorInvalidConfiguration;
+  }
+}
+
+}  // namespace swam

@@ -2,6 +2,8 @@
 //
 // Partial results of the pieces i of a row are merged exactly: with reference maxima m_i, sums l_i and unnormalised
 // outputs o_i, m = max m_i, out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i, lse = ln 2 (m + log2 sum).
+#include <string.h>
+
 #include "seg_attn.cuh"
 
 namespace swam {
@@ -12,8 +14,10 @@ constexpr int64_t kMaxItemKeys = 1 << 26;
 
 // One warp per row; lanes hold the pieces' weights and then D / 32 output columns each.  The first pieces' outputs are
 // requested before the weights are known (an output of weight 0 may never have been written and is not used).
-template <int D, typename T, int kMergeBatch>
-__global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ SegParams p, const int parts) {
+// kPaged: the tokens in front of the first sample and behind the last one are nobody's.
+template <int D, typename T, int kMergeBatch, bool kPaged>
+__global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ SegParams p, const int parts,
+                                                        const __grid_constant__ CacheArg<kPaged> pc) {
   constexpr int CPL = D / 32;
   const int lane = threadIdx.x & 31;
   const uint32_t row = blockIdx.x * 4 + (threadIdx.x >> 5);           // (sample, query, head)
@@ -24,6 +28,9 @@ __global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ 
   const float2* ml = p.part_ml + row;
   wait_previous();                                                    // everything above ran beside the last pieces
   if (row >= p.rows) return;
+  if constexpr (kPaged) {
+    if (pc.q_start && ((int)bt < __ldg(pc.q_start) || (int)bt >= __ldg(pc.q_start + pc.samples))) return;
+  }
   float v[kMergeBatch][CPL];
   auto load = [&](int i0) {
 #pragma unroll
@@ -81,20 +88,20 @@ __global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ 
   if (a.lse && lane == 0) a.lse[((int64_t)b * a.N_h + h) * a.n_q + t] = seg_lse(m, l);
 }
 
-template <int D, typename T>
-cudaError_t launch_merge_d(const SegParams& p, int parts, cudaStream_t st, int* launches) {
+template <int D, typename T, bool kPaged>
+cudaError_t launch_merge_d(const SegParams& p, int parts, const CacheArg<kPaged>& c, cudaStream_t st, int* launches) {
   const dim3 grid((unsigned)((p.rows + 3) / 4)), block(128);
   ++*launches;
   // (loads beyond the last piece are repeats of it: two pieces, the usual number of a shared plan, want a batch of their own)
-  if (parts <= 2) return launch_after(seg_merge_kernel<D, T, 2>, grid, block, 0, st, p, parts);
-  return launch_after(seg_merge_kernel<D, T, 8>, grid, block, 0, st, p, parts);
+  if (parts <= 2) return launch_after(seg_merge_kernel<D, T, 2, kPaged>, grid, block, 0, st, p, parts, c);
+  return launch_after(seg_merge_kernel<D, T, 8, kPaged>, grid, block, 0, st, p, parts, c);
 }
-template <typename T>
-cudaError_t launch_merge(const SegParams& p, int parts, cudaStream_t st, int* launches) {
+template <typename T, bool kPaged>
+cudaError_t launch_merge(const SegParams& p, int parts, const CacheArg<kPaged>& c, cudaStream_t st, int* launches) {
   switch (p.a.D) {
-    case 32: return launch_merge_d<32, T>(p, parts, st, launches);
-    case 64: return launch_merge_d<64, T>(p, parts, st, launches);
-    default: return launch_merge_d<128, T>(p, parts, st, launches);
+    case 32: return launch_merge_d<32, T, kPaged>(p, parts, c, st, launches);
+    case 64: return launch_merge_d<64, T, kPaged>(p, parts, c, st, launches);
+    default: return launch_merge_d<128, T, kPaged>(p, parts, c, st, launches);
   }
 }
 
@@ -217,7 +224,83 @@ cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& pl, bool warp_mma, 
     if (e != cudaSuccess) return e;
   }
   if (p.direct) return cudaSuccess;
-  return a.dtype == 0 ? launch_merge<float>(p, pl.parts(), st, launches) : launch_merge<__nv_bfloat16>(p, pl.parts(), st, launches);
+  return a.dtype == 0 ? launch_merge<float, false>(p, pl.parts(), NoCache(), st, launches)
+                      : launch_merge<__nv_bfloat16, false>(p, pl.parts(), NoCache(), st, launches);
+}
+
+// ---- paged keys: the same kernels where the pieces can be planned from sizes, and the warp-level one that shares the keys out on the device
+namespace {
+struct PagedPlan {
+  Kind kind;
+  int tile_rows, splits;     // kF32, kTc
+  int row_tiles;             // at most, per sample and key/value head
+  int64_t items;             // at most
+  int shares;                // kMma: CTAs
+  bool cut;
+};
+PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
+  PagedPlan pl;
+  const int g = a.N_h / a.N_kv;
+  const int64_t rows = (int64_t)c.max_q * g;
+  const PassPlan ps = plan_pass(a, c.samples, rows, c.max_kv, warp_mma, -1);
+  pl.kind = ps.kind;
+  pl.tile_rows = ps.tile_rows;
+  pl.row_tiles = (int)ceil_div(rows, ps.tile_rows);
+  // a sample fills its tiles but for the last one
+  int64_t tiles = (int64_t)a.n_q * g / ps.tile_rows + c.samples;
+  if (tiles > (int64_t)c.samples * pl.row_tiles) tiles = (int64_t)c.samples * pl.row_tiles;
+  int64_t s = 1;
+  if (pl.kind == kTc) {
+    s = a.sms / (tiles * a.N_kv);
+    if (s > c.max_kv / 512) s = c.max_kv / 512;
+    if (s > kMaxSplits) s = kMaxSplits;
+    if (s < ceil_div(c.max_kv, kMaxItemKeys)) s = ceil_div(c.max_kv, kMaxItemKeys);
+    if (s < 1) s = 1;
+  } else if (pl.kind == kF32) {
+    s = ps.splits;
+  }
+  pl.splits = (int)s;
+  pl.items = (pl.kind == kTc ? tiles : (int64_t)c.samples * pl.row_tiles) * a.N_kv * s;
+  pl.shares = paged_mma_shares(a.sms);
+  // A row tile's keys are cut only where they may be many: the second kernel costs more than 512 keys do.
+  pl.cut = c.max_kv > 512;
+  return pl;
+}
+}  // namespace
+
+size_t paged_scratch_bytes(const SegArgs& a, const PagedCache& c, bool warp_mma) {
+  if (a.n_q == 0 || c.samples == 0) return 0;
+  const PagedPlan pl = paged_plan(a, c, warp_mma);
+  if (pl.kind == kMma) return pl.cut ? paged_mma_scratch(pl.shares, pl.tile_rows, a.D) : 0;
+  return pl.splits > 1 ? (size_t)pl.splits * a.n_q * a.N_h * ((size_t)a.D * sizeof(float) + sizeof(float2)) : 0;
+}
+
+cudaError_t launch_paged_attn(const SegArgs& a, const PagedCache& c, bool warp_mma, void* scratch, int* status, cudaStream_t st,
+                              int* launches) {
+  const PagedPlan pl = paged_plan(a, c, warp_mma);
+  SegParams p;
+  memset(&p, 0, sizeof(p));
+  p.a = a;
+  p.g = a.N_h / a.N_kv;
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.rows = (int64_t)a.n_q * a.N_h;
+  p.status = status;
+  p.part_o = (float*)scratch;
+  if (pl.kind == kMma) return launch_paged_mma(p, c, pl.tile_rows, pl.shares, pl.cut, st, launches);
+  p.direct = pl.splits == 1;
+  p.part_ml = (float2*)((float*)scratch + (size_t)pl.splits * p.rows * a.D);
+  SegPass& ps = p.pass[0];
+  ps.seg_lo = ps.seg_hi = 1;
+  ps.block_samples = 1;
+  ps.blocks = c.samples;
+  ps.row_tiles = pl.row_tiles;
+  ps.splits = pl.splits;
+  if (pl.items > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  ps.items = (int)pl.items;
+  const cudaError_t e = pl.kind == kTc ? launch_paged_tc(p, c, pl.tile_rows == 128, st, launches)
+                                       : launch_paged_f32(p, c, pl.tile_rows, st, launches);
+  if (e != cudaSuccess || p.direct) return e;
+  return a.dtype == 0 ? launch_merge<float, true>(p, pl.splits, c, st, launches) : launch_merge<__nv_bfloat16, true>(p, pl.splits, c, st, launches);
 }
 
 }  // namespace swam

@@ -6,6 +6,7 @@
 // on the device, so the pieces are cut there: the real key tiles of an item's block are shared out evenly.
 #pragma once
 #include <atomic>
+#include <type_traits>
 
 #include "swam_internal.cuh"
 
@@ -148,6 +149,65 @@ cudaError_t launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// ---- paged keys: the call's tokens are rows of one sequence for all addresses (B = 1, n_q = tokens), and a sample owns a stretch of them
+struct NoCache {};
+template <bool kPaged>
+using CacheArg = std::conditional_t<kPaged, PagedCache, NoCache>;
+
+// first new token of a sample, how many there are, and the sample's keys
+struct PagedSample {
+  int q0, n, len;
+};
+// A stretch out of order, outside the tokens or longer than max_q counts as empty; lengths out of range are clamped; both are flagged.
+__device__ __forceinline__ PagedSample paged_sample(const PagedCache& c, int tokens, int b, int* status) {
+  PagedSample s;
+  int q1;
+  if (c.q_start) {
+    s.q0 = __ldg(c.q_start + b);
+    q1 = __ldg(c.q_start + b + 1);
+  } else {
+    s.q0 = b * c.max_q;
+    q1 = s.q0 + c.max_q;
+  }
+  const int len = __ldg(c.kv_len + b);
+  const bool stretch = s.q0 >= 0 && s.q0 <= q1 && q1 <= tokens && q1 - s.q0 <= c.max_q;
+  s.n = stretch ? q1 - s.q0 : 0;
+  s.len = min(max(len, 0), c.max_kv);
+  if (!stretch || s.len != len) atomicOr(status, ST_BAD_LEN);
+  return s;
+}
+// keys that the i-th new token sees
+__device__ __forceinline__ int paged_limit(int causal, const PagedSample& s, int i) { return causal ? max(0, s.len - s.n + i + 1) : s.len; }
+// A page number as a coordinate of the cache's tensor maps: one that does not exist becomes the first behind the last, which reads as
+// zeros.
+__device__ __forceinline__ int paged_page(const PagedCache& c, int page, int* status) {
+  if (page >= 0 && page < c.n_pages) return page;
+  atomicOr(status, ST_BAD_MAP);
+  return c.n_pages;
+}
+
+// Page numbers around a warp's cursor over the keys of a sample: lane l holds the l-th of 32 and of the next 32, whose load is under way
+// long before their use.
+struct PageWindow {
+  int sample = -1, first = 0, now = 0, next = 0;
+  __device__ __forceinline__ int fetch(const PagedCache& c, int page) const {
+    page += threadIdx.x & 31;
+    return page < (c.max_kv + (1 << c.page_shift) - 1) >> c.page_shift ? __ldg(c.table + sample * c.table_stride + page) : 0;
+  }
+  // the lane-th of the pages from `page` on, which lie in one aligned group of 32 (warp-wide)
+  __device__ __forceinline__ int get(const PagedCache& c, int smp, int page, int lane) {
+    const int at = page & ~31;
+    if (smp != sample || at != first) {
+      const bool on = smp == sample && at == first + 32;
+      sample = smp;
+      first = at;
+      now = on ? next : fetch(c, at);
+      next = fetch(c, at + 32);
+    }
+    return __shfl_sync(0xffffffffu, now, (page & 31) + lane);
+  }
+};
+
 // rows of a row tile of the warp-level and of the fp32 kernel for blocks of `rows` rows
 inline int seg_mma_tile_rows(int64_t rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
 // of the tcgen05 kernel: two query tiles, or one whose keys two streams take in turn
@@ -164,5 +224,13 @@ cudaError_t launch_seg_mma(const SegParams& p, int pass, int tile_rows, bool wid
 // both: the items of pass 1 follow those of pass 0 in the same launch; alt: 128-row tiles whose keys two streams take in turn
 cudaError_t launch_seg_tc(const SegParams& p, int pass, bool both, bool alt, cudaStream_t st, int* launches);
 cudaError_t launch_seg_f32(const SegParams& p, int pass, int tile_rows, cudaStream_t st, int* launches);
+// paged keys: pass 0 of p with items up to a bound known on the host
+cudaError_t launch_paged_tc(const SegParams& p, const PagedCache& c, bool alt, cudaStream_t st, int* launches);
+cudaError_t launch_paged_f32(const SegParams& p, const PagedCache& c, int tile_rows, cudaStream_t st, int* launches);
+// the warp-level kernel: `shares` CTAs share the key tiles out evenly; cut: a row tile's keys may be shared out too, and are
+// then joined by a second kernel
+int paged_mma_shares(int sms);
+size_t paged_mma_scratch(int shares, int tile_rows, int D);
+cudaError_t launch_paged_mma(const SegParams& p, const PagedCache& c, int tile_rows, int shares, bool cut, cudaStream_t st, int* launches);
 
 }  // namespace swam

@@ -43,8 +43,10 @@ struct F32Cfg {
   static constexpr int kBytes = (kQ + 2 * (kK + kV) + kP) * 4;
 };
 
-template <int D, int RPT>
-__global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constant__ SegParams p, const int pass) {
+// kPaged: an item is a row tile of one sample's new tokens, found from the block's number; its keys are found through the page table
+template <int D, int RPT, bool kPaged>
+__global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constant__ SegParams p, const int pass,
+                                                            const __grid_constant__ CacheArg<kPaged> pc) {
   using C = F32Cfg<D, RPT>;
   if (p.early && pass == 0) allow_next();
   constexpr int MR = C::MR, QS = C::QS, PS = MR + 4;
@@ -55,37 +57,79 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
   float* sP = sV + 2 * C::kV;    // [32][MR + 4], row ty + 16 i at column ty * RPT + i
   const SegPass& ps = p.pass[pass];
   const SegArgs& a = p.a;
-  const SegItem it = seg_item(ps, a.N_kv, MR, blockIdx.x);
-  const SegKeys kk = seg_keys(p, ps, it, MR, kKF);
+  SegItem it = seg_item(ps, a.N_kv, MR, blockIdx.x);
+  SegKeys kk;
+  PagedSample smp{0, 0, 0};
+  int row_end = 0;               // kPaged: rows of the call in front of the end of the sample's
+  if constexpr (kPaged) {
+    smp = paged_sample(pc, a.n_q, it.block, p.status);
+    const int rows = smp.n * p.g;
+    if (it.row0 >= rows) {       // (what the next kernel waits for is the end of all blocks)
+      allow_next();
+      return;
+    }
+    kk.len0 = kk.n0 = 0;
+    kk.len1 = paged_limit(a.causal, smp, (min(it.row0 + MR, rows) - 1) / p.g);
+    const int total = (kk.len1 + kKF - 1) / kKF, per = (total + ps.splits - 1) / ps.splits;
+    kk.begin = min(total, it.split * per);
+    kk.end = min(total, kk.begin + per);
+    it.row0 += smp.q0 * p.g;
+    row_end = smp.q0 * p.g + rows;
+  } else {
+    kk = seg_keys(p, ps, it, MR, kKF);
+  }
   const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3;
   const int b0 = it.block * ps.block_samples;
+  auto row_of = [&](int r) {
+    if constexpr (kPaged) {
+      SegRow x = seg_row(p, 1, 0, it.h_kv, it.row0 + r);
+      x.real = it.row0 + r < row_end;
+      return x;
+    } else {
+      return seg_row(p, ps, it, it.row0 + r);
+    }
+  };
 
   for (int i = threadIdx.x; i < MR * (D / 4); i += kThreadsF) {
     const int r = i / (D / 4), c = (i % (D / 4)) * 4;
-    const SegRow row = seg_row(p, ps, it, it.row0 + r);
+    const SegRow row = row_of(r);
     cp16(sQ + r * QS + c, (const float*)a.q + row.b * a.q_smp + row.t * a.q_tok + (int64_t)row.h * D + c, row.real ? 16u : 0u);
   }
   auto load_tile = [&](int t) {
     const int s = t >= kk.n0 ? 1 : 0;
     const int key0 = (s ? t - kk.n0 : t) * kKF;
     const int len = s ? kk.len1 : kk.len0;
-    const int64_t idx = s ? b0 : b0 / a.per_group;
+    const int64_t idx = kPaged ? 0 : (s ? b0 : b0 / a.per_group);
     const float* kb = (const float*)a.k[s] + idx * a.k_smp[s] + (int64_t)it.h_kv * D;
     const float* vb = (const float*)a.v[s] + idx * a.v_smp[s] + (int64_t)it.h_kv * D;
     const int st = (t - kk.begin) & 1;
     for (int i = threadIdx.x; i < kKF * (D / 4); i += kThreadsF) {
       const int r = i / (D / 4), c = (i % (D / 4)) * 4;
-      const bool in = key0 + r < len;
-      const int64_t key = in ? key0 + r : 0;
-      cp16(sK + st * C::kK + r * QS + c, kb + key * a.k_tok[s] + c, in ? 16u : 0u);
-      cp16(sV + st * C::kV + r * D + c, vb + key * a.v_tok[s] + c, in ? 16u : 0u);
+      bool in = key0 + r < len;
+      if constexpr (kPaged) {
+        const int key = in ? key0 + r : 0;
+        int page = in ? __ldg(pc.table + it.block * pc.table_stride + (key >> pc.page_shift)) : 0;
+        if (in && (page < 0 || page >= pc.n_pages)) {
+          atomicOr(p.status, ST_BAD_MAP);
+          in = false;                // zeros
+          page = 0;
+        }
+        const int64_t row = key & ((1 << pc.page_shift) - 1);
+        cp16(sK + st * C::kK + r * QS + c, kb + page * pc.k_page + row * pc.k_tok + c, in ? 16u : 0u);
+        cp16(sV + st * C::kV + r * D + c, vb + page * pc.v_page + row * pc.v_tok + c, in ? 16u : 0u);
+      } else {
+        const int64_t key = in ? key0 + r : 0;
+        cp16(sK + st * C::kK + r * QS + c, kb + key * a.k_tok[s] + c, in ? 16u : 0u);
+        cp16(sV + st * C::kV + r * D + c, vb + key * a.v_tok[s] + c, in ? 16u : 0u);
+      }
     }
   };
   int lim1[RPT];
 #pragma unroll
   for (int i = 0; i < RPT; ++i) {
-    const SegRow row = seg_row(p, ps, it, it.row0 + ty + 16 * i);
-    lim1[i] = seg_limit1(a, kk.end > kk.n0 ? seg_len(p, 1, row.b) : 0, row.t);
+    const SegRow row = row_of(ty + 16 * i);
+    if constexpr (kPaged) lim1[i] = row.real ? paged_limit(a.causal, smp, row.t - smp.q0) : 0;
+    else lim1[i] = seg_limit1(a, kk.end > kk.n0 ? seg_len(p, 1, row.b) : 0, row.t);
   }
   uint64_t o2[RPT][D / 16];                        // output columns 4 tx + 32 c + (0, 1) and (2, 3)
   float m[RPT], l[RPT];
@@ -199,7 +243,7 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
     float sum = l[i];
 #pragma unroll
     for (int s = 1; s < 8; s <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-    const SegRow row = seg_row(p, ps, it, it.row0 + ty + 16 * i);
+    const SegRow row = row_of(ty + 16 * i);
     if (!row.real) continue;
     const int64_t gr = ((int64_t)row.b * a.n_q + row.t) * a.N_h + row.h;
     const int64_t pr = (int64_t)(ps.part0 + it.split) * p.rows + gr;
@@ -220,32 +264,39 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
   if (pass == 1) wait_previous();
 }
 
-template <int D, int RPT>
-cudaError_t launch_one(const SegParams& p, int pass, cudaStream_t st, int* launches) {
+template <int D, int RPT, bool kPaged>
+cudaError_t launch_one(const SegParams& p, int pass, const CacheArg<kPaged>& c, cudaStream_t st, int* launches) {
   constexpr int smem = F32Cfg<D, RPT>::kBytes;
   static SmemOptIn opt_in;
-  cudaError_t e = opt_in((const void*)seg_f32_kernel<D, RPT>, smem, p.a.device);
+  cudaError_t e = opt_in((const void*)seg_f32_kernel<D, RPT, kPaged>, smem, p.a.device);
   if (e != cudaSuccess) return e;
   ++*launches;
-  if (pass == 1) return launch_after(seg_f32_kernel<D, RPT>, dim3(p.pass[pass].items), dim3(kThreadsF), smem, st, p, pass);
-  seg_f32_kernel<D, RPT><<<p.pass[pass].items, kThreadsF, smem, st>>>(p, pass);
+  if (pass == 1) return launch_after(seg_f32_kernel<D, RPT, kPaged>, dim3(p.pass[pass].items), dim3(kThreadsF), smem, st, p, pass, c);
+  seg_f32_kernel<D, RPT, kPaged><<<p.pass[pass].items, kThreadsF, smem, st>>>(p, pass, c);
   return cudaGetLastError();
 }
-template <int D>
-cudaError_t launch_rows(const SegParams& p, int pass, int tile_rows, cudaStream_t st, int* launches) {
-  return tile_rows == 16 ? launch_one<D, 1>(p, pass, st, launches)
-                         : (tile_rows == 32 ? launch_one<D, 2>(p, pass, st, launches) : launch_one<D, 4>(p, pass, st, launches));
+template <int D, bool kPaged>
+cudaError_t launch_rows(const SegParams& p, int pass, const CacheArg<kPaged>& c, int tile_rows, cudaStream_t st, int* launches) {
+  return tile_rows == 16 ? launch_one<D, 1, kPaged>(p, pass, c, st, launches)
+                         : (tile_rows == 32 ? launch_one<D, 2, kPaged>(p, pass, c, st, launches) : launch_one<D, 4, kPaged>(p, pass, c, st, launches));
+}
+template <bool kPaged>
+cudaError_t launch_dim(const SegParams& p, int pass, const CacheArg<kPaged>& c, int tile_rows, cudaStream_t st, int* launches) {
+  switch (p.a.D) {
+    case 32: return launch_rows<32, kPaged>(p, pass, c, tile_rows, st, launches);
+    case 64: return launch_rows<64, kPaged>(p, pass, c, tile_rows, st, launches);
+    case 128: return launch_rows<128, kPaged>(p, pass, c, tile_rows, st, launches);
+    default: return cudaErrorInvalidConfiguration;
+  }
 }
 
 }  // namespace
 
 cudaError_t launch_seg_f32(const SegParams& p, int pass, int tile_rows, cudaStream_t st, int* launches) {
-  switch (p.a.D) {
-    case 32: return launch_rows<32>(p, pass, tile_rows, st, launches);
-    case 64: return launch_rows<64>(p, pass, tile_rows, st, launches);
-    case 128: return launch_rows<128>(p, pass, tile_rows, st, launches);
-    default: return cudaErrorInvalidConfiguration;
-  }
+  return launch_dim<false>(p, pass, NoCache(), tile_rows, st, launches);
+}
+cudaError_t launch_paged_f32(const SegParams& p, const PagedCache& c, int tile_rows, cudaStream_t st, int* launches) {
+  return launch_dim<true>(p, 0, c, tile_rows, st, launches);
 }
 
 }  // namespace swam

@@ -58,6 +58,7 @@ struct __align__(16) SegDesc {
   int n, na, b0, h_kv;
   int row0, base0, base1, part;
   int len0, len1, own, kv0;         // real keys of segment 0, most that a row of the tile sees of segment 1, real keys of it; group
+  // Paged keys are all segment 1.  base0: where the sample's rows end (rows count from the call's first token); kv0: the sample.
 };
 
 template <int D, bool kAlt>
@@ -115,12 +116,12 @@ __device__ __forceinline__ void st_global_32(void* dst, const uint32_t* v) {
                ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
-template <int D, bool kAlt>
+template <int D, bool kAlt, bool kPaged>
 __global__ void __launch_bounds__(kThreadsS, 1)
 seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_o,
               const __grid_constant__ CUtensorMap map_k0, const __grid_constant__ CUtensorMap map_v0,
               const __grid_constant__ CUtensorMap map_k1, const __grid_constant__ CUtensorMap map_v1,
-              const __grid_constant__ SegParams p, const int pass0, const SegTcArgs x) {
+              const __grid_constant__ SegParams p, const int pass0, const SegTcArgs x, const __grid_constant__ CacheArg<kPaged> pc) {
   using C = SegCfg<D, kAlt>;
   constexpr int ST = C::ST, LK = C::LK, QB = C::QB, NB = C::NB, kW = C::kW;
   extern __shared__ unsigned char smem_raw[];
@@ -228,52 +229,104 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       // the samples, a guided batch whose first half has no text would start 30 us late.
       int i = 0;
       bool ok = true, empty = false;               // has an item without keys been passed over
-      auto walk = [&](bool keys) {
-        for (int w = blockIdx.x; ok && w < x.items; w += gridDim.x) {
-          const int q = pass0 == 0 && w >= p.pass[0].items ? 1 : pass0;
-          const SegPass& ps = p.pass[q];
-          const SegItem it = seg_item(ps, a.N_kv, C::kRows, q != pass0 ? w - p.pass[0].items : w);
-          const SegKeys kk = seg_keys(p, ps, it, C::kRows, kTile);
-          SegDesc o;
-          o.n = kk.end - kk.begin;
-          o.na = max(0, min(o.n, kk.n0 - kk.begin));
-          o.b0 = it.block * ps.block_samples;
-          o.h_kv = it.h_kv;
-          o.row0 = it.row0 | (q << 30);                // rows of a block stay below 2^30
-          o.base0 = kk.begin * kTile;
-          o.base1 = (kk.begin - kk.n0) * kTile;
-          o.part = ps.part0 + it.split;
-          o.len0 = kk.len0;
-          o.len1 = kk.len1;
-          o.own = o.na < o.n ? seg_len(p, 1, o.b0) : 0;
-          o.kv0 = o.b0 / a.per_group;
-          if (o.n == 0) empty = true;
-          if ((o.n > 0) != keys) continue;
-          if (o.n == 0) {
-            // rows of zeros (or a piece of weight 0)
-            for (int r0 = 0; r0 < C::kRows; r0 += 32) {
-              const SegRow r = seg_row(p, ps.block_samples, o.b0, o.h_kv, it.row0 + r0 + lane);
-              if (!p.direct) {
-                if (r.real) p.part_ml[(int64_t)o.part * p.rows + ((int64_t)r.b * a.n_q + r.t) * a.N_h + r.h] = make_float2(-INFINITY, 0.f);
-                continue;
-              }
-              const int64_t off = r.real ? r.b * a.o_smp + r.t * a.o_tok + (int64_t)r.h * D : -1;
-              if (r.real && a.lse) a.lse[((int64_t)r.b * a.N_h + r.h) * a.n_q + r.t] = -INFINITY;
-              constexpr int CPR = D / 8, RPI = 32 / CPR;
-              for (int j = 0; j < 32 / RPI; ++j) {
-                const int64_t to = __shfl_sync(0xffffffffu, off, j * RPI + lane / CPR);
-                if (to >= 0) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + to + (lane % CPR) * 8) = make_uint4(0u, 0u, 0u, 0u);
-              }
+      // hands one item to the other warps, or, without keys, writes its zeros: rows of zeros (or a piece of weight 0)
+      auto emit = [&](const SegDesc& o, int block_samples, int row0, int row_end, bool keys) {
+        if (o.n == 0) empty = true;
+        if ((o.n > 0) != keys) return;
+        if (o.n == 0) {
+          for (int r0 = 0; r0 < C::kRows; r0 += 32) {
+            SegRow r = seg_row(p, block_samples, o.b0, o.h_kv, row0 + r0 + lane);
+            if (kPaged) r.real = row0 + r0 + lane < row_end;
+            if (!p.direct) {
+              if (r.real) p.part_ml[(int64_t)o.part * p.rows + ((int64_t)r.b * a.n_q + r.t) * a.N_h + r.h] = make_float2(-INFINITY, 0.f);
+              continue;
             }
-            continue;
+            const int64_t off = r.real ? r.b * a.o_smp + r.t * a.o_tok + (int64_t)r.h * D : -1;
+            if (r.real && a.lse) a.lse[((int64_t)r.b * a.N_h + r.h) * a.n_q + r.t] = -INFINITY;
+            constexpr int CPR = D / 8, RPI = 32 / CPR;
+            for (int j = 0; j < 32 / RPI; ++j) {
+              const int64_t to = __shfl_sync(0xffffffffu, off, j * RPI + lane / CPR);
+              if (to >= 0) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + to + (lane % CPR) * 8) = make_uint4(0u, 0u, 0u, 0u);
+            }
           }
-          const int slot = i % kDesc;
-          if (i >= kDesc) ok = wait(bar_d_empty(slot), ((i / kDesc) & 1) ^ 1);
-          if (ok && lane == 0) {
-            desc[slot] = o;
-            mbar_arrive(bar_d_full(slot));
+          return;
+        }
+        const int slot = i % kDesc;
+        if (i >= kDesc) ok = wait(bar_d_empty(slot), ((i / kDesc) & 1) ^ 1);
+        if (ok && lane == 0) {
+          desc[slot] = o;
+          mbar_arrive(bar_d_full(slot));
+        }
+        ++i;
+      };
+      auto walk = [&](bool keys) {
+        if constexpr (kPaged) {
+          // The items of a sample: its key/value heads, pieces, row tiles (the last first: with causal it has the most keys).  Lane l
+          // knows sample base + l and where its items end among those of the 32.
+          int chunk = 0, before = 0, w = blockIdx.x;
+          while (ok && chunk < pc.samples) {
+            const int b = chunk + lane;
+            PagedSample smp{0, 0, 0};
+            if (b < pc.samples) smp = paged_sample(pc, a.n_q, b, p.status);
+            const int tiles = (smp.n * p.g + C::kRows - 1) / C::kRows;
+            int end = tiles * a.N_kv * p.pass[0].splits;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+              const int y = __shfl_up_sync(0xffffffffu, end, o);
+              if (lane >= o) end += y;
+            }
+            const int all = __shfl_sync(0xffffffffu, end, 31);
+            for (; ok && w - before < all; w += gridDim.x) {
+              const int src = __ffs(__ballot_sync(0xffffffffu, end > w - before)) - 1;
+              const PagedSample it{__shfl_sync(0xffffffffu, smp.q0, src), __shfl_sync(0xffffffffu, smp.n, src), __shfl_sync(0xffffffffu, smp.len, src)};
+              const int rt = __shfl_sync(0xffffffffu, tiles, src), splits = p.pass[0].splits;
+              int k = w - before - (__shfl_sync(0xffffffffu, end, src) - rt * a.N_kv * splits);
+              const int row0 = (rt - 1 - k % rt) * C::kRows;
+              k /= rt;
+              const int split = k % splits, rows = it.n * p.g;
+              const int sees = paged_limit(a.causal, it, (min(row0 + C::kRows, rows) - 1) / p.g);
+              const int total = (sees + kTile - 1) / kTile, per = (total + splits - 1) / splits;
+              const int begin = min(total, split * per);
+              SegDesc o;
+              o.n = min(total, begin + per) - begin;
+              o.na = 0;
+              o.b0 = 0;
+              o.h_kv = k / splits;
+              o.row0 = it.q0 * p.g + row0;
+              o.base0 = it.q0 * p.g + rows;          // the end of the sample's rows
+              o.base1 = begin * kTile;
+              o.part = split;
+              o.len0 = 0;
+              o.len1 = sees;
+              // (seg_limit1 counts from the call's last token: this sample's last one is number q0 + n - 1 of n_q)
+              o.own = a.causal ? it.len + a.n_q - it.n - it.q0 : it.len;
+              o.kv0 = chunk + src;
+              emit(o, 1, o.row0, o.base0, keys);
+            }
+            before += all;
+            chunk += 32;
           }
-          ++i;
+        } else {
+          for (int w = blockIdx.x; ok && w < x.items; w += gridDim.x) {
+            const int q = pass0 == 0 && w >= p.pass[0].items ? 1 : pass0;
+            const SegPass& ps = p.pass[q];
+            const SegItem it = seg_item(ps, a.N_kv, C::kRows, q != pass0 ? w - p.pass[0].items : w);
+            const SegKeys kk = seg_keys(p, ps, it, C::kRows, kTile);
+            SegDesc o;
+            o.n = kk.end - kk.begin;
+            o.na = max(0, min(o.n, kk.n0 - kk.begin));
+            o.b0 = it.block * ps.block_samples;
+            o.h_kv = it.h_kv;
+            o.row0 = it.row0 | (q << 30);                // rows of a block stay below 2^30
+            o.base0 = kk.begin * kTile;
+            o.base1 = (kk.begin - kk.n0) * kTile;
+            o.part = ps.part0 + it.split;
+            o.len0 = kk.len0;
+            o.len1 = kk.len1;
+            o.own = o.na < o.n ? seg_len(p, 1, o.b0) : 0;
+            o.kv0 = o.b0 / a.per_group;
+            emit(o, ps.block_samples, it.row0, 0, keys);
+          }
         }
       };
       walk(true);
@@ -295,12 +348,27 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             if (!ok) break;
             const int row0 = d.row0 + s * kTile;     // (one pass of single samples: no flag in row0)
             if (lane == 0) {
-              if (row0 < a.n_q * p.g) {
+              if (kPaged ? row0 + kTile <= d.base0 : row0 < a.n_q * p.g) {
                 for (int db = 0; db < C::DB; ++db)
                   tma_store_5d(&map_o, sQ + ((iter % QB) * C::NQ + s) * C::kTileBytes + db * C::kSub, db * 64, 0, row0 / p.g, d.h_kv, d.b0);
                 tma_store_commit_wait();
               }
-              mbar_arrive(bar_q_free(iter % QB));
+              if (!kPaged) mbar_arrive(bar_q_free(iter % QB));
+            }
+            if constexpr (kPaged) {
+              // the rows behind a sample's last one are another's: its last tile leaves row by row
+              if (row0 + kTile > d.base0) {
+                constexpr int CPR = D / 8;
+                const unsigned char* src = base_ptr + ((iter % QB) * C::NQ + s) * C::kTileBytes;
+                for (int i = lane; i < (d.base0 - row0) * CPR; i += 32) {
+                  const int rl = i / CPR, cc = i % CPR, tok = (row0 + rl) / p.g, h = d.h_kv * p.g + row0 + rl - tok * p.g;
+                  *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + cc * 8) =
+                      *reinterpret_cast<const uint4*>(src + (cc >> 3) * C::kSub + rl * 128 + (((cc & 7) ^ (rl & 7)) << 4));
+                }
+                fence_proxy_async();                 // the next loads of this buffer come through the other proxy
+              }
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar_q_free(iter % QB));
             }
             __syncwarp();
           }
@@ -340,8 +408,27 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       int pos = 0, iter = 0;                       // ring loads and items (of K) so far
       int ik = 0, nk = 0, iv = 0, nv = 0, dvi = 0; // next tile and tiles of the items of K (descriptor di - 1) and V (dvi - 1)
       bool ok = true, k_end = false;
+      PageWindow pages[2];                         // paged keys: around the cursors of K and V
       auto load = [&](const SegDesc& o, bool is_v, int i) {
         const int st = pos % ST;
+        if constexpr (kPaged) {
+          const int key0 = o.base1 + i * kTile, sh = pc.page_shift, first = key0 >> sh;
+          const int count = sh >= 7 ? 1 : min(kTile >> sh, ((o.len1 - key0) + (1 << sh) - 1) >> sh);       // pages with keys
+          const int page = pages[is_v].get(pc, o.kv0, first, lane < count ? lane : 0);
+          if (!wait(bar_empty(st), ((pos / ST) & 1) ^ 1)) return false;
+          const int rows = min(kTile, 1 << sh);
+          if (lane == 0) mbar_expect_tx(bar_full(st), count * rows * 128 * C::DB);
+          __syncwarp();
+          if (lane < count) {
+            const int at = paged_page(pc, page, p.status);
+            for (int db = 0; db < C::DB; ++db)
+              tma_load_4d(sR + st * C::kTileBytes + db * C::kSub + lane * rows * 128, is_v ? &map_v1 : &map_k1, bar_full(st), db * 64,
+                          key0 & ((1 << sh) - 1), o.h_kv, at);
+          }
+          __syncwarp();
+          ++pos;
+          return true;
+        }
         if (!wait(bar_empty(st), ((pos / ST) & 1) ^ 1)) return false;
         if (lane == 0) {
           const bool s1 = i >= o.na;
@@ -693,7 +780,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     while (ok && next_desc(di, d)) {
       const int n = d.n, na = d.na, part = d.part;
       const int row0 = (d.row0 & 0x3fffffff) + (kAlt ? 0 : s * kTile);       // of the stream's tile
-      const SegRow row = seg_row(p, p.pass[d.row0 >> 30].block_samples, d.b0, d.h_kv, row0 + r);
+      SegRow row = seg_row(p, p.pass[d.row0 >> 30].block_samples, d.b0, d.h_kv, row0 + r);
+      if (kPaged) row.real = row0 + r < d.base0;
       const int grow = (row.b * a.n_q + row.t) * a.N_h + row.h;
       const bool row_real = row.real, warp_real = __any_sync(0xffffffffu, row_real);
       // real keys ahead of each segment's first tile in this item, and those of segment 1 that this row sees
@@ -917,15 +1005,21 @@ bool make_q_map(CUtensorMap* map, const void* ptr, const SegArgs& a, int g, int6
   return encode_bf16(map, ptr, 5, dims, strides, box);
 }
 
-template <int D, bool kAlt>
-cudaError_t launch_tc(const SegParams& p, int pass, bool both, cudaStream_t st, int* launches) {
+template <int D, bool kAlt, bool kPaged>
+cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kPaged>& c, cudaStream_t st, int* launches) {
   const SegArgs& a = p.a;
   CUtensorMap mk[2], mv[2], mq, mo;
   memset(mk, 0, sizeof(mk));       // a segment without keys: its maps are never used
   memset(mv, 0, sizeof(mv));
   memset(&mq, 0, sizeof(mq));
   memset(&mo, 0, sizeof(mo));
-  for (int s = 0; s < 2; ++s) {
+  if constexpr (kPaged) {
+    const int page = 1 << c.page_shift, rows = page < kTile ? page : kTile;
+    if (!make_kv_map(&mk[1], a.k[1], c.n_pages, page, a.N_kv, D, c.k_tok, c.k_page, rows) ||
+        !make_kv_map(&mv[1], a.v[1], c.n_pages, page, a.N_kv, D, c.v_tok, c.v_page, rows))
+      return cudaErrorInvalidValue;
+  }
+  for (int s = 0; s < 2 && !kPaged; ++s) {
     if (a.n[s] == 0) continue;
     const int blocks = s == 0 ? a.B / a.per_group : a.B;
     if (!make_kv_map(&mk[s], a.k[s], blocks, a.n[s], a.N_kv, D, a.k_tok[s], a.k_smp[s], kTile) ||
@@ -945,23 +1039,31 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, cudaStream_t st, 
   x.items = p.pass[pass].items + (both ? p.pass[1].items : 0);
   constexpr int smem = SegCfg<D, kAlt>::kBytes;
   static SmemOptIn opt_in;
-  cudaError_t e = opt_in((const void*)seg_tc_kernel<D, kAlt>, smem, a.device);
+  cudaError_t e = opt_in((const void*)seg_tc_kernel<D, kAlt, kPaged>, smem, a.device);
   if (e != cudaSuccess) return e;
   const int grid = x.items < a.sms ? x.items : a.sms;
   ++*launches;
-  if (pass == 1) return launch_after(seg_tc_kernel<D, kAlt>, dim3(grid), dim3(kThreadsS), smem, st, mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x);
-  seg_tc_kernel<D, kAlt><<<grid, kThreadsS, smem, st>>>(mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x);
+  if (pass == 1) return launch_after(seg_tc_kernel<D, kAlt, kPaged>, dim3(grid), dim3(kThreadsS), smem, st, mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
+  seg_tc_kernel<D, kAlt, kPaged><<<grid, kThreadsS, smem, st>>>(mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
   return cudaGetLastError();
+}
+
+template <bool kPaged>
+cudaError_t launch_dim(const SegParams& p, int pass, bool both, bool alt, const CacheArg<kPaged>& c, cudaStream_t st, int* launches) {
+  switch (p.a.D) {
+    case 64: return alt ? launch_tc<64, true, kPaged>(p, pass, both, c, st, launches) : launch_tc<64, false, kPaged>(p, pass, both, c, st, launches);
+    case 128: return alt ? launch_tc<128, true, kPaged>(p, pass, both, c, st, launches) : launch_tc<128, false, kPaged>(p, pass, both, c, st, launches);
+    default: return cudaErrorInvalidConfiguration;
+  }
 }
 
 }  // namespace
 
 cudaError_t launch_seg_tc(const SegParams& p, int pass, bool both, bool alt, cudaStream_t st, int* launches) {
-  switch (p.a.D) {
-    case 64: return alt ? launch_tc<64, true>(p, pass, both, st, launches) : launch_tc<64, false>(p, pass, both, st, launches);
-    case 128: return alt ? launch_tc<128, true>(p, pass, both, st, launches) : launch_tc<128, false>(p, pass, both, st, launches);
-    default: return cudaErrorInvalidConfiguration;
-  }
+  return launch_dim<false>(p, pass, both, alt, NoCache(), st, launches);
+}
+cudaError_t launch_paged_tc(const SegParams& p, const PagedCache& c, bool alt, cudaStream_t st, int* launches) {
+  return launch_dim<true>(p, 0, false, alt, c, st, launches);
 }
 
 }  // namespace swam

@@ -276,6 +276,137 @@ int check_device(swam_ctx* c) {
   return SWAM_OK;
 }
 
+// ---- norms, rotary positions and the paged cache
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+int fail_named(swam_ctx* c, int code, const char* name, const char* why) {
+  snprintf(c->err, sizeof(c->err), "%s: %s", name, why);
+  return code;
+}
+int run_ready(swam_ctx* c, const char* name) {
+  if (!c->ws) return fail_named(c, SWAM_ERR_WORKSPACE, name, "no workspace bound");
+  return check_device(c);
+}
+
+// the rotation and the norms of a call
+int rope_args(swam_ctx* c, const char* name, const swam_rope* r, const float* q_weight, const float* k_weight, float eps,
+              const int32_t* positions, RopeParams& p) {
+  memset(&p, 0, sizeof(p));
+  p.N_h = c->d.N_h;
+  p.D = c->d.D;
+  p.dtype = c->d.dtype;
+  p.sms = c->sms;
+  p.axes = 1;
+  p.magnitude = 1.f;
+  if (r) {
+    if (r->rot_dim < 2 || r->rot_dim % 2 != 0 || r->rot_dim > c->d.D || !r->freq || r->n_axes < 1 || r->n_axes > 8)
+      return fail_named(c, SWAM_ERR_INVALID_ARG, name, "rot_dim must be even and 2 .. head_dim, n_axes 1 .. 8, freq given");
+    if (!(fabsf(r->magnitude) <= 1e30f)) return fail_named(c, SWAM_ERR_INVALID_ARG, name, "magnitude must be finite");
+    p.rot = r->rot_dim;
+    p.axes = r->n_axes;
+    p.interleaved = r->interleaved != 0;
+    if (r->magnitude != 0.f) p.magnitude = r->magnitude;
+    for (int i = 0; i < p.rot / 2; ++i) {
+      if (!(fabs(r->freq[i]) <= 1048576.0)) return fail_named(c, SWAM_ERR_INVALID_ARG, name, "frequencies must be finite and at most 2^20");
+      const int32_t ax = r->axis ? r->axis[i] : 0;
+      if (ax < 0 || ax >= p.axes) return fail_named(c, SWAM_ERR_INVALID_ARG, name, "axis out of range");
+      p.turn[i] = turns_of(r->freq[i]);
+      p.axis[i] = (uint8_t)ax;
+    }
+  }
+  if (!(eps >= 0.f) || eps > 1e30f) return fail_named(c, SWAM_ERR_INVALID_ARG, name, "eps must be finite and not negative");
+  if (!aligned16(q_weight) || !aligned16(k_weight) || !aligned4(positions)) return fail_named(c, SWAM_ERR_INVALID_ARG, name, "misaligned pointer");
+  p.eps = eps;
+  p.weight[0] = q_weight;
+  p.weight[1] = k_weight;
+  p.positions = positions;
+  return SWAM_OK;
+}
+
+// the cache of a call with n_tokens new tokens; max_q and max_kv: 0 = as many as there can be
+int cache_args(swam_ctx* c, const char* name, const swam_paged_cache* x, int32_t n_tokens, int32_t max_q, int32_t max_kv, int* N_kv, PagedCache& o) {
+  auto bad = [&](int code, const char* why) { return fail_named(c, code, name, why); };
+  const Dims& d = c->d;
+  memset(&o, 0, sizeof(o));
+  if (!x) return bad(SWAM_ERR_INVALID_ARG, "null cache");
+  if (x->reserved != 0) return bad(SWAM_ERR_INVALID_ARG, "reserved must be 0");
+  if (x->n_samples < 0 || x->n_pages < 0 || x->max_pages < 0 || n_tokens < 0 || max_q < 0 || max_kv < 0 || x->n_kv_heads < 0)
+    return bad(SWAM_ERR_INVALID_ARG, "negative size");
+  if (x->page_size < 16 || (x->page_size & (x->page_size - 1)) != 0 || x->page_size > 1 << 20)
+    return bad(SWAM_ERR_INVALID_ARG, "page_size must be a power of two, 16 .. 2^20");
+  *N_kv = x->n_kv_heads > 0 ? x->n_kv_heads : d.N_kv;
+  if (d.N_h % *N_kv != 0) return bad(SWAM_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
+  if (x->n_samples > 1 << 20) return bad(SWAM_ERR_UNSUPPORTED, "n_samples beyond 2^20");
+  if ((int64_t)x->max_pages * x->page_size > kMaxSegTokens) return bad(SWAM_ERR_UNSUPPORTED, "max_pages * page_size beyond 2^29");
+  if ((int64_t)n_tokens * d.N_h > 1ll << 30) return bad(SWAM_ERR_UNSUPPORTED, "n_tokens * n_heads beyond 2^30");
+  if (n_tokens > 0 && (x->n_samples == 0 || x->n_pages == 0 || x->max_pages == 0))
+    return bad(SWAM_ERR_INVALID_ARG, "tokens without samples or pages");
+  if (!x->q_start && x->n_samples > 0 && n_tokens % x->n_samples != 0)
+    return bad(SWAM_ERR_INVALID_ARG, "without q_start n_samples must divide n_tokens");
+  o.samples = x->n_samples;
+  o.n_pages = x->n_pages;
+  o.page_shift = __builtin_ctz((unsigned)x->page_size);
+  const int32_t capacity = x->max_pages * x->page_size;
+  o.max_kv = max_kv > 0 && max_kv < capacity ? max_kv : capacity;
+  const int32_t most = x->q_start || x->n_samples == 0 ? n_tokens : n_tokens / x->n_samples;
+  o.max_q = x->q_start && max_q > 0 && max_q < most ? max_q : most;
+  o.table = x->page_table;
+  o.kv_len = x->kv_len;
+  o.q_start = x->q_start;
+  o.table_stride = x->table_sample == 0 ? x->max_pages : x->table_sample;
+  if (o.table_stride < x->max_pages || o.table_stride > (int64_t)1 << 38) return bad(SWAM_ERR_INVALID_ARG, "table_sample must be at least max_pages");
+  o.k_page = x->k_page;
+  o.k_tok = x->k_token;
+  o.v_page = x->v_page;
+  o.v_tok = x->v_token;
+  const int64_t row = (int64_t)*N_kv * d.D;
+  const int64_t pages = x->n_pages > 0 ? x->n_pages : 1;
+  if (!set_strides(o.k_tok, o.k_page, x->page_size, pages, row, elem_bytes(d)) || !set_strides(o.v_tok, o.v_page, x->page_size, pages, row, elem_bytes(d)))
+    return bad(SWAM_ERR_INVALID_ARG, "strides must be non-negative multiples of 16 bytes without overlapping tokens");
+  // (a tensor map's strides stay below 2^40 bytes)
+  if ((o.k_page | o.v_page) >> 38 || (o.k_tok | o.v_tok) >> 38) return bad(SWAM_ERR_INVALID_ARG, "strides at most 2^38");
+  return SWAM_OK;
+}
+// its pointers, where the call has tokens
+int cache_pointers(swam_ctx* c, const char* name, const swam_paged_cache* x) {
+  if (!x->kv_len || !x->page_table || !x->k || !x->v) return fail_named(c, SWAM_ERR_INVALID_ARG, name, "null pointer in the cache");
+  if (!aligned16(x->k) || !aligned16(x->v) || !aligned4(x->page_table) || !aligned4(x->kv_len) || !aligned4(x->q_start))
+    return fail_named(c, SWAM_ERR_INVALID_ARG, name, "misaligned pointer in the cache");
+  return SWAM_OK;
+}
+TokenSpan k_span(const swam_paged_cache* x, const PagedCache& o, int64_t row) { return {x->k, x->page_size, x->n_pages, o.k_tok, o.k_page, row}; }
+TokenSpan v_span(const swam_paged_cache* x, const PagedCache& o, int64_t row) { return {x->v, x->page_size, x->n_pages, o.v_tok, o.v_page, row}; }
+
+// `out` may be `in` itself
+bool overlaps_but_for_in_place(const TokenSpan& out, const TokenSpan& in, size_t elem) {
+  if (out.ptr == in.ptr && out.row == in.row && (out.tok == in.tok || out.n_tok == 1) && (out.smp == in.smp || out.n_smp == 1)) return false;
+  return share_memory(out, in, elem);
+}
+
+int paged_args(swam_ctx* c, const swam_paged_args* x, SegArgs& a, PagedCache& cache) {
+  const char* name = "swam_paged_attn";
+  memset(&a, 0, sizeof(a));
+  if (int r = cache_args(c, name, x->cache, x->n_tokens, x->max_q, x->max_kv, &a.N_kv, cache)) return r;
+  const Dims& d = c->d;
+  a.q = x->q; a.out = x->out; a.lse = x->lse;
+  a.k[1] = x->cache->k; a.v[1] = x->cache->v;
+  a.n[1] = cache.max_kv;
+  a.n_q = x->n_tokens;
+  a.causal = x->causal != 0;
+  a.B = a.per_group = 1;
+  a.N_h = d.N_h;
+  a.D = d.D;
+  a.dtype = d.dtype;
+  a.scale = d.scale;
+  a.device = c->device;
+  a.sms = c->sms;
+  a.q_tok = x->q_token;
+  a.o_tok = x->out_token;
+  const int64_t row = (int64_t)d.N_h * d.D;
+  if (!set_strides(a.q_tok, a.q_smp, a.n_q, 1, row, elem_bytes(d)) || !set_strides(a.o_tok, a.o_smp, a.n_q, 1, row, elem_bytes(d)))
+    return fail_named(c, SWAM_ERR_INVALID_ARG, name, "strides must be non-negative multiples of 16 bytes without overlapping tokens");
+  return SWAM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -585,6 +716,140 @@ int swam_prefix_attn(swam_ctx* c, const swam_prefix_args* args, void* stream) {
   SegPlan plan;
   if (int r = prefix_args(c, args, a, &plan, true)) return r;
   return run_seg(c, a, plan, args->scratch, args->scratch_bytes, "swam_prefix_attn", (cudaStream_t)stream);
+}
+
+int swam_norm_rope(swam_ctx* c, const swam_norm_rope_args* x, void* stream) {
+  const char* name = "swam_norm_rope";
+  Range trace_range(name);
+  if (!c || !x) return fail(c, SWAM_ERR_INVALID_ARG, "swam_norm_rope: null argument");
+  auto bad = [&](int code, const char* why) { return fail_named(c, code, name, why); };
+  const Dims& d = c->d;
+  RopeParams p;
+  if (int r = rope_args(c, name, x->rope, x->q_weight, x->k_weight, x->eps, x->positions, p)) return r;
+  if (x->reserved != 0) return bad(SWAM_ERR_INVALID_ARG, "reserved must be 0");
+  if (x->n < 0 || x->n_kv_heads < 0 || x->pos_sample < 0) return bad(SWAM_ERR_INVALID_ARG, "negative size");
+  p.N_kv = x->n_kv_heads > 0 ? x->n_kv_heads : d.N_kv;
+  if (d.N_h % p.N_kv != 0) return bad(SWAM_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
+  if (x->n > kMaxSegTokens || (int64_t)x->n * d.N_h > (1ll << 30) / d.B) return bad(SWAM_ERR_UNSUPPORTED, "batch * n * n_heads beyond 2^30");
+  if (x->pos_sample > (int64_t)1 << 38 || (x->pos_sample > 0 && x->pos_sample < (int64_t)x->n * p.axes))
+    return bad(SWAM_ERR_INVALID_ARG, "pos_sample must be 0 or at least n * n_axes");
+  p.n = x->n;
+  p.tokens = (int64_t)d.B * x->n;
+  p.pos_smp = x->pos_sample;
+  p.src[0] = x->q; p.dst[0] = x->q_out; p.src[1] = x->k; p.dst[1] = x->k_out;
+  p.s_tok[0] = x->q_token; p.s_smp[0] = x->q_sample; p.s_tok[1] = x->k_token; p.s_smp[1] = x->k_sample;
+  p.d_tok[0] = x->q_out_token; p.d_smp[0] = x->q_out_sample; p.d_tok[1] = x->k_out_token; p.d_smp[1] = x->k_out_sample;
+  const size_t eb = elem_bytes(d);
+  const int64_t row[2] = {(int64_t)d.N_h * d.D, (int64_t)p.N_kv * d.D};
+  for (int i = 0; i < 2; ++i) {
+    if (!set_strides(p.s_tok[i], p.s_smp[i], x->n, d.B, row[i], eb) || !set_strides(p.d_tok[i], p.d_smp[i], x->n, d.B, row[i], eb))
+      return bad(SWAM_ERR_INVALID_ARG, "strides must be non-negative multiples of 16 bytes without overlapping tokens");
+    if ((!p.src[i]) != (!p.dst[i])) return bad(SWAM_ERR_INVALID_ARG, "unpaired tensor");
+    if (!aligned16(p.src[i]) || !aligned16(p.dst[i])) return bad(SWAM_ERR_INVALID_ARG, "misaligned pointer");
+  }
+  for (int i = 0; i < 2 && x->n > 0; ++i) {
+    if (!p.dst[i]) continue;
+    const TokenSpan out{p.dst[i], x->n, d.B, p.d_tok[i], p.d_smp[i], row[i]};
+    const TokenSpan in{p.src[i], x->n, d.B, p.s_tok[i], p.s_smp[i], row[i]};
+    const TokenSpan other_in{p.src[1 - i], x->n, d.B, p.s_tok[1 - i], p.s_smp[1 - i], row[1 - i]};
+    const TokenSpan other_out{p.dst[1 - i], x->n, d.B, p.d_tok[1 - i], p.d_smp[1 - i], row[1 - i]};
+    if (overlaps_but_for_in_place(out, in, eb) || (p.dst[1 - i] && (share_memory(out, other_in, eb) || share_memory(out, other_out, eb))))
+      return bad(SWAM_ERR_INVALID_ARG, "an output overlaps an input or the other output");
+  }
+  if (int r = run_ready(c, name)) return r;
+  if (p.tokens == 0 || (!p.src[0] && !p.src[1])) return SWAM_OK;
+  p.status = (int*)(c->ws + c->off_status);
+  const cudaError_t e = launch_norm_rope(p, (cudaStream_t)stream, &c->launches_i);
+  count(c);
+  return e == cudaSuccess ? SWAM_OK : fail_cuda(c, e, name);
+}
+
+int swam_append_kv(swam_ctx* c, const swam_append_args* x, void* stream) {
+  const char* name = "swam_append_kv";
+  Range trace_range(name);
+  if (!c || !x) return fail(c, SWAM_ERR_INVALID_ARG, "swam_append_kv: null argument");
+  auto bad = [&](int code, const char* why) { return fail_named(c, code, name, why); };
+  const Dims& d = c->d;
+  RopeParams p;
+  if (int r = rope_args(c, name, x->rope, x->q_weight, x->k_weight, x->eps, x->positions, p)) return r;
+  if (int r = cache_args(c, name, x->cache, x->n_tokens, 0, 0, &p.N_kv, p.cache)) return r;
+  p.paged = true;
+  p.n = x->n_tokens;
+  p.tokens = x->n_tokens;
+  p.src[0] = x->q; p.dst[0] = x->q_out; p.src[1] = x->k; p.src[2] = x->v;
+  p.dst[1] = x->cache->k; p.dst[2] = x->cache->v;
+  p.s_tok[0] = x->q_token; p.s_tok[1] = x->k_token; p.s_tok[2] = x->v_token; p.d_tok[0] = x->q_out_token;
+  const size_t eb = elem_bytes(d);
+  const int64_t row[3] = {(int64_t)d.N_h * d.D, (int64_t)p.N_kv * d.D, (int64_t)p.N_kv * d.D};
+  bool strides = set_strides(p.d_tok[0], p.d_smp[0], x->n_tokens, 1, row[0], eb);
+  for (int i = 0; i < 3; ++i) strides = strides && set_strides(p.s_tok[i], p.s_smp[i], x->n_tokens, 1, row[i], eb);
+  if (!strides) return bad(SWAM_ERR_INVALID_ARG, "strides must be non-negative multiples of 16 bytes without overlapping tokens");
+  if (x->n_tokens > 0) {
+    if (!x->k || !x->v) return bad(SWAM_ERR_INVALID_ARG, "null k or v");
+    if ((!x->q) != (!x->q_out)) return bad(SWAM_ERR_INVALID_ARG, "unpaired tensor");
+    if (!aligned16(x->q) || !aligned16(x->k) || !aligned16(x->v) || !aligned16(x->q_out)) return bad(SWAM_ERR_INVALID_ARG, "misaligned pointer");
+    if (int r = cache_pointers(c, name, x->cache)) return r;
+    const TokenSpan outs[3] = {{x->q_out, x->n_tokens, 1, p.d_tok[0], p.d_smp[0], row[0]}, k_span(x->cache, p.cache, row[1]), v_span(x->cache, p.cache, row[1])};
+    for (int o = 0; o < 3; ++o) {
+      if (!outs[o].ptr) continue;
+      for (int i = 0; i < 3; ++i) {
+        if (!p.src[i]) continue;
+        const TokenSpan in{p.src[i], x->n_tokens, 1, p.s_tok[i], p.s_smp[i], row[i]};
+        if (o == 0 && i == 0 ? overlaps_but_for_in_place(outs[o], in, eb) : share_memory(outs[o], in, eb))
+          return bad(SWAM_ERR_INVALID_ARG, "an output overlaps an input");
+      }
+      if (o > 0 && x->q_out && share_memory(outs[o], outs[0], eb)) return bad(SWAM_ERR_INVALID_ARG, "q_out overlaps the cache");
+    }
+    if (share_memory(outs[1], outs[2], eb)) return bad(SWAM_ERR_INVALID_ARG, "k and v of the cache overlap");
+  }
+  if (int r = run_ready(c, name)) return r;
+  if (x->n_tokens == 0) return SWAM_OK;
+  p.status = (int*)(c->ws + c->off_status);
+  const cudaError_t e = launch_norm_rope(p, (cudaStream_t)stream, &c->launches_i);
+  count(c);
+  return e == cudaSuccess ? SWAM_OK : fail_cuda(c, e, name);
+}
+
+int swam_paged_attn_scratch_bytes(swam_ctx* c, const swam_paged_args* x, size_t* bytes) {
+  if (!c || !x || !bytes) return fail(c, SWAM_ERR_INVALID_ARG, "swam_paged_attn_scratch_bytes: null argument");
+  SegArgs a;
+  PagedCache cache;
+  if (int r = paged_args(c, x, a, cache)) return r;
+  *bytes = paged_scratch_bytes(a, cache, c->attn_variant == SWAM_ATTN_WARP_MMA);
+  return SWAM_OK;
+}
+
+int swam_paged_attn(swam_ctx* c, const swam_paged_args* x, void* stream) {
+  const char* name = "swam_paged_attn";
+  Range trace_range(name);
+  if (!c || !x) return fail(c, SWAM_ERR_INVALID_ARG, "swam_paged_attn: null argument");
+  auto bad = [&](int code, const char* why) { return fail_named(c, code, name, why); };
+  SegArgs a;
+  PagedCache cache;
+  if (int r = paged_args(c, x, a, cache)) return r;
+  const bool warp_mma = c->attn_variant == SWAM_ATTN_WARP_MMA;
+  size_t need = 0;
+  if (a.n_q > 0) {
+    if (!a.q || !a.out) return bad(SWAM_ERR_INVALID_ARG, "null q or out");
+    if (!aligned16(a.q) || !aligned16(a.out) || !aligned4(a.lse)) return bad(SWAM_ERR_INVALID_ARG, "misaligned pointer");
+    if (int r = cache_pointers(c, name, x->cache)) return r;
+    const size_t eb = elem_bytes(c->d);
+    const int64_t row = (int64_t)a.N_h * a.D, row_kv = (int64_t)a.N_kv * a.D;
+    const TokenSpan out{a.out, a.n_q, 1, a.o_tok, a.o_smp, row};
+    if (share_memory(out, {a.q, a.n_q, 1, a.q_tok, a.q_smp, row}, eb) || share_memory(out, k_span(x->cache, cache, row_kv), eb) ||
+        share_memory(out, v_span(x->cache, cache, row_kv), eb))
+      return bad(SWAM_ERR_INVALID_ARG, "out must not overlap an input");
+  }
+  if (int r = run_ready(c, name)) return r;
+  if (a.n_q == 0) return SWAM_OK;
+  need = paged_scratch_bytes(a, cache, warp_mma);
+  if (need > 0 && (!x->scratch || x->scratch_bytes < need || (reinterpret_cast<uintptr_t>(x->scratch) & 255u) != 0)) {
+    snprintf(c->err, sizeof(c->err), "%s: needs %zu bytes of 256-byte aligned scratch", name, need);
+    return SWAM_ERR_WORKSPACE;
+  }
+  const cudaError_t e = launch_paged_attn(a, cache, warp_mma, x->scratch, (int*)(c->ws + c->off_status), (cudaStream_t)stream, &c->launches_i);
+  count(c);
+  return e == cudaSuccess ? SWAM_OK : fail_cuda(c, e, name);
 }
 
 int swam_scatter(swam_ctx* c, const void* out_p, const int32_t* pack_map, const int32_t* inv_map, const void* cached,

@@ -256,4 +256,49 @@ size_t seg_scratch_bytes(const SegArgs& a, const SegPlan& p);
 cudaError_t launch_seg_attn(const SegArgs& a, const SegPlan& p, bool warp_mma, void* scratch, int* status, cudaStream_t st,
                             int* launches);
 
+// ---- the paged cache ------------------------------------------------------
+// Keys and values of samples of any length in pages of 2^page_shift tokens [n_pages, page, N_kv, D]; token c of sample b is row
+// c % page of page table[b][c / page].  The call's n_tokens new tokens [n_tokens, heads, D] belong to the samples in order: those
+// of sample b are [q_start[b], q_start[b + 1]) (no q_start: max_q each) and are the sample's last ones.  Strides are in elements.
+struct PagedCache {
+  const int32_t* table;
+  const int32_t* kv_len;    // device: tokens of each sample, the new ones among them
+  const int32_t* q_start;   // device [samples + 1], or nullptr
+  int64_t table_stride, k_page, k_tok, v_page, v_tok;
+  int samples, n_pages, page_shift;
+  int max_q;                // new tokens that a sample has at most
+  int max_kv;               // tokens that a sample has at most (the table holds as many pages)
+};
+
+// ---- paged_attn.cu --------------------------------------------------------
+// Attention of the new tokens to their samples' cached keys: a.q, a.out [n_q = tokens, N_h, D], a.lse [N_h, tokens]; a.k[1] and
+// a.v[1] are the pages.
+size_t paged_scratch_bytes(const SegArgs& a, const PagedCache& c, bool warp_mma);
+cudaError_t launch_paged_attn(const SegArgs& a, const PagedCache& c, bool warp_mma, void* scratch, int* status, cudaStream_t st,
+                              int* launches);
+
+// ---- norm_rope.cu ---------------------------------------------------------
+struct RopeParams {
+  uint64_t turn[64];        // turns per position of each pair, in units of 2^-64
+  uint8_t axis[64];         // component of the position that turns it
+  int rot, axes, interleaved;
+  float magnitude, eps;
+  const int32_t* positions; // device [samples, n, axes], or nullptr: a token's number in its sample
+  int64_t pos_smp;
+  const float* weight[2];   // device [D], of q and k; nullptr: no norm
+  const void* src[3];       // q, k, v; nullptr: not part of the call (v: only with a cache)
+  void* dst[3];             // with a cache: k and v are its pages
+  int64_t s_tok[3], s_smp[3], d_tok[3], d_smp[3];
+  int64_t tokens;           // of all samples
+  int n;                    // of one
+  int N_h, N_kv, D, dtype, sms;
+  bool paged;
+  PagedCache cache;
+  int* status;
+  int slabs, slab_k, slab_v, per, parts;      // filled in by launch_norm_rope
+};
+// |freq| radians as turns in units of 2^-64, modulo a turn
+uint64_t turns_of(double freq);
+cudaError_t launch_norm_rope(RopeParams& p, cudaStream_t st, int* launches);
+
 }  // namespace swam

@@ -7,6 +7,7 @@ library is missing or cannot be loaded, importing a symbol raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional, Tuple
 
@@ -30,7 +31,8 @@ EXPORTS = [
     "swam_create", "swam_destroy", "swam_workspace_bytes", "swam_bind_workspace", "swam_score", "swam_score_noalloc",
     "swam_select", "swam_aggregate", "swam_select_maps",
     "swam_pack", "swam_sparse_attn", "swam_scatter", "swam_cross_attn", "swam_cross_attn_scratch_bytes",
-    "swam_prefix_attn", "swam_prefix_attn_scratch_bytes", "swam_step", "swam_host_io_bytes", "swam_bind_host_io",
+    "swam_prefix_attn", "swam_prefix_attn_scratch_bytes", "swam_norm_rope", "swam_append_kv", "swam_paged_attn",
+    "swam_paged_attn_scratch_bytes", "swam_step", "swam_host_io_bytes", "swam_bind_host_io",
     "swam_step_host", "swam_host_join", "swam_get_selection", "swam_get_scores", "swam_set_selection", "swam_state_bytes",
     "swam_state_export", "swam_state_import", "swam_check", "swam_selftest_timeout", "swam_launch_floor", "swam_set_option", "swam_launch_count",
     "swam_last_error", "swam_version",
@@ -63,6 +65,77 @@ class SwamPrefixArgs(ctypes.Structure):
                 + [(n, ctypes.c_int64) for n in ("q_token", "q_sample", "k_prefix_token", "k_prefix_group", "v_prefix_token",
                                                  "v_prefix_group", "k_token", "k_sample", "v_token", "v_sample",
                                                  "out_token", "out_sample")])
+
+
+class SwamRope(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float)]
+
+
+class SwamNormRopeArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("rope", "q", "k", "q_out", "k_out", "q_weight", "k_weight", "positions")]
+                + [("n", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+                + [(n, ctypes.c_int64) for n in ("pos_sample", "q_token", "q_sample", "k_token", "k_sample", "q_out_token",
+                                                 "q_out_sample", "k_out_token", "k_out_sample")])
+
+
+class SwamPagedCache(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "page_table", "kv_len", "q_start")]
+                + [(n, ctypes.c_int32) for n in ("n_samples", "n_pages", "page_size", "max_pages", "n_kv_heads", "reserved")]
+                + [(n, ctypes.c_int64) for n in ("table_sample", "k_page", "k_token", "v_page", "v_token")])
+
+
+class SwamAppendArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("cache", "rope", "q", "k", "v", "q_out", "q_weight", "k_weight", "positions")]
+                + [("n_tokens", ctypes.c_int32), ("eps", ctypes.c_float)]
+                + [(n, ctypes.c_int64) for n in ("q_token", "k_token", "v_token", "q_out_token")])
+
+
+class SwamPagedArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("cache", "q", "out", "lse", "scratch")] + [("scratch_bytes", ctypes.c_size_t)]
+                + [(n, ctypes.c_int32) for n in ("n_tokens", "max_q", "max_kv", "causal")]
+                + [(n, ctypes.c_int64) for n in ("q_token", "out_token")])
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, factor: float = 1.0, trained: int = 0, turns_low: float = 1.0,
+                     turns_high: float = 32.0):
+    """Radians per position of the rot_dim / 2 pairs: base^(-2i / rot_dim).  `factor` > 1 stretches them for contexts longer than
+    the `trained` positions: a pair that turns more than turns_high times in those stays as it is, one that turns less than
+    turns_low times is slowed down by the factor, in proportion between; trained = 0 slows down all of them alike (linear
+    interpolation).  Peng et al., YaRN (2023), whose magnitude is rope_magnitude(factor)."""
+    if rot_dim < 2 or rot_dim % 2 or not base > 0 or not factor >= 1 or trained < 0 or not turns_high > turns_low:
+        raise ValueError("rope_frequencies: rot_dim must be even, base positive, factor at least 1, turns_low < turns_high")
+    out = []
+    for i in range(rot_dim // 2):
+        f = base ** (-2 * i / rot_dim)
+        keep = min(1.0, max(0.0, (trained * f / (2 * math.pi) - turns_low) / (turns_high - turns_low))) if trained else 0.0
+        out.append(f * (keep + (1 - keep) / factor))
+    return out
+
+
+def rope_magnitude(factor: float) -> float:
+    return 1.0 if factor <= 1 else 0.1 * math.log(factor) + 1.0
+
+
+class Rope:
+    """Rotary positions: radians per position of each pair, the component of the position that turns it (default: the only one),
+    pairs (i, i + rot/2) or, interleaved, (2i, 2i + 1), and the factor on the rotated elements."""
+
+    def __init__(self, freq, axes=None, interleaved: bool = False, magnitude: float = 1.0):
+        freq = [float(f) for f in freq]
+        axes = None if axes is None else [int(a) for a in axes]
+        if not freq or (axes is not None and len(axes) != len(freq)):
+            raise ValueError("Rope: one frequency, and one axis where axes are given, for each pair")
+        if axes is not None and min(axes) < 0:
+            raise ValueError("Rope: negative axis")
+        if not magnitude > 0:
+            raise ValueError("Rope: magnitude must be positive")
+        self.rot_dim, self.n_axes = 2 * len(freq), 1 if axes is None else max(axes) + 1
+        self._freq = (ctypes.c_double * len(freq))(*freq)
+        self._axis = None if axes is None else (ctypes.c_int32 * len(axes))(*axes)
+        self._c = SwamRope(ctypes.addressof(self._freq), None if axes is None else ctypes.addressof(self._axis), self.rot_dim,
+                           self.n_axes, int(interleaved), magnitude)
+        self.address = ctypes.addressof(self._c)
 
 
 class SwamError(RuntimeError):
@@ -100,6 +173,9 @@ def load_library() -> ctypes.CDLL:
         for name, args in (("cross", SwamCrossArgs), ("prefix", SwamPrefixArgs)):
             getattr(lib, f"swam_{name}_attn").argtypes = [vp, ctypes.POINTER(args), vp]
             getattr(lib, f"swam_{name}_attn_scratch_bytes").argtypes = [vp, ctypes.POINTER(args), ctypes.POINTER(ctypes.c_size_t)]
+        for name, args in (("norm_rope", SwamNormRopeArgs), ("append_kv", SwamAppendArgs), ("paged_attn", SwamPagedArgs)):
+            getattr(lib, f"swam_{name}").argtypes = [vp, ctypes.POINTER(args), vp]
+        lib.swam_paged_attn_scratch_bytes.argtypes = [vp, ctypes.POINTER(SwamPagedArgs), ctypes.POINTER(ctypes.c_size_t)]
         lib.swam_step.argtypes = [vp, vp, vp, vp, i32, vp, vp]
         lib.swam_step_host.argtypes = [vp, vp, vp, vp, i32, vp, vp]
         lib.swam_host_join.argtypes = [vp, vp]
@@ -384,6 +460,160 @@ class Swam:
         key = (n_q, n_prefix, n_own, groups, heads, a.causal)
         scratch = self._scratch(self.lib.swam_prefix_attn_scratch_bytes, a, key)  # noqa: F841
         rc = self.lib.swam_prefix_attn(self.ctx, ctypes.byref(a), _raw_stream())
+        if rc != OK:
+            self._chk(rc)
+        return (out, lse) if want_lse else out
+
+    # -- norms, rotary positions and the paged cache -------------------------
+    def _weight(self, name: str, t: Optional[torch.Tensor]):
+        if t is None:
+            return None
+        if t.dtype is not torch.float32 or t.get_device() != self._device_index or t.shape != (self.D,) or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous float32 tensor of shape [{self.D}] on {self.device}")
+        return t.data_ptr()
+
+    def _ints(self, name: str, t: torch.Tensor, shape: tuple):
+        if t.dtype is not torch.int32 or t.get_device() != self._device_index or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {list(shape)} on {self.device}")
+        return t.data_ptr()
+
+    def _packed(self, name: str, t: torch.Tensor, tokens: int, heads: int) -> int:
+        """Token stride of a [tokens, heads, D] tensor whose heads are contiguous (0: contiguous)."""
+        if t.dtype is not self._torch_dtype or t.get_device() != self._device_index or t.shape != (tokens, heads, self.D):
+            raise ValueError(f"{name}: expected a {self._torch_dtype} tensor of shape [{tokens}, {heads}, {self.D}] on {self.device}")
+        if tokens == 0 or t.is_contiguous():
+            return 0
+        s0, s1, s2 = t.stride()
+        if s2 != 1 or (heads > 1 and s1 != self.D):
+            raise ValueError(f"{name}: the heads of a token must be contiguous")
+        if tokens > 1 and s0 == 0:
+            raise ValueError(f"{name}: expanded (stride 0) tokens are not accepted")
+        return s0 if tokens > 1 else heads * self.D
+
+    def norm_rope(self, q=None, k=None, rope: Optional[Rope] = None, positions=None, q_weight=None, k_weight=None,
+                  eps: float = 1e-6, q_out=None, k_out=None):
+        """Queries [B, n, N_h, D] and / or keys [B, n, heads, D] (any divisor of N_h heads) normalised per head (where a float32
+        weight [D] is given) and rotated (where `rope` is given).  positions: int32 [B, n, axes] or [n, axes] for all samples
+        alike ([B, n] or [n] with one axis); default: token t at position t.  Tensors may be strided views with
+        contiguous heads; an output may be its input.  Returns (q', k') (None where there was none)."""
+        if q is None and k is None:
+            raise ValueError("neither q nor k given")
+        n = (k if q is None else q).shape[1] if (k if q is None else q).dim() == 4 else -1
+        a = SwamNormRopeArgs()
+        if q is not None:
+            a.q_token, a.q_sample = self._tokens("q", q, self.B, self.N_h)
+            if q_out is None:
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            elif q_out.shape != q.shape:
+                raise ValueError(f"q_out: expected shape {list(q.shape)}")
+            a.q_out_token, a.q_out_sample = self._tokens("q_out", q_out, self.B, self.N_h)
+            a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if k is not None:
+            heads = k.shape[2] if k.dim() == 4 else 0
+            a.k_token, a.k_sample = self._tokens("k", k, self.B, heads)
+            if k.shape[1] != n:
+                raise ValueError("q and k differ in length")
+            if k_out is None:
+                k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+            elif k_out.shape != k.shape:
+                raise ValueError(f"k_out: expected shape {list(k.shape)}")
+            a.k_out_token, a.k_out_sample = self._tokens("k_out", k_out, self.B, heads)
+            a.k, a.k_out, a.n_kv_heads = k.data_ptr(), k_out.data_ptr(), heads
+        elif k_out is not None:
+            raise ValueError("k_out without k")
+        a.n, a.eps = n, eps
+        a.q_weight, a.k_weight = self._weight("q_weight", q_weight), self._weight("k_weight", k_weight)
+        if rope is not None:
+            a.rope = rope.address
+            if positions is not None:
+                ax = rope.n_axes
+                shape = tuple(positions.shape)
+                if shape in ((n, ax), (n,) if ax == 1 else None):
+                    a.positions = self._ints("positions", positions, shape)
+                elif shape in ((self.B, n, ax), (self.B, n) if ax == 1 else None):
+                    a.positions, a.pos_sample = self._ints("positions", positions, shape), n * ax
+                else:
+                    raise ValueError(f"positions: expected shape [{self.B}, {n}, {ax}] or [{n}, {ax}], got {list(shape)}")
+        rc = self.lib.swam_norm_rope(self.ctx, ctypes.byref(a), _raw_stream())
+        if rc != OK:
+            self._chk(rc)
+        return q_out, k_out
+
+    def _cache(self, k_pages, v_pages, page_table, kv_len, q_start) -> SwamPagedCache:
+        if k_pages.dim() != 4 or k_pages.shape != v_pages.shape:
+            raise ValueError("k_pages and v_pages: expected the same 4-dimensional shape [pages, page size, heads, head dim]")
+        n_pages, page, heads, _ = k_pages.shape
+        k_tok, k_page = self._tokens("k_pages", k_pages, None, heads)
+        v_tok, v_page = self._tokens("v_pages", v_pages, None, heads)
+        samples = kv_len.shape[0] if kv_len.dim() == 1 else 0
+        if page_table.dtype is not torch.int32 or page_table.get_device() != self._device_index or page_table.dim() != 2 or \
+                page_table.shape[0] != samples or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError(f"page_table: expected an int32 tensor of shape [{samples}, pages] with contiguous rows on {self.device}")
+        max_pages = page_table.shape[1]
+        stride = page_table.stride(0) if samples > 1 else max_pages
+        if samples > 1 and stride < max_pages:
+            raise ValueError("page_table: rows overlap")
+        return SwamPagedCache(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
+                              self._ints("kv_len", kv_len, (samples,)),
+                              None if q_start is None else self._ints("q_start", q_start, (samples + 1,)), samples, n_pages,
+                              page, max_pages, heads, 0, stride, k_page, k_tok, v_page, v_tok)
+
+    def append_kv(self, k, v, k_pages, v_pages, page_table, kv_len, q_start=None, q=None, rope: Optional[Rope] = None,
+                  positions=None, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None):
+        """New tokens' keys k (normalised and rotated on the way) and values v [tokens, heads, D] into the cache k_pages, v_pages
+        [pages, page size, heads, D]; where q [tokens, N_h, D] is given, returns it normalised and rotated.  Sample b owns the
+        tokens [q_start[b], q_start[b + 1]) (int32 [samples + 1]; default: all samples equally many), the last ones of its kv_len[b]
+        (int32 [samples]); token c of it lives in row c % page size of page page_table[b, c / page size] (int32 [samples, pages]).
+        positions: int32 [tokens, axes] ([tokens] with one axis); default: a token's number in its sample."""
+        tokens = k.shape[0] if k.dim() == 3 else 0
+        c = self._cache(k_pages, v_pages, page_table, kv_len, q_start)
+        heads = c.n_kv_heads
+        a = SwamAppendArgs()
+        a.cache = ctypes.addressof(c)
+        a.k, a.v = k.data_ptr(), v.data_ptr()
+        a.k_token, a.v_token = self._packed("k", k, tokens, heads), self._packed("v", v, tokens, heads)
+        if q is not None:
+            a.q_token = self._packed("q", q, tokens, self.N_h)
+            if q_out is None:
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            a.q_out_token = self._packed("q_out", q_out, tokens, self.N_h)
+            a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        a.q_weight, a.k_weight = self._weight("q_weight", q_weight), self._weight("k_weight", k_weight)
+        if rope is not None:
+            a.rope = rope.address
+            if positions is not None:
+                shape = (tokens, rope.n_axes)
+                if rope.n_axes == 1 and positions.dim() == 1:
+                    shape = (tokens,)
+                a.positions = self._ints("positions", positions, shape)
+        a.n_tokens, a.eps = tokens, eps
+        rc = self.lib.swam_append_kv(self.ctx, ctypes.byref(a), _raw_stream())
+        if rc != OK:
+            self._chk(rc)
+        return q_out
+
+    def paged_attn(self, q, k_pages, v_pages, page_table, kv_len, q_start=None, max_q: int = 0, max_kv: int = 0,
+                   causal: bool = False, out=None, want_lse: bool = False):
+        """New tokens' queries [tokens, N_h, D] attend their sample's cached keys [0, kv_len[b]); `causal`: token i of n sees those up
+        to kv_len[b] - n + i.  The cache and q_start as in append_kv.  max_q, max_kv: bounds of the new tokens and the keys of a
+        sample (0: all tokens, the table's pages); close ones pay.  A row without keys gives zeros (lse -inf).  Returns out, or
+        (out, lse [N_h, tokens])."""
+        tokens = q.shape[0] if q.dim() == 3 else 0
+        c = self._cache(k_pages, v_pages, page_table, kv_len, q_start)
+        q_tok = self._packed("q", q, tokens, self.N_h)
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        o_tok = self._packed("out", out, tokens, self.N_h)
+        lse = torch.empty((self.N_h, tokens), dtype=torch.float32, device=self.device) if want_lse else None
+        a = SwamPagedArgs(ctypes.addressof(c), q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else None, None, 0, tokens,
+                          max_q, max_kv, 1 if causal else 0, q_tok, o_tok)
+        key = ("paged", tokens, c.n_samples, c.n_pages, c.page_size, c.max_pages, c.n_kv_heads, q_start is None, max_q, max_kv)
+        scratch = self._scratch(self.lib.swam_paged_attn_scratch_bytes, a, key)  # noqa: F841
+        rc = self.lib.swam_paged_attn(self.ctx, ctypes.byref(a), _raw_stream())
         if rc != OK:
             self._chk(rc)
         return (out, lse) if want_lse else out
