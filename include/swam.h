@@ -276,7 +276,8 @@ typedef struct {
   const int32_t* page_table; /* dev [n_samples, max_pages], table_sample elements from one row to the next (0: max_pages) */
   const int32_t* kv_len;     /* dev [n_samples] */
   const int32_t* q_start;    /* dev [n_samples + 1], or NULL */
-  int32_t n_samples, n_pages;
+  int32_t n_samples;         /* at most 65535 */
+  int32_t n_pages;
   int32_t page_size;         /* a power of two, 16 .. 2^20 */
   int32_t max_pages;         /* max_pages * page_size at most 2^29 */
   int32_t n_kv_heads;        /* 0 = the context's; must divide n_heads */
@@ -313,7 +314,7 @@ int swam_append_kv(swam_ctx* ctx, const swam_append_args* args, void* stream);
  * page_size).  They choose the kernel and how the keys are cut, so close bounds pay.
  * scratch: device memory of swam_paged_attn_scratch_bytes (256-byte aligned, NULL if 0), as in (6): the size depends on the
  * sizes in the arguments only, and calls that may overlap need scratch of their own.  SWAM_OPT_ATTN_VARIANT applies.
- * Limits: n_tokens * N_h at most 2^30, n_samples at most 2^20 (SWAM_ERR_UNSUPPORTED beyond). */
+ * Limits: n_tokens * N_h at most 2^30 (SWAM_ERR_UNSUPPORTED beyond). */
 typedef struct {
   const swam_paged_cache* cache; /* host */
   const void* q;

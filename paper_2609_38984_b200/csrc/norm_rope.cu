@@ -7,47 +7,74 @@
 // angle: one 64-bit product, exact but for the frequency's own rounding, whatever the position.  The nearest quarter turn is
 // taken off as an integer; sine and cosine of the rest (at most an eighth of a turn) are their Taylor series up to x^9 and x^10,
 // whose next terms are below 2e-9 (of sin) and 2e-10.
-// Work: a warp owns a token and up to `per` slabs of its rows.  A slab is one kind of row (q, k or v), kBatch times as many as the warp
-// holds at 16 bytes a lane, all loaded before the first is used.  The warp works out the token's cosines and sines once, in
-// shared memory; a lane keeps those of its 16 bytes in registers for all rows.  The other half of a pair comes by shuffle (pairs i,
-// i + rot/2) or is in the same 16 bytes (2i, 2i + 1); a rot/2 that ends inside 16 bytes reads it from memory again (L1).
+// Work: a CTA of eight warps owns a few tokens.  It finds out where they are and works out their cosines and sines once, in shared
+// memory.  The rows of a token (of q, then k, then v) are cut into items, as many rows as a warp holds at two times 16 bytes a lane; a warp
+// owns a token's items, or a share of them where tokens are few.  Items arrive by asynchronous copies, kRing ahead, the first of them
+// requested before the tokens are looked up; a lane copies what it will read itself, so that no barrier is needed.  A lane holds both
+// halves of each of its pairs: 16 bytes of the first half and 16 of the second (pairs i, i + rot/2), or 32 in a row (2i, 2i + 1); it keeps
+// their cosines and sines, times the weights, for all items of a kind, so that an element costs a product, a fused one and the product with
+// the reciprocal root.  Where rot/2 ends inside 16 bytes the other half is read again, element by element (L1).
 #include <math.h>
 
-#include "swam_internal.cuh"
+#include "seg_attn.cuh"
 
 namespace swam {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kBatch = 4;
+constexpr int kTokens = 32;        // of a CTA, at most
+constexpr int kRing = 4;           // items in flight, of a warp
+
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 parts(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 
 template <typename T>
-struct Chunk;                      // 16 bytes
+struct Chunk;                      // 16 bytes as pairs of neighbours
 template <>
 struct Chunk<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void unpack(const uint4& u, float (&x)[4]) {
-    x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
+  static __device__ __forceinline__ void unpack(const uint4& u, uint64_t (&x)[2]) {
+    x[0] = pair(__uint_as_float(u.x), __uint_as_float(u.y));
+    x[1] = pair(__uint_as_float(u.z), __uint_as_float(u.w));
   }
-  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  static __device__ __forceinline__ uint4 pack(const uint64_t (&x)[2]) {
+    const float2 a = parts(x[0]), b = parts(x[1]);
+    return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
   }
 };
 template <>
 struct Chunk<__nv_bfloat16> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void unpack(const uint4& u, float (&x)[8]) {
+  static __device__ __forceinline__ void unpack(const uint4& u, uint64_t (&x)[4]) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i) x[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
   }
-  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+  static __device__ __forceinline__ uint4 pack(const uint64_t (&x)[4]) {
     uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = parts(x[i]);
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v.y), "f"(v.x));
+    }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
 };
@@ -71,187 +98,313 @@ __device__ __forceinline__ float2 cos_sin(uint64_t phase) {
   return make_float2((quarter == 1) | (quarter == 2) ? -a : a, quarter >= 2 ? -b : b);
 }
 
-// The sample of packed token t, and t's place behind the sample's first one.  Two levels of 32 at a time.
-__device__ __forceinline__ int find_sample(const int32_t* start, int n, int t, int lane) {
-  int lo = 0, hi = n;              // start[lo] <= t, and start[hi] > t where hi < n
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 31) / 32;
-    const int i = lo + lane * step;
-    const bool below = i < hi && (lane == 0 || __ldg(start + i) <= t);
-    const uint32_t m = __ballot_sync(0xffffffffu, below);
-    const int last = 31 - __clz(m);
-    const int next = lo + last * step;
-    hi = min(hi, next + step);
-    lo = next;
-  }
-  return lo;
+// A token: where its rows are (in elements; dst < 0: they are not written) and its position.
+struct Token {
+  int64_t src[3], dst[3], positions;
+  int number;                      // default position
+};
+
+__device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint4 shared_16(uint32_t src) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
+  return v;
 }
 
-// kPair: 0 = (i, i + rot/2) by shuffle, 1 = (2i, 2i + 1), 2 = (i, i + rot/2) from memory
+// kPair: 0 = (i, i + rot/2), 1 = (2i, 2i + 1), 2 = (i, i + rot/2) with a half that ends inside 16 bytes
 template <typename T, int D, int kPair, bool kCache>
-__global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_constant__ RopeParams p) {
-  constexpr int N = Chunk<T>::N;           // elements of a lane
-  constexpr int LPR = D / N;               // lanes of a row
-  constexpr int RPW = 32 / LPR;            // rows of a warp
-  __shared__ float2 turn[kWarps][64];
+__global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_kernel(const __grid_constant__ RopeParams p) {
+  constexpr int N = Chunk<T>::N, N2 = N / 2;     // elements of 16 bytes, and pairs of neighbours
+  constexpr int LPR = D / (2 * N);               // lanes of a row
+  constexpr int RPW = 32 / LPR;                  // rows of an item
+  extern __shared__ __align__(16) uint4 ring[];                  // [warp][kRing][2][lane], then the angles
+  float* cosv = reinterpret_cast<float*>(ring + kWarps * kRing * 64);        // [token][half]
+  float* sinv = cosv + p.per * (D / 2);
+  __shared__ Token token[kTokens];
+  __shared__ uint64_t turns[D / 2];
+  __shared__ int owner[kTokens];                 // kCache: sample, -1: nobody's
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t unit = (int64_t)blockIdx.x * kWarps + warp;
-  const int64_t t64 = unit / p.parts;
-  if (t64 >= p.tokens) return;
-  const int t = (int)t64;
-  const int slab0 = (int)(unit - t64 * p.parts) * p.per, slab1 = min(slab0 + p.per, p.slabs);
-  const int col = (lane % LPR) * N, sub = lane / LPR;
-
-  // where the token is, and its position
+  const int t0 = (int)blockIdx.x * p.per, count = min(p.per, (int)p.tokens - t0);
+  const int l = lane % LPR, sub = lane / LPR, half = p.rot >> 1;
+  // first elements of the lane's two times 16 bytes.  kPair = 0: the halves of its pairs, or neighbours of the part that does not turn
+  const int turning = kPair == 0 ? half / N : 0;
+  const int e0 = kPair == 0 && l >= turning ? (2 * l) * N : (kPair == 0 ? l : 2 * l) * N;
+  const int e1 = kPair == 0 && l < turning ? e0 + half : e0 + N;
+  if (threadIdx.x < half) turns[threadIdx.x] = p.turn[threadIdx.x];
+  // ---- where the tokens come from, one thread each (packed tokens are one sequence)
+  const int t = t0 + (int)threadIdx.x;
   int b = 0, i = t;
-  bool real = true;                        // kCache: has the token a place in the cache
-  int64_t k_at = 0, v_at = 0;
-  int number = t;
-  if constexpr (kCache) {
-    const PagedCache& c = p.cache;
-    int q0, q1;
-    if (c.q_start) {
-      b = find_sample(c.q_start, c.samples, t, lane);
-      q0 = __ldg(c.q_start + b);
-      q1 = __ldg(c.q_start + b + 1);
-      if (t < q0 || t >= q1) return;       // in front of the first sample or behind the last one
-      if (q0 < 0 || q1 > p.tokens) {
-        if (lane == 0) atomicOr(p.status, ST_BAD_LEN);
-        return;
-      }
-    } else {
-      b = t / c.max_q;
-      q0 = b * c.max_q;
-      q1 = q0 + c.max_q;
+  if (threadIdx.x < count) {
+    if (!kCache) {
+      b = t / p.n;
+      i = t - b * p.n;
     }
-    number = __ldg(c.kv_len + b) - (q1 - t);
-    const int slot = number;
-    real = slot >= 0 && slot < c.max_kv;
-    int bad = real ? 0 : ST_BAD_LEN;
-    if (real) {
-      const int page = __ldg(c.table + b * c.table_stride + (slot >> c.page_shift));
-      const int row = slot & ((1 << c.page_shift) - 1);
-      if (page < 0 || page >= c.n_pages) {
-        real = false;
-        bad = ST_BAD_MAP;
-      }
-      k_at = page * c.k_page + row * c.k_tok;
-      v_at = page * c.v_page + row * c.v_tok;
-    }
-    if (bad && lane == 0) atomicOr(p.status, bad);
-  } else {
-    b = t / p.n;
-    i = t - b * p.n;
-    number = i;
+    for (int j = 0; j < 3; ++j) token[threadIdx.x].src[j] = b * p.s_smp[j] + (int64_t)i * p.s_tok[j];
+    if (kCache) owner[threadIdx.x] = p.cache.q_start ? -1 : t / p.cache.max_q;
   }
-  float cs[N], sn[N];                      // of this lane's elements
-  const int half = p.rot >> 1;
-  const bool turned = col < p.rot;         // (some of) the lane's elements are
-  if (p.rot > 0) {
-    for (int j = lane; j < half; j += 32) {
-      const int pos = p.positions ? __ldg(p.positions + (kCache ? 0 : b * p.pos_smp) + (int64_t)i * p.axes + p.axis[j]) : number;
-      float2 x = cos_sin(p.turn[j] * (uint64_t)(int64_t)pos);
-      turn[warp][j] = make_float2(x.x * p.magnitude, x.y * p.magnitude);
-    }
-    __syncwarp();
-  }
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int e = col + j;
-    const float2 x = e < p.rot ? turn[warp][kPair == 1 ? e >> 1 : (e < half ? e : e - half)] : make_float2(1.f, 0.f);
-    cs[j] = x.x;
-    // the sign of the other element's share
-    sn[j] = (kPair == 1 ? (e & 1) == 0 : e < half) ? -x.y : x.y;
-  }
-  const int step = kPair == 0 ? half / N : 0;      // lanes to the other half of a pair
-  const int other = kPair == 0 && turned ? (lane - lane % LPR) + (col < half ? lane % LPR + step : lane % LPR - step) : lane;
+  __syncthreads();
 
-  for (int s = slab0; s < slab1; ++s) {
-    const int kind = s < p.slab_k ? 0 : (s < p.slab_v ? 1 : 2);
-    const int first = (s - (kind == 0 ? 0 : (kind == 1 ? p.slab_k : p.slab_v))) * (RPW * kBatch) + sub;
-    const int heads = kind == 0 ? p.N_h : p.N_kv;
-    // (packed tokens are one sequence: their sample does not matter to where they are)
-    const T* src = (const T*)p.src[kind] + (kCache ? 0 : b * p.s_smp[kind]) + (int64_t)i * p.s_tok[kind] + col;
-    T* dst;
-    if (kCache && kind > 0) dst = (T*)p.dst[kind] + (kind == 1 ? k_at : v_at) + col;
-    else dst = (T*)p.dst[kind] + (kCache ? 0 : b * p.d_smp[kind]) + (int64_t)i * p.d_tok[kind] + col;
-    uint4 u[kBatch];
-#pragma unroll
-    for (int r = 0; r < kBatch; ++r) {
-      const int h = first + r * RPW;
-      u[r] = h < heads ? *reinterpret_cast<const uint4*>(src + (int64_t)h * D) : make_uint4(0u, 0u, 0u, 0u);
-    }
-    if (kind == 2) {
-#pragma unroll
-      for (int r = 0; r < kBatch; ++r) {
-        const int h = first + r * RPW;
-        if (real && h < heads) *reinterpret_cast<uint4*>(dst + (int64_t)h * D) = u[r];
+  // ---- loads: the warp's items, one unit (a token, or share `u % split` of it) after the other
+  const uint32_t slots = (uint32_t)__cvta_generic_to_shared(ring) + (uint32_t)(warp * kRing * 64 + lane) * 16;
+  const int units = count * p.split;
+  auto begin_of = [&](int u) { return p.split == 1 ? 0 : (u % p.split) * p.share; };
+  auto end_of = [&](int u) { return p.split == 1 ? p.items : min((u % p.split + 1) * p.share, p.items); };
+  int lu = warp, ln = begin_of(warp), lend = ln, lrows = 0, issued = 0;       // lend: items up to the end of the kind; lrows: rows left of it
+  const T* lrow = nullptr;
+  auto request = [&]() {
+    if (ln == lend) {                    // another kind, or another unit
+      while (lu < units && ln >= end_of(lu)) {
+        lu += kWarps;
+        ln = begin_of(lu);
       }
-      continue;
-    }
-    float w[N];
-    const float* weight = p.weight[kind];
-    if (weight) {
-#pragma unroll
-      for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(w + j) = __ldg(reinterpret_cast<const float4*>(weight + col + j));
-    }
-#pragma unroll
-    for (int r = 0; r < kBatch; ++r) {
-      const int h = first + r * RPW;
-      float x[N], y[N];
-      Chunk<T>::unpack(u[r], x);
-      float inv = 1.f;
-      if (weight) {
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < N; ++j) sum = fmaf(x[j], x[j], sum);
-#pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        inv = rsqrtf(fmaf(sum, 1.f / D, p.eps));
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[j] *= inv * w[j];
+      lend = ln;
+      lrows = 0;
+      if (lu < units) {
+        const int kind = ln < p.items_k ? 0 : (ln < p.items_v ? 1 : 2);
+        lend = min(end_of(lu), kind == 0 ? p.items_k : (kind == 1 ? p.items_v : p.items));
+        const int h = (ln - (kind == 0 ? 0 : (kind == 1 ? p.items_k : p.items_v))) * RPW + sub;
+        lrows = (kind == 0 ? p.N_h : p.N_kv) - h;
+        lrow = (const T*)p.src[kind] + token[p.split == 1 ? lu : lu / p.split].src[kind] + h * D;
       }
-      if constexpr (kPair == 1) {
+    }
+    if (lrows > 0) {
+      const uint32_t slot = slots + (issued % kRing) * 1024;
+      copy_16(slot, lrow + e0);
+      copy_16(slot + 512, lrow + e1);
+    }
+    lrow += RPW * D;
+    lrows -= RPW;
+    if (ln < lend) ++ln;
+    ++issued;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll 1
+  for (int i = 0; i < kRing; ++i) request();
+
+  // ---- where they go, and their positions
+  if (kCache && p.cache.q_start) {
+    // every sample claims its tokens
+    for (int smp = threadIdx.x; smp < p.cache.samples; smp += 32 * kWarps) {
+      const int q0 = __ldg(p.cache.q_start + smp), q1 = __ldg(p.cache.q_start + smp + 1);
+      if (q0 < 0 || q0 > q1 || q1 > p.tokens) atomicOr(p.status, ST_BAD_LEN);
+      else
+        for (int x = max(q0, t0); x < min(q1, t0 + count); ++x) owner[x - t0] = smp;
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x < count) {
+    Token& k = token[threadIdx.x];
+    int number = i;
+    int64_t k_at = -1, v_at = -1;
+    bool mine = true;                      // somebody's token
+    if constexpr (kCache) {
+      const PagedCache& c = p.cache;
+      int bad = 0;
+      const int smp = owner[threadIdx.x];
+      mine = smp >= 0;
+      const int q1 = !mine ? 0 : (c.q_start ? __ldg(c.q_start + smp + 1) : (smp + 1) * c.max_q);
+      number = mine ? __ldg(c.kv_len + smp) - (q1 - t) : 0;
+      if (mine && number >= 0 && number < c.max_kv) {
+        const int page = __ldg(c.table + smp * c.table_stride + (number >> c.page_shift));
+        const int row = number & ((1 << c.page_shift) - 1);
+        if (page >= 0 && page < c.n_pages) {
+          k_at = page * c.k_page + row * c.k_tok;
+          v_at = page * c.v_page + row * c.v_tok;
+        } else {
+          bad = ST_BAD_MAP;
+        }
+      } else if (mine) {
+        bad = ST_BAD_LEN;
+      }
+      if (bad) atomicOr(p.status, bad);
+    }
+    k.dst[0] = mine ? b * p.d_smp[0] + (int64_t)i * p.d_tok[0] : -1;
+    k.dst[1] = kCache ? k_at : b * p.d_smp[1] + (int64_t)i * p.d_tok[1];
+    k.dst[2] = v_at;
+    k.positions = b * p.pos_smp + (int64_t)i * p.axes;
+    k.number = number;
+  }
+  __syncthreads();
+  // ---- their angles
+  for (int x = threadIdx.x; x < count * half; x += 32 * kWarps) {
+    const int k = x / half, j = x - k * half;
+    const uint64_t turn = turns[j];
+    const int pos = p.positions ? __ldg(p.positions + token[k].positions + (int)(turn & 7)) : token[k].number;
+    const float2 v = cos_sin((turn & ~7ull) * (uint64_t)(int64_t)pos);
+    cosv[k * (D / 2) + j] = v.x * p.magnitude;
+    sinv[k * (D / 2) + j] = v.y * p.magnitude;
+  }
+  __syncthreads();
+
+  int taken = 0;
+  for (int u = warp; u < units; u += kWarps) {
+    const int k = p.split == 1 ? u : u / p.split, end = end_of(u);
+    for (int n = begin_of(u); n < end;) {
+      const int kind = n < p.items_k ? 0 : (n < p.items_v ? 1 : 2);
+      const int first = kind == 0 ? 0 : (kind == 1 ? p.items_k : p.items_v), last = min(end, kind == 0 ? p.items_k : (kind == 1 ? p.items_v : p.items));
+      const int heads = kind == 0 ? p.N_h : p.N_kv;
+      const float* weight = kind < 2 ? p.weight[kind] : nullptr;
+      const int64_t to = token[k].dst[kind];
+      int rows = heads - (n - first) * RPW - sub;          // of the lane's place, left
+      T* dst = (T*)p.dst[kind] + to + (heads - rows) * D;
+      if (to < 0) rows = 0;
+      // what the lane's elements (x, y: its first and second 16 bytes) are multiplied with:
+      //   kPair 0: x' = x xx + y xy, y' = y yy + x yx;   kPair 1: x' = x xx + swapped(x) xy, y' = y yy + swapped(y) yx
+      uint64_t xx[N2], xy[N2], yx[N2], yy[N2];
+      if (kind < 2) {
+        // (kPair 0: the lane's pairs are e0 ..., kPair 1: e0 / 2 ...)
+        const int at = k * (D / 2) + (kPair == 0 ? e0 : e0 / 2);
+        const bool turns_any = kPair == 0 ? l < turning : (kPair == 1 && e0 < p.rot);
 #pragma unroll
-        for (int j = 0; j < N; ++j) y[j] = x[j ^ 1];
-      } else if constexpr (kPair == 0) {
+        for (int j = 0; j < N; j += 4) {
+          float4 wa = make_float4(1.f, 1.f, 1.f, 1.f), wb = wa, c = wa, sn = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (weight) {
+            wa = __ldg(reinterpret_cast<const float4*>(weight + e0 + (kPair == 1 ? 2 * j : j)));
+            wb = __ldg(reinterpret_cast<const float4*>(weight + (kPair == 1 ? e0 + 2 * j + 4 : e1 + j)));
+          }
+          if (turns_any) {
+            c = *reinterpret_cast<const float4*>(cosv + at + j);
+            sn = *reinterpret_cast<const float4*>(sinv + at + j);
+          }
+          if constexpr (kPair == 1) {
+            // four pairs: eight elements of the 2 N in a row; those behind rot / 2 do not turn
+            const float wv[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w}, cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {sn.x, sn.y, sn.z, sn.w};
 #pragma unroll
-        for (int j = 0; j < N; ++j) y[j] = __shfl_sync(0xffffffffu, x[j], other);
-      } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const int e = col + j, o = e < half ? e + half : e - half;
-          y[j] = 0.f;
-          if (e < p.rot && h < heads) {
-            y[j] = (float)src[(int64_t)h * D + o - col];
-            if (weight) y[j] *= inv * __ldg(weight + o);
+            for (int d = 0; d < 4; ++d) {
+              const bool on = p.rot == D || e0 + 2 * (j + d) < p.rot;
+              const float cd = on ? cc[d] : 1.f, sd = on ? ss[d] : 0.f;
+              uint64_t& own = j + d < N2 ? xx[(j + d) % N2] : yy[(j + d) % N2];
+              uint64_t& other = j + d < N2 ? xy[(j + d) % N2] : yx[(j + d) % N2];
+              own = pair(cd * wv[2 * d], cd * wv[2 * d + 1]);
+              other = pair(-sd * wv[2 * d + 1], sd * wv[2 * d]);
+            }
+          } else {
+            xx[j / 2] = pair(c.x * wa.x, c.y * wa.y);
+            xx[j / 2 + 1] = pair(c.z * wa.z, c.w * wa.w);
+            xy[j / 2] = pair(-sn.x * wb.x, -sn.y * wb.y);
+            xy[j / 2 + 1] = pair(-sn.z * wb.z, -sn.w * wb.w);
+            yx[j / 2] = pair(sn.x * wa.x, sn.y * wa.y);
+            yx[j / 2 + 1] = pair(sn.z * wa.z, sn.w * wa.w);
+            yy[j / 2] = pair(c.x * wb.x, c.y * wb.y);
+            yy[j / 2 + 1] = pair(c.z * wb.z, c.w * wb.w);
           }
         }
-        __syncwarp();                      // (in place: every element of the row has been read)
       }
+      for (; n < last; ++n) {
+        const uint32_t slot = slots + (taken % kRing) * 1024;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+        uint4 v0 = shared_16(slot), v1 = shared_16(slot + 512);
+        if (kind < 2) {
+          uint64_t x[N2], y[N2];
+          Chunk<T>::unpack(v0, x);
+          Chunk<T>::unpack(v1, y);
+          float inv = 1.f;
+          if (weight) {
+            uint64_t sum2 = 0ull;
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (col + j < p.rot) x[j] = fmaf(x[j], cs[j], y[j] * sn[j]);
-      if (real | (kind == 0) && h < heads) *reinterpret_cast<uint4*>(dst + (int64_t)h * D) = Chunk<T>::pack(x);
+            for (int j = 0; j < N2; ++j) sum2 = fma2(x[j], x[j], fma2(y[j], y[j], sum2));
+            float sum = parts(sum2).x + parts(sum2).y;
+#pragma unroll
+            for (int o = 1; o < LPR; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            inv = rsqrtf(fmaf(sum, 1.f / D, p.eps));
+          }
+          if constexpr (kPair == 0) {
+            if (l < turning) {
+#pragma unroll
+              for (int j = 0; j < N2; ++j) {
+                const uint64_t a = x[j];
+                x[j] = fma2(a, xx[j], mul2(y[j], xy[j]));
+                y[j] = fma2(y[j], yy[j], mul2(a, yx[j]));
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < N2; ++j) {
+                x[j] = mul2(x[j], xx[j]);
+                y[j] = mul2(y[j], yy[j]);
+              }
+            }
+          } else if constexpr (kPair == 1) {
+            // (an element that does not turn keeps nothing of its neighbour, an infinite one included)
+#pragma unroll
+            for (int j = 0; j < N2; ++j) {
+              const float2 a = parts(x[j]), c = parts(y[j]);
+              const uint64_t xt = mul2(pair(a.y, a.x), xy[j]), yt = mul2(pair(c.y, c.x), yx[j]);
+              x[j] = fma2(x[j], xx[j], p.rot == D || e0 + 2 * j < p.rot ? xt : 0ull);
+              y[j] = fma2(y[j], yy[j], p.rot == D || e1 + 2 * j < p.rot ? yt : 0ull);
+            }
+          } else {
+            const T* row = (const T*)p.src[kind] + token[k].src[kind] + ((n - first) * RPW + sub) * D;
+            const bool there = (n - first) * RPW + sub < heads;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+              uint64_t& v = j < N2 ? x[j % N2] : y[j % N2];
+              v = mul2(v, j < N2 ? xx[j % N2] : yy[j % N2]);
+              float own[2] = {parts(v).x, parts(v).y};
+#pragma unroll
+              for (int d = 0; d < 2; ++d) {
+                const int e = e0 + 2 * j + d, o = e < half ? e + half : e - half, at = k * (D / 2) + (e < half ? e : o);
+                if (e < p.rot && there) {
+                  float other = (float)row[o];
+                  if (weight) other *= __ldg(weight + o);
+                  own[d] = fmaf(own[d], cosv[at], e < half ? -other * sinv[at] : other * sinv[at]);
+                }
+              }
+              v = pair(own[0], own[1]);
+            }
+            __syncwarp();                          // (in place: every element of the rows has been read)
+          }
+          if (weight) {
+            const uint64_t inv2 = pair(inv, inv);
+#pragma unroll
+            for (int j = 0; j < N2; ++j) {
+              x[j] = mul2(x[j], inv2);
+              y[j] = mul2(y[j], inv2);
+            }
+          }
+          v0 = Chunk<T>::pack(x);
+          v1 = Chunk<T>::pack(y);
+        }
+        if (rows > 0) {
+          *reinterpret_cast<uint4*>(dst + e0) = v0;
+          *reinterpret_cast<uint4*>(dst + e1) = v1;
+        }
+        dst += RPW * D;
+        rows -= RPW;
+        ++taken;
+        request();                                 // (into the slot whose values have just been used)
+      }
     }
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 template <typename T, int D, int kPair>
 cudaError_t launch_kind(RopeParams& p, cudaStream_t st, int* launches) {
-  constexpr int rows = 32 / (D / Chunk<T>::N) * kBatch;        // of a slab
-  auto slabs = [&](int heads, int kind) { return p.src[kind] ? (heads + rows - 1) / rows : 0; };
-  p.slab_k = slabs(p.N_h, 0);
-  p.slab_v = p.slab_k + slabs(p.N_kv, 1);
-  p.slabs = p.slab_v + slabs(p.N_kv, 2);
-  // a warp for each slab where that does not fill the SMs, else for each token
-  p.per = (int64_t)p.tokens * p.slabs <= (int64_t)p.sms * 64 ? 1 : p.slabs;
-  p.parts = (p.slabs + p.per - 1) / p.per;
-  const int64_t blocks = ((int64_t)p.tokens * p.parts + kWarps - 1) / kWarps;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  constexpr int rows = 32 / (D / (2 * Chunk<T>::N));           // of an item
+  auto items = [&](int heads, int kind) { return p.src[kind] ? (heads + rows - 1) / rows : 0; };
+  p.items_k = items(p.N_h, 0);
+  p.items_v = p.items_k + items(p.N_kv, 1);
+  p.items = p.items_v + items(p.N_kv, 2);
+  // some sixteen items a warp, but at least two CTAs for every SM; of few tokens, several warps share one
+  const int64_t most = p.tokens / (2 * p.sms);
+  int64_t per = (16 * kWarps + p.items - 1) / p.items;
+  if (per > most) per = most;
+  p.per = per < 1 ? 1 : (per > kTokens ? kTokens : (int)per);
+  p.split = p.per >= kWarps ? 1 : kWarps / p.per;
+  if (p.split > p.items) p.split = p.items;
+  p.share = (p.items + p.split - 1) / p.split;
+  if (p.split > 1) p.split = (p.items + p.share - 1) / p.share;
+  const unsigned blocks = (unsigned)((p.tokens + p.per - 1) / p.per);
+  const int smem = kWarps * kRing * 1024 + p.per * D * (int)sizeof(float);
+  static SmemOptIn opt_in[2];
+  const void* kernel = p.paged ? (const void*)norm_rope_kernel<T, D, kPair, true> : (const void*)norm_rope_kernel<T, D, kPair, false>;
+  const cudaError_t e = opt_in[p.paged](kernel, kWarps * kRing * 1024 + kTokens * D * (int)sizeof(float), p.device);
+  if (e != cudaSuccess) return e;
   ++*launches;
-  if (p.paged) norm_rope_kernel<T, D, kPair, true><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(p);
-  else norm_rope_kernel<T, D, kPair, false><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(p);
+  if (p.paged) norm_rope_kernel<T, D, kPair, true><<<blocks, 32 * kWarps, smem, st>>>(p);
+  else norm_rope_kernel<T, D, kPair, false><<<blocks, 32 * kWarps, smem, st>>>(p);
   return cudaGetLastError();
 }
 template <typename T, int D>

@@ -295,6 +295,7 @@ int rope_args(swam_ctx* c, const char* name, const swam_rope* r, const float* q_
   p.D = c->d.D;
   p.dtype = c->d.dtype;
   p.sms = c->sms;
+  p.device = c->device;
   p.axes = 1;
   p.magnitude = 1.f;
   if (r) {
@@ -309,8 +310,7 @@ int rope_args(swam_ctx* c, const char* name, const swam_rope* r, const float* q_
       if (!(fabs(r->freq[i]) <= 1048576.0)) return fail_named(c, SWAM_ERR_INVALID_ARG, name, "frequencies must be finite and at most 2^20");
       const int32_t ax = r->axis ? r->axis[i] : 0;
       if (ax < 0 || ax >= p.axes) return fail_named(c, SWAM_ERR_INVALID_ARG, name, "axis out of range");
-      p.turn[i] = turns_of(r->freq[i]);
-      p.axis[i] = (uint8_t)ax;
+      p.turn[i] = ((turns_of(r->freq[i]) + 4) & ~7ull) | (uint64_t)ax;
     }
   }
   if (!(eps >= 0.f) || eps > 1e30f) return fail_named(c, SWAM_ERR_INVALID_ARG, name, "eps must be finite and not negative");
@@ -335,7 +335,7 @@ int cache_args(swam_ctx* c, const char* name, const swam_paged_cache* x, int32_t
     return bad(SWAM_ERR_INVALID_ARG, "page_size must be a power of two, 16 .. 2^20");
   *N_kv = x->n_kv_heads > 0 ? x->n_kv_heads : d.N_kv;
   if (d.N_h % *N_kv != 0) return bad(SWAM_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
-  if (x->n_samples > 1 << 20) return bad(SWAM_ERR_UNSUPPORTED, "n_samples beyond 2^20");
+  if (x->n_samples > 65535) return bad(SWAM_ERR_UNSUPPORTED, "n_samples beyond 65535");
   if ((int64_t)x->max_pages * x->page_size > kMaxSegTokens) return bad(SWAM_ERR_UNSUPPORTED, "max_pages * page_size beyond 2^29");
   if ((int64_t)n_tokens * d.N_h > 1ll << 30) return bad(SWAM_ERR_UNSUPPORTED, "n_tokens * n_heads beyond 2^30");
   if (n_tokens > 0 && (x->n_samples == 0 || x->n_pages == 0 || x->max_pages == 0))

@@ -279,8 +279,8 @@ cudaError_t launch_paged_attn(const SegArgs& a, const PagedCache& c, bool warp_m
 
 // ---- norm_rope.cu ---------------------------------------------------------
 struct RopeParams {
-  uint64_t turn[64];        // turns per position of each pair, in units of 2^-64
-  uint8_t axis[64];         // component of the position that turns it
+  uint64_t turn[64];        // turns per position of each pair, in units of 2^-64, with the component of the position that turns it in
+                            // place of the last three bits
   int rot, axes, interleaved;
   float magnitude, eps;
   const int32_t* positions; // device [samples, n, axes], or nullptr: a token's number in its sample
@@ -291,11 +291,12 @@ struct RopeParams {
   int64_t s_tok[3], s_smp[3], d_tok[3], d_smp[3];
   int64_t tokens;           // of all samples
   int n;                    // of one
-  int N_h, N_kv, D, dtype, sms;
+  int N_h, N_kv, D, dtype, sms, device;
   bool paged;
   PagedCache cache;
   int* status;
-  int slabs, slab_k, slab_v, per, parts;      // filled in by launch_norm_rope
+  // filled in by launch_norm_rope: tokens of a CTA; items of a token, the first of k and of v; shares of a token and their items
+  int per, items, items_k, items_v, split, share;
 };
 // |freq| radians as turns in units of 2^-64, modulo a turn
 uint64_t turns_of(double freq);

@@ -387,7 +387,7 @@ def test_refusals():
                    dict(out=c.k_pages.data_ptr())):
         assert call(**fields) == bad, fields
     assert call(cache_fields=dict(max_pages=1 << 26)) == swam.ERR_UNSUPPORTED
-    assert call(cache_fields=dict(n_samples=(1 << 20) + 1)) == swam.ERR_UNSUPPORTED
+    assert call(cache_fields=dict(n_samples=1 << 16)) == swam.ERR_UNSUPPORTED
     assert call(n_tokens=1 << 29) == swam.ERR_UNSUPPORTED
     # keys beyond 512 may be cut, which needs scratch
     x = swam.SwamPagedCache.from_buffer_copy(cache)
