@@ -70,9 +70,19 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
     }
     kk.len0 = kk.n0 = 0;
     kk.len1 = paged_limit(a.causal, smp, (min(it.row0 + MR, rows) - 1) / p.g);
-    const int total = (kk.len1 + kKF - 1) / kKF, per = (total + ps.splits - 1) / ps.splits;
+    // pieces of one size for all samples: a short one has fewer
+    const int total = (kk.len1 + kKF - 1) / kKF, per = ((pc.max_kv + kKF - 1) / kKF + ps.splits - 1) / ps.splits;
     kk.begin = min(total, it.split * per);
     kk.end = min(total, kk.begin + per);
+    if (it.split > 0 && kk.begin == kk.end) {
+      // a piece of weight 0
+      for (int r = threadIdx.x; r < min(MR, rows - it.row0); r += kThreadsF) {
+        const SegRow x = seg_row(p, 1, 0, it.h_kv, smp.q0 * p.g + it.row0 + r);
+        p.part_ml[(int64_t)it.split * p.rows + (int64_t)x.t * a.N_h + x.h] = make_float2(-INFINITY, 0.f);
+      }
+      allow_next();
+      return;
+    }
     it.row0 += smp.q0 * p.g;
     row_end = smp.q0 * p.g + rows;
   } else {

@@ -80,7 +80,7 @@ struct SegCfg {
   static constexpr int kData = QB * NQ * kTileBytes + ST * kTileBytes;
   static constexpr int kBars = 8 * (4 * QB + 2 * ST + 2 * kDesc + 2 * NB + 6);
   static constexpr int kDescOff = (kBars + 15) / 16 * 16;
-  static constexpr int kTail = kDescOff + kDesc * (int)sizeof(SegDesc) + 16;
+  static constexpr int kTail = kDescOff + kDesc * (int)sizeof(SegDesc) + 48;       // (paged: answer and barrier of a cancelled launch)
   static constexpr int kBytes = kData + 1024 /*alignment*/ + kTail + (kAlt ? kTile * 8 : 0) /*maxima and sums of stream 1*/;
   static_assert(ST >= 3 && kData <= 224 * 1024 && kBytes <= 227 * 1024, "shared memory");
   static constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 4) << 24);   // + N / 8 at bit 17
@@ -91,6 +91,7 @@ struct SegTcArgs {
   int box_q;        // queries come as boxes of map_q
   int box_out;      // finished tiles leave as boxes of map_o
   int items;        // of the passes of this launch
+  int steal;        // paged: more blocks than SMs, whose items running blocks take over
 };
 
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, int c4) {
@@ -180,6 +181,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     mbar_init(bar_o_free, 8);
     mbar_init(bar_x, 4);
     mbar_init(bar_drain, 1);
+    if (kPaged) mbar_init(base + C::kData + C::kTail - 32, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -261,50 +263,104 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       };
       auto walk = [&](bool keys) {
         if constexpr (kPaged) {
-          // The items of a sample: its key/value heads, pieces, row tiles (the last first: with causal it has the most keys).  Lane l
-          // knows sample base + l and where its items end among those of the 32.
-          int chunk = 0, before = 0, w = blockIdx.x;
-          while (ok && chunk < pc.samples) {
-            const int b = chunk + lane;
-            PagedSample smp{0, 0, 0};
-            if (b < pc.samples) smp = paged_sample(pc, a.n_q, b, p.status);
-            const int tiles = (smp.n * p.g + C::kRows - 1) / C::kRows;
-            int end = tiles * a.N_kv * p.pass[0].splits;
+          // A block per item (of as many as there can be), in the order: samples by falling length (32 at a time), their row tiles (the
+          // last first: with causal it has the most keys), pieces, key/value heads.  Where there are more blocks than SMs, a
+          // running one takes over blocks that have not started yet, one item ahead of need, so that the SMs finish
+          // together whatever the lengths.  Lane l knows sample order[l] and where its items end among those of the 32.
+          int chunk = -32, before = 0, all = 0, w = blockIdx.x, sample = 0, tiles = 0, end = 0, released = 0, held = 0, phase = 0;
+          PagedSample smp{0, 0, 0};
+          const uint32_t answer = base + C::kData + C::kTail - 48, bar_answer = answer + 16;
+          while (ok) {
+            // the 32 samples that item w is in
+            while (chunk < pc.samples && w >= before + all) {
+              before += all;
+              chunk += 32;
+              smp = PagedSample{0, 0, 0};
+              if (chunk + lane < pc.samples) smp = paged_sample(pc, a.n_q, chunk + lane, p.status);
+              int rank = 0;
+#pragma unroll 1
+              for (int j = 0; j < 32; ++j) {
+                const int other = __shfl_sync(0xffffffffu, smp.len, j);
+                rank += other > smp.len || (other == smp.len && j < lane) ? 1 : 0;
+              }
+              int from = 0;
+#pragma unroll 1
+              for (int j = 0; j < 32; ++j)
+                if (__shfl_sync(0xffffffffu, rank, j) == lane) from = j;
+              smp = PagedSample{__shfl_sync(0xffffffffu, smp.q0, from), __shfl_sync(0xffffffffu, smp.n, from), __shfl_sync(0xffffffffu, smp.len, from)};
+              sample = chunk + from;
+              tiles = (smp.n * p.g + C::kRows - 1) / C::kRows;
+              end = tiles * a.N_kv * p.pass[0].splits;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-              const int y = __shfl_up_sync(0xffffffffu, end, o);
-              if (lane >= o) end += y;
+              for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, end, o);
+                if (lane >= o) end += y;
+              }
+              all = __shfl_sync(0xffffffffu, end, 31);
             }
-            const int all = __shfl_sync(0xffffffffu, end, 31);
-            for (; ok && w - before < all; w += gridDim.x) {
+            if (w < before) {
+              chunk = -32;
+              before = all = 0;
+              continue;
+            }
+            if (chunk < pc.samples) {                      // (there may be more blocks than items)
               const int src = __ffs(__ballot_sync(0xffffffffu, end > w - before)) - 1;
               const PagedSample it{__shfl_sync(0xffffffffu, smp.q0, src), __shfl_sync(0xffffffffu, smp.n, src), __shfl_sync(0xffffffffu, smp.len, src)};
               const int rt = __shfl_sync(0xffffffffu, tiles, src), splits = p.pass[0].splits;
               int k = w - before - (__shfl_sync(0xffffffffu, end, src) - rt * a.N_kv * splits);
-              const int row0 = (rt - 1 - k % rt) * C::kRows;
-              k /= rt;
-              const int split = k % splits, rows = it.n * p.g;
-              const int sees = paged_limit(a.causal, it, (min(row0 + C::kRows, rows) - 1) / p.g);
-              const int total = (sees + kTile - 1) / kTile, per = (total + splits - 1) / splits;
-              const int begin = min(total, split * per);
               SegDesc o;
+              o.h_kv = k % a.N_kv;
+              k /= a.N_kv;
+              o.part = k % splits;
+              const int row0 = (rt - 1 - k / splits) * C::kRows, rows = it.n * p.g;
+              const int sees = paged_limit(a.causal, it, (min(row0 + C::kRows, rows) - 1) / p.g);
+              // pieces of one size for all samples: a short one has fewer
+              const int total = (sees + kTile - 1) / kTile, per = ((pc.max_kv + kTile - 1) / kTile + splits - 1) / splits;
+              const int begin = min(total, o.part * per);
               o.n = min(total, begin + per) - begin;
               o.na = 0;
               o.b0 = 0;
-              o.h_kv = k / splits;
               o.row0 = it.q0 * p.g + row0;
               o.base0 = it.q0 * p.g + rows;          // the end of the sample's rows
               o.base1 = begin * kTile;
-              o.part = split;
               o.len0 = 0;
               o.len1 = sees;
               // (seg_limit1 counts from the call's last token: this sample's last one is number q0 + n - 1 of n_q)
               o.own = a.causal ? it.len + a.n_q - it.n - it.q0 : it.len;
-              o.kv0 = chunk + src;
-              emit(o, 1, o.row0, o.base0, keys);
+              o.kv0 = __shfl_sync(0xffffffffu, sample, src);
+              emit(o, 1, o.row0, o.base0, o.n > 0);
+              held += o.n;
             }
-            before += all;
-            chunk += 32;
+            if (!x.steal) break;
+            // The next item is taken when the one before the last is done.  (While those behind it have few tiles it is taken at once,
+            // so that Q K^T and its keys, three tiles ahead at most, never wait for an item that waits for them.)
+            while (ok && i > released && held - desc[released % kDesc].n >= 6) {
+              held -= desc[released % kDesc].n;
+              ok = wait(bar_d_empty(released % kDesc), (released / kDesc) & 1);
+              ++released;
+            }
+            if (!ok) break;
+            if (lane == 0) {
+              mbar_expect_tx(bar_answer, 16);
+              asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar_answer) : "memory");
+            }
+            __syncwarp();
+            ok = wait(bar_answer, phase);
+            if (!ok) {
+              mbar_wait_bounded(bar_answer, phase, kDrainCycles, nullptr);       // the answer must not outlive the block
+              break;
+            }
+            phase ^= 1;
+            uint32_t got, first;
+            asm volatile(
+                "{\n .reg .pred c;\n .reg .b128 a;\n ld.shared.b128 a, [%2];\n"
+                " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 c, a;\n selp.u32 %0, 1, 0, c;\n mov.u32 %1, 0;\n"
+                " @c clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, _, _, _}, a;\n}"
+                : "=r"(got), "=r"(first) : "r"(answer) : "memory");
+            fence_proxy_async();                           // the next answer comes through the other proxy
+            __syncwarp();
+            if (!got) break;                               // none is left (and none may be asked for again)
+            w = (int)first;
           }
         } else {
           for (int w = blockIdx.x; ok && w < x.items; w += gridDim.x) {
@@ -336,7 +392,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         desc[slot].n = 0;                            // the end
         mbar_arrive(bar_d_full(slot));
       }
-      if (empty) walk(false);
+      if (!kPaged && empty) walk(false);
     } else if (warp == 10) {
       // ------------------------------------------------------------------ finished tiles, as boxes
       if (x.box_out) {
@@ -1041,7 +1097,8 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kP
   static SmemOptIn opt_in;
   cudaError_t e = opt_in((const void*)seg_tc_kernel<D, kAlt, kPaged>, smem, a.device);
   if (e != cudaSuccess) return e;
-  const int grid = x.items < a.sms ? x.items : a.sms;
+  const int grid = kPaged || x.items < a.sms ? x.items : a.sms;
+  x.steal = kPaged && x.items > a.sms;
   ++*launches;
   if (pass == 1) return launch_after(seg_tc_kernel<D, kAlt, kPaged>, dim3(grid), dim3(kThreadsS), smem, st, mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
   seg_tc_kernel<D, kAlt, kPaged><<<grid, kThreadsS, smem, st>>>(mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
