@@ -2,16 +2,18 @@
 // head dim 32, and the independent second opinion on the tcgen05 kernel.
 //
 // The new tokens' rows of a sample and key/value head, in the order (token, head of the group), are cut into row tiles of 16 * WR
-// rows.  A unit of work is a tile of 64 keys of a row tile, in the order (sample, key/value head, row tile, key tile); `shares` CTAs
+// rows.  A unit of work is a tile of 64 or 128 keys of a row tile, in the order (sample, key/value head, row tile, key tile); `shares` CTAs
 // own equal stretches of that sequence, so that samples of any lengths load the SMs evenly.  Lengths are on the device: every
 // CTA adds up the samples' units and finds its own first one.  A CTA keeps one pipeline of TMA loads running over the borders of its
-// row tiles; keys arrive page by page through the table, into the layout that seg_mma.cuh describes.
+// row tiles; keys arrive page by page through the table.
 // A row tile that one CTA holds as a whole is finished there.  One that is cut leaves an unnormalised fp32 piece per CTA, which a second
 // kernel joins: the block with the number of the CTA that holds the first piece.  A CTA has two pieces at most (it may end one row tile
 // and begin another), so the scratch does not depend on the lengths.
-// Inside a CTA, WR warps lie along the rows and WK along the keys, each with its own running maximum and sum (WR * WK = 4); they are
-// merged once per row tile, through the ring stage that was read last.
-// Rows of V behind the last key become zeros in shared memory, so whatever a page holds there (NaN included) never meets a product.
+// Inside a CTA a fifth warp issues the loads, a box for K and one for V per page, into a ring of stages; four warps multiply: WR along
+// the rows and WK along the keys of a tile (WR * WK = 4), each with its own running maximum and sum.  They never wait for one another
+// inside a row tile; its end merges them through the ring stage that was read last, which is given back only then.
+// Rows of V behind the last key become zeros in shared memory (each warp's own ones), so whatever a page holds there (NaN included) never
+// meets a product.
 // Scores, maxima, sums and outputs are fp32; the probabilities are rounded to bf16 for the second product (the operand type of
 // the matrix instruction; half a step, 2^-8, of each weight).
 #include <string.h>
@@ -22,18 +24,19 @@
 namespace swam {
 namespace {
 
-constexpr int kKT = 64;                // keys per tile
-constexpr int kThreadsP = 128;
+constexpr int kMathThreads = 128;      // of the warps that multiply
+constexpr int kThreadsP = kMathThreads + 32;
 constexpr int kCtasPerSm = 2;
 constexpr int kMinUnits = 2;           // key tiles that a share has at least, where row tiles may be cut
 
 template <int D, int WR>
 struct PagedCfg {
-  static constexpr int WK = 4 / WR, MR = 16 * WR, KW = kKT / WK;
-  static constexpr int kTileB = kKT * D * 2;
-  static constexpr int kStages = D == 128 ? 3 : (D == 64 ? 6 : 8);       // 96 KB (64 at head dim 32): two CTAs an SM
+  static constexpr int KT = D == 128 ? 64 : 128;                         // keys per tile: 16 KB of K (8 at head dim 32)
+  static constexpr int WK = 4 / WR, MR = 16 * WR, KW = KT / WK;
+  static constexpr int kTileB = KT * D * 2;
+  static constexpr int kStages = D == 32 ? 6 : 3;                        // 96 KB: two CTAs an SM
   static constexpr int kRing = kStages * 2 * kTileB;
-  static constexpr int kBytes = kRing + 1024 /*alignment*/ + 8 * kStages + 64 * 8 /*maxima and sums of the warps*/;
+  static constexpr int kBytes = kRing + 1024 /*alignment*/ + 16 * kStages + 64 * 8 /*maxima and sums of the warps*/;
 };
 
 // A stretch of the sequence of units.  [t, t_end) are the key tiles of the current row tile that belong to it.
@@ -47,23 +50,27 @@ struct Walk {
 
 struct Place {
   int64_t offset;          // units of the sample in front of the share's first one
+  PagedSample s;
   int b;
 };
 
+// the math warps' own barrier
+__device__ __forceinline__ void math_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
 template <int MR>
 __device__ __forceinline__ int row_tiles(const PagedSample& s, int g) { return (s.n * g + MR - 1) / MR; }
-template <int MR>
+template <int MR, int KT>
 __device__ __forceinline__ int key_tiles(const SegParams& p, const PagedSample& s, int r) {
   const int last = min((r + 1) * MR, s.n * p.g) - 1;
-  return (paged_limit(p.a.causal, s, last / p.g) + kKT - 1) / kKT;
+  return (paged_limit(p.a.causal, s, last / p.g) + KT - 1) / KT;
 }
 // units of one key/value head (a row tile without keys still has its zeros to write)
-template <int MR>
+template <int MR, int KT>
 __device__ __forceinline__ int64_t head_units(const SegParams& p, const PagedSample& s) {
   const int rt = row_tiles<MR>(s, p.g);
-  if (!p.a.causal) return (int64_t)rt * max(1, (s.len + kKT - 1) / kKT);
+  if (!p.a.causal) return (int64_t)rt * max(1, (s.len + KT - 1) / KT);
   int64_t u = 0;
-  for (int r = 0; r < rt; ++r) u += max(1, key_tiles<MR>(p, s, r));
+  for (int r = 0; r < rt; ++r) u += max(1, key_tiles<MR, KT>(p, s, r));
   return u;
 }
 
@@ -82,38 +89,50 @@ __global__ void __launch_bounds__(kThreadsP, kCtasPerSm)
 paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ SegParams p,
                  const __grid_constant__ PagedCache pc, const bool cut, int4* join) {
   using C = PagedCfg<D, WR>;
-  constexpr int MR = C::MR, WK = C::WK, KW = C::KW, kStages = C::kStages, kTileB = C::kTileB;
-  constexpr int CPR = D / 8;
+  constexpr int MR = C::MR, WK = C::WK, KT = C::KT, KW = C::KW, kStages = C::kStages, kTileB = C::kTileB;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ int64_t warp_sum[4];
+  __shared__ int64_t warp_sum[5];
   __shared__ Place place;
-  __shared__ int abort_flag;
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
   const uint32_t s0 = (smem_addr(smem_raw) + 1023u) & ~1023u;
   unsigned char* base = smem_raw + (s0 - smem_addr(smem_raw));
   const uint32_t bars = s0 + C::kRing;
-  float2* ml = reinterpret_cast<float2*>(base + C::kRing + 8 * kStages);       // [WK][MR]
+  auto bar_full = [&](int st) { return bars + 16 * st; };
+  auto bar_empty = [&](int st) { return bars + 16 * st + 8; };
+  float2* ml = reinterpret_cast<float2*>(base + C::kRing + 16 * kStages);      // [WK][MR]
   const SegArgs& a = p.a;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) mbar_init(bars + 8 * i, 1);
-    abort_flag = 0;
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(bar_full(i), 1);
+      mbar_init(bar_empty(i), 4);
+    }
+    abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (cut) join[blockIdx.x] = make_int4(0, 0, 0, 0);
   }
+  if (warp == 4 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_k : &map_v) : "memory");
 
   // ---- the share of this CTA: add up the units, then find the sample of its first one
   int64_t mine0 = 0, sum = 0;
+  PagedSample smp0{0, 0, 0};
   for (int b0 = 0; b0 < pc.samples; b0 += kThreadsP) {
     const int b = b0 + threadIdx.x;
-    const int64_t u = b < pc.samples ? head_units<MR>(p, paged_sample(pc, a.n_q, b, p.status)) * a.N_kv : 0;
-    if (b0 == 0) mine0 = u;
+    PagedSample smp{0, 0, 0};
+    if (b < pc.samples) smp = paged_sample(pc, a.n_q, b, p.status);
+    const int64_t u = head_units<MR, KT>(p, smp) * a.N_kv;
+    if (b0 == 0) {
+      mine0 = u;
+      smp0 = smp;
+    }
     sum += u;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) warp_sum[warp] = sum;
   __syncthreads();
-  const int64_t total = warp_sum[0] + warp_sum[1] + warp_sum[2] + warp_sum[3];
+  const int64_t total = warp_sum[0] + warp_sum[1] + warp_sum[2] + warp_sum[3] + warp_sum[4];
   const int64_t most = cut ? (total + kMinUnits - 1) / kMinUnits : total;
   const int shares = (int)min((int64_t)gridDim.x, most);
   if ((int)blockIdx.x >= shares) {
@@ -124,7 +143,12 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   int64_t before = 0;
   for (int b0 = 0; b0 < pc.samples && before <= u0; b0 += kThreadsP) {
     const int b = b0 + threadIdx.x;
-    const int64_t u = b0 == 0 ? mine0 : (b < pc.samples ? head_units<MR>(p, paged_sample(pc, a.n_q, b, p.status)) * a.N_kv : 0);
+    PagedSample smp = smp0;
+    if (b0 > 0) {
+      smp = PagedSample{0, 0, 0};
+      if (b < pc.samples) smp = paged_sample(pc, a.n_q, b, p.status);
+    }
+    const int64_t u = b0 == 0 ? mine0 : head_units<MR, KT>(p, smp) * a.N_kv;
     int64_t end = u;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -134,18 +158,18 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     __syncthreads();
     if (lane == 31) warp_sum[warp] = end;
     __syncthreads();
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < 5; ++w) {
       if (w < warp) end += warp_sum[w];
     }
     end += before;
-    if (u0 >= end - u && u0 < end) place = Place{u0 - (end - u), b};
-    before += warp_sum[0] + warp_sum[1] + warp_sum[2] + warp_sum[3];
+    if (u0 >= end - u && u0 < end) place = Place{u0 - (end - u), smp, b};
+    for (int w = 0; w < 5; ++w) before += warp_sum[w];
   }
   __syncthreads();
 
   // makes the current row tile's part of the stretch: from tile t on, as far as `left` reaches
   auto take = [&](Walk& w) {
-    w.tiles = key_tiles<MR>(p, w.s, w.r);
+    w.tiles = key_tiles<MR, KT>(p, w.s, w.r);
     const int units = max(1, w.tiles);
     const int64_t n = cut ? min((int64_t)(units - w.t), w.left) : units;
     w.left -= n;
@@ -174,73 +198,87 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   {
     w.left = u1 - u0;
     w.b = place.b;
-    w.s = paged_sample(pc, a.n_q, w.b, p.status);
+    w.s = place.s;
     w.rt = row_tiles<MR>(w.s, p.g);
-    const int64_t units = head_units<MR>(p, w.s);
+    const int64_t units = head_units<MR, KT>(p, w.s);
     w.h = (int)(place.offset / units);
     int64_t off = place.offset - w.h * units;
     w.r = 0;
     if (!a.causal) {
-      const int each = max(1, (w.s.len + kKT - 1) / kKT);
+      const int each = max(1, (w.s.len + KT - 1) / KT);
       w.r = (int)(off / each);
       off -= (int64_t)w.r * each;
     } else {
-      for (int n; off >= (n = max(1, key_tiles<MR>(p, w.s, w.r))); ++w.r) off -= n;
+      for (int n; off >= (n = max(1, key_tiles<MR, KT>(p, w.s, w.r))); ++w.r) off -= n;
     }
     w.t = (int)off;
     if (!cut && w.t > 0) {
       // a row tile belongs to the share that holds its first unit
-      w.left -= max(1, key_tiles<MR>(p, w.s, w.r)) - w.t;
+      w.left -= max(1, key_tiles<MR, KT>(p, w.s, w.r)) - w.t;
       more = next(w);
     } else {
       take(w);
     }
   }
+  // A page's rows of a tile are [64-column block][row]: one box.  (A tile inside a page: that many rows of it.)
+  const int sh = pc.page_shift, rows = min(KT, 1 << sh);
 
-  // ---- loads (warp 0): ahead of the products by kStages - 1 tiles
-  constexpr int DB = D == 32 ? 1 : D / 64, kCols = D == 32 ? 32 : 64, kColB = kCols * 2;       // boxes per row of a tile, their columns and bytes
-  Walk lw = w;
-  bool lmore = more;
-  int issued = 0;
-  PageWindow pages;
-  auto load_next = [&]() {
-    while (lmore && lw.t >= lw.t_end) lmore = next(lw);
-    if (!lmore) return;
-    const int key0 = lw.t * kKT, sh = pc.page_shift, first = key0 >> sh;
-    const int last = min((lw.r + 1) * MR, lw.s.n * p.g) - 1;
-    const int keys = paged_limit(a.causal, lw.s, last / p.g) - key0;
-    const int count = sh >= 6 ? 1 : min(kKT >> sh, (keys + (1 << sh) - 1) >> sh), rows = min(kKT, 1 << sh);
-    const int page = pages.get(pc, lw.b, first, lane < count ? lane : 0);
-    const int st = issued % kStages;
-    const uint32_t ks = s0 + (uint32_t)st * 2 * kTileB, bar = bars + 8 * st;
-    if (lane == 0) mbar_expect_tx(bar, 2 * count * rows * D * 2);
-    __syncwarp();
-    if (lane < count) {
-      const int at = paged_page(pc, page, p.status);
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const uint32_t dst = ks + db * kKT * kColB + lane * rows * kColB;
-        tma_load_4d(dst, &map_k, bar, db * kCols, key0 & ((1 << sh) - 1), lw.h, at);
-        tma_load_4d(dst + kTileB, &map_v, bar, db * kCols, key0 & ((1 << sh) - 1), lw.h, at);
+  if (warp == 4) {
+    // ------------------------------------------------------------------ loads
+    PageWindow pages;
+    bool ok = true;
+    int cnt = 0;
+    for (; more && ok; more = next(w)) {
+      const int keys_all = paged_limit(a.causal, w.s, (min((w.r + 1) * MR, w.s.n * p.g) - 1) / p.g);
+      for (int t = w.t; t < w.t_end; ++t, ++cnt) {
+        const int key0 = t * KT, keys = keys_all - key0;
+        const int count = min(KT / rows, (keys + rows - 1) / rows);
+        const int page = pages.get(pc, w.b, key0 >> sh, lane < count ? lane : 0);
+        const int st = cnt % kStages;
+        if (cnt >= kStages) ok = __all_sync(0xffffffffu, mbar_wait(bar_empty(st), ((cnt / kStages) & 1) ^ 1, abort_flag) ? 1 : 0) != 0;
+        if (!ok) break;
+        const uint32_t dst = s0 + (uint32_t)st * 2 * kTileB + lane * rows * D * 2, bar = bar_full(st);
+        if (lane == 0) mbar_expect_tx(bar, 2 * count * rows * D * 2);
+        __syncwarp();
+        if (lane < count) {
+          const int at = paged_page(pc, page, p.status), row = key0 & ((1 << sh) - 1);
+          if constexpr (D == 32) {
+            tma_load_4d(dst, &map_k, bar, 0, row, w.h, at);
+            tma_load_4d(dst + kTileB, &map_v, bar, 0, row, w.h, at);
+          } else {
+            tma_load_5d(dst, &map_k, bar, 0, row, 0, w.h, at);
+            tma_load_5d(dst + kTileB, &map_v, bar, 0, row, 0, w.h, at);
+          }
+        }
+        __syncwarp();
       }
     }
-    __syncwarp();
-    ++issued;
-    ++lw.t;
-  };
-  if (warp == 0)
-    for (int i = 0; i < kStages - 1; ++i) load_next();
+    allow_next();
+    if (!ok) {
+      // copies in flight must not outlive the CTA
+      for (int i = max(0, cnt - kStages); i < cnt; ++i) mbar_wait_bounded(bar_full(i % kStages), (i / kStages) & 1, kDrainCycles, nullptr);
+    }
+    return;
+  }
 
+  // ---------------------------------------------------------------------- products
   const int wr = warp % WR, wk = warp / WR;
+  const int block_b = rows * (D == 32 ? 64 : 128);                   // bytes of a 64-column block of a page's rows
+  // byte offset of the 16 keys from R on (they are in one page), and of a lane's row and chunk inside them
+  auto group_off = [&](int R) { return (uint32_t)(R / rows * rows * D * 2 + (R & (rows - 1)) * (D == 32 ? 64 : 128)); };
+  auto lane_off = [&](int r, int c) {
+    if (D == 32) return (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+    return (uint32_t)((c >> 3) * block_b + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+  };
   int cnt = 0;                                     // key tiles so far
+  // When a wait has run out every warp still walks through its tiles, without products, so that all meet at the same barriers.
   bool ok = true;
   for (; more; more = next(w)) {
     const int row0 = (w.s.q0 * p.g) + w.r * MR;    // first row, counted from the call's first token
     const int row_end = (w.s.q0 + w.s.n) * p.g;
     const int t0 = w.t;
     const bool whole = t0 == 0 && w.t_end == w.tiles;
-    const int last = min((w.r + 1) * MR, w.s.n * p.g) - 1;
-    const int len = paged_limit(a.causal, w.s, last / p.g);
+    const int len = paged_limit(a.causal, w.s, (min((w.r + 1) * MR, w.s.n * p.g) - 1) / p.g);
     // this thread's two rows (accumulator rows lane / 4 and lane / 4 + 8 of the warp's 16), their queries as A fragments
     uint32_t qf[D / 16][4];
     int lim[2];
@@ -265,121 +303,127 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 
     for (int t = t0; t < w.t_end; ++t, ++cnt) {
       const int st = cnt % kStages;
-      ok = mbar_wait(bars + 8 * st, (cnt / kStages) & 1, &abort_flag);
-      ok = __syncthreads_and(ok ? 1 : 0);          // (and every warp is through with the tile before)
-      if (!ok) break;
-      if (warp == 0) load_next();
-      const int key0 = t * kKT + wk * KW;          // first key of this warp
-      const uint32_t ks = s0 + (uint32_t)st * 2 * kTileB, vs = ks + kTileB;
-      const int real = len - t * kKT;              // real keys of this tile
-      if (real < kKT) {
-        for (int i = threadIdx.x; i < (kKT - real) * CPR; i += kThreadsP)
-          st_shared_16(vs + tile_off<D, kKT>(real + i / CPR, i % CPR), 0u, 0u, 0u, 0u);
-        fence_proxy_async();                       // the stage's next load comes through the other proxy
-        __syncthreads();
-      }
-      if (key0 >= len) continue;                   // none of this warp's keys is real
-
-      float sc[KW / 8][4];
-#pragma unroll
-      for (int nb = 0; nb < KW / 16; ++nb) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[2 * nb][e] = sc[2 * nb + 1][e] = 0.f;
-#pragma unroll
-        for (int kd = 0; kd < D / 16; ++kd) {
-          uint32_t f[4];
-          ldsm4(f, ks + tile_off<D, kKT>(wk * KW + nb * 16 + (lane & 7) + ((lane >> 4) << 3), kd * 2 + ((lane >> 3) & 1)));
-          mma_bf16(sc[2 * nb], qf[kd], f[0], f[1]);
-          mma_bf16(sc[2 * nb + 1], qf[kd], f[2], f[3]);
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(bar_full(st), (cnt / kStages) & 1, abort_flag) ? 1 : 0) != 0;
+      const int key0 = t * KT + wk * KW;           // first key of this warp
+      if (ok && key0 < len) {                      // (some of this warp's keys are real)
+        const uint32_t ks = s0 + (uint32_t)st * 2 * kTileB, vs = ks + kTileB;
+        if (len - key0 < KW) {
+          // this warp's rows of V behind the last key become zeros
+          constexpr int CPR = D / 8;
+          for (int i = lane; i < (KW - (len - key0)) * CPR; i += 32) {
+            const int r = len - key0 + i / CPR;
+            st_shared_16(vs + group_off(wk * KW + (r & ~15)) + lane_off(r & 15, i % CPR), 0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async();                     // the stage's next load comes through the other proxy
+          __syncwarp();
         }
-      }
-      const int v0 = lim[0] - key0, v1 = lim[1] - key0;       // keys of the warp's range that the rows see
-      if (min(v0, v1) < KW) {
+        float sc[KW / 8][4];
+#pragma unroll
+        for (int nb = 0; nb < KW / 16; ++nb) {
+          const uint32_t at = ks + group_off(wk * KW + nb * 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[2 * nb][e] = sc[2 * nb + 1][e] = 0.f;
+#pragma unroll
+          for (int kd = 0; kd < D / 16; ++kd) {
+            uint32_t f[4];
+            ldsm4(f, at + lane_off((lane & 7) + ((lane >> 4) << 3), kd * 2 + ((lane >> 3) & 1)));
+            mma_bf16(sc[2 * nb], qf[kd], f[0], f[1]);
+            mma_bf16(sc[2 * nb + 1], qf[kd], f[2], f[3]);
+          }
+        }
+        const int v0 = lim[0] - key0, v1 = lim[1] - key0;       // keys of the warp's range that the rows see
+        if (min(v0, v1) < KW) {
+#pragma unroll
+          for (int nb = 0; nb < KW / 8; ++nb) {
+            const int c = nb * 8 + (lane & 3) * 2;
+            if (c >= v0) sc[nb][0] = -INFINITY;
+            if (c + 1 >= v0) sc[nb][1] = -INFINITY;
+            if (c >= v1) sc[nb][2] = -INFINITY;
+            if (c + 1 >= v1) sc[nb][3] = -INFINITY;
+          }
+        }
+        float corr[2], ref[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int nb = 0; nb < KW / 8; ++nb) mx = fmaxf(mx, fmaxf(sc[nb][2 * i], sc[nb][2 * i + 1]));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          const float mn = fmaxf(m[i], mx * p.scale_log2);
+          ref[i] = mn == -INFINITY ? 0.f : mn;       // a row that has seen no key yet: every exponent stays -inf
+          corr[i] = ex2(m[i] - ref[i]);
+          m[i] = mn;
+          l[i] *= corr[i];
+        }
+        const bool moved = __any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f);       // rare after the first tiles
+        if (moved) big = __any_sync(0xffffffffu, !(fmaxf(fabsf(ref[0]), fabsf(ref[1])) < kSegBig));
+        float scale = p.scale_log2;
+        if (big) {
+          scale = 1.f;
+#pragma unroll
+          for (int nb = 0; nb < KW / 8; ++nb) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[nb][e] *= p.scale_log2;
+          }
+        }
 #pragma unroll
         for (int nb = 0; nb < KW / 8; ++nb) {
-          const int c = nb * 8 + (lane & 3) * 2;
-          if (c >= v0) sc[nb][0] = -INFINITY;
-          if (c + 1 >= v0) sc[nb][1] = -INFINITY;
-          if (c >= v1) sc[nb][2] = -INFINITY;
-          if (c + 1 >= v1) sc[nb][3] = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sc[nb][e] = ex2(fmaf(sc[nb][e], scale, -ref[e >> 1]));
+            l[e >> 1] += sc[nb][e];
+          }
+        }
+        if (moved) {
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) {
+            o[i][0] *= corr[0];
+            o[i][1] *= corr[0];
+            o[i][2] *= corr[1];
+            o[i][3] *= corr[1];
+          }
+        }
+#pragma unroll
+        for (int nb = 0; nb < KW / 16; ++nb) {
+          const uint32_t at = vs + group_off(wk * KW + nb * 16);
+          const uint32_t pf[4] = {pack_bf16x2(sc[2 * nb][0], sc[2 * nb][1]), pack_bf16x2(sc[2 * nb][2], sc[2 * nb][3]),
+                                  pack_bf16x2(sc[2 * nb + 1][0], sc[2 * nb + 1][1]), pack_bf16x2(sc[2 * nb + 1][2], sc[2 * nb + 1][3])};
+#pragma unroll
+          for (int dn = 0; dn < D / 16; ++dn) {
+            uint32_t f[4];
+            ldsm4_t(f, at + lane_off((lane & 7) + (((lane >> 3) & 1) << 3), dn * 2 + (lane >> 4)));
+            mma_bf16(o[2 * dn], pf, f[0], f[1]);
+            mma_bf16(o[2 * dn + 1], pf, f[2], f[3]);
+          }
         }
       }
-      float corr[2], ref[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int nb = 0; nb < KW / 8; ++nb) mx = fmaxf(mx, fmaxf(sc[nb][2 * i], sc[nb][2 * i + 1]));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        const float mn = fmaxf(m[i], mx * p.scale_log2);
-        ref[i] = mn == -INFINITY ? 0.f : mn;       // a row that has seen no key yet: every exponent stays -inf
-        corr[i] = ex2(m[i] - ref[i]);
-        m[i] = mn;
-        l[i] *= corr[i];
-      }
-      const bool moved = __any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f);       // rare after the first tiles
-      if (moved) big = __any_sync(0xffffffffu, !(fmaxf(fabsf(ref[0]), fabsf(ref[1])) < kSegBig));
-      float scale = p.scale_log2;
-      if (big) {
-        scale = 1.f;
-#pragma unroll
-        for (int nb = 0; nb < KW / 8; ++nb) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[nb][e] *= p.scale_log2;
-        }
-      }
-#pragma unroll
-      for (int nb = 0; nb < KW / 8; ++nb) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          sc[nb][e] = ex2(fmaf(sc[nb][e], scale, -ref[e >> 1]));
-          l[e >> 1] += sc[nb][e];
-        }
-      }
-      if (moved) {
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          o[i][0] *= corr[0];
-          o[i][1] *= corr[0];
-          o[i][2] *= corr[1];
-          o[i][3] *= corr[1];
-        }
-      }
-#pragma unroll
-      for (int nb = 0; nb < KW / 16; ++nb) {
-        const uint32_t pf[4] = {pack_bf16x2(sc[2 * nb][0], sc[2 * nb][1]), pack_bf16x2(sc[2 * nb][2], sc[2 * nb][3]),
-                                pack_bf16x2(sc[2 * nb + 1][0], sc[2 * nb + 1][1]), pack_bf16x2(sc[2 * nb + 1][2], sc[2 * nb + 1][3])};
-#pragma unroll
-        for (int dn = 0; dn < D / 16; ++dn) {
-          uint32_t f[4];
-          ldsm4_t(f, vs + tile_off<D, kKT>(wk * KW + nb * 16 + (lane & 7) + (((lane >> 3) & 1) << 3), dn * 2 + (lane >> 4)));
-          mma_bf16(o[2 * dn], pf, f[0], f[1]);
-          mma_bf16(o[2 * dn + 1], pf, f[2], f[3]);
-        }
+      // the stage is free, but for the row tile's last one, which serves the merge first
+      if (WK == 1 || t + 1 < w.t_end) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_empty(st));
       }
     }
-    if (!ok) break;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
     }
 
-    // ---- the row tile's result.  The warps of a row are merged through the ring stage that was read last, which nobody loads into
-    // before the next tile's barrier; every warp takes 1 / WK of the columns.  (A row tile without keys has nothing to merge.)
+    // ---- the row tile's result: every warp takes 1 / WK of the columns.  (A row tile without keys has nothing to merge.)
     constexpr int NB = D / 8 / WK;                 // 8-column blocks of a warp
     float out[NB][4], mm[2], ll[2];
-    if (WK > 1 && w.tiles > 0) {
-      float4* frag = reinterpret_cast<float4*>(base + (size_t)((cnt - 1) % kStages) * 2 * kTileB);       // [warp][D / 8][lane]
-      __syncthreads();
+    if (WK > 1 && w.t_end > t0) {
+      const int st = (cnt - 1) % kStages;
+      float4* frag = reinterpret_cast<float4*>(base + (size_t)st * 2 * kTileB);       // [warp][D / 8][lane]
+      math_sync();                                 // all warps are through with the stage
 #pragma unroll
       for (int i = 0; i < D / 8; ++i) frag[(warp * (D / 8) + i) * 32 + lane] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
       if ((lane & 3) == 0) {
         ml[wk * MR + wr * 16 + (lane >> 2)] = make_float2(m[0], l[0]);
         ml[wk * MR + wr * 16 + (lane >> 2) + 8] = make_float2(m[1], l[1]);
       }
-      __syncthreads();
+      math_sync();
       float f[WK][2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -408,6 +452,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
       }
       fence_proxy_async();                         // the stage's next load comes through the other proxy
+      math_sync();                                 // (the maxima and sums have been read too)
+      if (lane == 0) mbar_arrive(bar_empty(st));
     } else {
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
@@ -447,11 +493,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
   }
   allow_next();
-  if (!ok) {
-    if (threadIdx.x == 0) atomicOr(p.status, ST_TIMEOUT);
-    if (warp == 0) drain_loads(bars, kStages, issued);       // copies in flight must not outlive the CTA
-    __syncthreads();
-  }
+  if (!ok && lane == 0) atomicOr(p.status, ST_TIMEOUT);
 }
 
 // Joins the pieces of one row tile: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i, pieces in order.
@@ -532,6 +574,15 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
   }
 }
 
+// Pages [n_pages, page, N_kv, D] with strides as (column of a 64-column block, row, block, head, page); box = `rows` rows of all columns
+bool make_page_map(CUtensorMap* map, const void* ptr, int n_pages, int page, int N_kv, int D, int64_t tok, int64_t stride, int rows) {
+  if (D == 32) return make_kv_map(map, ptr, n_pages, page, N_kv, D, tok, stride, rows);
+  const cuuint64_t dims[5] = {64, (cuuint64_t)page, (cuuint64_t)D / 64, (cuuint64_t)N_kv, (cuuint64_t)n_pages};
+  const cuuint64_t strides[4] = {(cuuint64_t)tok * 2, 128, (cuuint64_t)D * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[5] = {64, (cuuint32_t)rows, (cuuint32_t)D / 64, 1, 1};
+  return encode_bf16(map, ptr, 5, dims, strides, box);
+}
+
 template <int D, int WR>
 cudaError_t launch_one(const SegParams& p0, const PagedCache& c, int shares, bool cut, cudaStream_t st, int* launches) {
   using C = PagedCfg<D, WR>;
@@ -541,9 +592,9 @@ cudaError_t launch_one(const SegParams& p0, const PagedCache& c, int shares, boo
   p.part_ml = (float2*)(p.part_o + (size_t)shares * 2 * C::MR * D);
   int4* join = (int4*)(p.part_ml + (size_t)shares * 2 * C::MR);
   CUtensorMap mk, mv;
-  const int page = 1 << c.page_shift, rows = page < kKT ? page : kKT;
-  if (!make_kv_map(&mk, a.k[1], c.n_pages, page, a.N_kv, D, c.k_tok, c.k_page, rows) ||
-      !make_kv_map(&mv, a.v[1], c.n_pages, page, a.N_kv, D, c.v_tok, c.v_page, rows))
+  const int page = 1 << c.page_shift, rows = page < C::KT ? page : C::KT;
+  if (!make_page_map(&mk, a.k[1], c.n_pages, page, a.N_kv, D, c.k_tok, c.k_page, rows) ||
+      !make_page_map(&mv, a.v[1], c.n_pages, page, a.N_kv, D, c.v_tok, c.v_page, rows))
     return cudaErrorInvalidValue;
   static SmemOptIn opt_in;
   cudaError_t e = opt_in((const void*)paged_mma_kernel<D, WR>, C::kBytes, a.device);
