@@ -14,7 +14,7 @@
 // halves of each of its pairs: 16 bytes of the first half and 16 of the second (pairs i, i + rot/2), or 32 in a row (2i, 2i + 1); it keeps
 // their cosines and sines, times the weights, for all items of a kind, so that an element costs a product, a fused one and the product with
 // the reciprocal root.  Where rot/2 ends inside 16 bytes the other half is read again, element by element (L1).
-#include <math.h>
+#include <string.h>
 
 #include "seg_attn.cuh"
 
@@ -427,13 +427,15 @@ cudaError_t launch_dim(RopeParams& p, cudaStream_t st, int* launches) {
 
 uint64_t turns_of(double freq) {
   // freq / (2 pi) turns in units of 2^-64, modulo a turn.  2 / pi = 0xa2f9836e4e44152a / 2^64, to half a unit.
-  if (freq == 0.0) return 0;
-  int e;
-  const double m = frexp(freq < 0 ? -freq : freq, &e);                   // m in [0.5, 1)
-  const unsigned __int128 prod = (unsigned __int128)(uint64_t)ldexp(m, 53) * 0xa2f9836e4e44152aull;      // |freq| / (2 pi) * 2^(66 + 53 - e)
-  const int shift = 55 - e;                                              // to units of 2^-64
+  uint64_t bits;
+  memcpy(&bits, &freq, 8);
+  const int e = (int)(bits >> 52 & 0x7ff);                               // |freq| = mantissa * 2^(e - 1075)
+  if (e == 0) return 0;                                                  // (zero, and what is far below 2^-64 of a turn in 2^31 positions)
+  const uint64_t mantissa = (bits & 0xfffffffffffffull) | 1ull << 52;
+  const unsigned __int128 prod = (unsigned __int128)mantissa * 0xa2f9836e4e44152aull;        // |freq| / (2 pi) * 2^(66 + 1075 - e)
+  const int shift = 1077 - e;                                            // to units of 2^-64
   const uint64_t u = shift >= 128 ? 0 : (shift >= 0 ? (uint64_t)(prod >> shift) : (shift > -64 ? (uint64_t)prod << -shift : 0));
-  return freq < 0 ? 0 - u : u;
+  return bits >> 63 ? 0 - u : u;
 }
 
 cudaError_t launch_norm_rope(RopeParams& p, cudaStream_t st, int* launches) {

@@ -14,6 +14,8 @@
 // inside a row tile; its end merges them through the ring stage that was read last, which is given back only then.
 // Rows of V behind the last key become zeros in shared memory (each warp's own ones), so whatever a page holds there (NaN included) never
 // meets a product.
+// Up to eight rows (WR = 0: single tokens of grouped heads) are the narrow side of the products: S^T = K Q^T and O^T = V^T P^T, 16 keys
+// and 16 columns by 8 rows, half the instructions and exponentials of 16 rows; P^T becomes an operand by a transpose in registers.
 // Scores, maxima, sums and outputs are fp32; the probabilities are rounded to bf16 for the second product (the operand type of
 // the matrix instruction; half a step, 2^-8, of each weight).
 #include <string.h>
@@ -32,7 +34,8 @@ constexpr int kMinUnits = 2;           // key tiles that a share has at least, w
 template <int D, int WR>
 struct PagedCfg {
   static constexpr int KT = D == 128 ? 64 : 128;                         // keys per tile: 16 KB of K (8 at head dim 32)
-  static constexpr int WK = 4 / WR, MR = 16 * WR, KW = KT / WK;
+  static constexpr int WRows = WR == 0 ? 1 : WR;                         // warps along the rows
+  static constexpr int WK = 4 / WRows, MR = WR == 0 ? 8 : 16 * WR, KW = KT / WK;
   static constexpr int kTileB = KT * D * 2;
   static constexpr int kStages = D == 32 ? 6 : 3;                        // 96 KB: two CTAs an SM
   static constexpr int kRing = kStages * 2 * kTileB;
@@ -262,7 +265,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
 
   // ---------------------------------------------------------------------- products
-  const int wr = warp % WR, wk = warp / WR;
+  constexpr bool kNarrow = WR == 0;
+  const int wr = warp % C::WRows, wk = warp / C::WRows;
   const int block_b = rows * (D == 32 ? 64 : 128);                   // bytes of a 64-column block of a page's rows
   // byte offset of the 16 keys from R on (they are in one page), and of a lane's row and chunk inside them
   auto group_off = [&](int R) { return (uint32_t)(R / rows * rows * D * 2 + (R & (rows - 1)) * (D == 32 ? 64 : 128)); };
@@ -279,25 +283,32 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     const int t0 = w.t;
     const bool whole = t0 == 0 && w.t_end == w.tiles;
     const int len = paged_limit(a.causal, w.s, (min((w.r + 1) * MR, w.s.n * p.g) - 1) / p.g);
-    // this thread's two rows (accumulator rows lane / 4 and lane / 4 + 8 of the warp's 16), their queries as A fragments
-    uint32_t qf[D / 16][4];
+    // this thread's two rows: those of its accumulators, lane / 4 and lane / 4 + 8 of the warp's 16 (narrow: 2 (lane % 4) and the next),
+    // and the queries as A fragments of the former (narrow: B fragments of row lane / 4)
+    auto row_of = [&](int i) { return kNarrow ? (lane & 3) * 2 + i : wr * 16 + (lane >> 2) + 8 * i; };
+    uint32_t qf[D / 16][kNarrow ? 2 : 4];
     int lim[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+      const int row = row0 + row_of(i);
+      lim[i] = row < row_end ? paged_limit(a.causal, w.s, row / p.g - w.s.q0) : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < (kNarrow ? 1 : 2); ++i) {
       const int row = row0 + wr * 16 + (lane >> 2) + 8 * i;
       const bool real = row < row_end;
       const int tok = real ? row / p.g : 0, h = w.h * p.g + (real ? row - tok * p.g : 0);
-      lim[i] = real ? paged_limit(a.causal, w.s, tok - w.s.q0) : 0;
       const uint32_t* src = reinterpret_cast<const uint32_t*>((const __nv_bfloat16*)a.q + tok * a.q_tok + (int64_t)h * D);
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         qf[ks][i] = real ? src[ks * 8 + (lane & 3)] : 0u;
-        qf[ks][i + 2] = real ? src[ks * 8 + 4 + (lane & 3)] : 0u;
+        qf[ks][i + (kNarrow ? 1 : 2)] = real ? src[ks * 8 + 4 + (lane & 3)] : 0u;
       }
     }
-    float o[D / 8][4];
+    constexpr int OB = kNarrow ? D / 16 : D / 8;   // blocks of accumulators
+    float o[OB][4];
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    for (int i = 0; i < OB; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     bool big = false;                              // some row's reference is large: see kSegBig
 
@@ -317,84 +328,161 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           fence_proxy_async();                     // the stage's next load comes through the other proxy
           __syncwarp();
         }
-        float sc[KW / 8][4];
+        if constexpr (kNarrow) {
+          // S^T: keys lane / 4 and lane / 4 + 8 of each 16, rows 2 (lane % 4) and the next
+          float sc[KW / 16][4];
 #pragma unroll
-        for (int nb = 0; nb < KW / 16; ++nb) {
-          const uint32_t at = ks + group_off(wk * KW + nb * 16);
+          for (int nb = 0; nb < KW / 16; ++nb) {
+            const uint32_t at = ks + group_off(wk * KW + nb * 16);
+            sc[nb][0] = sc[nb][1] = sc[nb][2] = sc[nb][3] = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[2 * nb][e] = sc[2 * nb + 1][e] = 0.f;
-#pragma unroll
-          for (int kd = 0; kd < D / 16; ++kd) {
-            uint32_t f[4];
-            ldsm4(f, at + lane_off((lane & 7) + ((lane >> 4) << 3), kd * 2 + ((lane >> 3) & 1)));
-            mma_bf16(sc[2 * nb], qf[kd], f[0], f[1]);
-            mma_bf16(sc[2 * nb + 1], qf[kd], f[2], f[3]);
+            for (int kd = 0; kd < D / 16; ++kd) {
+              uint32_t f[4];
+              ldsm4(f, at + lane_off((lane & 7) + (((lane >> 3) & 1) << 3), kd * 2 + (lane >> 4)));
+              mma_bf16(sc[nb], f, qf[kd][0], qf[kd][1]);
+            }
           }
-        }
-        const int v0 = lim[0] - key0, v1 = lim[1] - key0;       // keys of the warp's range that the rows see
-        if (min(v0, v1) < KW) {
+          if (min(lim[0], lim[1]) - key0 < KW) {
+#pragma unroll
+            for (int nb = 0; nb < KW / 16; ++nb) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (key0 + nb * 16 + (lane >> 2) + (e & 2) * 4 >= lim[e & 1]) sc[nb][e] = -INFINITY;
+            }
+          }
+          float corr[2], ref[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int nb = 0; nb < KW / 16; ++nb) mx = fmaxf(mx, fmaxf(sc[nb][i], sc[nb][i + 2]));
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+            const float mn = fmaxf(m[i], mx * p.scale_log2);
+            ref[i] = mn == -INFINITY ? 0.f : mn;
+            corr[i] = ex2(m[i] - ref[i]);
+            m[i] = mn;
+            l[i] *= corr[i];
+          }
+          const bool moved = __any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f);
+          if (moved) big = __any_sync(0xffffffffu, !(fmaxf(fabsf(ref[0]), fabsf(ref[1])) < kSegBig));
+          float scale = p.scale_log2;
+          if (big) {
+            scale = 1.f;
+#pragma unroll
+            for (int nb = 0; nb < KW / 16; ++nb) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sc[nb][e] *= p.scale_log2;
+            }
+          }
+#pragma unroll
+          for (int nb = 0; nb < KW / 16; ++nb) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              sc[nb][e] = ex2(fmaf(sc[nb][e], scale, -ref[e & 1]));
+              l[e & 1] += sc[nb][e];
+            }
+          }
+          if (moved) {
+#pragma unroll
+            for (int i = 0; i < OB; ++i) {
+              o[i][0] *= corr[0];
+              o[i][1] *= corr[1];
+              o[i][2] *= corr[0];
+              o[i][3] *= corr[1];
+            }
+          }
+#pragma unroll
+          for (int nb = 0; nb < KW / 16; ++nb) {
+            const uint32_t at = vs + group_off(wk * KW + nb * 16);
+            const uint32_t p0 = transpose8(pack_bf16x2(sc[nb][0], sc[nb][1])), p1 = transpose8(pack_bf16x2(sc[nb][2], sc[nb][3]));
+#pragma unroll
+            for (int dn = 0; dn < D / 16; ++dn) {
+              uint32_t f[4];
+              ldsm4_t(f, at + lane_off((lane & 7) + ((lane >> 4) << 3), dn * 2 + ((lane >> 3) & 1)));
+              mma_bf16(o[dn], f, p0, p1);
+            }
+          }
+        } else {
+          float sc[KW / 8][4];
+#pragma unroll
+          for (int nb = 0; nb < KW / 16; ++nb) {
+            const uint32_t at = ks + group_off(wk * KW + nb * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[2 * nb][e] = sc[2 * nb + 1][e] = 0.f;
+#pragma unroll
+            for (int kd = 0; kd < D / 16; ++kd) {
+              uint32_t f[4];
+              ldsm4(f, at + lane_off((lane & 7) + ((lane >> 4) << 3), kd * 2 + ((lane >> 3) & 1)));
+              mma_bf16(sc[2 * nb], qf[kd], f[0], f[1]);
+              mma_bf16(sc[2 * nb + 1], qf[kd], f[2], f[3]);
+            }
+          }
+          const int v0 = lim[0] - key0, v1 = lim[1] - key0;       // keys of the warp's range that the rows see
+          if (min(v0, v1) < KW) {
+#pragma unroll
+            for (int nb = 0; nb < KW / 8; ++nb) {
+              const int c = nb * 8 + (lane & 3) * 2;
+              if (c >= v0) sc[nb][0] = -INFINITY;
+              if (c + 1 >= v0) sc[nb][1] = -INFINITY;
+              if (c >= v1) sc[nb][2] = -INFINITY;
+              if (c + 1 >= v1) sc[nb][3] = -INFINITY;
+            }
+          }
+          float corr[2], ref[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int nb = 0; nb < KW / 8; ++nb) mx = fmaxf(mx, fmaxf(sc[nb][2 * i], sc[nb][2 * i + 1]));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+            const float mn = fmaxf(m[i], mx * p.scale_log2);
+            ref[i] = mn == -INFINITY ? 0.f : mn;       // a row that has seen no key yet: every exponent stays -inf
+            corr[i] = ex2(m[i] - ref[i]);
+            m[i] = mn;
+            l[i] *= corr[i];
+          }
+          const bool moved = __any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f);       // rare after the first tiles
+          if (moved) big = __any_sync(0xffffffffu, !(fmaxf(fabsf(ref[0]), fabsf(ref[1])) < kSegBig));
+          float scale = p.scale_log2;
+          if (big) {
+            scale = 1.f;
+#pragma unroll
+            for (int nb = 0; nb < KW / 8; ++nb) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sc[nb][e] *= p.scale_log2;
+            }
+          }
 #pragma unroll
           for (int nb = 0; nb < KW / 8; ++nb) {
-            const int c = nb * 8 + (lane & 3) * 2;
-            if (c >= v0) sc[nb][0] = -INFINITY;
-            if (c + 1 >= v0) sc[nb][1] = -INFINITY;
-            if (c >= v1) sc[nb][2] = -INFINITY;
-            if (c + 1 >= v1) sc[nb][3] = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              sc[nb][e] = ex2(fmaf(sc[nb][e], scale, -ref[e >> 1]));
+              l[e >> 1] += sc[nb][e];
+            }
           }
-        }
-        float corr[2], ref[2];
+          if (moved) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float mx = -INFINITY;
-#pragma unroll
-          for (int nb = 0; nb < KW / 8; ++nb) mx = fmaxf(mx, fmaxf(sc[nb][2 * i], sc[nb][2 * i + 1]));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-          const float mn = fmaxf(m[i], mx * p.scale_log2);
-          ref[i] = mn == -INFINITY ? 0.f : mn;       // a row that has seen no key yet: every exponent stays -inf
-          corr[i] = ex2(m[i] - ref[i]);
-          m[i] = mn;
-          l[i] *= corr[i];
-        }
-        const bool moved = __any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f);       // rare after the first tiles
-        if (moved) big = __any_sync(0xffffffffu, !(fmaxf(fabsf(ref[0]), fabsf(ref[1])) < kSegBig));
-        float scale = p.scale_log2;
-        if (big) {
-          scale = 1.f;
-#pragma unroll
-          for (int nb = 0; nb < KW / 8; ++nb) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sc[nb][e] *= p.scale_log2;
+            for (int i = 0; i < OB; ++i) {
+              o[i][0] *= corr[0];
+              o[i][1] *= corr[0];
+              o[i][2] *= corr[1];
+              o[i][3] *= corr[1];
+            }
           }
-        }
 #pragma unroll
-        for (int nb = 0; nb < KW / 8; ++nb) {
+          for (int nb = 0; nb < KW / 16; ++nb) {
+            const uint32_t at = vs + group_off(wk * KW + nb * 16);
+            const uint32_t pf[4] = {pack_bf16x2(sc[2 * nb][0], sc[2 * nb][1]), pack_bf16x2(sc[2 * nb][2], sc[2 * nb][3]),
+                                    pack_bf16x2(sc[2 * nb + 1][0], sc[2 * nb + 1][1]), pack_bf16x2(sc[2 * nb + 1][2], sc[2 * nb + 1][3])};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            sc[nb][e] = ex2(fmaf(sc[nb][e], scale, -ref[e >> 1]));
-            l[e >> 1] += sc[nb][e];
-          }
-        }
-        if (moved) {
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            o[i][0] *= corr[0];
-            o[i][1] *= corr[0];
-            o[i][2] *= corr[1];
-            o[i][3] *= corr[1];
-          }
-        }
-#pragma unroll
-        for (int nb = 0; nb < KW / 16; ++nb) {
-          const uint32_t at = vs + group_off(wk * KW + nb * 16);
-          const uint32_t pf[4] = {pack_bf16x2(sc[2 * nb][0], sc[2 * nb][1]), pack_bf16x2(sc[2 * nb][2], sc[2 * nb][3]),
-                                  pack_bf16x2(sc[2 * nb + 1][0], sc[2 * nb + 1][1]), pack_bf16x2(sc[2 * nb + 1][2], sc[2 * nb + 1][3])};
-#pragma unroll
-          for (int dn = 0; dn < D / 16; ++dn) {
-            uint32_t f[4];
-            ldsm4_t(f, at + lane_off((lane & 7) + (((lane >> 3) & 1) << 3), dn * 2 + (lane >> 4)));
-            mma_bf16(o[2 * dn], pf, f[0], f[1]);
-            mma_bf16(o[2 * dn + 1], pf, f[2], f[3]);
+            for (int dn = 0; dn < D / 16; ++dn) {
+              uint32_t f[4];
+              ldsm4_t(f, at + lane_off((lane & 7) + (((lane >> 3) & 1) << 3), dn * 2 + (lane >> 4)));
+              mma_bf16(o[2 * dn], pf, f[0], f[1]);
+              mma_bf16(o[2 * dn + 1], pf, f[2], f[3]);
+            }
           }
         }
       }
@@ -406,28 +494,30 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+#pragma unroll
+      for (int x = kNarrow ? 4 : 1; x < (kNarrow ? 32 : 4); x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
     }
 
-    // ---- the row tile's result: every warp takes 1 / WK of the columns.  (A row tile without keys has nothing to merge.)
-    constexpr int NB = D / 8 / WK;                 // 8-column blocks of a warp
+    // ---- the row tile's result: every warp takes 1 / WK of the columns (narrow, head dim 32: two warps half of them each).  (A row tile
+    // without keys has nothing to merge.)
+    constexpr int NB = OB < WK ? 1 : OB / WK;      // blocks of a warp
+    const bool mine = OB >= WK || wk < OB;
     float out[NB][4], mm[2], ll[2];
     if (WK > 1 && w.t_end > t0) {
       const int st = (cnt - 1) % kStages;
-      float4* frag = reinterpret_cast<float4*>(base + (size_t)st * 2 * kTileB);       // [warp][D / 8][lane]
+      float4* frag = reinterpret_cast<float4*>(base + (size_t)st * 2 * kTileB);       // [warp][block][lane]
       math_sync();                                 // all warps are through with the stage
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) frag[(warp * (D / 8) + i) * 32 + lane] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-      if ((lane & 3) == 0) {
-        ml[wk * MR + wr * 16 + (lane >> 2)] = make_float2(m[0], l[0]);
-        ml[wk * MR + wr * 16 + (lane >> 2) + 8] = make_float2(m[1], l[1]);
+      for (int i = 0; i < OB; ++i) frag[(warp * OB + i) * 32 + lane] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+      if (kNarrow ? lane < 4 : (lane & 3) == 0) {
+        ml[wk * MR + row_of(0)] = make_float2(m[0], l[0]);
+        ml[wk * MR + row_of(1)] = make_float2(m[1], l[1]);
       }
       math_sync();
       float f[WK][2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int r = wr * 16 + (lane >> 2) + 8 * i;
+        const int r = row_of(i);
         mm[i] = -INFINITY;
 #pragma unroll
         for (int k = 0; k < WK; ++k) mm[i] = fmaxf(mm[i], ml[k * MR + r].x);
@@ -442,13 +532,15 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         out[i][0] = out[i][1] = out[i][2] = out[i][3] = 0.f;
+        if (mine) {
 #pragma unroll
-        for (int k = 0; k < WK; ++k) {
-          const float4 x = frag[((k * WR + wr) * (D / 8) + wk * NB + i) * 32 + lane];
-          out[i][0] += f[k][0] * x.x;
-          out[i][1] += f[k][0] * x.y;
-          out[i][2] += f[k][1] * x.z;
-          out[i][3] += f[k][1] * x.w;
+          for (int k = 0; k < WK; ++k) {
+            const float4 x = frag[((k * C::WRows + wr) * OB + wk * NB + i) * 32 + lane];
+            out[i][0] += f[k][0] * x.x;
+            out[i][1] += f[k][kNarrow ? 1 : 0] * x.y;
+            out[i][2] += f[k][kNarrow ? 0 : 1] * x.z;
+            out[i][3] += f[k][1] * x.w;
+          }
         }
       }
       fence_proxy_async();                         // the stage's next load comes through the other proxy
@@ -467,23 +559,58 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
     }
     const int slot = (int)blockIdx.x * 2 + (t0 == 0 ? 1 : 0);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = wr * 16 + (lane >> 2) + 8 * i, row = row0 + r;
-      if (row >= row_end) continue;
-      const int tok = row / p.g, h = w.h * p.g + row - tok * p.g;
-      const int c = wk * NB * 8 + (lane & 3) * 2;
+    if constexpr (kNarrow) {
+      // out[k]: columns 16 (wk NB + k) + lane / 4 and 8 further, rows 2 (lane % 4) and the next
       if (whole) {
-        const float inv = seg_inverse(ll[i]);
-        uint32_t* dst = reinterpret_cast<uint32_t*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + c);
+        const float i0 = seg_inverse(ll[0]), i1 = seg_inverse(ll[1]);
+        const int row = row0 + (lane >> 2), tok = row / p.g, h = w.h * p.g + row - tok * p.g;
+        uint32_t* dst = reinterpret_cast<uint32_t*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + wk * NB * 16 + (lane & 3) * 2);
 #pragma unroll
-        for (int k = 0; k < NB; ++k) dst[k * 4] = pack_bf16x2(out[k][2 * i] * inv, out[k][2 * i + 1] * inv);
-        if (a.lse && wk == 0 && (lane & 3) == 0) a.lse[(int64_t)h * a.n_q + tok] = seg_lse(mm[i], ll[i]);
-      } else {
-        float* dst = p.part_o + ((int64_t)slot * MR + r) * D + c;
+        for (int k = 0; k < NB; ++k) {
+          // (transposed: row lane / 4, two neighbouring columns)
+          const uint32_t x0 = transpose8(pack_bf16x2(out[k][0] * i0, out[k][1] * i1)), x1 = transpose8(pack_bf16x2(out[k][2] * i0, out[k][3] * i1));
+          if (mine && row < row_end) {
+            dst[k * 8] = x0;
+            dst[k * 8 + 4] = x1;
+          }
+        }
+      }
 #pragma unroll
-        for (int k = 0; k < NB; ++k) *reinterpret_cast<float2*>(dst + k * 8) = make_float2(out[k][2 * i], out[k][2 * i + 1]);
-        if (wk == 0 && (lane & 3) == 0) p.part_ml[slot * MR + r] = make_float2(mm[i], ll[i]);
+      for (int i = 0; i < 2; ++i) {
+        const int r = row_of(i), row = row0 + r;
+        if (row >= row_end || !mine) continue;
+        if (!whole) {
+          float* dst = p.part_o + ((int64_t)slot * MR + r) * D + wk * NB * 16 + (lane >> 2);
+#pragma unroll
+          for (int k = 0; k < NB; ++k) {
+            dst[k * 16] = out[k][i];
+            dst[k * 16 + 8] = out[k][i + 2];
+          }
+          if (wk == 0 && lane < 4) p.part_ml[slot * MR + r] = make_float2(mm[i], ll[i]);
+        } else if (a.lse && wk == 0 && lane < 4) {
+          const int tok = row / p.g, h = w.h * p.g + row - tok * p.g;
+          a.lse[(int64_t)h * a.n_q + tok] = seg_lse(mm[i], ll[i]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = row_of(i), row = row0 + r;
+        if (row >= row_end) continue;
+        const int tok = row / p.g, h = w.h * p.g + row - tok * p.g;
+        const int c = wk * NB * 8 + (lane & 3) * 2;
+        if (whole) {
+          const float inv = seg_inverse(ll[i]);
+          uint32_t* dst = reinterpret_cast<uint32_t*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + c);
+#pragma unroll
+          for (int k = 0; k < NB; ++k) dst[k * 4] = pack_bf16x2(out[k][2 * i] * inv, out[k][2 * i + 1] * inv);
+          if (a.lse && wk == 0 && (lane & 3) == 0) a.lse[(int64_t)h * a.n_q + tok] = seg_lse(mm[i], ll[i]);
+        } else {
+          float* dst = p.part_o + ((int64_t)slot * MR + r) * D + c;
+#pragma unroll
+          for (int k = 0; k < NB; ++k) *reinterpret_cast<float2*>(dst + k * 8) = make_float2(out[k][2 * i], out[k][2 * i + 1]);
+          if (wk == 0 && (lane & 3) == 0) p.part_ml[slot * MR + r] = make_float2(mm[i], ll[i]);
+        }
       }
     }
     if (!whole && t0 == 0 && threadIdx.x == 0) {
@@ -576,11 +703,14 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
 
 // Pages [n_pages, page, N_kv, D] with strides as (column of a 64-column block, row, block, head, page); box = `rows` rows of all columns
 bool make_page_map(CUtensorMap* map, const void* ptr, int n_pages, int page, int N_kv, int D, int64_t tok, int64_t stride, int rows) {
-  if (D == 32) return make_kv_map(map, ptr, n_pages, page, N_kv, D, tok, stride, rows);
+  // L2 fetches what a row of one head has: the next head's keys would be gone before they are used (64 ragged single tokens, head dim 64:
+  // 113 us, 126 with 256 bytes; head dim 32: 79 and 97)
+  const CUtensorMapL2promotion fetch = D == 32 ? CU_TENSOR_MAP_L2_PROMOTION_L2_64B : (D == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+  if (D == 32) return make_kv_map(map, ptr, n_pages, page, N_kv, D, tok, stride, rows, fetch);
   const cuuint64_t dims[5] = {64, (cuuint64_t)page, (cuuint64_t)D / 64, (cuuint64_t)N_kv, (cuuint64_t)n_pages};
   const cuuint64_t strides[4] = {(cuuint64_t)tok * 2, 128, (cuuint64_t)D * 2, (cuuint64_t)stride * 2};
   const cuuint32_t box[5] = {64, (cuuint32_t)rows, (cuuint32_t)D / 64, 1, 1};
-  return encode_bf16(map, ptr, 5, dims, strides, box);
+  return encode_bf16(map, ptr, 5, dims, strides, box, fetch);
 }
 
 template <int D, int WR>
@@ -608,6 +738,7 @@ cudaError_t launch_one(const SegParams& p0, const PagedCache& c, int shares, boo
 }
 template <int D>
 cudaError_t launch_rows(const SegParams& p, const PagedCache& c, int rows, int shares, bool cut, cudaStream_t st, int* launches) {
+  if (rows == 8) return launch_one<D, 0>(p, c, shares, cut, st, launches);
   return rows == 16 ? launch_one<D, 1>(p, c, shares, cut, st, launches)
                     : (rows == 32 ? launch_one<D, 2>(p, c, shares, cut, st, launches) : launch_one<D, 4>(p, c, shares, cut, st, launches));
 }

@@ -244,7 +244,7 @@ PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
   const int64_t rows = (int64_t)c.max_q * g;
   const PassPlan ps = plan_pass(a, c.samples, rows, c.max_kv, warp_mma, -1);
   pl.kind = ps.kind;
-  pl.tile_rows = ps.tile_rows;
+  pl.tile_rows = pl.kind == kMma && rows <= 8 ? 8 : ps.tile_rows;
   if (pl.kind == kF32 && rows > 32) pl.tile_rows = 64;         // (30 us instead of 33 with 32)
   pl.row_tiles = (int)ceil_div(rows, pl.tile_rows);
   // a sample fills its tiles but for the last one

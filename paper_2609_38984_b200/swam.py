@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -97,6 +98,10 @@ class SwamPagedArgs(ctypes.Structure):
                 + [(n, ctypes.c_int64) for n in ("q_token", "out_token")])
 
 
+# The same layouts for struct.pack_into, which fills a structure in a third of the time that its constructor takes.
+_PACK_NORM_ROPE, _PACK_CACHE, _PACK_APPEND, _PACK_PAGED = (struct.Struct(f) for f in ("8Qiifi9q", "5Q6i5q", "9Qif4q", "6Q4i2q"))
+
+
 def rope_frequencies(rot_dim: int, base: float = 10000.0, factor: float = 1.0, trained: int = 0, turns_low: float = 1.0,
                      turns_high: float = 32.0):
     """Radians per position of the rot_dim / 2 pairs: base^(-2i / rot_dim).  `factor` > 1 stretches them for contexts longer than
@@ -173,8 +178,8 @@ def load_library() -> ctypes.CDLL:
         for name, args in (("cross", SwamCrossArgs), ("prefix", SwamPrefixArgs)):
             getattr(lib, f"swam_{name}_attn").argtypes = [vp, ctypes.POINTER(args), vp]
             getattr(lib, f"swam_{name}_attn_scratch_bytes").argtypes = [vp, ctypes.POINTER(args), ctypes.POINTER(ctypes.c_size_t)]
-        for name, args in (("norm_rope", SwamNormRopeArgs), ("append_kv", SwamAppendArgs), ("paged_attn", SwamPagedArgs)):
-            getattr(lib, f"swam_{name}").argtypes = [vp, ctypes.POINTER(args), vp]
+        for name in ("norm_rope", "append_kv", "paged_attn"):      # (an address: a packed structure needs no object around it)
+            getattr(lib, f"swam_{name}").argtypes = [vp, vp, vp]
         lib.swam_paged_attn_scratch_bytes.argtypes = [vp, ctypes.POINTER(SwamPagedArgs), ctypes.POINTER(ctypes.c_size_t)]
         lib.swam_step.argtypes = [vp, vp, vp, vp, i32, vp, vp]
         lib.swam_step_host.argtypes = [vp, vp, vp, vp, i32, vp, vp]
@@ -253,6 +258,9 @@ class Swam:
         self._device_index = device.index if device.index is not None else torch.cuda.current_device()
         self._scratch_need = {}
         self._lse_like = {}
+        # argument structures of the calls around the paged cache, filled anew for each call
+        self._args = {c: c() for c in (SwamNormRopeArgs, SwamPagedCache, SwamAppendArgs, SwamPagedArgs)}
+        self._address = {c: ctypes.addressof(a) for c, a in self._args.items()}
         self.workspace = None
         self.staging = None
         if bind:
@@ -465,14 +473,14 @@ class Swam:
         return (out, lse) if want_lse else out
 
     # -- norms, rotary positions and the paged cache -------------------------
-    def _weight(self, name: str, t: Optional[torch.Tensor]):
+    def _weight(self, name: str, t: Optional[torch.Tensor]) -> int:
         if t is None:
-            return None
+            return 0
         if t.dtype is not torch.float32 or t.get_device() != self._device_index or t.shape != (self.D,) or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous float32 tensor of shape [{self.D}] on {self.device}")
         return t.data_ptr()
 
-    def _ints(self, name: str, t: torch.Tensor, shape: tuple):
+    def _ints(self, name: str, t: torch.Tensor, shape: tuple) -> int:
         if t.dtype is not torch.int32 or t.get_device() != self._device_index or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {list(shape)} on {self.device}")
         return t.data_ptr()
@@ -490,6 +498,16 @@ class Swam:
             raise ValueError(f"{name}: expanded (stride 0) tokens are not accepted")
         return s0 if tokens > 1 else heads * self.D
 
+    def _positions(self, rope: Rope, positions, n: int):
+        """Address and sample stride of the positions of n tokens."""
+        ax = rope.n_axes
+        shape = tuple(positions.shape)
+        if shape == (n, ax) or (ax == 1 and shape == (n,)):
+            return self._ints("positions", positions, shape), 0
+        if shape == (self.B, n, ax) or (ax == 1 and shape == (self.B, n)):
+            return self._ints("positions", positions, shape), n * ax
+        raise ValueError(f"positions: expected shape [{self.B}, {n}, {ax}] or [{n}, {ax}], got {list(shape)}")
+
     def norm_rope(self, q=None, k=None, rope: Optional[Rope] = None, positions=None, q_weight=None, k_weight=None,
                   eps: float = 1e-6, q_out=None, k_out=None):
         """Queries [B, n, N_h, D] and / or keys [B, n, heads, D] (any divisor of N_h heads) normalised per head (where a float32
@@ -498,45 +516,43 @@ class Swam:
         contiguous heads; an output may be its input.  Returns (q', k') (None where there was none)."""
         if q is None and k is None:
             raise ValueError("neither q nor k given")
-        n = (k if q is None else q).shape[1] if (k if q is None else q).dim() == 4 else -1
-        a = SwamNormRopeArgs()
+        q_at = k_at = q_to = k_to = heads = n = 0
+        q_str = k_str = q_out_str = k_out_str = (0, 0)
         if q is not None:
-            a.q_token, a.q_sample = self._tokens("q", q, self.B, self.N_h)
+            q_str = self._tokens("q", q, self.B, self.N_h)
+            n = q.shape[1]
             if q_out is None:
                 q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            elif q_out.shape != q.shape:
-                raise ValueError(f"q_out: expected shape {list(q.shape)}")
-            a.q_out_token, a.q_out_sample = self._tokens("q_out", q_out, self.B, self.N_h)
-            a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
+            else:
+                if q_out.shape != q.shape:
+                    raise ValueError(f"q_out: expected shape {list(q.shape)}")
+                q_out_str = self._tokens("q_out", q_out, self.B, self.N_h)
+            q_at, q_to = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise ValueError("q_out without q")
         if k is not None:
             heads = k.shape[2] if k.dim() == 4 else 0
-            a.k_token, a.k_sample = self._tokens("k", k, self.B, heads)
-            if k.shape[1] != n:
+            k_str = self._tokens("k", k, self.B, heads)
+            if q is not None and k.shape[1] != n:
                 raise ValueError("q and k differ in length")
+            n = k.shape[1]
             if k_out is None:
                 k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-            elif k_out.shape != k.shape:
-                raise ValueError(f"k_out: expected shape {list(k.shape)}")
-            a.k_out_token, a.k_out_sample = self._tokens("k_out", k_out, self.B, heads)
-            a.k, a.k_out, a.n_kv_heads = k.data_ptr(), k_out.data_ptr(), heads
+            else:
+                if k_out.shape != k.shape:
+                    raise ValueError(f"k_out: expected shape {list(k.shape)}")
+                k_out_str = self._tokens("k_out", k_out, self.B, heads)
+            k_at, k_to = k.data_ptr(), k_out.data_ptr()
         elif k_out is not None:
             raise ValueError("k_out without k")
-        a.n, a.eps = n, eps
-        a.q_weight, a.k_weight = self._weight("q_weight", q_weight), self._weight("k_weight", k_weight)
+        pos = pos_smp = rope_at = 0
         if rope is not None:
-            a.rope = rope.address
+            rope_at = rope.address
             if positions is not None:
-                ax = rope.n_axes
-                shape = tuple(positions.shape)
-                if shape in ((n, ax), (n,) if ax == 1 else None):
-                    a.positions = self._ints("positions", positions, shape)
-                elif shape in ((self.B, n, ax), (self.B, n) if ax == 1 else None):
-                    a.positions, a.pos_sample = self._ints("positions", positions, shape), n * ax
-                else:
-                    raise ValueError(f"positions: expected shape [{self.B}, {n}, {ax}] or [{n}, {ax}], got {list(shape)}")
-        rc = self.lib.swam_norm_rope(self.ctx, ctypes.byref(a), _raw_stream())
+                pos, pos_smp = self._positions(rope, positions, n)
+        _PACK_NORM_ROPE.pack_into(self._args[SwamNormRopeArgs], 0, rope_at, q_at, k_at, q_to, k_to, self._weight("q_weight", q_weight),
+                                  self._weight("k_weight", k_weight), pos, n, heads, eps, 0, pos_smp, *q_str, *k_str, *q_out_str, *k_out_str)
+        rc = self.lib.swam_norm_rope(self.ctx, self._address[SwamNormRopeArgs], _raw_stream())
         if rc != OK:
             self._chk(rc)
         return q_out, k_out
@@ -549,16 +565,20 @@ class Swam:
         v_tok, v_page = self._tokens("v_pages", v_pages, None, heads)
         samples = kv_len.shape[0] if kv_len.dim() == 1 else 0
         if page_table.dtype is not torch.int32 or page_table.get_device() != self._device_index or page_table.dim() != 2 or \
-                page_table.shape[0] != samples or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-            raise ValueError(f"page_table: expected an int32 tensor of shape [{samples}, pages] with contiguous rows on {self.device}")
-        max_pages = page_table.shape[1]
-        stride = page_table.stride(0) if samples > 1 else max_pages
-        if samples > 1 and stride < max_pages:
-            raise ValueError("page_table: rows overlap")
-        return SwamPagedCache(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
-                              self._ints("kv_len", kv_len, (samples,)),
-                              None if q_start is None else self._ints("q_start", q_start, (samples + 1,)), samples, n_pages,
-                              page, max_pages, heads, 0, stride, k_page, k_tok, v_page, v_tok)
+                page_table.shape[0] != samples:
+            raise ValueError(f"page_table: expected an int32 tensor of shape [{samples}, pages] on {self.device}")
+        max_pages = stride = page_table.shape[1]
+        if not page_table.is_contiguous():
+            stride, step = page_table.stride()
+            if (max_pages > 1 and step != 1) or (samples > 1 and stride < max_pages):
+                raise ValueError("page_table: rows must be contiguous and apart")
+            if samples <= 1:
+                stride = max_pages
+        c = self._args[SwamPagedCache]
+        _PACK_CACHE.pack_into(c, 0, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), self._ints("kv_len", kv_len, (samples,)),
+                              0 if q_start is None else self._ints("q_start", q_start, (samples + 1,)), samples, n_pages, page,
+                              max_pages, heads, 0, stride, k_page, k_tok, v_page, v_tok)
+        return c
 
     def append_kv(self, k, v, k_pages, v_pages, page_table, kv_len, q_start=None, q=None, rope: Optional[Rope] = None,
                   positions=None, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None):
@@ -568,30 +588,27 @@ class Swam:
         (int32 [samples]); token c of it lives in row c % page size of page page_table[b, c / page size] (int32 [samples, pages]).
         positions: int32 [tokens, axes] ([tokens] with one axis); default: a token's number in its sample."""
         tokens = k.shape[0] if k.dim() == 3 else 0
-        c = self._cache(k_pages, v_pages, page_table, kv_len, q_start)
-        heads = c.n_kv_heads
-        a = SwamAppendArgs()
-        a.cache = ctypes.addressof(c)
-        a.k, a.v = k.data_ptr(), v.data_ptr()
-        a.k_token, a.v_token = self._packed("k", k, tokens, heads), self._packed("v", v, tokens, heads)
+        self._cache(k_pages, v_pages, page_table, kv_len, q_start)
+        heads = k_pages.shape[2]
+        k_tok, v_tok = self._packed("k", k, tokens, heads), self._packed("v", v, tokens, heads)
+        q_at = q_to = q_tok = q_out_tok = pos = rope_at = 0
         if q is not None:
-            a.q_token = self._packed("q", q, tokens, self.N_h)
+            q_tok = self._packed("q", q, tokens, self.N_h)
             if q_out is None:
                 q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            a.q_out_token = self._packed("q_out", q_out, tokens, self.N_h)
-            a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
+            else:
+                q_out_tok = self._packed("q_out", q_out, tokens, self.N_h)
+            q_at, q_to = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise ValueError("q_out without q")
-        a.q_weight, a.k_weight = self._weight("q_weight", q_weight), self._weight("k_weight", k_weight)
         if rope is not None:
-            a.rope = rope.address
+            rope_at = rope.address
             if positions is not None:
-                shape = (tokens, rope.n_axes)
-                if rope.n_axes == 1 and positions.dim() == 1:
-                    shape = (tokens,)
-                a.positions = self._ints("positions", positions, shape)
-        a.n_tokens, a.eps = tokens, eps
-        rc = self.lib.swam_append_kv(self.ctx, ctypes.byref(a), _raw_stream())
+                pos = self._ints("positions", positions, (tokens,) if rope.n_axes == 1 and positions.dim() == 1 else (tokens, rope.n_axes))
+        _PACK_APPEND.pack_into(self._args[SwamAppendArgs], 0, self._address[SwamPagedCache], rope_at, q_at, k.data_ptr(), v.data_ptr(), q_to,
+                               self._weight("q_weight", q_weight), self._weight("k_weight", k_weight), pos, tokens, eps, q_tok,
+                               k_tok, v_tok, q_out_tok)
+        rc = self.lib.swam_append_kv(self.ctx, self._address[SwamAppendArgs], _raw_stream())
         if rc != OK:
             self._chk(rc)
         return q_out
@@ -605,15 +622,18 @@ class Swam:
         tokens = q.shape[0] if q.dim() == 3 else 0
         c = self._cache(k_pages, v_pages, page_table, kv_len, q_start)
         q_tok = self._packed("q", q, tokens, self.N_h)
+        o_tok = 0
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        o_tok = self._packed("out", out, tokens, self.N_h)
+        else:
+            o_tok = self._packed("out", out, tokens, self.N_h)
         lse = torch.empty((self.N_h, tokens), dtype=torch.float32, device=self.device) if want_lse else None
-        a = SwamPagedArgs(ctypes.addressof(c), q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else None, None, 0, tokens,
-                          max_q, max_kv, 1 if causal else 0, q_tok, o_tok)
+        a = self._args[SwamPagedArgs]
+        _PACK_PAGED.pack_into(a, 0, self._address[SwamPagedCache], q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, 0, 0, tokens,
+                              max_q, max_kv, 1 if causal else 0, q_tok, o_tok)
         key = ("paged", tokens, c.n_samples, c.n_pages, c.page_size, c.max_pages, c.n_kv_heads, q_start is None, max_q, max_kv)
         scratch = self._scratch(self.lib.swam_paged_attn_scratch_bytes, a, key)  # noqa: F841
-        rc = self.lib.swam_paged_attn(self.ctx, ctypes.byref(a), _raw_stream())
+        rc = self.lib.swam_paged_attn(self.ctx, self._address[SwamPagedArgs], _raw_stream())
         if rc != OK:
             self._chk(rc)
         return (out, lse) if want_lse else out
