@@ -128,10 +128,12 @@ __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_kernel(const __grid_
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t0 = (int)blockIdx.x * p.per, count = min(p.per, (int)p.tokens - t0);
   const int l = lane % LPR, sub = lane / LPR, half = p.rot >> 1;
-  // first elements of the lane's two times 16 bytes.  kPair = 0: the halves of its pairs, or neighbours of the part that does not turn
+  // First elements of the lane's two times 16 bytes: kPair = 0: the halves of its pairs; otherwise, and where nothing turns, any two, so
+  // that the lanes of a row follow one another (neighbouring chunks in one lane fetch and write every 32-byte sector twice: 145
+  // instead of 107 us for the multi-view batch).
   const int turning = kPair == 0 ? half / N : 0;
-  const int e0 = kPair == 0 && l >= turning ? (2 * l) * N : (kPair == 0 ? l : 2 * l) * N;
-  const int e1 = kPair == 0 && l < turning ? e0 + half : e0 + N;
+  const int e0 = (kPair == 0 && l >= turning ? turning + l : l) * N;
+  const int e1 = e0 + (kPair == 0 ? (l < turning ? half : (LPR - turning) * N) : D / 2);
   if (threadIdx.x < half) turns[threadIdx.x] = p.turn[threadIdx.x];
   // ---- where the tokens come from, one thread each (packed tokens are one sequence)
   const int t = t0 + (int)threadIdx.x;
@@ -254,41 +256,47 @@ __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_kernel(const __grid_
       //   kPair 0: x' = x xx + y xy, y' = y yy + x yx;   kPair 1: x' = x xx + swapped(x) xy, y' = y yy + swapped(y) yx
       uint64_t xx[N2], xy[N2], yx[N2], yy[N2];
       if (kind < 2) {
-        // (kPair 0: the lane's pairs are e0 ..., kPair 1: e0 / 2 ...)
-        const int at = k * (D / 2) + (kPair == 0 ? e0 : e0 / 2);
-        const bool turns_any = kPair == 0 ? l < turning : (kPair == 1 && e0 < p.rot);
+        const float* cv = cosv + k * (D / 2);
+        const float* sv = sinv + k * (D / 2);
 #pragma unroll
-        for (int j = 0; j < N; j += 4) {
-          float4 wa = make_float4(1.f, 1.f, 1.f, 1.f), wb = wa, c = wa, sn = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int j = 0; j < N2; j += 2) {
+          float4 wa = make_float4(1.f, 1.f, 1.f, 1.f), wb = wa;
           if (weight) {
-            wa = __ldg(reinterpret_cast<const float4*>(weight + e0 + (kPair == 1 ? 2 * j : j)));
-            wb = __ldg(reinterpret_cast<const float4*>(weight + (kPair == 1 ? e0 + 2 * j + 4 : e1 + j)));
+            wa = __ldg(reinterpret_cast<const float4*>(weight + e0 + 2 * j));
+            wb = __ldg(reinterpret_cast<const float4*>(weight + e1 + 2 * j));
           }
-          if (turns_any) {
-            c = *reinterpret_cast<const float4*>(cosv + at + j);
-            sn = *reinterpret_cast<const float4*>(sinv + at + j);
-          }
-          if constexpr (kPair == 1) {
-            // four pairs: eight elements of the 2 N in a row; those behind rot / 2 do not turn
-            const float wv[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w}, cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {sn.x, sn.y, sn.z, sn.w};
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-              const bool on = p.rot == D || e0 + 2 * (j + d) < p.rot;
-              const float cd = on ? cc[d] : 1.f, sd = on ? ss[d] : 0.f;
-              uint64_t& own = j + d < N2 ? xx[(j + d) % N2] : yy[(j + d) % N2];
-              uint64_t& other = j + d < N2 ? xy[(j + d) % N2] : yx[(j + d) % N2];
-              own = pair(cd * wv[2 * d], cd * wv[2 * d + 1]);
-              other = pair(-sd * wv[2 * d + 1], sd * wv[2 * d]);
+          xx[j] = pair(wa.x, wa.y);
+          xx[j + 1] = pair(wa.z, wa.w);
+          yy[j] = pair(wb.x, wb.y);
+          yy[j + 1] = pair(wb.z, wb.w);
+          xy[j] = xy[j + 1] = yx[j] = yx[j + 1] = 0ull;
+          if constexpr (kPair == 0) {
+            if (l < turning) {
+              const float4 c = *reinterpret_cast<const float4*>(cv + e0 + 2 * j), sn = *reinterpret_cast<const float4*>(sv + e0 + 2 * j);
+              xx[j] = pair(c.x * wa.x, c.y * wa.y);
+              xx[j + 1] = pair(c.z * wa.z, c.w * wa.w);
+              xy[j] = pair(-sn.x * wb.x, -sn.y * wb.y);
+              xy[j + 1] = pair(-sn.z * wb.z, -sn.w * wb.w);
+              yx[j] = pair(sn.x * wa.x, sn.y * wa.y);
+              yx[j + 1] = pair(sn.z * wa.z, sn.w * wa.w);
+              yy[j] = pair(c.x * wb.x, c.y * wb.y);
+              yy[j + 1] = pair(c.z * wb.z, c.w * wb.w);
             }
-          } else {
-            xx[j / 2] = pair(c.x * wa.x, c.y * wa.y);
-            xx[j / 2 + 1] = pair(c.z * wa.z, c.w * wa.w);
-            xy[j / 2] = pair(-sn.x * wb.x, -sn.y * wb.y);
-            xy[j / 2 + 1] = pair(-sn.z * wb.z, -sn.w * wb.w);
-            yx[j / 2] = pair(sn.x * wa.x, sn.y * wa.y);
-            yx[j / 2 + 1] = pair(sn.z * wa.z, sn.w * wa.w);
-            yy[j / 2] = pair(c.x * wb.x, c.y * wb.y);
-            yy[j / 2 + 1] = pair(c.z * wb.z, c.w * wb.w);
+          } else if constexpr (kPair == 1) {
+            // two pairs of each 16 bytes; those behind rot / 2 do not turn
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+              const int pa = e0 / 2 + j + d, pb = e1 / 2 + j + d;
+              const float2 va = d == 0 ? make_float2(wa.x, wa.y) : make_float2(wa.z, wa.w), vb = d == 0 ? make_float2(wb.x, wb.y) : make_float2(wb.z, wb.w);
+              if (pa < half) {
+                xx[j + d] = pair(cv[pa] * va.x, cv[pa] * va.y);
+                xy[j + d] = pair(-sv[pa] * va.y, sv[pa] * va.x);
+              }
+              if (pb < half) {
+                yy[j + d] = pair(cv[pb] * vb.x, cv[pb] * vb.y);
+                yx[j + d] = pair(-sv[pb] * vb.y, sv[pb] * vb.x);
+              }
+            }
           }
         }
       }
@@ -344,7 +352,7 @@ __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_kernel(const __grid_
               float own[2] = {parts(v).x, parts(v).y};
 #pragma unroll
               for (int d = 0; d < 2; ++d) {
-                const int e = e0 + 2 * j + d, o = e < half ? e + half : e - half, at = k * (D / 2) + (e < half ? e : o);
+                const int e = (j < N2 ? e0 : e1) + 2 * (j % N2) + d, o = e < half ? e + half : e - half, at = k * (D / 2) + (e < half ? e : o);
                 if (e < p.rot && there) {
                   float other = (float)row[o];
                   if (weight) other *= __ldg(weight + o);
