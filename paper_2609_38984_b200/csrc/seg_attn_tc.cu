@@ -27,6 +27,9 @@
 // kAlt = true: a row tile has at most 128 rows; both streams hold the same rows and take the key tiles in turn (over the
 //   borders of items), each with its own maximum, sum and output accumulator, and are merged in the epilogue.  The memory of the second query tile
 //   goes to the ring.
+// Paged keys, at most 64 rows: the tile holds the rows twice, and stream 1 works on the second half, so that its exponentials run on the
+//   sub-cores of the TMEM lanes that stream 0 leaves idle (16 chunks of 64 tokens, head dim 64: 131 us with both in the first half).
+//   Its accumulators are out of stream 0's reach there and come through the item's query buffer as fp32.
 // A tile that ends early costs what its real keys cost: Q K^T and P V stop at the 16-key step of the last one, the exponentials
 // at its 32.  Rows of V between it and the end of the step are overwritten with zeros in shared memory (0 * NaN would poison
 // the row); scores behind a row's limit become -inf.
@@ -92,6 +95,7 @@ struct SegTcArgs {
   int box_out;      // finished tiles leave as boxes of map_o
   int items;        // of the passes of this launch
   int steal;        // paged: more blocks than SMs, whose items running blocks take over
+  int twice;        // paged, kAlt, at most 64 rows: the rows lie twice in the tile, see below
 };
 
 __device__ __forceinline__ void tma_store_5d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3, int c4) {
@@ -149,12 +153,14 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const SegArgs& a = p.a;
 
+  const bool twice = kPaged && kAlt && x.twice;
+
   if (p.early && pass0 == 0) allow_next();
 
   if (threadIdx.x == 0) {
     for (int b = 0; b < QB; ++b) {
       mbar_init(bar_q(b), x.box_q ? 1 : 32);
-      mbar_init(bar_q_free(b), 1 + (!p.direct ? 0 : C::NQ * (x.box_out ? 1 : 4)));
+      mbar_init(bar_q_free(b), 1 + (twice ? 4 : (!p.direct ? 0 : C::NQ * (x.box_out ? 1 : 4))));
     }
     for (int s = 0; s < ST; ++s) {
       mbar_init(bar_full(s), 1);
@@ -438,7 +444,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         const int row0 = d.row0 & 0x3fffffff, block_samples = p.pass[d.row0 >> 30].block_samples;
         for (int blk = 0; blk < C::kRows / 32; ++blk) {
           // lane l knows row blk * 32 + l; the rows are then copied RPI at a time
-          const SegRow r = seg_row(p, block_samples, d.b0, d.h_kv, row0 + blk * 32 + lane);
+          const SegRow r = seg_row(p, block_samples, d.b0, d.h_kv, row0 + (twice ? blk & 1 : blk) * 32 + lane);
           const int64_t off = r.real ? r.b * a.q_smp + r.t * a.q_tok + (int64_t)r.h * D : -1;
           const uint32_t dst = sQ + (uint32_t)((qb * C::NQ + (blk >> 2)) * C::kTileBytes + (cc >> 3) * C::kSub + (blk & 3) * 32 * 128);
 #pragma unroll 4
@@ -511,8 +517,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               for (int q = 0; q < C::NQ; ++q) {
                 const int r = (o.row0 & 0x3fffffff) + q * kTile;
                 const int smp = mixed ? r / (a.n_q * p.g) : 0, tok = mixed ? 0 : r / p.g;
-                for (int db = 0; db < C::DB; ++db)
+                for (int db = 0; db < C::DB; ++db) {
                   tma_load_5d(sQ + (qb * C::NQ + q) * C::kTileBytes + db * C::kSub, &map_q, bar_q(qb), db * 64, 0, tok, o.h_kv, o.b0 + smp);
+                  if (twice) tma_load_5d(sQ + qb * C::kTileBytes + db * C::kSub + 64 * 128, &map_q, bar_q(qb), db * 64, 0, tok, o.h_kv, o.b0);
+                }
               }
             }
           }
@@ -720,6 +728,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     // ------------------------------------------------------------------ softmax: one thread per row and stream
     const int s = warp >> 2;                     // stream
     const int r = (warp & 3) * 32 + lane;        // row inside the tile == TMEM lane
+    const int r_item = twice && s == 1 ? r - 64 : r;       // row of the item (negative, or 64 and more with `twice`: none)
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tO = tm_O(s) + lane_off;
     bool ok = true;
@@ -732,9 +741,31 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     // Writes one row: accumulators times their weights; an accumulator of weight 0 may hold anything.
     auto flush = [&]() {
       pend = false;
-      if (kAlt && s == 1) return true;           // stream 0 writes for both
+      if (kAlt && s == 1 && !twice) return true;           // stream 0 writes for both
       if (!wait(bar_o_final, (iter - 1) & 1)) return false;
       const int qb = (iter - 1) % QB;
+      if (kPaged && kAlt && s == 1) {
+        // the accumulators for stream 0, [4 columns][64 rows]
+        tc_fence_after();
+        if (pend_warp) {
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            float ov[32];
+            __syncwarp();
+            tmem_ld32(tO + c * 32, ov);
+            tmem_ld_wait();
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              st_shared_16(sQ + (uint32_t)(qb * C::kTileBytes + ((c * 8 + q) * 64 + r_item) * 16), __float_as_uint(ov[q * 4]), __float_as_uint(ov[q * 4 + 1]),
+                           __float_as_uint(ov[q * 4 + 2]), __float_as_uint(ov[q * 4 + 3]));
+          }
+        }
+        tc_fence_before();
+        fence_proxy_async();                   // the next loads of this buffer come through the other proxy
+        arrive(bar_x);
+        arrive(bar_o_free);
+        return true;
+      }
       // (the addresses are computed here, once per item: hoisted out of the loop over the items they would live, or be
       // spilled, across the softmax pass)
       int rr = r;
@@ -775,12 +806,33 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           for (int j = 0; j < 32; ++j) ov[j] *= f0;
           if constexpr (kAlt) {
             float o1[32];
-            tmem_ld32(tm_O(1) + lane_off + c * 32, o1);
-            tmem_ld_wait();
+            if (twice) {
+              const float4* src = reinterpret_cast<const float4*>(base_ptr + qb * C::kTileBytes) + c * 8 * 64 + rr;
+#pragma unroll
+              for (int q = 0; q < 8; ++q) *reinterpret_cast<float4*>(o1 + q * 4) = src[q * 64];
+            } else {
+              tmem_ld32(tm_O(1) + lane_off + c * 32, o1);
+              tmem_ld_wait();
+            }
 #pragma unroll
             for (int j = 0; j < 32; ++j) ov[j] = f1 != 0.f ? fmaf(o1[j], f1, ov[j]) : ov[j];
           }
-          if (p.direct) {
+          if (twice && p.direct) {
+            if (pend_real) {
+              const int tok = pend_row / a.N_h, h = pend_row - tok * a.N_h;
+              uint32_t w[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(ov[2 * j], ov[2 * j + 1]);
+              unsigned char* dst = (unsigned char*)((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + c * 32);
+              if ((a.o_tok & 15) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 31) == 0) {
+                st_global_32(dst, w);
+                st_global_32(dst + 32, w + 8);
+              } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(dst + q * 16) = make_uint4(w[q * 4], w[q * 4 + 1], w[q * 4 + 2], w[q * 4 + 3]);
+              }
+            }
+          } else if (p.direct) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               const int c16 = c * 4 + q;
@@ -799,7 +851,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       }
       tc_fence_before();
       arrive(bar_o_free);                   // the accumulators have been read
-      if (p.direct) {
+      if (twice) {
+        fence_proxy_async();                     // the next loads of this buffer come through the other proxy
+        arrive(bar_q_free(qb));
+      } else if (p.direct) {
         // the staged tile leaves as a box, or row by row with 16-byte stores, a row or two per instruction
         if (x.box_out) {
           fence_proxy_async();
@@ -831,8 +886,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     while (ok && next_desc(di, d)) {
       const int n = d.n, na = d.na, part = d.part;
       const int row0 = (d.row0 & 0x3fffffff) + (kAlt ? 0 : s * kTile);       // of the stream's tile
-      SegRow row = seg_row(p, p.pass[d.row0 >> 30].block_samples, d.b0, d.h_kv, row0 + r);
-      if (kPaged) row.real = row0 + r < d.base0;
+      SegRow row = seg_row(p, p.pass[d.row0 >> 30].block_samples, d.b0, d.h_kv, row0 + max(r_item, 0));
+      if (kPaged) row.real = row0 + r_item < d.base0 && (!twice || (unsigned)r_item < 64u);
       const int grow = (row.b * a.n_q + row.t) * a.N_h + row.h;
       const bool row_real = row.real, warp_real = __any_sync(0xffffffffu, row_real);
       // real keys ahead of each segment's first tile in this item, and those of segment 1 that this row sees
@@ -1027,9 +1082,11 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         // stream 0 has read the previous item's values
         if (iter > 0) ok = wait(bar_o_free, (iter - 1) & 1);
         if (!ok) break;
-        ml_x[r] = make_float2(pend_m, pend_l);
-        arrive(bar_x);
-        arrive(bar_o_free);
+        if (r_item >= 0) ml_x[r_item] = make_float2(pend_m, pend_l);
+        if (!twice) {
+          arrive(bar_x);
+          arrive(bar_o_free);
+        }
       }
       ++iter;
       pos0 += n;
@@ -1066,8 +1123,10 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kP
   memset(&mo, 0, sizeof(mo));
   if constexpr (kPaged) {
     const int page = 1 << c.page_shift, rows = page < kTile ? page : kTile;
-    if (!make_kv_map(&mk[1], a.k[1], c.n_pages, page, a.N_kv, D, c.k_tok, c.k_page, rows) ||
-        !make_kv_map(&mv[1], a.v[1], c.n_pages, page, a.N_kv, D, c.v_tok, c.v_page, rows))
+    // (L2 fetches what a row of one head has: see paged_mma.cu)
+    const CUtensorMapL2promotion fetch = D == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B;
+    if (!make_kv_map(&mk[1], a.k[1], c.n_pages, page, a.N_kv, D, c.k_tok, c.k_page, rows, fetch) ||
+        !make_kv_map(&mv[1], a.v[1], c.n_pages, page, a.N_kv, D, c.v_tok, c.v_page, rows, fetch))
       return cudaErrorInvalidValue;
   }
   for (int s = 0; s < 2 && !kPaged; ++s) {
@@ -1083,8 +1142,13 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kP
   const bool mixed = p.pass[pass].block_samples > 1;
   const int per_sample = a.n_q * p.g;
   x.box_q = mixed ? per_sample <= kTile && kTile % per_sample == 0 : p.g <= kTile && kTile % p.g == 0;
-  x.box_out = p.direct && !mixed && x.box_q;
-  const int bt = mixed ? a.n_q : kTile / p.g, bs = mixed ? kTile / per_sample : 1;
+  x.twice = 0;
+  if constexpr (kPaged && kAlt) {
+    x.twice = (int64_t)c.max_q * p.g <= 64;
+    if (x.twice) x.box_q = p.g <= 64 && 64 % p.g == 0;
+  }
+  x.box_out = p.direct && !mixed && x.box_q && !x.twice;
+  const int bt = mixed ? a.n_q : (x.twice ? 64 : kTile) / p.g, bs = mixed ? kTile / per_sample : 1;
   if (x.box_q && !make_q_map(&mq, a.q, a, p.g, a.q_tok, a.q_smp, bt, bs)) return cudaErrorInvalidValue;
   if (x.box_out && !make_q_map(&mo, a.out, a, p.g, a.o_tok, a.o_smp, bt, bs)) return cudaErrorInvalidValue;
   x.items = p.pass[pass].items + (both ? p.pass[1].items : 0);
