@@ -623,81 +623,73 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   if (!ok && lane == 0) atomicOr(p.status, ST_TIMEOUT);
 }
 
-// Joins the pieces of one row tile: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i, pieces in order.
+// Joins the pieces of one row tile: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i.  A thread takes four columns of a row and every
+// groups-th piece, eight at a time with their maxima and sums (one trip to memory for up to 8 * groups pieces); the groups are then
+// merged in order.
+constexpr int kJoinThreads = 256;
+struct Joined {
+  float4 o;
+  float m, l;
+};
 template <int D, int MR>
-__global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ SegParams p, const int4* join) {
-  __shared__ float2 row_ml[MR];
-  __shared__ float4 part[256];
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ SegParams p, const int4* join) {
+  __shared__ Joined part[kJoinThreads];
+  constexpr int V = D / 4, kAhead = 8;
   const SegArgs& a = p.a;
   wait_previous();
   const int4 j = join[blockIdx.x];
-  const int pieces = j.w, rows = j.y - j.x;
+  const int pieces = j.w, rows = j.y - j.x, items = rows * V;
   if (pieces <= 1) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int first = (int)blockIdx.x;                         // piece 0 in its second slot, piece i in the first slot of share first + i
-  auto slot = [&](int i) { return i == 0 ? first * 2 + 1 : (first + i) * 2; };
-  for (int r = warp; r < rows; r += 8) {
-    float m = -INFINITY, l = 0.f;
-    for (int i = lane; i < pieces; i += 32) {
-      const float2 x = p.part_ml[slot(i) * MR + r];
-      const float mn = fmaxf(m, x.x);
-      if (mn != -INFINITY) l = l * exp2f(m - mn) + x.y * exp2f(x.x - mn);
-      m = mn;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
-      const float mn = fmaxf(m, m2);
-      // (both lanes of a pair form the same sum)
-      if (mn != -INFINITY) l = l * exp2f(m - mn) + l2 * exp2f(m2 - mn);
-      m = mn;
-    }
-    if (lane == 0) row_ml[r] = make_float2(m, l);
-  }
-  __syncthreads();
-  constexpr int V = D / 4;
-  const int items = rows * V, groups = items >= 256 ? 1 : 256 / items;
-  for (int x0 = 0; x0 < items; x0 += 256) {
-    const int x = x0 + (int)threadIdx.x;
-    const int grp = groups > 1 ? x / items : 0, item = x - grp * items;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  // piece 0 is in its share's second slot, piece i in the first slot of the i-th share behind it
+  auto slot = [&](int i) { return i == 0 ? (int)blockIdx.x * 2 + 1 : ((int)blockIdx.x + i) * 2; };
+  auto add = [](Joined& x, float m, float l, const float4& o) {
+    const float mn = fmaxf(x.m, m);
+    if (mn == -INFINITY) return;             // neither has keys
+    const float f = exp2f(x.m - mn), g = exp2f(m - mn);
+    x.l = x.l * f + l * g;
+    x.o = make_float4(fmaf(o.x, g, x.o.x * f), fmaf(o.y, g, x.o.y * f), fmaf(o.z, g, x.o.z * f), fmaf(o.w, g, x.o.w * f));
+    x.m = mn;
+  };
+  const int groups = items >= kJoinThreads ? 1 : kJoinThreads / items;
+  for (int x0 = 0; x0 < items; x0 += kJoinThreads) {
+    const int x = x0 + (int)threadIdx.x, grp = groups > 1 ? x / items : 0, item = x - grp * items;
+    const int r = item / V, c = (item - r * V) * 4;
     const bool on = groups > 1 ? grp < groups : x < items;
-    if (on) {
-      const int r = item / V, c = (item - r * V) * 4;
-      const float m = row_ml[r].x;
-#pragma unroll 4
-      for (int i = grp; i < pieces; i += groups) {
-        const float mi = p.part_ml[slot(i) * MR + r].x;
-        const float4 v = *reinterpret_cast<const float4*>(p.part_o + ((int64_t)slot(i) * MR + r) * D + c);
-        const float f = mi == -INFINITY ? 0.f : exp2f(mi - m);
-        if (f != 0.f) {
-          acc.x = fmaf(f, v.x, acc.x);
-          acc.y = fmaf(f, v.y, acc.y);
-          acc.z = fmaf(f, v.z, acc.z);
-          acc.w = fmaf(f, v.w, acc.w);
+    Joined sum{make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
+    for (int i0 = grp; on && i0 < pieces; i0 += kAhead * groups) {
+      float4 o[kAhead];
+      float2 ml[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = i0 + k * groups;
+        if (i < pieces) {
+          const int at = slot(i) * MR + r;
+          ml[k] = p.part_ml[at];
+          o[k] = *reinterpret_cast<const float4*>(p.part_o + (int64_t)at * D + c);
+        } else {
+          ml[k] = make_float2(-INFINITY, 0.f);
+          o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
       }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        add(sum, ml[k].x, ml[k].y, o[k]);
     }
     if (groups > 1) {
-      part[threadIdx.x] = acc;
+      part[threadIdx.x] = sum;
       __syncthreads();
       if ((int)threadIdx.x >= items) break;
       for (int k = 1; k < groups; ++k) {
-        const float4 y = part[threadIdx.x + k * items];
-        acc.x += y.x;
-        acc.y += y.y;
-        acc.z += y.z;
-        acc.w += y.w;
+        const Joined& y = part[threadIdx.x + k * items];
+        add(sum, y.m, y.l, y.o);
       }
     }
-    if (x < items) {
-      const int r = x / V, c = (x - r * V) * 4, row = j.x + r, tok = row / p.g, h = j.z * p.g + row - tok * p.g;
-      const float2 s = row_ml[r];
-      const float inv = seg_inverse(s.y);
-      *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + c) =
-          make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-      if (a.lse && c == 0) a.lse[(int64_t)h * a.n_q + tok] = seg_lse(s.x, s.y);
-    }
+    if (!on) continue;
+    const int row = j.x + r, tok = row / p.g, h = j.z * p.g + row - tok * p.g;
+    const float inv = seg_inverse(sum.l);
+    *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + c) =
+        make_uint2(pack_bf16x2(sum.o.x * inv, sum.o.y * inv), pack_bf16x2(sum.o.z * inv, sum.o.w * inv));
+    if (a.lse && c == 0) a.lse[(int64_t)h * a.n_q + tok] = seg_lse(sum.m, sum.l);
   }
 }
 
@@ -734,7 +726,7 @@ cudaError_t launch_one(const SegParams& p0, const PagedCache& c, int shares, boo
   e = cudaGetLastError();
   if (e != cudaSuccess || !cut) return e;
   ++*launches;
-  return launch_after(paged_join_kernel<D, C::MR>, dim3(shares), dim3(256), 0, st, p, (const int4*)join);
+  return launch_after(paged_join_kernel<D, C::MR>, dim3(shares), dim3(kJoinThreads), 0, st, p, (const int4*)join);
 }
 template <int D>
 cudaError_t launch_rows(const SegParams& p, const PagedCache& c, int rows, int shares, bool cut, cudaStream_t st, int* launches) {

@@ -65,7 +65,16 @@ __global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ 
   float acc[CPL];
 #pragma unroll
   for (int c = 0; c < CPL; ++c) acc[c] = 0.f;
-  for (int i0 = 0; i0 < parts; i0 += kMergeBatch) {
+  int used = parts;                                     // paged: pieces behind a sample's last key have weight 0
+  if constexpr (kPaged) {
+    used = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t some = __ballot_sync(0xffffffffu, wi[j] != 0.f);
+      if (some) used = j * 32 + 32 - __clz(some);
+    }
+  }
+  for (int i0 = 0; i0 < used; i0 += kMergeBatch) {
     if (i0 > 0) load(i0);
     const float w4 = i0 < 32 ? wi[0] : (i0 < 64 ? wi[1] : (i0 < 96 ? wi[2] : wi[3]));
 #pragma unroll
