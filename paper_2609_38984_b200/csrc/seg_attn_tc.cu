@@ -64,6 +64,20 @@ struct __align__(16) SegDesc {
   // Paged keys are all segment 1.  base0: where the sample's rows end (rows count from the call's first token); kv0: the sample.
 };
 
+// A place in a ring of N and the parity of its barrier's phase.  (The issuing warp's instructions count: a division for each place cost
+// it more than the products' issue.)
+template <int N>
+struct Turn {
+  int at = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step() {
+    if (++at == N) {
+      at = 0;
+      phase ^= 1;
+    }
+  }
+};
+
 template <int D, bool kAlt>
 struct SegCfg {
   static constexpr int DB = D / 64;                  // 64-column (128-byte) blocks per row
@@ -557,6 +571,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       // ------------------------------------------------------------------ MMA issuer (warp converged, one lane issues)
       const uint32_t el = elect_one();
       const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sR, 16), v_lo = desc_lo(sR, C::kSub);
+      // what all lanes read alike, as the compiler cannot know
+      auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
       // k16: 16-key steps with real keys.  A tile that ends early takes no more columns of Q K^T and steps of P V than these.
       auto issue_qk = [&](int qt, int buf, int st, int k16) {
         const uint32_t a_lo = q_lo + ((uint32_t)(qt * C::kTileBytes) >> 4), b_lo = k_lo + ((uint32_t)(st * C::kTileBytes) >> 4);
@@ -587,12 +603,13 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       // other buffer, and the tensor pipe runs one thread's instructions in order, so that a score buffer is free for the
       // Q K^T issued behind the P V that reads it.
       bool ok = true, k_end = false;
-      int pos = 0;                                  // ring slots taken so far
+      Turn<ST> ring;                                // next ring slot
       int kn = 0, ki = 0, kiter = -1;               // item of Q K^T (descriptor di - 1): tiles, next tile, number
       int vn = 0, vi = 0, viter = -1;               // item of P V (descriptor viter)
       int kna = 0, kr0 = 0, kr1 = 0;                // their tiles of segment 0, and real keys ahead of each segment's first tile
       int vna = 0, vr0 = 0, vr1 = 0;
-      int qk_u = 0, pv_u = 0;                       // units issued so far: unit u uses score buffer u % NB
+      Turn<NB> qk_at, pv_at;                        // score buffers of the next units
+      int qk_s = 0, pv_s = 0;                       // kAlt: their streams
       int k_st = 0, k_k16 = 0;                      // slot and steps of the current K tile
       // makes (kn, ki) the next tile of Q K^T and takes its ring slot; false at the end
       auto next_k = [&]() {
@@ -600,20 +617,19 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           const int slot = di % kDesc;
           ok = wait(bar_d_full(slot), (di / kDesc) & 1);
           if (!ok) return false;
-          kn = desc[slot].n;
-          kna = desc[slot].na;
-          kr0 = desc[slot].len0 - desc[slot].base0;
-          kr1 = desc[slot].len1 - desc[slot].base1;
+          kn = uniform(desc[slot].n);
+          kna = uniform(desc[slot].na);
+          kr0 = uniform(desc[slot].len0 - desc[slot].base0);
+          kr1 = uniform(desc[slot].len1 - desc[slot].base1);
           ++di;
           ki = 0;
           k_end = kn == 0;
         }
         if (k_end) {
           // the empty slot in the place of a missing K
-          const int st = pos % ST;
-          ok = wait(bar_full(st), (pos / ST) & 1);
-          if (lane == 0) mbar_arrive(bar_empty(st));
-          ++pos;
+          ok = wait(bar_full(ring.at), ring.phase);
+          if (lane == 0) mbar_arrive(bar_empty(ring.at));
+          ring.step();
           return false;
         }
         if (ki == 0) {
@@ -622,17 +638,17 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           if (!ok) return false;
           if (!x.box_q) fence_proxy_async();
         }
-        k_st = pos % ST;
+        k_st = ring.at;
         k_k16 = steps16((ki >= kna ? kr1 : kr0) - ki * kTile);
-        ok = wait(bar_full(k_st), (pos / ST) & 1);
-        ++pos;
+        ok = wait(bar_full(k_st), ring.phase);
+        ring.step();
         return ok;
       };
       // Q K^T of the current K tile and stream s; `last` releases the tile (and with the item's last tile the queries)
       auto qk = [&](int s, bool last) {
         tc_fence_after();
-        issue_qk((kiter % QB) * C::NQ + (kAlt ? 0 : s), qk_u % NB, k_st, k_k16);
-        ++qk_u;
+        issue_qk((kiter % QB) * C::NQ + (kAlt ? 0 : s), qk_at.at, k_st, k_k16);
+        qk_at.step();
         if (last) {
           tc_commit(bar_empty(k_st), el);
           if (++ki == kn) tc_commit(bar_q_free(kiter % QB), el);
@@ -650,14 +666,14 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           ++viter;
           vi = 0;
           const SegDesc& o = desc[viter % kDesc];
-          vn = o.n;
-          vna = o.na;
-          vr0 = o.len0 - o.base0;
-          vr1 = o.len1 - o.base1;
+          vn = uniform(o.n);
+          vna = uniform(o.na);
+          vr0 = uniform(o.len0 - o.base0);
+          vr1 = uniform(o.len1 - o.base1);
         }
-        v_st = pos % ST;
-        ok = wait(bar_full(v_st), (pos / ST) & 1);
-        ++pos;
+        v_st = ring.at;
+        ok = wait(bar_full(v_st), ring.phase);
+        ring.step();
         const int real = (vi >= vna ? vr1 : vr0) - vi * kTile;
         v_k16 = steps16(real);
         if (ok && real < v_k16 * 16) {
@@ -674,11 +690,11 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         return ok;
       };
       auto pv = [&](int s, bool last) {
-        ok = wait(bar_p_full(pv_u % NB), (pv_u / NB) & 1);
+        ok = wait(bar_p_full(pv_at.at), pv_at.phase);
         if (!ok) return;
         tc_fence_after();
-        issue_pv(s, pv_u % NB, v_st, kAlt ? vi > 1 : vi > 0, v_k16);
-        ++pv_u;
+        issue_pv(s, pv_at.at, v_st, kAlt ? vi > 1 : vi > 0, v_k16);
+        pv_at.step();
         if (last) {
           tc_commit(bar_empty(v_st), el);
           if (++vi == vn) tc_commit(bar_o_final, el);
@@ -707,13 +723,16 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       } else {
         auto qk_alt = [&]() {
           if (!next_k()) return;
-          if (qk_u & 1) qk(1, true);
-          else qk(0, true);
+          if (qk_s) qk(1, true);         // (a stream that is known here keeps the addresses out of the vector registers: 187 and 176 us for
+          else qk(0, true);              // 144 items of 64 rows and 20064 keys)
+          qk_s ^= 1;
         };
+#pragma unroll 1
         for (int j = 0; j < LK && ok; ++j) qk_alt();
         while (v_left() && next_v()) {
-          if (pv_u & 1) pv(1, true);
+          if (pv_s) pv(1, true);
           else pv(0, true);
+          pv_s ^= 1;
           if (v_left()) qk_alt();
         }
       }
@@ -728,7 +747,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     // ------------------------------------------------------------------ softmax: one thread per row and stream
     const int s = warp >> 2;                     // stream
     const int r = (warp & 3) * 32 + lane;        // row inside the tile == TMEM lane
-    const int r_item = twice && s == 1 ? r - 64 : r;       // row of the item (negative, or 64 and more with `twice`: none)
+    // row of the item (negative, or 64 and more with `twice`: none)
+    auto item_row = [&]() { return kPaged && kAlt && x.twice && s == 1 ? r - 64 : r; };
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tO = tm_O(s) + lane_off;
     bool ok = true;
@@ -756,7 +776,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             tmem_ld_wait();
 #pragma unroll
             for (int q = 0; q < 8; ++q)
-              st_shared_16(sQ + (uint32_t)(qb * C::kTileBytes + ((c * 8 + q) * 64 + r_item) * 16), __float_as_uint(ov[q * 4]), __float_as_uint(ov[q * 4 + 1]),
+              st_shared_16(sQ + (uint32_t)(qb * C::kTileBytes + ((c * 8 + q) * 64 + item_row()) * 16), __float_as_uint(ov[q * 4]), __float_as_uint(ov[q * 4 + 1]),
                            __float_as_uint(ov[q * 4 + 2]), __float_as_uint(ov[q * 4 + 3]));
           }
         }
@@ -886,12 +906,12 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     while (ok && next_desc(di, d)) {
       const int n = d.n, na = d.na, part = d.part;
       const int row0 = (d.row0 & 0x3fffffff) + (kAlt ? 0 : s * kTile);       // of the stream's tile
-      SegRow row = seg_row(p, p.pass[d.row0 >> 30].block_samples, d.b0, d.h_kv, row0 + max(r_item, 0));
-      if (kPaged) row.real = row0 + r_item < d.base0 && (!twice || (unsigned)r_item < 64u);
+      SegRow row = seg_row(p, p.pass[d.row0 >> 30].block_samples, d.b0, d.h_kv, row0 + max(item_row(), 0));
+      if (kPaged) row.real = row0 + item_row() < d.base0 && (!twice || (unsigned)item_row() < 64u);
       const int grow = (row.b * a.n_q + row.t) * a.N_h + row.h;
       const bool row_real = row.real, warp_real = __any_sync(0xffffffffu, row_real);
       // real keys ahead of each segment's first tile in this item, and those of segment 1 that this row sees
-      const int real0 = d.len0 - d.base0, real1 = d.len1 - d.base1, sees1 = seg_limit1(a, d.own, row.t) - d.base1;
+      const int real0 = d.len0 - d.base0, real1 = d.len1 - d.base1, sees1 = (kPaged && !row_real ? d.len1 : seg_limit1(a, d.own, row.t)) - d.base1;
       float m_used = -INFINITY, l_run = 0.f;
       bool any_key = false;
       const int i0 = kAlt ? (s ^ pos0) & 1 : 0;                  // the stream's first tile of the item
@@ -1082,7 +1102,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         // stream 0 has read the previous item's values
         if (iter > 0) ok = wait(bar_o_free, (iter - 1) & 1);
         if (!ok) break;
-        if (r_item >= 0) ml_x[r_item] = make_float2(pend_m, pend_l);
+        if (item_row() >= 0) ml_x[item_row()] = make_float2(pend_m, pend_l);
         if (!twice) {
           arrive(bar_x);
           arrive(bar_o_free);

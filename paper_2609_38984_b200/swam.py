@@ -178,7 +178,7 @@ def load_library() -> ctypes.CDLL:
         for name, args in (("cross", SwamCrossArgs), ("prefix", SwamPrefixArgs)):
             getattr(lib, f"swam_{name}_attn").argtypes = [vp, ctypes.POINTER(args), vp]
             getattr(lib, f"swam_{name}_attn_scratch_bytes").argtypes = [vp, ctypes.POINTER(args), ctypes.POINTER(ctypes.c_size_t)]
-        for name in ("norm_rope", "append_kv", "paged_attn"):      # (an address: a packed structure needs no object around it)
+        for name in ("norm_rope", "append_kv", "paged_attn"):      # (any address will do: it is a packed structure's)
             getattr(lib, f"swam_{name}").argtypes = [vp, vp, vp]
         lib.swam_paged_attn_scratch_bytes.argtypes = [vp, ctypes.POINTER(SwamPagedArgs), ctypes.POINTER(ctypes.c_size_t)]
         lib.swam_step.argtypes = [vp, vp, vp, vp, i32, vp, vp]
@@ -258,9 +258,6 @@ class Swam:
         self._device_index = device.index if device.index is not None else torch.cuda.current_device()
         self._scratch_need = {}
         self._lse_like = {}
-        # argument structures of the calls around the paged cache, filled anew for each call
-        self._args = {c: c() for c in (SwamNormRopeArgs, SwamPagedCache, SwamAppendArgs, SwamPagedArgs)}
-        self._address = {c: ctypes.addressof(a) for c, a in self._args.items()}
         self.workspace = None
         self.staging = None
         if bind:
@@ -550,9 +547,10 @@ class Swam:
             rope_at = rope.address
             if positions is not None:
                 pos, pos_smp = self._positions(rope, positions, n)
-        _PACK_NORM_ROPE.pack_into(self._args[SwamNormRopeArgs], 0, rope_at, q_at, k_at, q_to, k_to, self._weight("q_weight", q_weight),
+        a = SwamNormRopeArgs()
+        _PACK_NORM_ROPE.pack_into(a, 0, rope_at, q_at, k_at, q_to, k_to, self._weight("q_weight", q_weight),
                                   self._weight("k_weight", k_weight), pos, n, heads, eps, 0, pos_smp, *q_str, *k_str, *q_out_str, *k_out_str)
-        rc = self.lib.swam_norm_rope(self.ctx, self._address[SwamNormRopeArgs], _raw_stream())
+        rc = self.lib.swam_norm_rope(self.ctx, ctypes.byref(a), _raw_stream())
         if rc != OK:
             self._chk(rc)
         return q_out, k_out
@@ -574,7 +572,7 @@ class Swam:
                 raise ValueError("page_table: rows must be contiguous and apart")
             if samples <= 1:
                 stride = max_pages
-        c = self._args[SwamPagedCache]
+        c = SwamPagedCache()
         _PACK_CACHE.pack_into(c, 0, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), self._ints("kv_len", kv_len, (samples,)),
                               0 if q_start is None else self._ints("q_start", q_start, (samples + 1,)), samples, n_pages, page,
                               max_pages, heads, 0, stride, k_page, k_tok, v_page, v_tok)
@@ -588,7 +586,7 @@ class Swam:
         (int32 [samples]); token c of it lives in row c % page size of page page_table[b, c / page size] (int32 [samples, pages]).
         positions: int32 [tokens, axes] ([tokens] with one axis); default: a token's number in its sample."""
         tokens = k.shape[0] if k.dim() == 3 else 0
-        self._cache(k_pages, v_pages, page_table, kv_len, q_start)
+        c = self._cache(k_pages, v_pages, page_table, kv_len, q_start)
         heads = k_pages.shape[2]
         k_tok, v_tok = self._packed("k", k, tokens, heads), self._packed("v", v, tokens, heads)
         q_at = q_to = q_tok = q_out_tok = pos = rope_at = 0
@@ -605,10 +603,11 @@ class Swam:
             rope_at = rope.address
             if positions is not None:
                 pos = self._ints("positions", positions, (tokens,) if rope.n_axes == 1 and positions.dim() == 1 else (tokens, rope.n_axes))
-        _PACK_APPEND.pack_into(self._args[SwamAppendArgs], 0, self._address[SwamPagedCache], rope_at, q_at, k.data_ptr(), v.data_ptr(), q_to,
+        a = SwamAppendArgs()
+        _PACK_APPEND.pack_into(a, 0, ctypes.addressof(c), rope_at, q_at, k.data_ptr(), v.data_ptr(), q_to,
                                self._weight("q_weight", q_weight), self._weight("k_weight", k_weight), pos, tokens, eps, q_tok,
                                k_tok, v_tok, q_out_tok)
-        rc = self.lib.swam_append_kv(self.ctx, self._address[SwamAppendArgs], _raw_stream())
+        rc = self.lib.swam_append_kv(self.ctx, ctypes.byref(a), _raw_stream())
         if rc != OK:
             self._chk(rc)
         return q_out
@@ -628,12 +627,12 @@ class Swam:
         else:
             o_tok = self._packed("out", out, tokens, self.N_h)
         lse = torch.empty((self.N_h, tokens), dtype=torch.float32, device=self.device) if want_lse else None
-        a = self._args[SwamPagedArgs]
-        _PACK_PAGED.pack_into(a, 0, self._address[SwamPagedCache], q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, 0, 0, tokens,
+        a = SwamPagedArgs()
+        _PACK_PAGED.pack_into(a, 0, ctypes.addressof(c), q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, 0, 0, tokens,
                               max_q, max_kv, 1 if causal else 0, q_tok, o_tok)
         key = ("paged", tokens, c.n_samples, c.n_pages, c.page_size, c.max_pages, c.n_kv_heads, q_start is None, max_q, max_kv)
         scratch = self._scratch(self.lib.swam_paged_attn_scratch_bytes, a, key)  # noqa: F841
-        rc = self.lib.swam_paged_attn(self.ctx, self._address[SwamPagedArgs], _raw_stream())
+        rc = self.lib.swam_paged_attn(self.ctx, ctypes.byref(a), _raw_stream())
         if rc != OK:
             self._chk(rc)
         return (out, lse) if want_lse else out

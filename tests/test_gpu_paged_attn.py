@@ -152,6 +152,43 @@ def test_very_many_samples(kind):
     check(kind, False, new, lens, 4, 2, 64, 16)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D,kv,new,lens", [(64, 2, 20, 300), (128, 2, 20, 300), (64, 2, 40, 300), (128, 8, 300, 1000)])
+def test_more_row_tiles_than_sms(D, kv, new, lens, causal):
+    """Blocks that running ones take over: samples in no order of lengths, some of them empty; at most 64, at most 128 and more rows."""
+    n = 150 if kv == 2 else 14
+    counts = [0 if b % 9 == 4 else 1 + (b * 7919) % new for b in range(n)]
+    lengths = [0 if b % 13 == 5 else 1 + (b * 104729) % lens for b in range(n)]
+    counts[3], lengths[7] = new, lens
+    check(KINDS[0], causal, counts, lengths, 2 * kv, kv, D, 32)
+
+
+def test_two_threads_with_one_context():
+    """Calls from two threads, each on a stream of its own: the binding keeps nothing of a call in the context."""
+    import threading
+    cases = [case(KINDS[0], [n] * 3, [700, 30 + n, 1500], 8, 2, 64, 16, seed=n) for n in (1, 70)]
+    ctx = cases[0].ctx
+    want = [c.run(True) for c in cases]
+    for c in cases:
+        c.ctx = ctx
+    wrong = []
+
+    def work(c, w):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(200):
+                out, lse = c.run(True)
+                torch.cuda.current_stream().synchronize()
+                if not (torch.equal(out, w[0]) and torch.equal(lse, w[1])):
+                    wrong.append(c.new)
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=x) for x in zip(cases, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("new", [[2, 3], [80, 200]])
 def test_rows_of_nobody_stay_as_they_are(kind, new):
