@@ -8,7 +8,7 @@
 //                and the queries where a row tile is a box of the query tensor
 //   warp 10      fetches the query rows one by one where it is not (a number of heads per key/value head that does not
 //                divide the tile, samples that do not tile it), with 16-byte asynchronous copies into the same layout;
-//                where final results leave as boxes of the output tensor, it sends these instead
+//                where final results leave as boxes of the output tensor, it sends these instead; paged and kAlt: it loads V too
 //   warp 8       one elected thread issues every tcgen05.mma: S = Q K^T into TMEM, then O += P V with P in TMEM and V in
 //                shared memory; O stays in TMEM for the whole range of keys
 //   warps 0-3    softmax of stream 0, one thread per row: S row from TMEM, exponentials against a running reference
@@ -130,6 +130,9 @@ __device__ __forceinline__ void st_global_32(void* dst, const uint32_t* v) {
                ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
+__device__ __forceinline__ int page_shift_of(const PagedCache& c) { return c.page_shift; }
+__device__ __forceinline__ int page_shift_of(const NoCache&) { return 0; }
+
 template <int D, bool kAlt, bool kPaged>
 __global__ void __launch_bounds__(kThreadsS, 1)
 seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_o,
@@ -240,6 +243,61 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   // other two takes)
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    // Loads of K or V, one tile after the other: what a load needs of its item stays in registers.
+    struct Cursor {
+      int i = 0, n = 0, na = 0, base0, base1, h, idx0, idx1, len1;
+      PageWindow pages;                          // paged keys
+      __device__ __forceinline__ void enter(const SegDesc& o) {
+        i = 0;
+        n = o.n;
+        na = o.na;
+        base0 = o.base0;
+        base1 = o.base1;
+        h = o.h_kv;
+        idx0 = o.kv0;
+        idx1 = o.b0;
+        len1 = o.len1;
+      }
+    };
+    const int sh = kPaged ? page_shift_of(pc) : 0, page_rows = min(kTile, 1 << sh);
+    auto load = [&](Cursor& c, Turn<ST>& ring, const CUtensorMap* m0, const CUtensorMap* m1) {
+      const uint32_t dst = sR + ring.at * C::kTileBytes, full = bar_full(ring.at);
+      if constexpr (kPaged) {
+        const int key0 = c.base1 + c.i * kTile;
+        const int count = sh >= 7 ? 1 : min(kTile >> sh, ((c.len1 - key0) + (1 << sh) - 1) >> sh);       // pages with keys
+        const int page = c.pages.get(pc, c.idx0, key0 >> sh, lane < count ? lane : 0);
+        if (!wait(bar_empty(ring.at), ring.phase ^ 1)) return false;
+        if (lane == 0) mbar_expect_tx(full, count * page_rows * 128 * C::DB);
+        __syncwarp();
+        if (lane < count) {
+          const int at = paged_page(pc, page, p.status);
+#pragma unroll
+          for (int db = 0; db < C::DB; ++db)
+            tma_load_4d(dst + db * C::kSub + lane * page_rows * 128, m1, full, db * 64, key0 & ((1 << sh) - 1), c.h, at);
+        }
+        __syncwarp();
+      } else {
+        if (!wait(bar_empty(ring.at), ring.phase ^ 1)) return false;
+        if (lane == 0) {
+          const bool s1 = c.i >= c.na;
+          mbar_expect_tx(full, C::kTileBytes);
+#pragma unroll
+          for (int db = 0; db < C::DB; ++db)
+            tma_load_4d(dst + db * C::kSub, s1 ? m1 : m0, full, db * 64, (s1 ? c.base1 : c.base0) + c.i * kTile, c.h, s1 ? c.idx1 : c.idx0);
+        }
+      }
+      ++c.i;
+      ring.step();
+      return true;
+    };
+    // Paged keys, row tiles that use every key tile once: K and V have a warp each, since two loads a tile of up to eight boxes were what set
+    // the period (1830 of 1890 clk a tile).
+    constexpr bool kSplit = kPaged && kAlt;
+    // the last loads of a warp that has issued so many, each in the place that place(i) gives
+    auto drain = [&](int loads, auto place) {
+      for (int i = max(0, loads - ST); i < loads; ++i)
+        mbar_wait_bounded(bar_full(place(i) % ST), (place(i) / ST) & 1, kDrainCycles, nullptr);
+    };
     if (warp == 11) {
       // ------------------------------------------------------------------ scheduler
       // Items with keys first, for the other warps; then the rows of those without, which are written here: in the order of
@@ -451,10 +509,9 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       const int cc = lane % CPR, sub = lane / CPR;
       const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + cc * 8;
       int iter = 0;
-      while (!x.box_out && next_desc(di, d)) {
-        if (x.box_q) continue;
+      auto fetch_queries = [&]() {
         const int qb = iter % QB;
-        if (iter >= QB && !wait(bar_q_free(qb), ((iter / QB) & 1) ^ 1)) break;
+        if (iter >= QB && !wait(bar_q_free(qb), ((iter / QB) & 1) ^ 1)) return false;
         const int row0 = d.row0 & 0x3fffffff, block_samples = p.pass[d.row0 >> 30].block_samples;
         for (int blk = 0; blk < C::kRows / 32; ++blk) {
           // lane l knows row blk * 32 + l; the rows are then copied RPI at a time
@@ -470,102 +527,130 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
         cp_async_arrive(bar_q(qb));
         ++iter;
+        return true;
+      };
+      if constexpr (kSplit) {
+        // and the loads of V
+        Cursor vc;
+        Turn<ST> ring;
+        for (int j = 0; j < LK; ++j) ring.step();
+        int loads = 0;
+        bool ok = true;
+        while (ok && next_desc(di, d)) {
+          ok = x.box_q || fetch_queries();
+          vc.enter(d);
+          while (ok && vc.i < vc.n) {
+            ok = load(vc, ring, &map_v0, &map_v1);
+            if (ok) ++loads;
+            ring.step();
+          }
+        }
+        if (!ok) drain(loads, [](int i) { return LK + 2 * i; });
+      } else {
+        while (!x.box_out && next_desc(di, d)) {
+          if (!x.box_q && !fetch_queries()) break;
+        }
       }
       cp_async_wait_all();
     } else if (warp == 9) {
       // ------------------------------------------------------------------ TMA producer
       // The key tiles of all items form one sequence T = 0, 1, ...  Behind the last K an empty slot takes the place of each
       // missing one, so that V_T is always load LK + 2 T.  A descriptor is released when the cursor of V leaves it.
-      int pos = 0, iter = 0;                       // ring loads and items (of K) so far
-      int ik = 0, nk = 0, iv = 0, nv = 0, dvi = 0; // next tile and tiles of the items of K (descriptor di - 1) and V (dvi - 1)
-      bool ok = true, k_end = false;
-      PageWindow pages[2];                         // paged keys: around the cursors of K and V
-      auto load = [&](const SegDesc& o, bool is_v, int i) {
-        const int st = pos % ST;
-        if constexpr (kPaged) {
-          const int key0 = o.base1 + i * kTile, sh = pc.page_shift, first = key0 >> sh;
-          const int count = sh >= 7 ? 1 : min(kTile >> sh, ((o.len1 - key0) + (1 << sh) - 1) >> sh);       // pages with keys
-          const int page = pages[is_v].get(pc, o.kv0, first, lane < count ? lane : 0);
-          if (!wait(bar_empty(st), ((pos / ST) & 1) ^ 1)) return false;
-          const int rows = min(kTile, 1 << sh);
-          if (lane == 0) mbar_expect_tx(bar_full(st), count * rows * 128 * C::DB);
-          __syncwarp();
-          if (lane < count) {
-            const int at = paged_page(pc, page, p.status);
-            for (int db = 0; db < C::DB; ++db)
-              tma_load_4d(sR + st * C::kTileBytes + db * C::kSub + lane * rows * 128, is_v ? &map_v1 : &map_k1, bar_full(st), db * 64,
-                          key0 & ((1 << sh) - 1), o.h_kv, at);
-          }
-          __syncwarp();
-          ++pos;
-          return true;
-        }
-        if (!wait(bar_empty(st), ((pos / ST) & 1) ^ 1)) return false;
+      int iter = 0;                                // items of K so far
+      bool ok = true;
+      Turn<ST> ring;
+      Cursor kc;
+      auto load_queries = [&](const SegDesc& o) {
+        const int qb = iter % QB;
+        if (iter >= QB && !wait(bar_q_free(qb), ((iter / QB) & 1) ^ 1)) return false;
         if (lane == 0) {
-          const bool s1 = i >= o.na;
-          const CUtensorMap* m = s1 ? (is_v ? &map_v1 : &map_k1) : (is_v ? &map_v0 : &map_k0);
-          mbar_expect_tx(bar_full(st), C::kTileBytes);
-          for (int db = 0; db < C::DB; ++db)
-            tma_load_4d(sR + st * C::kTileBytes + db * C::kSub, m, bar_full(st), db * 64, (s1 ? o.base1 : o.base0) + i * kTile, o.h_kv,
-                        s1 ? o.b0 : o.kv0);
-        }
-        ++pos;
-        return true;
-      };
-      auto load_k = [&]() {
-        if (ik == nk && !k_end) {
-          const int slot = di % kDesc;
-          if (!wait(bar_d_full(slot), (di / kDesc) & 1)) return false;
-          ++di;
-          ik = 0;
-          nk = desc[slot].n;
-          k_end = nk == 0;
-          if (!k_end && x.box_q) {
-            // the item's queries
-            const int qb = iter % QB;
-            if (iter >= QB && !wait(bar_q_free(qb), ((iter / QB) & 1) ^ 1)) return false;
-            if (lane == 0) {
-              const SegDesc& o = desc[slot];
-              mbar_expect_tx(bar_q(qb), C::NQ * C::kTileBytes);
-              const bool mixed = p.pass[o.row0 >> 30].block_samples > 1;
-              for (int q = 0; q < C::NQ; ++q) {
-                const int r = (o.row0 & 0x3fffffff) + q * kTile;
-                const int smp = mixed ? r / (a.n_q * p.g) : 0, tok = mixed ? 0 : r / p.g;
-                for (int db = 0; db < C::DB; ++db) {
-                  tma_load_5d(sQ + (qb * C::NQ + q) * C::kTileBytes + db * C::kSub, &map_q, bar_q(qb), db * 64, 0, tok, o.h_kv, o.b0 + smp);
-                  if (twice) tma_load_5d(sQ + qb * C::kTileBytes + db * C::kSub + 64 * 128, &map_q, bar_q(qb), db * 64, 0, tok, o.h_kv, o.b0);
-                }
-              }
+          mbar_expect_tx(bar_q(qb), C::NQ * C::kTileBytes);
+          const bool mixed = p.pass[o.row0 >> 30].block_samples > 1;
+          for (int q = 0; q < C::NQ; ++q) {
+            const int r = (o.row0 & 0x3fffffff) + q * kTile;
+            const int smp = mixed ? r / (a.n_q * p.g) : 0, tok = mixed ? 0 : r / p.g;
+            for (int db = 0; db < C::DB; ++db) {
+              tma_load_5d(sQ + (qb * C::NQ + q) * C::kTileBytes + db * C::kSub, &map_q, bar_q(qb), db * 64, 0, tok, o.h_kv, o.b0 + smp);
+              if (twice) tma_load_5d(sQ + qb * C::kTileBytes + db * C::kSub + 64 * 128, &map_q, bar_q(qb), db * 64, 0, tok, o.h_kv, o.b0);
             }
           }
-          ++iter;
         }
-        if (!k_end) return load(desc[(di - 1) % kDesc], false, ik++);
-        const int st = pos % ST;
-        if (!wait(bar_empty(st), ((pos / ST) & 1) ^ 1)) return false;
-        if (lane == 0) mbar_arrive(bar_full(st));
-        ++pos;
         return true;
       };
-      for (int j = 0; j < LK && ok; ++j) ok = load_k();
-      while (ok) {
-        if (iv == nv) {
-          if (dvi > 0) {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_d_empty((dvi - 1) % kDesc));
+      // the empty slot in the place of a missing K
+      auto no_k = [&]() {
+        if (!wait(bar_empty(ring.at), ring.phase ^ 1)) return false;
+        if (lane == 0) mbar_arrive(bar_full(ring.at));
+        ring.step();
+        return true;
+      };
+      if constexpr (kSplit) {
+        // K alone: loads 0 .. LK - 1 and then every second one
+        int loads = 0;
+        auto step = [&]() {
+          if (loads >= LK - 1) ring.step();
+          ++loads;
+        };
+        while (ok) {
+          const int slot = di % kDesc;
+          ok = wait(bar_d_full(slot), (di / kDesc) & 1);
+          if (!ok) break;
+          kc.enter(desc[slot]);
+          if (kc.n == 0) break;
+          if (x.box_q) ok = load_queries(desc[slot]);
+          ++iter;
+          ++di;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_d_empty(slot));
+          while (ok && kc.i < kc.n) {
+            ok = load(kc, ring, &map_k0, &map_k1);
+            if (ok) step();
           }
-          // (K is a tile ahead at least, so an item that V could enter has been entered by K)
-          if (dvi == di - (k_end ? 1 : 0)) break;
-          nv = desc[dvi % kDesc].n;
-          ++dvi;
-          iv = 0;
         }
-        ok = load(desc[(dvi - 1) % kDesc], true, iv++);
-        if (ok) ok = load_k();
-      }
-      if (!ok) {
-        drain_loads(bar_full(0), ST, pos);
-        if (x.box_q) drain_loads(bar_q(0), QB, k_end ? iter - 1 : iter);
+        const int real = loads;
+        for (int j = 0; j < LK && ok; ++j) {
+          ok = no_k();
+          step();
+        }
+        if (!ok) drain(real, [](int i) { return i < LK ? i : 2 * i - LK + 1; });
+        if (!ok && x.box_q) drain_loads(bar_q(0), QB, iter);
+      } else {
+        Cursor vc;                                 // (K is at descriptor di - 1, V at dvi - 1)
+        int pos = 0, dvi = 0;                      // ring loads so far; descriptors that V has entered
+        bool k_end = false;
+        auto load_k = [&]() {
+          if (kc.i == kc.n && !k_end) {
+            const int slot = di % kDesc;
+            if (!wait(bar_d_full(slot), (di / kDesc) & 1)) return false;
+            ++di;
+            kc.enter(desc[slot]);
+            k_end = kc.n == 0;
+            if (!k_end && x.box_q && !load_queries(desc[slot])) return false;
+            ++iter;
+          }
+          ++pos;
+          return k_end ? no_k() : load(kc, ring, &map_k0, &map_k1);
+        };
+        for (int j = 0; j < LK && ok; ++j) ok = load_k();
+        while (ok) {
+          if (vc.i == vc.n) {
+            if (dvi > 0) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar_d_empty((dvi - 1) % kDesc));
+            }
+            // (K is a tile ahead at least, so an item that V could enter has been entered by K)
+            if (dvi == di - (k_end ? 1 : 0)) break;
+            vc.enter(desc[dvi % kDesc]);
+            ++dvi;
+          }
+          ++pos;
+          ok = load(vc, ring, &map_v0, &map_v1);
+          if (ok) ok = load_k();
+        }
+        if (!ok) {
+          drain_loads(bar_full(0), ST, pos - 1);   // (the last one has not been issued)
+          if (x.box_q) drain_loads(bar_q(0), QB, k_end ? iter - 1 : iter);
+        }
       }
     } else {
       // ------------------------------------------------------------------ MMA issuer (warp converged, one lane issues)
@@ -1167,7 +1252,7 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kP
     x.twice = (int64_t)c.max_q * p.g <= 64;
     if (x.twice) x.box_q = p.g <= 64 && 64 % p.g == 0;
   }
-  x.box_out = p.direct && !mixed && x.box_q && !x.twice;
+  x.box_out = p.direct && !mixed && x.box_q && !(kPaged && kAlt);        // (the warp that would send the boxes loads V)
   const int bt = mixed ? a.n_q : (x.twice ? 64 : kTile) / p.g, bs = mixed ? kTile / per_sample : 1;
   if (x.box_q && !make_q_map(&mq, a.q, a, p.g, a.q_tok, a.q_smp, bt, bs)) return cudaErrorInvalidValue;
   if (x.box_out && !make_q_map(&mo, a.out, a, p.g, a.o_tok, a.o_smp, bt, bs)) return cudaErrorInvalidValue;
