@@ -262,13 +262,13 @@ PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
   int64_t s = 1;
   if (pl.kind == kTc) {
     s = a.sms / (tiles * a.N_kv);
-    if (s > c.max_kv / 512) s = c.max_kv / 512;
+    if (s > c.max_kv / 256) s = c.max_kv / 256;      // (148 tokens of 24 heads on 8 and 1281 keys: 23 us, 27 with pieces of 512)
     if (s > kMaxSplits) s = kMaxSplits;
     if (s < ceil_div(c.max_kv, kMaxItemKeys)) s = ceil_div(c.max_kv, kMaxItemKeys);
     if (s < 1) s = 1;
   } else if (pl.kind == kF32) {
     // Many small pieces, of one size for all samples: those of short samples are empty, and the long ones are what takes time (6 samples
-    // of 10 to 1550 keys, 90 row tiles: 56 us with 4 SMs' worth of CTAs, 30 with 12 or 16).
+    // of 41 to 1521 keys, 90 row tiles: 56 us with 4 SMs' worth of CTAs, 30 with 12 or 16).
     s = 16 * a.sms / (c.samples * (int64_t)pl.row_tiles * a.N_kv);
     if (s > c.max_kv / 96) s = c.max_kv / 96;
     if (s > kMaxSplits) s = kMaxSplits;

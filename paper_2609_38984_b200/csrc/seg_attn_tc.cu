@@ -27,8 +27,12 @@
 // kAlt = true: a row tile has at most 128 rows; both streams hold the same rows and take the key tiles in turn (over the
 //   borders of items), each with its own maximum, sum and output accumulator, and are merged in the epilogue.  The memory of the second query tile
 //   goes to the ring.
+// Paged keys: a block per item, and running blocks take over those that have not started (16 chunks behind 640 to 8704 keys, 384 items:
+// 131 us, 171 in turn); K and V are boxes of pages.  What bounds them: head dim 128 as below (chunks of 300 to 2520 tokens, 8 heads on 32,
+// causal, 1.17 TFLOP: 974 us, 0.70 of the measured burst rate; 0.75 of the sustained one where it runs for longer); head dim 64 with up to
+// 128 rows the issuing warp, some 1600 clk a tile for 640 of products (the 16 chunks: 117 us, 4.0 TB/s).
 // Paged keys, at most 64 rows: the tile holds the rows twice, and stream 1 works on the second half, so that its exponentials run on the
-//   sub-cores of the TMEM lanes that stream 0 leaves idle (16 chunks of 64 tokens, head dim 64: 131 us with both in the first half).
+//   sub-cores of the TMEM lanes that stream 0 leaves idle (16 chunks of 64 tokens, head dim 64: 127 us, 131 with both in the first half).
 //   Its accumulators are out of stream 0's reach there and come through the item's query buffer as fp32.
 // A tile that ends early costs what its real keys cost: Q K^T and P V stop at the 16-key step of the last one, the exponentials
 // at its 32.  Rows of V between it and the end of the step are overwritten with zeros in shared memory (0 * NaN would poison
