@@ -70,8 +70,20 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
     }
     kk.len0 = kk.n0 = 0;
     kk.len1 = paged_limit(a.causal, smp, (min(it.row0 + MR, rows) - 1) / p.g);
-    // pieces of one size for all samples: a short one has fewer
-    const int total = (kk.len1 + kKF - 1) / kKF, per = ((pc.max_kv + kKF - 1) / kKF + ps.splits - 1) / ps.splits;
+    // pieces of one size for all samples, so that a short one has fewer: a share of the longest
+    int longest = smp.len;
+    if (ps.splits > 1) {
+      __shared__ int most;
+      if (threadIdx.x == 0) most = 0;
+      __syncthreads();
+      for (int b = threadIdx.x; b < pc.samples; b += kThreadsF) {
+        const PagedSample s = paged_sample(pc, a.n_q, b, p.status);
+        if (s.n > 0) atomicMax(&most, s.len);
+      }
+      __syncthreads();
+      longest = most;
+    }
+    const int total = (kk.len1 + kKF - 1) / kKF, per = ((longest + kKF - 1) / kKF + ps.splits - 1) / ps.splits;
     kk.begin = min(total, it.split * per);
     kk.end = min(total, kk.begin + per);
     if (it.split > 0 && kk.begin == kk.end) {

@@ -347,6 +347,16 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           int chunk = -32, before = 0, all = 0, w = blockIdx.x, sample = 0, tiles = 0, end = 0, released = 0, held = 0, phase = 0;
           PagedSample smp{0, 0, 0};
           const uint32_t answer = base + C::kData + C::kTail - 48, bar_answer = answer + 16;
+          // pieces of one size for all samples, so that a short one has fewer: a share of the longest (a plan of pieces has few samples)
+          int piece = (pc.max_kv + kTile - 1) / kTile;
+          if (p.pass[0].splits > 1) {
+            int longest = 0;
+            for (int b = lane; b < pc.samples; b += 32) {
+              const PagedSample s = paged_sample(pc, a.n_q, b, p.status);
+              if (s.n > 0) longest = max(longest, s.len);
+            }
+            piece = (__reduce_max_sync(0xffffffffu, (longest + kTile - 1) / kTile) + p.pass[0].splits - 1) / p.pass[0].splits;
+          }
           while (ok) {
             // the 32 samples that item w is in
             while (chunk < pc.samples && w >= before + all) {
@@ -391,10 +401,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               o.part = k % splits;
               const int row0 = (rt - 1 - k / splits) * C::kRows, rows = it.n * p.g;
               const int sees = paged_limit(a.causal, it, (min(row0 + C::kRows, rows) - 1) / p.g);
-              // pieces of one size for all samples: a short one has fewer
-              const int total = (sees + kTile - 1) / kTile, per = ((pc.max_kv + kTile - 1) / kTile + splits - 1) / splits;
-              const int begin = min(total, o.part * per);
-              o.n = min(total, begin + per) - begin;
+              const int total = (sees + kTile - 1) / kTile, begin = min(total, o.part * piece);
+              o.n = min(total, begin + piece) - begin;
               o.na = 0;
               o.b0 = 0;
               o.row0 = it.q0 * p.g + row0;
@@ -844,6 +852,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     int iter = 0, cnt = 0, pos0 = 0, u0 = 0;     // items; tiles of this stream; tiles and units of finished items
     // the finished item whose output is still in the accumulators
     bool pend = false, pend_real = false, pend_warp = false;
+    bool pend_odd = false;                       // kAlt: this stream had the odd tiles
     int pend_row = 0, pend_part = 0;             // row in the order (sample, query, head)
     int pend_lse = 0;                            // and in the order (sample, head, query)
     float pend_m = 0.f, pend_l = 0.f;
@@ -887,7 +896,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         const float mm = fmaxf(m, x1.x);
         f0 = m == -INFINITY ? 0.f : ex2(m - mm);
         f1 = x1.x == -INFINITY ? 0.f : ex2(x1.x - mm);
-        l = f0 * l + f1 * x1.y;
+        // (which stream has the even tiles depends on the items before this one, which with paged keys depend on when this block took
+        // them: the even tiles come first in every sum, so that the result does not)
+        if (kPaged) l = pend_odd ? fmaf(f0, l, __fmul_rn(f1, x1.y)) : fmaf(f1, x1.y, __fmul_rn(f0, l));
+        else l = f0 * l + f1 * x1.y;
         m = mm;
       }
       tc_fence_after();
@@ -911,8 +923,10 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 #pragma unroll
             for (int j = 0; j < 32; ++j) ov[j] = f0 != 0.f ? ov[j] : 0.f;
           }
+          if (!(kPaged && kAlt && pend_odd)) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) ov[j] *= f0;
+            for (int j = 0; j < 32; ++j) ov[j] = kPaged && kAlt ? __fmul_rn(ov[j], f0) : ov[j] * f0;
+          }
           if constexpr (kAlt) {
             float o1[32];
             if (twice) {
@@ -923,8 +937,16 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               tmem_ld32(tm_O(1) + lane_off + c * 32, o1);
               tmem_ld_wait();
             }
+            if (kPaged && pend_odd) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) ov[j] = f1 != 0.f ? fmaf(o1[j], f1, ov[j]) : ov[j];
+              for (int j = 0; j < 32; ++j) {
+                const float even = f1 != 0.f ? __fmul_rn(o1[j], f1) : 0.f;
+                ov[j] = f0 != 0.f ? fmaf(ov[j], f0, even) : even;
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) ov[j] = f1 != 0.f ? fmaf(o1[j], f1, ov[j]) : ov[j];
+            }
           }
           if (twice && p.direct) {
             if (pend_real) {
@@ -1186,6 +1208,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       pend_l = any_key ? l_run : 0.f;
       pend_row = grow;
       pend_part = part;
+      pend_odd = kAlt && i0 == 1;
       pend_lse = (row.b * a.N_h + row.h) * a.n_q + row.t;
       if (kAlt && s == 1) {
         // stream 0 has read the previous item's values

@@ -160,7 +160,28 @@ def test_more_row_tiles_than_sms(D, kv, new, lens, causal):
     counts = [0 if b % 9 == 4 else 1 + (b * 7919) % new for b in range(n)]
     lengths = [0 if b % 13 == 5 else 1 + (b * 104729) % lens for b in range(n)]
     counts[3], lengths[7] = new, lens
-    check(KINDS[0], causal, counts, lengths, 2 * kv, kv, D, 32)
+    c, want, want_lse = check(KINDS[0], causal, counts, lengths, 2 * kv, kv, D, 32)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        out, lse = c.run(causal)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("new", [[1, 1], [40, 3], [300, 20]])
+def test_tables_with_room_for_much_more(kind, new):
+    """Lengths far below what the table could hold, with and without bounds."""
+    c = case(kind, new, [2500, 700], 8, 2, 64, 16)
+    wide = torch.full((2, 8000), -1, dtype=torch.int32, device="cuda")
+    wide[:, :c.table.shape[1]] = c.table
+    c.table = wide
+    for kw in (dict(), dict(max_kv=2500), dict(max_kv=100000), dict(max_q=0)):
+        out, lse = c.run(True, **kw)
+        c.compare(out, lse, True)
 
 
 def test_two_threads_with_one_context():
