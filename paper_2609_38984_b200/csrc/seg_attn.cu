@@ -251,7 +251,9 @@ PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
   PagedPlan pl;
   const int g = a.N_h / a.N_kv;
   const int64_t rows = (int64_t)c.max_q * g;
-  const PassPlan ps = plan_pass(a, c.samples, rows, c.max_kv, warp_mma, -1);
+  SegArgs as64 = a;                // (paged keys of head dim 32 have a tensor-core kernel: planned as 64; up to 64 rows it is no faster)
+  if (a.D == 32 && rows > 64) as64.D = 64;
+  const PassPlan ps = plan_pass(as64, c.samples, rows, c.max_kv, warp_mma, -1);
   pl.kind = ps.kind;
   pl.tile_rows = pl.kind == kMma && rows <= 8 ? 8 : ps.tile_rows;
   if (pl.kind == kF32 && rows > 32) pl.tile_rows = 64;         // (30 us instead of 33 with 32)

@@ -1,5 +1,5 @@
 // Segment attention for bf16 tensors on the 5th-generation tensor cores (tcgen05 + TMEM), keys and values fed by TMA:
-// the kernel for many query rows per key/value head (head dim 64 and 128).
+// the kernel for many query rows per key/value head (head dim 64 and 128; paged keys: 32 too).
 //
 // A persistent CTA per SM walks through work items (seg_attn.cuh): a row tile and a range of 128-key tiles.
 //   warp 11      scheduler: decodes the items ahead of everybody else (divisions, lengths from memory) into a small ring of
@@ -82,7 +82,7 @@ struct Turn {
   }
 };
 
-template <int D, bool kAlt>
+template <int D, bool kAlt, int DH = D>
 struct SegCfg {
   static constexpr int DB = D / 64;                  // 64-column (128-byte) blocks per row
   static constexpr int kSub = kTile * 128;           // bytes of a [128 rows x 64 columns] block
@@ -105,7 +105,7 @@ struct SegCfg {
   static constexpr int kBytes = kData + 1024 /*alignment*/ + kTail + (kAlt ? kTile * 8 : 0) /*maxima and sums of stream 1*/;
   static_assert(ST >= 3 && kData <= 224 * 1024 && kBytes <= 227 * 1024, "shared memory");
   static constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 4) << 24);   // + N / 8 at bit 17
-  static constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+  static constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
 };
 
 struct SegTcArgs {
@@ -137,13 +137,14 @@ __device__ __forceinline__ void st_global_32(void* dst, const uint32_t* v) {
 __device__ __forceinline__ int page_shift_of(const PagedCache& c) { return c.page_shift; }
 __device__ __forceinline__ int page_shift_of(const NoCache&) { return 0; }
 
-template <int D, bool kAlt, bool kPaged>
+// DH: the tensors' head dim, 32 or D.  (Head dim 32 lies in the first half of a tile's 128-byte rows; the products stop there.)
+template <int D, bool kAlt, bool kPaged, int DH>
 __global__ void __launch_bounds__(kThreadsS, 1)
 seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_o,
               const __grid_constant__ CUtensorMap map_k0, const __grid_constant__ CUtensorMap map_v0,
               const __grid_constant__ CUtensorMap map_k1, const __grid_constant__ CUtensorMap map_v1,
               const __grid_constant__ SegParams p, const int pass0, const SegTcArgs x, const __grid_constant__ CacheArg<kPaged> pc) {
-  using C = SegCfg<D, kAlt>;
+  using C = SegCfg<D, kAlt, DH>;
   constexpr int ST = C::ST, LK = C::LK, QB = C::QB, NB = C::NB, kW = C::kW;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -320,9 +321,9 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               if (r.real) p.part_ml[(int64_t)o.part * p.rows + ((int64_t)r.b * a.n_q + r.t) * a.N_h + r.h] = make_float2(-INFINITY, 0.f);
               continue;
             }
-            const int64_t off = r.real ? r.b * a.o_smp + r.t * a.o_tok + (int64_t)r.h * D : -1;
+            const int64_t off = r.real ? r.b * a.o_smp + r.t * a.o_tok + (int64_t)r.h * DH : -1;
             if (r.real && a.lse) a.lse[((int64_t)r.b * a.N_h + r.h) * a.n_q + r.t] = -INFINITY;
-            constexpr int CPR = D / 8, RPI = 32 / CPR;
+            constexpr int CPR = DH / 8, RPI = 32 / CPR;
             for (int j = 0; j < 32 / RPI; ++j) {
               const int64_t to = __shfl_sync(0xffffffffu, off, j * RPI + lane / CPR);
               if (to >= 0) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + to + (lane % CPR) * 8) = make_uint4(0u, 0u, 0u, 0u);
@@ -499,11 +500,11 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             if constexpr (kPaged) {
               // the rows behind a sample's last one are another's: its last tile leaves row by row
               if (row0 + kTile > d.base0) {
-                constexpr int CPR = D / 8;
+                constexpr int CPR = DH / 8;
                 const unsigned char* src = base_ptr + ((iter % QB) * C::NQ + s) * C::kTileBytes;
                 for (int i = lane; i < (d.base0 - row0) * CPR; i += 32) {
                   const int rl = i / CPR, cc = i % CPR, tok = (row0 + rl) / p.g, h = d.h_kv * p.g + row0 + rl - tok * p.g;
-                  *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + cc * 8) =
+                  *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * DH + cc * 8) =
                       *reinterpret_cast<const uint4*>(src + (cc >> 3) * C::kSub + rl * 128 + (((cc & 7) ^ (rl & 7)) << 4));
                 }
                 fence_proxy_async();                 // the next loads of this buffer come through the other proxy
@@ -517,7 +518,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
       }
       // ------------------------------------------------------------------ or query rows one by one
-      constexpr int CPR = D / 8, RPI = 32 / CPR;     // 16-byte chunks per row, rows per warp instruction
+      constexpr int CPR = DH / 8, RPI = 32 / CPR;     // 16-byte chunks per row, rows per warp instruction
       const int cc = lane % CPR, sub = lane / CPR;
       const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + cc * 8;
       int iter = 0;
@@ -528,7 +529,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         for (int blk = 0; blk < C::kRows / 32; ++blk) {
           // lane l knows row blk * 32 + l; the rows are then copied RPI at a time
           const SegRow r = seg_row(p, block_samples, d.b0, d.h_kv, row0 + (twice ? blk & 1 : blk) * 32 + lane);
-          const int64_t off = r.real ? r.b * a.q_smp + r.t * a.q_tok + (int64_t)r.h * D : -1;
+          const int64_t off = r.real ? r.b * a.q_smp + r.t * a.q_tok + (int64_t)r.h * DH : -1;
           const uint32_t dst = sQ + (uint32_t)((qb * C::NQ + (blk >> 2)) * C::kTileBytes + (cc >> 3) * C::kSub + (blk & 3) * 32 * 128);
 #pragma unroll 4
           for (int i = 0; i < 32 / RPI; ++i) {
@@ -676,7 +677,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         const uint32_t idesc = C::kIdescQK + ((uint32_t)k16 << 18);
         mma_ss<false>(tm_S(buf), a_lo, b_lo, kDescHi, idesc, el);
 #pragma unroll
-        for (int ks = 1; ks < D / 16; ++ks) {
+        for (int ks = 1; ks < DH / 16; ++ks) {
           constexpr int kSub16 = C::kSub >> 4;
           const uint32_t off = (uint32_t)((ks >> 2) * kSub16 + (ks & 3) * 2);
           mma_ss<true>(tm_S(buf), a_lo + off, b_lo + off, kDescHi, idesc, el);
@@ -775,8 +776,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         v_k16 = steps16(real);
         if (ok && real < v_k16 * 16) {
           // rows of V behind the last real key become zeros up to the end of the product's last step
-          for (int c = lane; c < (v_k16 * 16 - real) * (D / 8); c += 32) {
-            const int rr = real + c / (D / 8), cc = c % (D / 8);
+          for (int c = lane; c < (v_k16 * 16 - real) * (DH / 8); c += 32) {
+            const int rr = real + c / (DH / 8), cc = c % (DH / 8);
             st_shared_16(sR + (uint32_t)(v_st * C::kTileBytes + (cc >> 3) * C::kSub + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)), 0u, 0u, 0u, 0u);
           }
           fence_proxy_async();
@@ -867,7 +868,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         tc_fence_after();
         if (pend_warp) {
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
+          for (int c = 0; c < DH / 32; ++c) {
             float ov[32];
             __syncwarp();
             tmem_ld32(tO + c * 32, ov);
@@ -914,7 +915,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         if (!p.direct && pend_real) p.part_ml[pr] = make_float2(m, l);
         const bool any_empty = __any_sync(0xffffffffu, f0 == 0.f);
 #pragma unroll 1          // (unrolled: 257 instead of 251 us for the ragged multi-view batch, in instruction fetches)
-        for (int c = 0; c < D / 32; ++c) {
+        for (int c = 0; c < DH / 32; ++c) {
           float ov[32];
           __syncwarp();
           tmem_ld32(tO + c * 32, ov);
@@ -954,7 +955,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               uint32_t w[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(ov[2 * j], ov[2 * j + 1]);
-              unsigned char* dst = (unsigned char*)((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * D + c * 32);
+              unsigned char* dst = (unsigned char*)((__nv_bfloat16*)a.out + tok * a.o_tok + (int64_t)h * DH + c * 32);
               if ((a.o_tok & 15) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 31) == 0) {
                 st_global_32(dst, w);
                 st_global_32(dst + 32, w + 8);
@@ -976,7 +977,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 #pragma unroll
             for (int j = 0; j < 32; ++j) w[j] = __float_as_uint(ov[j]);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) st_global_32((unsigned char*)(p.part_o + pr * D) + c * 128 + q * 32, w + q * 8);
+            for (int q = 0; q < 4; ++q) st_global_32((unsigned char*)(p.part_o + pr * DH) + c * 128 + q * 32, w + q * 8);
           }
         }
       }
@@ -992,7 +993,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           arrive(bar_staged(qb, s));        // warp 10 sends it
         } else {
           __syncwarp();
-          constexpr int CPR = D / 8, RPI = 32 / CPR;
+          constexpr int CPR = DH / 8, RPI = 32 / CPR;
           int ln = lane;
           asm volatile("" : "+r"(ln));
           const int cc = ln % CPR, sub = ln / CPR;
@@ -1004,7 +1005,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             const int o = __shfl_sync(0xffffffffu, row, rl);
             const int bt = o / a.N_h, h = o - bt * a.N_h, b = bt / a.n_q, t = bt - b * a.n_q;
             if (o >= 0)
-              *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + b * a.o_smp + t * a.o_tok + (int64_t)h * D + cc * 8) =
+              *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + b * a.o_smp + t * a.o_tok + (int64_t)h * DH + cc * 8) =
                   *reinterpret_cast<const uint4*>(src + rl * 128 + (((cc & 7) ^ (rl & 7)) << 4));
           }
           __syncwarp();
@@ -1166,7 +1167,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                   if (!ok) break;
                   tc_fence_after();
 #pragma unroll 1
-                  for (int b = 0; b < D / 32; ++b) {
+                  for (int b = 0; b < DH / 32; ++b) {
                     float ov[32];
                     tmem_ld32(tO + b * 32, ov);
                     tmem_ld_wait();
@@ -1245,7 +1246,17 @@ bool make_q_map(CUtensorMap* map, const void* ptr, const SegArgs& a, int g, int6
   return encode_bf16(map, ptr, 5, dims, strides, box);
 }
 
-template <int D, bool kAlt, bool kPaged>
+// Pages [n_pages, page, N_kv, DH] with strides as (d, row, head, page); box = 64 columns (those behind head dim 32 read as zeros) x rows
+bool make_page_map(CUtensorMap* map, const void* ptr, int n_pages, int page, int N_kv, int DH, int64_t tok, int64_t stride, int rows) {
+  const cuuint64_t dims[4] = {(cuuint64_t)DH, (cuuint64_t)page, (cuuint64_t)N_kv, (cuuint64_t)n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)tok * 2, (cuuint64_t)DH * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1};
+  // (L2 fetches what a row of one head has: see paged_mma.cu)
+  return encode_bf16(map, ptr, 4, dims, strides, box,
+                     DH == 32 ? CU_TENSOR_MAP_L2_PROMOTION_L2_64B : (DH == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B));
+}
+
+template <int D, bool kAlt, bool kPaged, int DH>
 cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kPaged>& c, cudaStream_t st, int* launches) {
   const SegArgs& a = p.a;
   CUtensorMap mk[2], mv[2], mq, mo;
@@ -1255,10 +1266,8 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kP
   memset(&mo, 0, sizeof(mo));
   if constexpr (kPaged) {
     const int page = 1 << c.page_shift, rows = page < kTile ? page : kTile;
-    // (L2 fetches what a row of one head has: see paged_mma.cu)
-    const CUtensorMapL2promotion fetch = D == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B;
-    if (!make_kv_map(&mk[1], a.k[1], c.n_pages, page, a.N_kv, D, c.k_tok, c.k_page, rows, fetch) ||
-        !make_kv_map(&mv[1], a.v[1], c.n_pages, page, a.N_kv, D, c.v_tok, c.v_page, rows, fetch))
+    if (!make_page_map(&mk[1], a.k[1], c.n_pages, page, a.N_kv, DH, c.k_tok, c.k_page, rows) ||
+        !make_page_map(&mv[1], a.v[1], c.n_pages, page, a.N_kv, DH, c.v_tok, c.v_page, rows))
       return cudaErrorInvalidValue;
   }
   for (int s = 0; s < 2 && !kPaged; ++s) {
@@ -1284,23 +1293,26 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kP
   if (x.box_q && !make_q_map(&mq, a.q, a, p.g, a.q_tok, a.q_smp, bt, bs)) return cudaErrorInvalidValue;
   if (x.box_out && !make_q_map(&mo, a.out, a, p.g, a.o_tok, a.o_smp, bt, bs)) return cudaErrorInvalidValue;
   x.items = p.pass[pass].items + (both ? p.pass[1].items : 0);
-  constexpr int smem = SegCfg<D, kAlt>::kBytes;
+  constexpr int smem = SegCfg<D, kAlt, DH>::kBytes;
   static SmemOptIn opt_in;
-  cudaError_t e = opt_in((const void*)seg_tc_kernel<D, kAlt, kPaged>, smem, a.device);
+  cudaError_t e = opt_in((const void*)seg_tc_kernel<D, kAlt, kPaged, DH>, smem, a.device);
   if (e != cudaSuccess) return e;
   const int grid = kPaged || x.items < a.sms ? x.items : a.sms;
   x.steal = kPaged && x.items > a.sms;
   ++*launches;
-  if (pass == 1) return launch_after(seg_tc_kernel<D, kAlt, kPaged>, dim3(grid), dim3(kThreadsS), smem, st, mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
-  seg_tc_kernel<D, kAlt, kPaged><<<grid, kThreadsS, smem, st>>>(mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
+  if (pass == 1) return launch_after(seg_tc_kernel<D, kAlt, kPaged, DH>, dim3(grid), dim3(kThreadsS), smem, st, mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
+  seg_tc_kernel<D, kAlt, kPaged, DH><<<grid, kThreadsS, smem, st>>>(mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
   return cudaGetLastError();
 }
 
 template <bool kPaged>
 cudaError_t launch_dim(const SegParams& p, int pass, bool both, bool alt, const CacheArg<kPaged>& c, cudaStream_t st, int* launches) {
+  if constexpr (kPaged) {
+    if (p.a.D == 32) return alt ? launch_tc<64, true, kPaged, 32>(p, pass, both, c, st, launches) : launch_tc<64, false, kPaged, 32>(p, pass, both, c, st, launches);
+  }
   switch (p.a.D) {
-    case 64: return alt ? launch_tc<64, true, kPaged>(p, pass, both, c, st, launches) : launch_tc<64, false, kPaged>(p, pass, both, c, st, launches);
-    case 128: return alt ? launch_tc<128, true, kPaged>(p, pass, both, c, st, launches) : launch_tc<128, false, kPaged>(p, pass, both, c, st, launches);
+    case 64: return alt ? launch_tc<64, true, kPaged, 64>(p, pass, both, c, st, launches) : launch_tc<64, false, kPaged, 64>(p, pass, both, c, st, launches);
+    case 128: return alt ? launch_tc<128, true, kPaged, 128>(p, pass, both, c, st, launches) : launch_tc<128, false, kPaged, 128>(p, pass, both, c, st, launches);
     default: return cudaErrorInvalidConfiguration;
   }
 }
