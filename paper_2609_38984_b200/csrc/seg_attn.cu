@@ -263,7 +263,10 @@ PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
   if (tiles > (int64_t)c.samples * pl.row_tiles) tiles = (int64_t)c.samples * pl.row_tiles;
   int64_t s = 1;
   if (pl.kind == kTc) {
+    // No more pieces than SMs.  Where samples differ in length, the longest may have more than its share, which the kernel decides (6 samples
+    // of 3000 to 30000 keys: 76 us, 88 without).  256 rows of partial results cost more than that gains.
     s = a.sms / (tiles * a.N_kv);
+    if (s > 1 && pl.tile_rows == 128) s *= 4;
     if (s > c.max_kv / 256) s = c.max_kv / 256;      // (148 tokens of 24 heads on 8 and 1281 keys: 23 us, 27 with pieces of 512)
     if (s > kMaxSplits) s = kMaxSplits;
     if (s < ceil_div(c.max_kv, kMaxItemKeys)) s = ceil_div(c.max_kv, kMaxItemKeys);

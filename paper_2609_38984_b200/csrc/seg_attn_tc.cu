@@ -82,6 +82,8 @@ struct Turn {
   }
 };
 
+constexpr int kMaxItemTiles = 1 << 19;     // key tiles of an item, of a plan of 2^26 keys at most
+
 template <int D, bool kAlt, int DH = D>
 struct SegCfg {
   static constexpr int DB = D / 64;                  // 64-column (128-byte) blocks per row
@@ -170,6 +172,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   SegDesc* desc = reinterpret_cast<SegDesc*>(base_ptr + C::kData + C::kDescOff);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + C::kData + C::kTail - 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::kData + C::kTail - 8);
+  volatile int* progress = reinterpret_cast<volatile int*>(base_ptr + C::kData + C::kTail - 12);      // paged: key tiles that stream 0 is through with
   float2* ml_x = reinterpret_cast<float2*>(base_ptr + C::kData + C::kTail);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -206,6 +209,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     mbar_init(bar_drain, 1);
     if (kPaged) mbar_init(base + C::kData + C::kTail - 32, 1);
     *abort_flag = 0;
+    *progress = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 8) {
@@ -343,20 +347,32 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         if constexpr (kPaged) {
           // A block per item (of as many as there can be), in the order: samples by falling length (32 at a time), their row tiles (the
           // last first: with causal it has the most keys), pieces, key/value heads.  Where there are more blocks than SMs, a
-          // running one takes over blocks that have not started yet, one item ahead of need, so that the SMs finish
+          // running one takes over blocks that have not started yet, when it is nearly through with what it has, so that the SMs finish
           // together whatever the lengths.  Lane l knows sample order[l] and where its items end among those of the 32.
-          int chunk = -32, before = 0, all = 0, w = blockIdx.x, sample = 0, tiles = 0, end = 0, released = 0, held = 0, phase = 0;
+          int chunk = -32, before = 0, all = 0, w = blockIdx.x, sample = 0, tiles = 0, cuts = 1, end = 0, published = 0, phase = 0;
           PagedSample smp{0, 0, 0};
           const uint32_t answer = base + C::kData + C::kTail - 48, bar_answer = answer + 16;
-          // pieces of one size for all samples, so that a short one has fewer: a share of the longest (a plan of pieces has few samples)
+          // Pieces of one size for all samples, so that a short one has fewer, and no more pieces than SMs: a share of the longest sample
+          // that fits whatever the others have, or, where that is finer, the keys of all row tiles over the SMs that are left when each
+          // row tile has one for its odd piece.  (A plan of pieces has few samples.)
           int piece = (pc.max_kv + kTile - 1) / kTile;
           if (p.pass[0].splits > 1) {
-            int longest = 0;
+            int longest = 0, items = 0;
+            unsigned keys = 0;
             for (int b = lane; b < pc.samples; b += 32) {
               const PagedSample s = paged_sample(pc, a.n_q, b, p.status);
-              if (s.n > 0) longest = max(longest, s.len);
+              const int n = (s.n * p.g + C::kRows - 1) / C::kRows * a.N_kv, len = (s.len + kTile - 1) / kTile;
+              if (n > 0) longest = max(longest, len);
+              items += n;
+              keys += (unsigned)n * len;                   // (of use with fewer row tiles than SMs: no more than 148 x 2^24)
             }
-            piece = (__reduce_max_sync(0xffffffffu, (longest + kTile - 1) / kTile) + p.pass[0].splits - 1) / p.pass[0].splits;
+            longest = __reduce_max_sync(0xffffffffu, longest);
+            items = max(1, __reduce_add_sync(0xffffffffu, items));
+            keys = __reduce_add_sync(0xffffffffu, keys);
+            const int fit = max(1, a.sms / items);
+            piece = (longest + fit - 1) / fit;
+            if (items < a.sms) piece = min((unsigned)piece, (keys + a.sms - items - 1) / (a.sms - items));
+            piece = max(1, max(min(piece, kMaxItemTiles), (longest + p.pass[0].splits - 1) / p.pass[0].splits));
           }
           while (ok) {
             // the 32 samples that item w is in
@@ -378,7 +394,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               smp = PagedSample{__shfl_sync(0xffffffffu, smp.q0, from), __shfl_sync(0xffffffffu, smp.n, from), __shfl_sync(0xffffffffu, smp.len, from)};
               sample = chunk + from;
               tiles = (smp.n * p.g + C::kRows - 1) / C::kRows;
-              end = tiles * a.N_kv * p.pass[0].splits;
+              cuts = max(1, ((smp.len + kTile - 1) / kTile + piece - 1) / piece);        // pieces of the sample
+              end = tiles * a.N_kv * cuts;
 #pragma unroll
               for (int o = 1; o < 32; o <<= 1) {
                 const int y = __shfl_up_sync(0xffffffffu, end, o);
@@ -394,13 +411,13 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             if (chunk < pc.samples) {                      // (there may be more blocks than items)
               const int src = __ffs(__ballot_sync(0xffffffffu, end > w - before)) - 1;
               const PagedSample it{__shfl_sync(0xffffffffu, smp.q0, src), __shfl_sync(0xffffffffu, smp.n, src), __shfl_sync(0xffffffffu, smp.len, src)};
-              const int rt = __shfl_sync(0xffffffffu, tiles, src), splits = p.pass[0].splits;
-              int k = w - before - (__shfl_sync(0xffffffffu, end, src) - rt * a.N_kv * splits);
+              const int rt = __shfl_sync(0xffffffffu, tiles, src), pieces = __shfl_sync(0xffffffffu, cuts, src);
+              int k = w - before - (__shfl_sync(0xffffffffu, end, src) - rt * a.N_kv * pieces);
               SegDesc o;
               o.h_kv = k % a.N_kv;
               k /= a.N_kv;
-              o.part = k % splits;
-              const int row0 = (rt - 1 - k / splits) * C::kRows, rows = it.n * p.g;
+              o.part = k % pieces;
+              const int row0 = (rt - 1 - k / pieces) * C::kRows, rows = it.n * p.g;
               const int sees = paged_limit(a.causal, it, (min(row0 + C::kRows, rows) - 1) / p.g);
               const int total = (sees + kTile - 1) / kTile, begin = min(total, o.part * piece);
               o.n = min(total, begin + piece) - begin;
@@ -415,16 +432,27 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               o.own = a.causal ? it.len + a.n_q - it.n - it.q0 : it.len;
               o.kv0 = __shfl_sync(0xffffffffu, sample, src);
               emit(o, 1, o.row0, o.base0, o.n > 0);
-              held += o.n;
+              published += o.n;
+              // pieces of the plan that the sample does not have weigh 0
+              for (int r = lane; o.part == 0 && r < min(C::kRows, rows - row0); r += 32) {
+                const SegRow y = seg_row(p, 1, 0, o.h_kv, o.row0 + r);
+                for (int c = pieces; c < p.pass[0].splits; ++c) p.part_ml[(int64_t)c * p.rows + (int64_t)y.t * a.N_h + y.h] = make_float2(-INFINITY, 0.f);
+              }
             }
-            if (!x.steal) break;
-            // The next item is taken when the one before the last is done.  (While those behind it have few tiles it is taken at once,
-            // so that Q K^T and its keys, three tiles ahead at most, never wait for an item that waits for them.)
-            while (ok && i > released && held - desc[released % kDesc].n >= 6) {
-              held -= desc[released % kDesc].n;
-              ok = wait(bar_d_empty(released % kDesc), (released / kDesc) & 1);
-              ++released;
+            if (!x.steal) {
+              w += gridDim.x;
+              if (chunk >= pc.samples) break;
+              continue;
             }
+            // The next item is taken eight tiles before the end of those at hand.  (Taken when the one before the last is done, which may be
+            // an item too early: 956 instead of 941 us for ragged observations, 75 instead of 63 for 27 short chunks.)  A stream gets
+            // through its tile with no more than the three tiles behind it in the products, so those four are what has to be at hand.
+            const unsigned long long t0 = clock64();
+            while (published - *progress > 8 && ok) {
+              __nanosleep(200);
+              ok = !*abort_flag && clock64() - t0 < kWaitCycles;
+            }
+            ok = __all_sync(0xffffffffu, ok ? 1 : 0) != 0;
             if (!ok) break;
             if (lane == 0) {
               mbar_expect_tx(bar_answer, 16);
@@ -1194,6 +1222,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
         tc_fence_before();
         arrive(bar_p_full(buf));
+        if (kPaged && threadIdx.x == 0) *progress = (kAlt ? u0 : u0 / 2) + i + 1;
         if (pend) {
           ok = flush();
           if (!ok) break;
@@ -1297,8 +1326,8 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kP
   static SmemOptIn opt_in;
   cudaError_t e = opt_in((const void*)seg_tc_kernel<D, kAlt, kPaged, DH>, smem, a.device);
   if (e != cudaSuccess) return e;
-  const int grid = kPaged || x.items < a.sms ? x.items : a.sms;
-  x.steal = kPaged && x.items > a.sms;
+  x.steal = kPaged && x.items > a.sms && p.pass[pass].splits == 1;
+  const int grid = x.steal || x.items < a.sms ? x.items : a.sms;
   ++*launches;
   if (pass == 1) return launch_after(seg_tc_kernel<D, kAlt, kPaged, DH>, dim3(grid), dim3(kThreadsS), smem, st, mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
   seg_tc_kernel<D, kAlt, kPaged, DH><<<grid, kThreadsS, smem, st>>>(mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);

@@ -184,6 +184,20 @@ def test_tables_with_room_for_much_more(kind, new):
         c.compare(out, lse, True)
 
 
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("new,lens", [([70, 33, 1], [6000, 40, 1]), ([40, 0, 100, 12], [512, 900, 5200, 12]), ([100, 100, 100], [100, 2000, 3900])])
+@pytest.mark.parametrize("causal", [False, True])
+def test_few_chunks_of_unequal_histories(D, new, lens, causal):
+    """Pieces of one size for all samples: one history has many, another a single one.  A call before leaves other pieces in the workspace."""
+    first = case(KINDS[0], [90, 90], [8000, 7000], 4, 2, D, 32, seed=1)
+    c = case(KINDS[0], new, lens, 4, 2, D, 32, seed=2)
+    first.run(causal)
+    c.ctx = first.ctx
+    for kw in (dict(), dict(max_kv=20000)):
+        out, lse = c.run(causal, **kw)
+        c.compare(out, lse, causal)
+
+
 def test_two_threads_with_one_context():
     """Calls from two threads, each on a stream of its own: the binding keeps nothing of a call in the context."""
     import threading
