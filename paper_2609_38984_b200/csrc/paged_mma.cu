@@ -1,5 +1,5 @@
-// Attention of few new tokens to paged keys, bf16, on warp-level matrix instructions: the kernel for single tokens and short chunks, for
-// head dim 32, and the independent second opinion on the tcgen05 kernel.
+// Attention of few new tokens to paged keys, bf16, on warp-level matrix instructions: the kernel for single tokens and short chunks,
+// and the independent second opinion on the tcgen05 kernel.
 //
 // The new tokens' rows of a sample and key/value head, in the order (token, head of the group), are cut into row tiles of 16 * WR
 // rows.  A unit of work is a tile of 64 or 128 keys of a row tile, in the order (sample, key/value head, row tile, key tile); `shares` CTAs

@@ -29,8 +29,8 @@
 //   goes to the ring.
 // Paged keys: a block per item, and running blocks take over those that have not started (16 chunks behind 640 to 8704 keys, 384 items:
 // 131 us, 171 in turn); K and V are boxes of pages.  What bounds them: head dim 128 as below (chunks of 300 to 2520 tokens, 8 heads on 32,
-// causal, 1.17 TFLOP: 974 us, 0.70 of the measured burst rate; 0.75 of the sustained one where it runs for longer); head dim 64 with up to
-// 128 rows the issuing warp, some 1600 clk a tile for 640 of products (the 16 chunks: 117 us, 4.0 TB/s).
+// causal, 1.17 TFLOP: 940 us, 0.73 of the measured burst rate); head dim 64 with up to
+// 128 rows the issuing warp, some 1600 clk a tile for 640 of products (the 16 chunks: 115 us, 4.1 TB/s).
 // Paged keys, at most 64 rows: the tile holds the rows twice, and stream 1 works on the second half, so that its exponentials run on the
 //   sub-cores of the TMEM lanes that stream 0 leaves idle (16 chunks of 64 tokens, head dim 64: 127 us, 131 with both in the first half).
 //   Its accumulators are out of stream 0's reach there and come through the item's query buffer as fp32.
@@ -735,7 +735,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       int kna = 0, kr0 = 0, kr1 = 0;                // their tiles of segment 0, and real keys ahead of each segment's first tile
       int vna = 0, vr0 = 0, vr1 = 0;
       Turn<NB> qk_at, pv_at;                        // score buffers of the next units
-      int qk_s = 0, pv_s = 0;                       // kAlt: their streams
+      int pv_s = 0;                                 // kAlt: the stream of P V
       int k_st = 0, k_k16 = 0;                      // slot and steps of the current K tile
       // makes (kn, ki) the next tile of Q K^T and takes its ring slot; false at the end
       auto next_k = [&]() {
@@ -847,19 +847,50 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           if (half) qk(0, false);
         }
       } else {
-        auto qk_alt = [&]() {
-          if (!next_k()) return;
-          if (qk_s) qk(1, true);         // (a stream that is known here keeps the addresses out of the vector registers: 187 and 176 us for
-          else qk(0, true);              // 144 items of 64 rows and 20064 keys)
-          qk_s ^= 1;
+        // tiles from i on of which each is whole, not its item's last one and in the segment of tile i
+        auto inner = [&](int i, int n, int na, int r0, int r1) { return (i < na ? min(min(na, n - 1), r0 / kTile) : min(n - 1, r1 / kTile)) - i; };
+        // (the next Q K^T takes the score buffer that this P V leaves: LK = NB)
+        auto step = [&](auto stream) {
+          const int st = ring.at;
+          ok = wait(bar_full(st), ring.phase) && wait(bar_p_full(pv_at.at), pv_at.phase);
+          if (!ok) return;
+          ring.step();
+          tc_fence_after();
+          issue_pv(decltype(stream)::value, pv_at.at, st, true, kTile / 16);
+          tc_commit(bar_empty(st), el);
+          const int k = ring.at;
+          ok = wait(bar_full(k), ring.phase);
+          if (!ok) return;
+          ring.step();
+          tc_fence_after();
+          issue_qk(kiter % QB, pv_at.at, k, kTile / 16);
+          tc_commit(bar_empty(k), el);
+          pv_at.step();
         };
 #pragma unroll 1
-        for (int j = 0; j < LK && ok; ++j) qk_alt();
-        while (v_left() && next_v()) {
-          if (pv_s) pv(1, true);
-          else pv(0, true);
+        for (int j = 0; j < LK && ok; ++j)
+          if (next_k()) qk(0, true);
+        while (v_left()) {
+          // Two tiles at a time from the middle of their items, without a look at anything but the four barriers: with the checks below
+          // each tile took 1570 clk of this warp, 700 of them for the checks.
+          int both = vi > 1 && pv_s == 0 && ki > 0 ? min(inner(vi, vn, vna, vr0, vr1), inner(ki, kn, kna, kr0, kr1)) / 2 : 0;
+          if (both > 0) {
+            vi += 2 * both;
+            ki += 2 * both;
+#pragma unroll 1
+            do {
+              step(std::integral_constant<int, 0>());
+              if (!ok) break;
+              step(std::integral_constant<int, 1>());
+            } while (--both > 0 && ok);
+            if (!ok) break;
+            qk_at.at = pv_at.at;
+          }
+          if (!next_v()) break;
+          if (pv_s) pv(1, true);         // (a stream that is known here keeps the addresses out of the vector registers: 187 and 176 us for
+          else pv(0, true);              // 144 items of 64 rows and 20064 keys)
           pv_s ^= 1;
-          if (v_left()) qk_alt();
+          if (v_left() && next_k()) qk(0, true);
         }
       }
       if (!ok) {
