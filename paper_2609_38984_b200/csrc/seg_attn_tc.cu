@@ -29,8 +29,8 @@
 //   goes to the ring.
 // Paged keys: a block per item, and running blocks take over those that have not started (16 chunks behind 640 to 8704 keys, 384 items:
 // 131 us, 171 in turn); K and V are boxes of pages.  What bounds them: head dim 128 as below (chunks of 300 to 2520 tokens, 8 heads on 32,
-// causal, 1.17 TFLOP: 940 us, 0.73 of the measured burst rate); head dim 64 with up to
-// 128 rows the issuing warp, some 1600 clk a tile for 640 of products (the 16 chunks: 115 us, 4.1 TB/s).
+// causal, 1.17 TFLOP: 908 us, 0.75 of the measured burst rate); head dim 64 with up to
+// 64 rows memory, less the changes of items (the 16 chunks: 95 us, 4.9 TB/s; items of 20064 keys 5.4); up to 128 rows the exponentials.
 // Paged keys, at most 64 rows: the tile holds the rows twice, and stream 1 works on the second half, so that its exponentials run on the
 //   sub-cores of the TMEM lanes that stream 0 leaves idle (16 chunks of 64 tokens, head dim 64: 127 us, 131 with both in the first half).
 //   Its accumulators are out of stream 0's reach there and come through the item's query buffer as fp32.
@@ -826,9 +826,52 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           if (++vi == vn) tc_commit(bar_o_final, el);
         }
       };
+      // tiles from i on of which each is whole, not its item's last one and in the segment of tile i
+      auto inner = [&](int i, int n, int na, int r0, int r1) { return (i < na ? min(min(na, n - 1), r0 / kTile) : min(n - 1, r1 / kTile)) - i; };
+      // waits for the next tile of the ring
+      auto take = [&]() {
+        const int st = ring.at;
+        ok = wait(bar_full(st), ring.phase);
+        ring.step();
+        return st;
+      };
+      // P V of the next unit with the V tile st, in the middle of an item
+      auto inner_pv = [&](int s, int st) {
+        ok = ok && wait(bar_p_full(pv_at.at), pv_at.phase);
+        if (!ok) return;
+        tc_fence_after();
+        issue_pv(s, pv_at.at, st, true, kTile / 16);
+      };
       if constexpr (!kAlt && NB == 2) {
         if (next_k()) qk(0, false), qk(1, true);
-        while (v_left() && next_v()) {
+        while (v_left()) {
+          // Paged keys: tiles from the middle of their items without a look at anything but the barriers (ragged observations 934 us, 908
+          // with this.  For segments it is a choice between 1 % of long items and 1 % of short ones, in instruction fetches.)
+          int both = kPaged && vi > 0 && ki > 0 ? min(inner(vi, vn, vna, vr0, vr1), inner(ki, kn, kna, kr0, kr1)) : 0;
+          if (both > 0) {
+            const int qt = (kiter % QB) * C::NQ;
+            vi += both;
+            ki += both;
+#pragma unroll 1
+            do {
+              const int v = take();
+              inner_pv(0, v);
+              pv_at.step();
+              if (!ok) break;
+              const int k = take();
+              if (!ok) break;
+              tc_fence_after();
+              issue_qk(qt, 0, k, kTile / 16);
+              inner_pv(1, v);
+              pv_at.step();
+              if (!ok) break;
+              tc_commit(bar_empty(v), el);
+              issue_qk(qt + 1, 1, k, kTile / 16);
+              tc_commit(bar_empty(k), el);
+            } while (--both > 0);
+            if (!ok) break;
+          }
+          if (!next_v()) break;
           pv(0, false);
           const bool k = ok && next_k();            // (behind the last V too: only the descriptors tell that it was the last)
           if (k) qk(0, false);
@@ -847,21 +890,14 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           if (half) qk(0, false);
         }
       } else {
-        // tiles from i on of which each is whole, not its item's last one and in the segment of tile i
-        auto inner = [&](int i, int n, int na, int r0, int r1) { return (i < na ? min(min(na, n - 1), r0 / kTile) : min(n - 1, r1 / kTile)) - i; };
         // (the next Q K^T takes the score buffer that this P V leaves: LK = NB)
         auto step = [&](auto stream) {
-          const int st = ring.at;
-          ok = wait(bar_full(st), ring.phase) && wait(bar_p_full(pv_at.at), pv_at.phase);
+          const int v = take();
+          inner_pv(decltype(stream)::value, v);
           if (!ok) return;
-          ring.step();
-          tc_fence_after();
-          issue_pv(decltype(stream)::value, pv_at.at, st, true, kTile / 16);
-          tc_commit(bar_empty(st), el);
-          const int k = ring.at;
-          ok = wait(bar_full(k), ring.phase);
+          tc_commit(bar_empty(v), el);
+          const int k = take();
           if (!ok) return;
-          ring.step();
           tc_fence_after();
           issue_qk(kiter % QB, pv_at.at, k, kTile / 16);
           tc_commit(bar_empty(k), el);
