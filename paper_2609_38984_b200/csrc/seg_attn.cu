@@ -247,19 +247,30 @@ struct PagedPlan {
   int shares;                // kMma: CTAs
   bool cut;
 };
+// The kernel for paged keys, up to `rows` of a sample and key/value head and up to `keys` of them.  More than 64 rows fill a tile of the tensor
+// cores, at every head dim; more than 32 do with more than 512 keys.  From 17 rows on it streams long histories faster than the warp-level
+// kernel (24 heads of 128, 16 samples of 32 rows and up to 8704 keys: 160 us instead of 192; of 16 rows: 160 and 166), but starts later: head
+// dim 128 with up to 1232 keys 52 and 57 us, with up to 432 keys 36 and 29; head dim 64, whose keys are half as many bytes,
+// 96 and 112 with up to 8704 keys, 41 and 32 with up to 1232, 30 and 26 with 48 items of the SMs' 148.  At head dim 32 it is slower or even.
+Kind paged_kind(const SegArgs& a, const PagedCache& c, int64_t rows, bool warp_mma) {
+  if (a.dtype == 0) return kF32;
+  if (warp_mma) return kMma;
+  if (rows > 64) return kTc;
+  if (a.D == 32 || rows <= 16) return kMma;
+  if (rows > 32) return c.max_kv > 512 ? kTc : kMma;
+  return a.D == 128 ? (c.max_kv > 1024 ? kTc : kMma) : (c.max_kv > 2048 && (int64_t)c.samples * a.N_kv >= 2 * a.sms ? kTc : kMma);
+}
 PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
   PagedPlan pl;
   const int g = a.N_h / a.N_kv;
   const int64_t rows = (int64_t)c.max_q * g;
-  SegArgs as64 = a;                // (paged keys of head dim 32 have a tensor-core kernel: planned as 64; up to 64 rows it is no faster)
-  if (a.D == 32 && rows > 64) as64.D = 64;
-  const PassPlan ps = plan_pass(as64, c.samples, rows, c.max_kv, warp_mma, -1);
-  pl.kind = ps.kind;
-  pl.tile_rows = pl.kind == kMma && rows <= 8 ? 8 : ps.tile_rows;
-  if (pl.kind == kF32 && rows > 32) pl.tile_rows = 64;         // (30 us instead of 33 with 32)
+  pl.kind = paged_kind(a, c, rows, warp_mma);
+  if (pl.kind == kTc) pl.tile_rows = seg_tc_tile_rows(rows);
+  else if (pl.kind == kMma) pl.tile_rows = rows <= 8 ? 8 : seg_mma_tile_rows(rows);
+  else pl.tile_rows = rows > 32 ? 64 : seg_f32_tile_rows(rows, c.samples * (int64_t)a.N_kv, a.sms);       // (30 us instead of 33 with 32)
   pl.row_tiles = (int)ceil_div(rows, pl.tile_rows);
   // a sample fills its tiles but for the last one
-  int64_t tiles = (int64_t)a.n_q * g / ps.tile_rows + c.samples;
+  int64_t tiles = (int64_t)a.n_q * g / pl.tile_rows + c.samples;
   if (tiles > (int64_t)c.samples * pl.row_tiles) tiles = (int64_t)c.samples * pl.row_tiles;
   int64_t s = 1;
   if (pl.kind == kTc) {

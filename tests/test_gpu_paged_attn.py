@@ -198,6 +198,16 @@ def test_few_chunks_of_unequal_histories(D, new, lens, causal):
         c.compare(out, lse, causal)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D,H,kv", [(128, 6, 2), (64, 12, 4)])
+def test_many_short_chunks_behind_long_histories(kind, D, H, kv):
+    """17 to 32 rows of a sample and key/value head, some samples with fewer or none, histories of 1 to 2600 keys."""
+    new = [6 + i % 5 - 6 * (i % 7 == 3) for i in range(76)]
+    lens = [max(new[i], (i * 353) % 2600 + 1) for i in range(76)]
+    for causal in (False, True):
+        check(kind, causal, new, lens, H, kv, D, 64)
+
+
 def test_two_threads_with_one_context():
     """Calls from two threads, each on a stream of its own: the binding keeps nothing of a call in the context."""
     import threading
