@@ -270,7 +270,7 @@ struct PagedCache {
   int max_kv;               // tokens that a sample has at most (the table holds as many pages)
 };
 
-// ---- paged_attn.cu --------------------------------------------------------
+// ---- seg_attn.cu, paged_mma.cu ---------------------------------------------
 // Attention of the new tokens to their samples' cached keys: a.q, a.out [n_q = tokens, N_h, D], a.lse [N_h, tokens]; a.k[1] and
 // a.v[1] are the pages.
 size_t paged_scratch_bytes(const SegArgs& a, const PagedCache& c, bool warp_mma);
