@@ -194,8 +194,8 @@ struct PageWindow {
     page += threadIdx.x & 31;
     return page < (c.max_kv + (1 << c.page_shift) - 1) >> c.page_shift ? __ldg(c.table + sample * c.table_stride + page) : 0;
   }
-  // the lane-th of the pages from `page` on, which lie in one aligned group of 32 (warp-wide)
-  __device__ __forceinline__ int get(const PagedCache& c, int smp, int page, int lane) {
+  // requests the pages around `page`, which are waited for at their first use (warp-wide)
+  __device__ __forceinline__ void prefetch(const PagedCache& c, int smp, int page) {
     const int at = page & ~31;
     if (smp != sample || at != first) {
       const bool on = smp == sample && at == first + 32;
@@ -204,6 +204,10 @@ struct PageWindow {
       now = on ? next : fetch(c, at);
       next = fetch(c, at + 32);
     }
+  }
+  // the lane-th of the pages from `page` on, which lie in one aligned group of 32 (warp-wide)
+  __device__ __forceinline__ int get(const PagedCache& c, int smp, int page, int lane) {
+    prefetch(c, smp, page);
     return __shfl_sync(0xffffffffu, now, (page & 31) + lane);
   }
 };

@@ -30,7 +30,7 @@
 // Paged keys: a block per item, and running blocks take over those that have not started (16 chunks behind 640 to 8704 keys, 384 items:
 // 131 us, 171 in turn); K and V are boxes of pages.  What bounds them: head dim 128 as below (chunks of 300 to 2520 tokens, 8 heads on 32,
 // causal, 1.17 TFLOP: 908 us, 0.75 of the measured burst rate); head dim 64 with up to
-// 64 rows memory, less the changes of items (the 16 chunks: 95 us, 4.9 TB/s; items of 20064 keys 5.4); up to 128 rows the exponentials.
+// 64 rows memory, less the changes of items (the 16 chunks: 96 us, 4.8 TB/s; an item of 20064 keys for every SM: 127 us, 6.0); up to 128 rows the exponentials.
 // Paged keys, at most 64 rows: the tile holds the rows twice, and stream 1 works on the second half, so that its exponentials run on the
 //   sub-cores of the TMEM lanes that stream 0 leaves idle (16 chunks of 64 tokens, head dim 64: 127 us, 131 with both in the first half).
 //   Its accumulators are out of stream 0's reach there and come through the item's query buffer as fp32.
@@ -345,9 +345,9 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       };
       auto walk = [&](bool keys) {
         if constexpr (kPaged) {
-          // A block per item (of as many as there can be), in the order: samples by falling length (32 at a time), their row tiles (the
-          // last first: with causal it has the most keys), pieces, key/value heads.  Where there are more blocks than SMs, a
-          // running one takes over blocks that have not started yet, when it is nearly through with what it has, so that the SMs finish
+          // A block per item (of as many as there can be), in the order: samples, their row tiles (the last first: with causal it has the most
+          // keys), pieces, key/value heads.  Where there are more blocks than SMs, the samples come by falling length (32 at a time), and a
+          // running block takes over others that have not started yet, when it is nearly through with what it has, so that the SMs finish
           // together whatever the lengths.  Lane l knows sample order[l] and where its items end among those of the 32.
           int chunk = -32, before = 0, all = 0, w = blockIdx.x, sample = 0, tiles = 0, cuts = 1, end = 0, published = 0, phase = 0;
           PagedSample smp{0, 0, 0};
@@ -381,16 +381,20 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               chunk += 32;
               smp = PagedSample{0, 0, 0};
               if (chunk + lane < pc.samples) smp = paged_sample(pc, a.n_q, chunk + lane, p.status);
-              int rank = 0;
-#pragma unroll 1
-              for (int j = 0; j < 32; ++j) {
-                const int other = __shfl_sync(0xffffffffu, smp.len, j);
-                rank += other > smp.len || (other == smp.len && j < lane) ? 1 : 0;
+              int from = lane;
+              if (x.steal) {
+                // a bitonic network on (key tiles, lane), the longest first; of equal ones the first
+                int key = ((smp.len + kTile - 1) / kTile) << 5 | (31 - lane);
+#pragma unroll
+                for (int k = 2; k <= 32; k <<= 1) {
+#pragma unroll
+                  for (int j = k >> 1; j > 0; j >>= 1) {
+                    const int other = __shfl_xor_sync(0xffffffffu, key, j);
+                    key = ((lane & k) == 0) == ((lane & j) == 0) ? max(key, other) : min(key, other);
+                  }
+                }
+                from = 31 - (key & 31);
               }
-              int from = 0;
-#pragma unroll 1
-              for (int j = 0; j < 32; ++j)
-                if (__shfl_sync(0xffffffffu, rank, j) == lane) from = j;
               smp = PagedSample{__shfl_sync(0xffffffffu, smp.q0, from), __shfl_sync(0xffffffffu, smp.n, from), __shfl_sync(0xffffffffu, smp.len, from)};
               sample = chunk + from;
               tiles = (smp.n * p.g + C::kRows - 1) / C::kRows;
@@ -599,6 +603,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       // missing one, so that V_T is always load LK + 2 T.  A descriptor is released when the cursor of V leaves it.
       int iter = 0;                                // items of K so far
       bool ok = true;
+      if (kPaged && lane < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : (lane == 1 ? &map_k1 : &map_v1)) : "memory");
       Turn<ST> ring;
       Cursor kc;
       auto load_queries = [&](const SegDesc& o) {
@@ -638,6 +643,7 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           if (!ok) break;
           kc.enter(desc[slot]);
           if (kc.n == 0) break;
+          kc.pages.prefetch(pc, kc.idx0, kc.base1 >> sh);
           if (x.box_q) ok = load_queries(desc[slot]);
           ++iter;
           ++di;
@@ -666,6 +672,9 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             ++di;
             kc.enter(desc[slot]);
             k_end = kc.n == 0;
+            if constexpr (kPaged) {
+              if (!k_end) kc.pages.prefetch(pc, kc.idx0, kc.base1 >> sh);
+            }
             if (!k_end && x.box_q && !load_queries(desc[slot])) return false;
             ++iter;
           }
