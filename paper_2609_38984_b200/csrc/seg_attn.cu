@@ -273,6 +273,11 @@ PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
   int64_t tiles = (int64_t)a.n_q * g / pl.tile_rows + c.samples;
   if (tiles > (int64_t)c.samples * pl.row_tiles) tiles = (int64_t)c.samples * pl.row_tiles;
   int64_t s = 1;
+  // Long histories, and row tiles for fewer than one or two rounds of the SMs: pieces for several blocks an SM, which load the SMs evenly
+  // whatever the lengths (5 samples of some 290 tokens, 16 heads of 64 on 2, 17430 to 89139 keys: 544 us instead of 1154; 2 samples of 300 tokens,
+  // 32 heads of 128 on 8, up to 60000 keys: 374 and 778; 144 tiles of 64 rows and 30000 keys each, where there is nothing to even out: 181 and
+  // 172, the join; 240 such tiles, bound by memory on fewer SMs too, 289 and 277).
+  const bool even = c.max_kv >= 16384 && tiles * a.N_kv < (pl.tile_rows == 128 ? 1 : 2) * a.sms;
   if (pl.kind == kTc) {
     // No more pieces than SMs.  Where samples differ in length, the longest may have more than its share, which the kernel decides (6 samples
     // of 3000 to 30000 keys: 76 us, 88 without).  256 rows of partial results cost more than that gains.
@@ -280,6 +285,7 @@ PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
     if (s > 1 && pl.tile_rows == 128) s *= 4;
     if (s > c.max_kv / 256) s = c.max_kv / 256;      // (148 tokens of 24 heads on 8 and 1281 keys: 23 us, 27 with pieces of 512)
     if (s > kMaxSplits) s = kMaxSplits;
+    if (s < 8 && even) s = 8;
     if (s < ceil_div(c.max_kv, kMaxItemKeys)) s = ceil_div(c.max_kv, kMaxItemKeys);
     if (s < 1) s = 1;
   } else if (pl.kind == kF32) {
@@ -292,6 +298,7 @@ PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
   }
   pl.splits = (int)s;
   pl.items = (pl.kind == kTc ? tiles : (int64_t)c.samples * pl.row_tiles) * a.N_kv * s;
+  if (pl.kind == kTc && s > 1 && pl.items > (even ? 4 : 1) * a.sms) pl.items = (even ? 4 : 1) * a.sms;      // blocks: each takes what is left in turn
   pl.shares = paged_mma_shares(a.sms);
   // A row tile's keys are cut only where they may be many: the second kernel costs more than 512 keys do.
   pl.cut = c.max_kv > 512;

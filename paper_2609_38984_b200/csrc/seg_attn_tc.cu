@@ -354,7 +354,8 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           const uint32_t answer = base + C::kData + C::kTail - 48, bar_answer = answer + 16;
           // Pieces of one size for all samples, so that a short one has fewer, and no more pieces than SMs: a share of the longest sample
           // that fits whatever the others have, or, where that is finer, the keys of all row tiles over the SMs that are left when each
-          // row tile has one for its odd piece.  (A plan of pieces has few samples.)
+          // row tile has one for its odd piece.  Where the plan has several blocks an SM (long histories): as many pieces as blocks, if by
+          // that the SMs, which then take over blocks, end earlier.  (A plan of pieces has few samples.)
           int piece = (pc.max_kv + kTile - 1) / kTile;
           if (p.pass[0].splits > 1) {
             int longest = 0, items = 0;
@@ -372,6 +373,13 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             const int fit = max(1, a.sms / items);
             piece = (longest + fit - 1) / fit;
             if (items < a.sms) piece = min((unsigned)piece, (keys + a.sms - items - 1) / (a.sms - items));
+            const int blocks = gridDim.x;
+            if (x.steal && items < blocks) {
+              // in key tiles: the longest piece, or so many row tiles one after the other; an even load, half a piece and the join
+              const int end = items <= a.sms ? piece : max(longest, (items + a.sms - 1) / a.sms * (int)(keys / items));
+              const int finer = max(16u, (keys + blocks - items - 1) / (blocks - items));
+              if ((int)(keys / a.sms) + finer / 2 + 16 < end) piece = finer;
+            }
             piece = max(1, max(min(piece, kMaxItemTiles), (longest + p.pass[0].splits - 1) / p.pass[0].splits));
           }
           while (ok) {
@@ -443,11 +451,11 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 for (int c = pieces; c < p.pass[0].splits; ++c) p.part_ml[(int64_t)c * p.rows + (int64_t)y.t * a.N_h + y.h] = make_float2(-INFINITY, 0.f);
               }
             }
-            if (!x.steal) {
+            if (chunk < pc.samples && p.pass[0].splits > 1) {
               w += gridDim.x;
-              if (chunk >= pc.samples) break;
               continue;
             }
+            if (!x.steal) break;
             // The next item is taken eight tiles before the end of those at hand.  (Taken when the one before the last is done, which may be
             // an item too early: 956 instead of 941 us for ragged observations, 75 instead of 63 for 27 short chunks.)  A stream gets
             // through its tile with no more than the three tiles behind it in the products, so those four are what has to be at hand.
@@ -1402,8 +1410,8 @@ cudaError_t launch_tc(const SegParams& p, int pass, bool both, const CacheArg<kP
   static SmemOptIn opt_in;
   cudaError_t e = opt_in((const void*)seg_tc_kernel<D, kAlt, kPaged, DH>, smem, a.device);
   if (e != cudaSuccess) return e;
-  x.steal = kPaged && x.items > a.sms && p.pass[pass].splits == 1;
-  const int grid = x.steal || x.items < a.sms ? x.items : a.sms;
+  const int grid = kPaged || x.items < a.sms ? x.items : a.sms;
+  x.steal = kPaged && x.items > a.sms;
   ++*launches;
   if (pass == 1) return launch_after(seg_tc_kernel<D, kAlt, kPaged, DH>, dim3(grid), dim3(kThreadsS), smem, st, mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);
   seg_tc_kernel<D, kAlt, kPaged, DH><<<grid, kThreadsS, smem, st>>>(mq, mo, mk[0], mv[0], mk[1], mv[1], p, pass, x, c);

@@ -198,6 +198,17 @@ def test_few_chunks_of_unequal_histories(D, new, lens, causal):
         c.compare(out, lse, causal)
 
 
+@pytest.mark.parametrize("D,H,kv,new,lens", [(64, 8, 2, [245, 130, 77], [5000, 21000, 17500]), (128, 4, 2, [300, 1, 64], [18000, 700, 40]),
+                                             (64, 4, 4, [100, 33, 0, 90, 120], [33, 30000, 17000, 19000, 2]), (32, 4, 1, [60, 80], [20000, 16500])])
+@pytest.mark.parametrize("causal", [False, True])
+def test_long_ragged_histories_of_few_row_tiles(D, H, kv, new, lens, causal):
+    """Pieces for several blocks an SM, of one size; a repeat, with other blocks taken over, gives the same bits."""
+    c, out, lse = check(KINDS[0], causal, new, lens, H, kv, D, 128)
+    for _ in range(3):
+        again, lse2 = c.run(causal)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("D,H,kv", [(128, 6, 2), (64, 12, 4)])
 def test_many_short_chunks_behind_long_histories(kind, D, H, kv):
