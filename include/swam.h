@@ -266,9 +266,10 @@ int swam_norm_rope(swam_ctx* ctx, const swam_norm_rope_args* args, void* stream)
  * [q_start[b], q_start[b + 1]), which are the last ones of its kv_len[b] tokens, new ones included; both calls of a step take
  * the same kv_len.  Without q_start every sample has n_tokens / n_samples.  Tokens in front of q_start[0] and behind
  * q_start[n_samples] are nobody's: nothing is done with them and their rows of any output stay as they are.
- * On the device: a q_start that is out of order, out of range or gives a sample more than max_q tokens leaves that sample out; a
- * kv_len outside [0, max_kv] is clamped; a page number outside [0, n_pages) that is needed reads as zeros and is not
- * written; swam_check reports all of them (SWAM_ERR_DEVICE_CHECK).  Table entries behind a sample's last page are not used,
+ * On the device: a q_start that is out of order, out of range or gives a sample more than max_q tokens leaves that sample out (its
+ * rows of any output stay as they are; where two samples claim a token, its rows are one's or the other's or a mix); a kv_len
+ * outside [0, max_kv] is clamped; a page number outside [0, n_pages) that is needed reads as zeros and is not written;
+ * swam_check reports all of them (SWAM_ERR_DEVICE_CHECK).  Table entries behind a sample's last page are not used,
  * and neither is what a page holds behind its sample's last token.  Samples may share pages that no call writes. */
 typedef struct {
   void* k;                   /* dev [n_pages, page_size, n_kv_heads, D]; the heads of a token are contiguous */

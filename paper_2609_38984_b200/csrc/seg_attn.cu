@@ -14,7 +14,8 @@ constexpr int64_t kMaxItemKeys = 1 << 26;
 
 // One warp per row; lanes hold the pieces' weights and then D / 32 output columns each.  The first pieces' outputs are
 // requested before the weights are known (an output of weight 0 may never have been written and is not used).
-// kPaged: the tokens in front of the first sample and behind the last one are nobody's.
+// kPaged: only rows of samples that have pieces are joined; tokens in front of the first sample, behind the last one or of a sample that is
+// left out have none.  (A plan with pieces has few samples, and looking the row's up runs beside the last pieces.)
 template <int D, typename T, int kMergeBatch, bool kPaged>
 __global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ SegParams p, const int parts,
                                                         const __grid_constant__ CacheArg<kPaged> pc) {
@@ -26,11 +27,10 @@ __global__ void __launch_bounds__(128) seg_merge_kernel(const __grid_constant__ 
   T* out = (T*)a.out + b * a.o_smp + t * a.o_tok + (int64_t)h * D + lane * CPL;
   const float* src = p.part_o + (int64_t)row * D + lane * CPL;
   const float2* ml = p.part_ml + row;
+  bool owned = row < p.rows;
+  if constexpr (kPaged) owned = owned && paged_owned(pc, a.n_q, (int)bt);
   wait_previous();                                                    // everything above ran beside the last pieces
-  if (row >= p.rows) return;
-  if constexpr (kPaged) {
-    if (pc.q_start && ((int)bt < __ldg(pc.q_start) || (int)bt >= __ldg(pc.q_start + pc.samples))) return;
-  }
+  if (!owned) return;
   float v[kMergeBatch][CPL];
   auto load = [&](int i0) {
 #pragma unroll

@@ -158,7 +158,11 @@ using CacheArg = std::conditional_t<kPaged, PagedCache, NoCache>;
 struct PagedSample {
   int q0, n, len;
 };
-// A stretch out of order, outside the tokens or longer than max_q counts as empty; lengths out of range are clamped; both are flagged.
+// A stretch out of order, outside the tokens or longer than max_q is left out.
+__device__ __forceinline__ bool paged_stretch(const PagedCache& c, int tokens, int q0, int q1) {
+  return q0 >= 0 && q0 <= q1 && q1 <= tokens && q1 - q0 <= c.max_q;
+}
+// It counts as empty; lengths out of range are clamped; both are flagged.
 __device__ __forceinline__ PagedSample paged_sample(const PagedCache& c, int tokens, int b, int* status) {
   PagedSample s;
   int q1;
@@ -170,11 +174,21 @@ __device__ __forceinline__ PagedSample paged_sample(const PagedCache& c, int tok
     q1 = s.q0 + c.max_q;
   }
   const int len = __ldg(c.kv_len + b);
-  const bool stretch = s.q0 >= 0 && s.q0 <= q1 && q1 <= tokens && q1 - s.q0 <= c.max_q;
+  const bool stretch = paged_stretch(c, tokens, s.q0, q1);
   s.n = stretch ? q1 - s.q0 : 0;
   s.len = min(max(len, 0), c.max_kv);
   if (!stretch || s.len != len) atomicOr(status, ST_BAD_LEN);
   return s;
+}
+// Does new token t belong to a sample that is not left out?  (warp-wide; the stretches may be in any order)
+__device__ __forceinline__ bool paged_owned(const PagedCache& c, int tokens, int t) {
+  if (!c.q_start) return true;
+  bool mine = false;
+  for (int b = threadIdx.x & 31; b < c.samples; b += 32) {
+    const int q0 = __ldg(c.q_start + b), q1 = __ldg(c.q_start + b + 1);
+    mine |= paged_stretch(c, tokens, q0, q1) && t >= q0 && t < q1;
+  }
+  return __any_sync(0xffffffffu, mine);
 }
 // keys that the i-th new token sees
 __device__ __forceinline__ int paged_limit(int causal, const PagedSample& s, int i) { return causal ? max(0, s.len - s.n + i + 1) : s.len; }
