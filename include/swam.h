@@ -226,8 +226,8 @@ int swam_prefix_attn(swam_ctx* ctx, const swam_prefix_args* args, void* stream);
  *
  * Rotary positions: pair i of the first rot_dim elements of a head turns by freq[i] radians per position along component
  * axis[i] of the token's position:  (a, b) -> magnitude * (a cos - b sin, b cos + a sin).  Pairs are (i, i + rot_dim / 2), or
- * (2i, 2i + 1) when interleaved.  The angle of any int32 position is reduced exactly (64-bit fixed point), so that far
- * positions lose nothing.  Frequencies stretched for longer contexts are just other values of freq (and magnitude). */
+ * (2i, 2i + 1) when interleaved.  The angle of any int32 position and any accepted frequency is reduced to within
+ * 2^-30 turns (64-bit fixed point), so that far positions lose nothing.  Frequencies stretched for longer contexts are just other values of freq (and magnitude). */
 typedef struct {
   const double* freq;   /* host, [rot_dim / 2], finite, |freq| <= 2^20; read during the call */
   const int32_t* axis;  /* host, [rot_dim / 2] in [0, n_axes), or NULL: component 0 */

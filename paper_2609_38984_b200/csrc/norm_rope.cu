@@ -4,7 +4,8 @@
 // magnitude * (a cos - b sin, b cos + a sin), rounded once to the storage type.
 // Angles.  A position times a frequency in fp32 would be off by half a step of the product, 0.004 radians at position 131072.  The
 // frequencies arrive as turns per position in units of 2^-64 turns (the last three bits name the component of the position), so that
-// position * turn modulo 2^64 IS the reduced angle: one 64-bit product, off by 2^-30 turns at most, whatever the position.  The nearest quarter turn is
+// position * turn modulo 2^64 IS the reduced angle: one 64-bit product, off by 2^-30 turns at most (five units of the turns
+// times 2^31, and the product's last 32 bits), whatever the position and the frequency.  The nearest quarter turn is
 // taken off as an integer; sine and cosine of the rest (at most an eighth of a turn) are their Taylor series up to x^9 and x^10,
 // whose next terms are below 2e-9 (of sin) and 2e-10.
 // Work: a CTA of eight warps owns a few tokens.  It finds out where they are and works out their cosines and sines once, in shared
@@ -439,15 +440,18 @@ cudaError_t launch_dim(RopeParams& p, cudaStream_t st, int* launches) {
 }  // namespace
 
 uint64_t turns_of(double freq) {
-  // freq / (2 pi) turns in units of 2^-64, modulo a turn.  2 / pi = 0xa2f9836e4e44152a / 2^64, to half a unit.
+  // |freq| / (2 pi) turns in units of 2^-64, modulo a turn.  2 / pi = 0xa2f9836e4e441529fc2757d1f534ddc1 / 2^128, to half a unit: for the
+  // largest frequency, 2^20, that is 2^-111 turns.  (With 2 / pi to 64 bits it would be 2^-52, and 2^-21 at the ends of int32.)
   uint64_t bits;
   memcpy(&bits, &freq, 8);
   const int e = (int)(bits >> 52 & 0x7ff);                               // |freq| = mantissa * 2^(e - 1075)
   if (e == 0) return 0;                                                  // (zero, and what is far below 2^-64 of a turn in 2^31 positions)
   const uint64_t mantissa = (bits & 0xfffffffffffffull) | 1ull << 52;
-  const unsigned __int128 prod = (unsigned __int128)mantissa * 0xa2f9836e4e44152aull;        // |freq| / (2 pi) * 2^(66 + 1075 - e)
-  const int shift = 1077 - e;                                            // to units of 2^-64
-  const uint64_t u = shift >= 128 ? 0 : (shift >= 0 ? (uint64_t)(prod >> shift) : (shift > -64 ? (uint64_t)prod << -shift : 0));
+  // mantissa * (2 / pi * 2^128) = |freq| / (2 pi) * 2^(130 + 1075 - e), without its last 64 bits
+  const unsigned __int128 low = (unsigned __int128)mantissa * 0xfc2757d1f534ddc1ull;
+  const unsigned __int128 prod = (unsigned __int128)mantissa * 0xa2f9836e4e441529ull + (uint64_t)(low >> 64);
+  const int shift = 1077 - e;                                            // to units of 2^-64; at least 34, as frequencies end at 2^20
+  const uint64_t u = shift >= 128 ? 0 : (uint64_t)(prod >> shift);
   return bits >> 63 ? 0 - u : u;
 }
 
