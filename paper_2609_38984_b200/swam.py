@@ -123,10 +123,11 @@ def rope_magnitude(factor: float) -> float:
 
 
 class Rope:
-    """Rotary positions: radians per position of each pair, the component of the position that turns it (default: the only one),
-    pairs (i, i + rot/2) or, interleaved, (2i, 2i + 1), and the factor on the rotated elements."""
+    """Rotary positions: radians per position of each pair, the component of the position that turns it (default: the first),
+    pairs (i, i + rot/2) or, interleaved, (2i, 2i + 1), the factor on the rotated elements, and how many components a
+    position has, 1 .. 8 (default: as many as `axes` names; more where the last ones turn nothing)."""
 
-    def __init__(self, freq, axes=None, interleaved: bool = False, magnitude: float = 1.0):
+    def __init__(self, freq, axes=None, interleaved: bool = False, magnitude: float = 1.0, n_axes: Optional[int] = None):
         freq = [float(f) for f in freq]
         axes = None if axes is None else [int(a) for a in axes]
         if not freq or (axes is not None and len(axes) != len(freq)):
@@ -135,7 +136,10 @@ class Rope:
             raise ValueError("Rope: negative axis")
         if not magnitude > 0:
             raise ValueError("Rope: magnitude must be positive")
-        self.rot_dim, self.n_axes = 2 * len(freq), 1 if axes is None else max(axes) + 1
+        named = 1 if axes is None else max(axes) + 1
+        if n_axes is not None and not named <= n_axes <= 8:
+            raise ValueError(f"Rope: n_axes must be {named} .. 8")
+        self.rot_dim, self.n_axes = 2 * len(freq), named if n_axes is None else int(n_axes)
         self._freq = (ctypes.c_double * len(freq))(*freq)
         self._axis = None if axes is None else (ctypes.c_int32 * len(axes))(*axes)
         self._c = SwamRope(ctypes.addressof(self._freq), None if axes is None else ctypes.addressof(self._axis), self.rot_dim,
