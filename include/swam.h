@@ -267,7 +267,7 @@ int swam_norm_rope(swam_ctx* ctx, const swam_norm_rope_args* args, void* stream)
  * the same kv_len.  Without q_start every sample has n_tokens / n_samples.  Tokens in front of q_start[0] and behind
  * q_start[n_samples] are nobody's: nothing is done with them and their rows of any output stay as they are.
  * On the device: a q_start that is out of order, out of range or gives a sample more than max_q tokens leaves that sample out (its
- * rows of any output stay as they are; where two samples claim a token, its rows are one's or the other's or a mix); a kv_len
+ * rows of any output stay as they are; where two samples claim a token, its rows may hold anything); a kv_len
  * outside [0, max_kv] is clamped; a page number outside [0, n_pages) that is needed reads as zeros and is not written;
  * swam_check reports all of them (SWAM_ERR_DEVICE_CHECK).  Table entries behind a sample's last page are not used,
  * and neither is what a page holds behind its sample's last token.  Samples may share pages that no call writes. */

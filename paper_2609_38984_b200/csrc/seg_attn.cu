@@ -242,8 +242,8 @@ namespace {
 struct PagedPlan {
   Kind kind;
   int tile_rows, splits;     // kF32, kTc
-  int row_tiles;             // at most, per sample and key/value head
-  int64_t items;             // at most
+  int blocks, row_tiles;     // kF32: samples and row tiles per sample and key/value head, or all samples' row tiles (at most) and 0
+  int items;                 // at most
   int shares;                // kMma: CTAs
   bool cut;
 };
@@ -268,10 +268,13 @@ PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
   if (pl.kind == kTc) pl.tile_rows = seg_tc_tile_rows(rows);
   else if (pl.kind == kMma) pl.tile_rows = rows <= 8 ? 8 : seg_mma_tile_rows(rows);
   else pl.tile_rows = rows > 32 ? 64 : seg_f32_tile_rows(rows, c.samples * (int64_t)a.N_kv, a.sms);       // (30 us instead of 33 with 32)
+  pl.blocks = c.samples;
   pl.row_tiles = (int)ceil_div(rows, pl.tile_rows);
-  // a sample fills its tiles but for the last one
-  int64_t tiles = (int64_t)a.n_q * g / pl.tile_rows + c.samples;
-  if (tiles > (int64_t)c.samples * pl.row_tiles) tiles = (int64_t)c.samples * pl.row_tiles;
+  // A sample fills its tiles but for the last one; one without new tokens has none.  (A call has 2^30 rows at most, so that tiles * N_kv
+  // stays below 2^30 + 2^26, and half as much again below 2^31.)
+  const int64_t longest = (int64_t)c.samples * pl.row_tiles;       // if all samples had as many as the longest may have
+  int64_t tiles = (int64_t)a.n_q * g / pl.tile_rows + (c.samples < a.n_q ? c.samples : a.n_q);
+  if (tiles > longest) tiles = longest;
   int64_t s = 1;
   // Long histories, and row tiles for fewer than one or two rounds of the SMs: pieces for several blocks an SM, which load the SMs evenly
   // whatever the lengths (5 samples of some 290 tokens, 16 heads of 64 on 2, 17430 to 89139 keys: 544 us instead of 1154; 2 samples of 300 tokens,
@@ -291,14 +294,23 @@ PagedPlan paged_plan(const SegArgs& a, const PagedCache& c, bool warp_mma) {
   } else if (pl.kind == kF32) {
     // Many small pieces, of one size for all samples: those of short samples are empty, and the long ones are what takes time (6 samples
     // of 41 to 1521 keys, 90 row tiles: 56 us with 4 SMs' worth of CTAs, 30 with 12 or 16).
-    s = 16 * a.sms / (c.samples * (int64_t)pl.row_tiles * a.N_kv);
+    // A block each for as many row tiles as the longest sample may have; where that is half as many again as there can be (a call that
+    // does not say how many new tokens a sample has), the blocks look for theirs, which takes a pass over q_start.
+    if (2 * longest > 3 * tiles) {
+      pl.blocks = (int)tiles;
+      pl.row_tiles = 0;
+    } else {
+      tiles = longest;
+    }
+    s = 16 * a.sms / (tiles * a.N_kv);
     if (s > c.max_kv / 96) s = c.max_kv / 96;
     if (s > kMaxSplits) s = kMaxSplits;
     if (s < 1) s = 1;
   }
   pl.splits = (int)s;
-  pl.items = (pl.kind == kTc ? tiles : (int64_t)c.samples * pl.row_tiles) * a.N_kv * s;
-  if (pl.kind == kTc && s > 1 && pl.items > (even ? 4 : 1) * a.sms) pl.items = (even ? 4 : 1) * a.sms;      // blocks: each takes what is left in turn
+  int64_t items = tiles * a.N_kv * s;                              // (more than one piece only of few row tiles)
+  if (pl.kind == kTc && s > 1 && items > (even ? 4 : 1) * a.sms) items = (even ? 4 : 1) * a.sms;      // blocks: each takes what is left in turn
+  pl.items = (int)items;
   pl.shares = paged_mma_shares(a.sms);
   // A row tile's keys are cut only where they may be many: the second kernel costs more than 512 keys do.
   pl.cut = c.max_kv > 512;
@@ -330,11 +342,10 @@ cudaError_t launch_paged_attn(const SegArgs& a, const PagedCache& c, bool warp_m
   SegPass& ps = p.pass[0];
   ps.seg_lo = ps.seg_hi = 1;
   ps.block_samples = 1;
-  ps.blocks = c.samples;
+  ps.blocks = pl.blocks;
   ps.row_tiles = pl.row_tiles;
   ps.splits = pl.splits;
-  if (pl.items > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  ps.items = (int)pl.items;
+  ps.items = pl.items;
   const cudaError_t e = pl.kind == kTc ? launch_paged_tc(p, c, pl.tile_rows == 128, st, launches)
                                        : launch_paged_f32(p, c, pl.tile_rows, st, launches);
   if (e != cudaSuccess || p.direct) return e;

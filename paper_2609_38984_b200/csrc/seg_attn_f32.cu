@@ -8,7 +8,9 @@
 // length are filled with zeros and masked.
 // What bounds it: latency.  4 x 1000 rows, 8 heads of 64, 100 to 333 keys take 84 us (21 TFLOP/s of some 70 on the FMA pipes): three
 // CTAs an SM leave 2.3 warps a scheduler, which issue every 2.2 clk.  Four CTAs with single K and V buffers took 86 us, 32-row
-// tiles 92.  (Compiled to 128 registers, that instance, <64, 4>, spills 12 bytes a thread and loads 24; <128, 1> spills 4.)
+// tiles 92.  (Compiled to 128 registers, that instance, <64, 4>, spills 12 bytes a thread and loads 24; <128, 1> spills 4;
+// for paged keys <64, 2> spills 48 and loads 40 in front of its loop, which costs nothing that shows: 40 samples of 4 tokens 47 us with and
+// without.)
 #include "seg_attn.cuh"
 
 namespace swam {
@@ -43,7 +45,44 @@ struct F32Cfg {
   static constexpr int kBytes = (kQ + 2 * (kK + kV) + kP) * 4;
 };
 
-// kPaged: an item is a row tile of one sample's new tokens, found from the block's number; its keys are found through the page table
+// The sample of the tile-th of all samples' row tiles of MR rows, and its first row in the sample; false behind the last one.  (For the
+// whole block: every thread adds up the tiles of a few neighbouring samples, and the one that has the tile among them looks for it.)
+template <int MR>
+__device__ __forceinline__ bool paged_find_tile(const PagedCache& c, int tokens, int g, int tile, int* sample, int* row0) {
+  __shared__ int64_t warp_sum[kThreadsF / 32];
+  __shared__ int2 found;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int per = (c.samples + kThreadsF - 1) / kThreadsF, b0 = min(c.samples, (int)threadIdx.x * per), b1 = min(c.samples, b0 + per);
+  auto tiles = [&](int b) {
+    const int q0 = __ldg(c.q_start + b), q1 = __ldg(c.q_start + b + 1);
+    return paged_stretch(c, tokens, q0, q1) ? ((q1 - q0) * g + MR - 1) / MR : 0;
+  };
+  int64_t sum = 0;               // (stretches out of order may overlap)
+  for (int b = b0; b < b1; ++b) sum += tiles(b);
+  int64_t end = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, end, o);
+    if (lane >= o) end += y;
+  }
+  if (lane == 31) warp_sum[warp] = end;
+  if (threadIdx.x == 0) found = make_int2(-1, 0);
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) end += warp_sum[w];
+  int64_t left = tile - (end - sum);
+  if (left >= 0 && left < sum) {
+    int b = b0;
+    for (int n; left >= (n = tiles(b)); ++b) left -= n;
+    found = make_int2(b, (int)left * MR);
+  }
+  __syncthreads();
+  *sample = found.x;
+  *row0 = found.y;
+  return found.x >= 0;
+}
+
+// kPaged: an item is a row tile of one sample's new tokens, found from the block's number (and, where the plan counts the row tiles of all
+// samples together, row_tiles = 0, from the samples' own lengths); its keys are found through the page table
 template <int D, int RPT, bool kPaged>
 __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constant__ SegParams p, const int pass,
                                                             const __grid_constant__ CacheArg<kPaged> pc) {
@@ -57,11 +96,22 @@ __global__ void __launch_bounds__(kThreadsF) seg_f32_kernel(const __grid_constan
   float* sP = sV + 2 * C::kV;    // [32][MR + 4], row ty + 16 i at column ty * RPT + i
   const SegPass& ps = p.pass[pass];
   const SegArgs& a = p.a;
-  SegItem it = seg_item(ps, a.N_kv, MR, blockIdx.x);
+  SegItem it;
+  if (kPaged && ps.row_tiles == 0) {
+    const int w = blockIdx.x / ps.blocks;
+    it.split = w % ps.splits;
+    it.h_kv = w / ps.splits;
+  } else {
+    it = seg_item(ps, a.N_kv, MR, blockIdx.x);
+  }
   SegKeys kk;
   PagedSample smp{0, 0, 0};
   int row_end = 0;               // kPaged: rows of the call in front of the end of the sample's
   if constexpr (kPaged) {
+    if (ps.row_tiles == 0 && !paged_find_tile<MR>(pc, a.n_q, p.g, blockIdx.x % ps.blocks, &it.block, &it.row0)) {
+      allow_next();
+      return;
+    }
     smp = paged_sample(pc, a.n_q, it.block, p.status);
     const int rows = smp.n * p.g;
     if (it.row0 >= rows) {       // (what the next kernel waits for is the end of all blocks)
