@@ -227,7 +227,8 @@ int swam_prefix_attn(swam_ctx* ctx, const swam_prefix_args* args, void* stream);
  * Rotary positions: pair i of the first rot_dim elements of a head turns by freq[i] radians per position along component
  * axis[i] of the token's position:  (a, b) -> magnitude * (a cos - b sin, b cos + a sin).  Pairs are (i, i + rot_dim / 2), or
  * (2i, 2i + 1) when interleaved.  The angle of any int32 position and any accepted frequency is reduced to within
- * 2^-30 turns (64-bit fixed point), so that far positions lose nothing.  Frequencies stretched for longer contexts are just other values of freq (and magnitude). */
+ * 2^-30 turns (64-bit fixed point), so that far positions lose nothing.  Frequencies stretched for longer contexts
+ * are just other values of freq (and magnitude). */
 typedef struct {
   const double* freq;   /* host, [rot_dim / 2], finite, |freq| <= 2^20; read during the call */
   const int32_t* axis;  /* host, [rot_dim / 2] in [0, n_axes), or NULL: component 0 */
@@ -239,7 +240,8 @@ typedef struct {
 
 /* swam_norm_rope: q and k as a projection writes them -> q and k as calls (1) to (6) expect them, in one pass.
  *   x' = x / sqrt(mean(x^2) + eps) * weight over the head dim (where the weight is given), then the rotation (where rope is given),
- * in fp32, rounded once.  q, q_out: [B, n, N_h, D]; k, k_out: [B, n, n_kv_heads, D]; q or k may be NULL (with its output).
+ * in fp32, rounded once.  (The sum of the squares is fp32 too: under a norm a finite row for which it overflows, of elements of
+ * 1e18 and more, gives zeros, or NaN where the rotation overflows as well.)  q, q_out: [B, n, N_h, D]; k, k_out: [B, n, n_kv_heads, D]; q or k may be NULL (with its output).
  * The heads of a token are contiguous.  An output may be its own input (same pointer and strides), and must not overlap an
  * input otherwise (refused where that is certain).  q_weight, k_weight: dev float [D] or NULL (no norm).
  * positions: dev int32 [B, n, n_axes], pos_sample elements from one sample's to the next (0: all samples share one
@@ -268,9 +270,10 @@ int swam_norm_rope(swam_ctx* ctx, const swam_norm_rope_args* args, void* stream)
  * q_start[n_samples] are nobody's: nothing is done with them and their rows of any output stay as they are.
  * On the device: a q_start that is out of order, out of range or gives a sample more than max_q tokens leaves that sample out (its
  * rows of any output stay as they are; where two samples claim a token, its rows may hold anything); a kv_len
- * outside [0, max_kv] is clamped; a page number outside [0, n_pages) that is needed reads as zeros and is not written;
- * swam_check reports all of them (SWAM_ERR_DEVICE_CHECK).  Table entries behind a sample's last page are not used,
- * and neither is what a page holds behind its sample's last token.  Samples may share pages that no call writes. */
+ * outside [0, max_kv] is clamped (for the attention; an appended token's number follows from kv_len as it is); a page number
+ * outside [0, n_pages) that is needed reads as zeros and is not written; swam_check reports all of them (SWAM_ERR_DEVICE_CHECK).
+ * Table entries behind a sample's last page are not used, and neither is what a page holds behind its sample's last token.
+ * Samples may share pages that no call writes. */
 typedef struct {
   void* k;                   /* dev [n_pages, page_size, n_kv_heads, D]; the heads of a token are contiguous */
   void* v;
@@ -290,7 +293,7 @@ typedef struct {
  * does, v as it is; and, where q is given, q_out = q normalised and rotated, for the swam_paged_attn that follows.
  * q, q_out: [n_tokens, N_h, D]; k, v: [n_tokens, n_kv_heads, D].  positions: dev int32 [n_tokens, n_axes] or NULL: a token's
  * number in its sample (kv_len[b] - new tokens + i) on every axis.  A token whose number is outside [0, max_pages * page_size) is
- * not written and reported.  Two new tokens with one place in the cache: either may stay.
+ * not written and reported.  Two new tokens with one place in the cache: what stays there may be of either, in parts too.
  * Limits: n_tokens * N_h at most 2^30 (SWAM_ERR_UNSUPPORTED beyond). */
 typedef struct {
   const swam_paged_cache* cache; /* host */
@@ -312,7 +315,9 @@ int swam_append_kv(swam_ctx* ctx, const swam_append_args* args, void* stream);
  * causal != 0 the keys [0, kv_len[b] - n + i + 1); results, special values and precision as in (6).
  * q, out: [n_tokens, N_h, D]; lse: dev float [N_h, n_tokens] or NULL; out must not overlap q or the cache.
  * max_q: no sample has more new tokens (0: n_tokens; without q_start n_tokens / n_samples); max_kv: no kv_len is larger (0: max_pages *
- * page_size).  They choose the kernel and how the keys are cut, so close bounds pay.
+ * page_size).  They choose the kernel and how the keys are cut, so close bounds pay where a table has room for much more than its
+ * samples have: four chunks of 300 tokens behind 100 to 1700, 32 heads on 8 of 128, take 41 us with either max_kv or a table of
+ * that width, 82 with a table for 32768 tokens and no max_kv; 16 single tokens behind up to 400 keys 12.6 and 15.9.
  * scratch: device memory of swam_paged_attn_scratch_bytes (256-byte aligned, NULL if 0), as in (6): the size depends on the
  * sizes in the arguments only, and calls that may overlap need scratch of their own.  SWAM_OPT_ATTN_VARIANT applies.
  * Limits: n_tokens * N_h at most 2^30 (SWAM_ERR_UNSUPPORTED beyond). */

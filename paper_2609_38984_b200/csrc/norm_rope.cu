@@ -14,11 +14,16 @@
 // requested before the tokens are looked up; a lane copies what it will read itself, so that no barrier is needed.  A lane holds both
 // elements of each of its pairs, and keeps their cosines and sines, times the weights, for all items of a kind, so that an element costs a
 // product, a fused one and the product with the reciprocal root.  Where rot/2 ends inside 16 bytes the other half of a pair is read again,
-// element by element (L1).
+// element by element (L1), which takes 2.4 to 3.1 times as long (9280 tokens of 32 + 32 heads of 128: 160 us with 120 elements rotated, 51 with 128
+// or with 120 in neighbouring pairs; 14631 tokens of 3 x 24 heads of 64 into a cache: 123 us with 56, 52 with 64).
 // What bounds it: memory, and the issue of some 160 instructions an item (1 KB).  q and k of 9280 tokens, 32 heads of 128 each, 304 MB in
 // 56 us (5.4 TB/s); 69376 tokens of 24 and 8 heads of 64, 569 MB in 107 us (5.3 TB/s, 73 % of the issue slots); 14631 tokens of 3 x 24 heads
 // of 64 into a cache, 270 MB in 56 us (4.8 TB/s: the places in the cache are looked up first).  A ring of three or six, items in
-// registers instead, one token a warp, cosines and sines unfolded: 0 to 30 % slower.  Few tokens: 4 to 5 us, a launch and one item.
+// registers instead, one token a warp, cosines and sines unfolded: 0 to 30 % slower.  Few tokens: 4 to 5 us, a launch and one item.  Narrow heads
+// and few of them spread what a token costs by itself over fewer items: 16449 tokens of 3 x 32 heads of 32 into a cache, 202 MB in 52 us (3.9
+// TB/s); 6000 tokens of 32 + 2 x 8 heads of 128, 32 elements rotated, 147 MB in 37.5 us (3.9 TB/s).
+// Three CTAs an SM leave 80 registers: bf16 instances spill 12 bytes a thread and load 16 (32 to 36 each where rot/2 ends inside 16
+// bytes; none with neighbouring pairs outside the cache), fp32 ones nothing.
 #include <string.h>
 
 #include "seg_attn.cuh"

@@ -20,8 +20,13 @@
 // the matrix instruction; half a step, 2^-8, of each weight).
 // What bounds it: HBM.  64 single tokens, 32 heads on 8 of 128, 16 to 8192 keys (1.08 GB): 168 us of streaming at 6.4 TB/s, 177 with the
 // join; two samples of 100001 and 131072 keys 155 us.  With 16 tokens a page the same call takes 177 us, 205 when the math warps issued
-// the loads, two boxes for each of K and V.  Head dim 64 reaches 4.8 TB/s and 32 3.4 (rows of 128 and 64 bytes a head).  The narrow form
-// changes nothing where memory bounds; it saves registers and a microsecond of the smallest calls (one sample of 501 keys: 11 us).
+// the loads, two boxes for each of K and V.  Head dim 64 reaches 4.4 to 4.8 TB/s and 32 2.7 to 3.4: units go through a head's keys before the
+// next head's, so that a CTA reads 128 or 64 bytes of a token's row at a time.  The narrow form
+// changes nothing where memory bounds; it saves registers and a microsecond of the smallest calls (one sample of 501 keys: 11 us).  Short and
+// ordinary histories are bound by the start, in which every CTA adds up the samples before its first load, and by the join: 51 samples of 62 to
+// 153 keys 12 us, 30 of 900 to 1300 keys, 5 key/value heads of 128, 85 MB in 25 us.
+// Two CTAs an SM leave 168 registers; instances with more rows a warp spill: <128, 4> 284 bytes a thread (236 loaded), <128, 2> 92 (96),
+// <64, 4> 88 (92), the others nothing.
 #include <string.h>
 
 #include "seg_maps.cuh"

@@ -9,8 +9,9 @@
 // What bounds it: latency.  4 x 1000 rows, 8 heads of 64, 100 to 333 keys take 84 us (21 TFLOP/s of some 70 on the FMA pipes): three
 // CTAs an SM leave 2.3 warps a scheduler, which issue every 2.2 clk.  Four CTAs with single K and V buffers took 86 us, 32-row
 // tiles 92.  (Compiled to 128 registers, that instance, <64, 4>, spills 12 bytes a thread and loads 24; <128, 1> spills 4;
-// for paged keys <64, 2> spills 48 and loads 40 in front of its loop, which costs nothing that shows: 40 samples of 4 tokens 47 us with and
-// without.)
+// for paged keys <64, 2> spills 48 and loads 40, which costs nothing that shows: 40 samples of 4 tokens 47 us with and without.)
+// Paged single tokens have 15 of the 16 rows to no purpose and one tile in flight: 2 tokens, 32 heads of 128, 1500 and 1983 keys, 114 MB in 90
+// us (1.3 TB/s).
 #include "seg_attn.cuh"
 
 namespace swam {

@@ -29,8 +29,11 @@
 //   goes to the ring.
 // Paged keys: a block per item, and running blocks take over those that have not started (16 chunks behind 640 to 8704 keys, 384 items:
 // 131 us, 171 in turn); K and V are boxes of pages.  What bounds them: head dim 128 as below (chunks of 300 to 2520 tokens, 8 heads on 32,
-// causal, 1.17 TFLOP: 908 us, 0.75 of the measured burst rate); head dim 64 with up to
-// 64 rows memory, less the changes of items (the 16 chunks: 96 us, 4.8 TB/s; an item of 20064 keys for every SM: 127 us, 6.0); up to 128 rows the exponentials.
+// causal, 1.17 TFLOP: 908 us, 0.75 of the measured burst rate; 1085 in eager calls on changing inputs, with the clock down); head dim 64 with up to
+// 64 rows memory, less the changes of items (the 16 chunks: 96 us, 4.8 TB/s, and 110 in eager calls on changing inputs; an item of 20064
+// keys for every SM: 127 us, 6.0); up to 128 rows the exponentials.
+// Spills (168 registers at the launch): the instance for paged keys, head dim 128 and 256 rows 8 bytes a thread (132 loaded), the one for
+// segments, head dim 128 and 128 rows 8 (8), the others nothing.
 // Paged keys, at most 64 rows: the tile holds the rows twice, and stream 1 works on the second half, so that its exponentials run on the
 //   sub-cores of the TMEM lanes that stream 0 leaves idle (16 chunks of 64 tokens, head dim 64: 127 us, 131 with both in the first half).
 //   Its accumulators are out of stream 0's reach there and come through the item's query buffer as fp32.
@@ -365,7 +368,9 @@ seg_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               const int n = (s.n * p.g + C::kRows - 1) / C::kRows * a.N_kv, len = (s.len + kTile - 1) / kTile;
               if (n > 0) longest = max(longest, len);
               items += n;
-              keys += (unsigned)n * len;                   // (of use with fewer row tiles than SMs: no more than 148 x 2^24)
+              // (Of use with no more row tiles than two an SM, of at most 2^22 key tiles each: below 2^32 with up to 511 SMs.  Stretches that
+              // overlap may be more; whatever comes out then, a piece stays within the plan below.)
+              keys += (unsigned)n * len;
             }
             longest = __reduce_max_sync(0xffffffffu, longest);
             items = max(1, __reduce_add_sync(0xffffffffu, items));

@@ -26,7 +26,7 @@ def through_the_c_entry(c, out, lse, max_q, causal=True):
 @pytest.mark.parametrize("kind", paged.KINDS)
 @pytest.mark.parametrize("new", [[2, 4, 1, 3], [20, 33, 9, 30], [70, 95, 3, 90]])
 @pytest.mark.parametrize("lens", [[900, 1400, 300, 2000], [100, 130, 99, 110], [20000, 17000, 700, 30000]])
-@pytest.mark.parametrize("spoilt", ["max_q", "order"])
+@pytest.mark.parametrize("spoilt", ["max_q", "order", "order, no bound"])
 def test_rows_of_a_sample_that_is_left_out_stay_as_they_are(kind, new, lens, spoilt):
     H, kv, D = 8, 2, 64
     c = paged.case(kind, list(new), lens, H, kv, D, 64, front=2, behind=3)
@@ -35,7 +35,7 @@ def test_rows_of_a_sample_that_is_left_out_stay_as_they_are(kind, new, lens, spo
     if spoilt == "max_q":          # the second sample has more new tokens than the call says
         left, max_q = [1], new[3]
     else:                          # the end of the first sample's stretch, and with it the start of the second's, is nowhere
-        left, max_q = [0, 1], max(new)
+        left, max_q = [0, 1], 0 if "no bound" in spoilt else max(new)
         c.q_start[1] = 10 ** 9
     through_the_c_entry(c, out, lse, max_q)
     with pytest.raises(swam.SwamError) as e:

@@ -56,3 +56,15 @@ def test_the_whole_range_of_frequencies_and_positions():
     err = (got[0, :, 0].double().cpu() - want).abs()
     tol = 7 * 2.0 ** -24 + 2 * math.pi * 2.0 ** -30
     assert (err <= tol).all(), [(pos[i], freq[j % 16], float(err[i, j])) for i, j in (err > tol).nonzero().tolist()[:8]]
+
+
+@pytest.mark.parametrize("dtype", rope_tests.TYPES)
+def test_rows_whose_squares_outgrow_32_bits_give_zeros(dtype):
+    D = 64
+    ctx = rope_tests.ctx_for(1, 2, 2, D, dtype)
+    x = torch.randn(1, 3, 2, D, device="cuda")
+    want, _ = ctx.norm_rope(x.to(dtype), rope=swam.Rope(rope_tests.ladder(D)), q_weight=torch.ones(D, device="cuda"))
+    x[0, 1, 1] = 1e30
+    got, _ = ctx.norm_rope(x.to(dtype), rope=swam.Rope(rope_tests.ladder(D)), q_weight=torch.ones(D, device="cuda"))
+    assert (got[0, 1, 1] == 0).all()
+    assert torch.equal(got[0, [0, 2]], want[0, [0, 2]]) and torch.equal(got[0, 1, 0], want[0, 1, 0])
